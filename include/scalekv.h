@@ -354,6 +354,105 @@ scalekv_status scalekv_launch_count(scalekv_ctx *ctx, int64_t *count);
 scalekv_status scalekv_profile_enable(scalekv_ctx *ctx, int32_t on);
 scalekv_status scalekv_profile_read(scalekv_ctx *ctx, int32_t which, double *ms_total, int64_t *launches);
 
+/* ---- a paged cache of token sequences ---------------------------------------------------------- */
+
+/* Beside token maps a model of this kind reads captions and writes text.  This cache holds such sequences: every one of its own
+ * length, heads in groups that share a kv head, prompts that arrive in chunks, tokens that arrive one by one, pages that a table
+ * of the caller's assigns.  It is independent of a scalekv_ctx.  The ways to make it small are fewer bits (SCALEKV_STORE_Q8) and a
+ * window with sinks (Sec. 4.1's positional rules, here as a mask over a cache that stays whole).
+ *
+ * Conventions
+ *  - Every call enqueues on the given cudaStream_t of the handle's device (which must be current) and returns; no call but init and sync waits
+ *    for the device, and all but these can be captured into a CUDA graph (a batch's arrays are read on the device when the kernels run; its sizes
+ *    are the call's).
+ *  - Calls on one handle share its workspace: attends on different streams have to be ordered by the caller.
+ *  - Lengths, starts and pages are read on the device.  One that is out of range is never followed: what it would lead to is left out (a row
+ *    read comes back as zeros, a key counts as hidden), and the sticky device status, SCALEKV_ERR_DEVICE_CHECK, says so. */
+typedef struct scalekv_paged scalekv_paged; /* opaque, host-side, library-owned */
+
+/* How a row (one token of one kv head, of K or of V) is held.
+ * SCALEKV_STORE_BF16  as bf16.
+ * SCALEKV_STORE_Q8    as signed 8-bit codes with one fp32 scale: s = max_i |x_i| / 127, c_i = x_i / s rounded half to even (both
+ *                     quotients in fp32), read as c_i s.  A row of zeros has s = 0.  A row that holds an infinity or a NaN has
+ *                     s = NaN and codes 0: it reads back as NaN, and a query that sees it gets NaN. */
+#define SCALEKV_STORE_BF16 0
+#define SCALEKV_STORE_Q8 1
+
+typedef struct {
+  int32_t n_layers;
+  int32_t n_pages;        /* pages of a layer; a page id means the same in every layer                  */
+  int32_t page_tokens;    /* a power of two >= 16                                                       */
+  int32_t n_kv_heads;
+  int32_t head_dim;       /* 64 or 128                                                                  */
+  int32_t store;          /* SCALEKV_STORE_*                                                            */
+  void *pool;             /* device memory for the rows, 256-byte aligned (borrowed): K rows, V rows and, for Q8, K scales, V scales, */
+  size_t pool_bytes;      /* each [layer][page][kv head][row of the page]; need not be initialised      */
+  void *workspace;        /* device scratch for partial results and the status word, 256-byte aligned (borrowed) */
+  size_t workspace_bytes;
+  int32_t device;
+} scalekv_paged_config;
+
+/* The sequences of a call.  Sequence b has lengths[b] cache entries once its new tokens are in, which are rows starts[b] ..
+ * starts[b + 1] - 1 of the call's token tensors (none is allowed) and positions lengths[b] - (starts[b + 1] - starts[b]) .. of the cache.
+ * Position p lies in row p mod page_tokens of page page_table[b * table_stride + p / page_tokens].  Entries of the table that hold no
+ * position, and those of pages that a window hides from all of a sequence's new tokens, may hold anything. */
+typedef struct {
+  const int32_t *page_table;  /* device [n_seqs][table_stride]                                          */
+  const int32_t *lengths;     /* device [n_seqs]                                                        */
+  const int32_t *starts;      /* device [n_seqs + 1], ascending, starts[0] = 0, starts[n_seqs] = n_tokens */
+  int32_t table_stride;       /* from one sequence's entries to the next one's                          */
+  int32_t table_pages;        /* entries of a sequence: no position behind them is looked up            */
+  int32_t n_seqs, n_tokens;
+  int32_t max_new;            /* no sequence has more new tokens than this (reported otherwise)         */
+  int32_t max_length;         /* no sequence is longer than this; only sizes launches                   */
+} scalekv_paged_batch;
+
+/* A [tokens][heads][head_dim] view: device pointer + ELEMENT strides; the innermost axis is contiguous and every row starts on a
+ * 16-byte boundary. */
+typedef struct {
+  const void *ptr;
+  int64_t stride_t, stride_h;
+} scalekv_rows;
+
+/* What the query at position p of a sequence sees of its positions j < length: all of them; causal != 0: only j <= p;
+ * window > 0: only j > p - window and the n_sink first ones. */
+typedef struct {
+  int32_t causal, window, n_sink;
+} scalekv_paged_mask;
+
+scalekv_status scalekv_paged_query_sizes(const scalekv_paged_config *cfg, size_t *pool_bytes, size_t *workspace_bytes);
+/* Creates a handle (the reason of a refusal goes to stderr).  Synchronous.  *out is NULL on failure. */
+scalekv_status scalekv_paged_init(const scalekv_paged_config *cfg, scalekv_paged **out);
+/* Frees the handle.  Does not wait: kernels under way only use the caller's memory. */
+scalekv_status scalekv_paged_destroy(scalekv_paged *kv);
+
+/* Writes the new tokens' K and V rows (dtype: SCALEKV_BF16 or SCALEKV_F32) into the cache, quantised where it holds codes. */
+scalekv_status scalekv_paged_write(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, scalekv_rows K,
+                                   scalekv_rows V, int32_t dtype, void *stream);
+
+/* The reverse: fills K and V with the cached rows of the batch's new tokens (the last positions of every sequence, all of it where
+ * starts[b + 1] - starts[b] is its length), as numbers of the given dtype. */
+scalekv_status scalekv_paged_read(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, scalekv_rows K,
+                                  scalekv_rows V, int32_t dtype, void *stream);
+
+/* Attention of the new tokens over the cache: O = softmax(scale * q K^T) V over the keys that a query sees.  Q and O are
+ * bf16 views with n_heads heads, a multiple of n_kv_heads (head h reads kv head h / (n_heads / n_kv_heads)).  The new tokens' own rows are
+ * read from the cache like all others (write them first); queries may also attend over a cache that does not hold them, causal = 0.
+ * lse (nullable) is a dense float [n_tokens][n_heads] that receives max + log-sum-exp of the scaled products.  A query that sees
+ * nothing gets O = 0 and lse = -inf.  softmax_scale 0: 1 / sqrt(head_dim).  Products are exact, sums are fp32, P is rounded to
+ * bf16 before its product with V.  What hidden keys hold never matters, whatever it is, with one exception: bf16 rows of V must be
+ * finite where another query of the call sees them. */
+scalekv_status scalekv_paged_attend(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, int32_t n_heads,
+                                    scalekv_rows Q, scalekv_rows O, float *lse, const scalekv_paged_mask *mask,
+                                    float softmax_scale, void *stream);
+
+/* Waits for the stream; returns the handle's sticky device status (OK, TIMEOUT or DEVICE_CHECK). */
+scalekv_status scalekv_paged_sync(scalekv_paged *kv, void *stream);
+/* Number of kernels this handle has launched (HOST out). */
+scalekv_status scalekv_paged_launch_count(scalekv_paged *kv, int64_t *count);
+/* Text of the last error of this handle (never NULL; valid until the next call). */
+const char *scalekv_paged_error_string(scalekv_paged *kv);
+
 /* ---- allocation-free top-k ------------------------------------------------------------------ */
 
 /* (The paper has no counterpart of this call; it exists for integration reasons only.)

@@ -17,8 +17,8 @@ import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libscalekv.so")
-SOURCES = [os.path.join(_HERE, "csrc", f) for f in ("scalekv.cu", "select_static.cu", "kernels_simt.cuh", "attend_tc.cuh", "attend_f32.cuh", "key_split.h",
-                                                 "common.cuh")]
+SOURCES = [os.path.join(_HERE, "csrc", f) for f in ("scalekv.cu", "select_static.cu", "paged.cu", "kernels_simt.cuh", "attend_tc.cuh", "attend_f32.cuh",
+                                                 "key_split.h", "tc.cuh", "common.cuh", "paged_view.cuh", "paged_store.cuh", "paged_stream.cuh")]
 HEADER = os.path.join(os.path.dirname(_HERE), "include", "scalekv.h")
 CALL_SOURCE = os.path.join(_HERE, "csrc", "call.cpp")
 
@@ -26,6 +26,7 @@ KEEP_ALL = -1
 MAX_WINDOW = 64
 BF16, F32 = 0, 1
 STATUS_NAMES = ["OK", "INVALID_ARG", "BAD_STATE", "CAPACITY", "UNSUPPORTED", "CUDA", "TIMEOUT", "DEVICE_CHECK"]
+STORES = {"bf16": 0, "q8": 1}
 KERNEL_CLASSES = ["append", "attend", "score", "select", "compact", "other", "compress"]
 
 
@@ -58,6 +59,26 @@ class scalekv_tensor(C.Structure):
     _fields_ = [("ptr", C.c_void_p), ("stride_b", C.c_int64), ("stride_h", C.c_int64), ("stride_t", C.c_int64)]
 
 
+class scalekv_paged_config(C.Structure):
+    _fields_ = [("n_layers", C.c_int32), ("n_pages", C.c_int32), ("page_tokens", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("store", C.c_int32), ("pool", C.c_void_p), ("pool_bytes", C.c_size_t),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("device", C.c_int32)]
+
+
+class scalekv_paged_batch(C.Structure):
+    _fields_ = [("page_table", C.c_void_p), ("lengths", C.c_void_p), ("starts", C.c_void_p), ("table_stride", C.c_int32),
+                ("table_pages", C.c_int32), ("n_seqs", C.c_int32), ("n_tokens", C.c_int32), ("max_new", C.c_int32),
+                ("max_length", C.c_int32)]
+
+
+class scalekv_rows(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("stride_t", C.c_int64), ("stride_h", C.c_int64)]
+
+
+class scalekv_paged_mask(C.Structure):
+    _fields_ = [("causal", C.c_int32), ("window", C.c_int32), ("n_sink", C.c_int32)]
+
+
 def build_library(force=False, verbose=False):
     """Compiles the CUDA sources for sm_100a into libscalekv.so, and the native module of the hot calls (both in-tree), when out
     of date."""
@@ -67,7 +88,7 @@ def build_library(force=False, verbose=False):
         if os.path.getmtime(LIB_PATH) >= newest:
             return LIB_PATH
     cmd = ["nvcc", "-shared", "-Xcompiler", "-fPIC", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-           "-O3", "-std=c++17", SOURCES[0], SOURCES[1], "-o", LIB_PATH]
+           "-O3", "-std=c++17", "--threads", "3", *(f for f in SOURCES if f.endswith(".cu")), "-o", LIB_PATH]
     if verbose:
         cmd.insert(1, "-Xptxas=-v")
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -167,14 +188,24 @@ def load_library():
         "scalekv_launch_count": [ctx_p, P(i64)],
         "scalekv_profile_enable": [ctx_p, i32],
         "scalekv_profile_read": [ctx_p, i32, P(f64), P(i64)],
+        "scalekv_paged_query_sizes": [P(scalekv_paged_config), P(C.c_size_t), P(C.c_size_t)],
+        "scalekv_paged_init": [P(scalekv_paged_config), P(ctx_p)],
+        "scalekv_paged_destroy": [ctx_p],
+        "scalekv_paged_write": [ctx_p, i32, P(scalekv_paged_batch), scalekv_rows, scalekv_rows, i32, C.c_void_p],
+        "scalekv_paged_read": [ctx_p, i32, P(scalekv_paged_batch), scalekv_rows, scalekv_rows, i32, C.c_void_p],
+        "scalekv_paged_attend": [ctx_p, i32, P(scalekv_paged_batch), i32, scalekv_rows, scalekv_rows, C.c_void_p,
+                                 P(scalekv_paged_mask), C.c_float, C.c_void_p],
+        "scalekv_paged_sync": [ctx_p, C.c_void_p],
+        "scalekv_paged_launch_count": [ctx_p, P(i64)],
         "scalekv_select_static": [C.c_void_p, i32, i32, i32, i32, C.c_void_p, C.c_void_p],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
         fn.argtypes = args
         fn.restype = C.c_int
-    lib.scalekv_error_string.argtypes = [ctx_p]
-    lib.scalekv_error_string.restype = C.c_char_p
+    for name in ("scalekv_error_string", "scalekv_paged_error_string"):
+        getattr(lib, name).argtypes = [ctx_p]
+        getattr(lib, name).restype = C.c_char_p
     _lib = lib
     return lib
 
@@ -503,3 +534,116 @@ class ScaleKV:
             self._check(self.lib.scalekv_profile_read(self.ctx, i, C.byref(ms), C.byref(n)))
             out[name] = (ms.value, n.value)
         return out
+
+
+# ---- the paged cache of token sequences ------------------------------------------------------
+class PagedBatch:
+    """The sequences of a call, kept for all layers of a step: page_table [n_seqs, pages], lengths [n_seqs] and starts
+    [n_seqs + 1], int32 on the device and read there when the kernels run; the sizes are the host's: n_tokens new tokens in all, at
+    most max_new of a sequence, no sequence longer than max_length (which only sizes launches)."""
+
+    def __init__(self, page_table, lengths, starts, n_tokens, max_new, max_length):
+        n = lengths.shape[0] if lengths.dim() == 1 else -1
+        for name, t, shape in (("page_table", page_table, (n, None)), ("lengths", lengths, (n,)), ("starts", starts, (n + 1,))):
+            if t.dtype != torch.int32 or t.dim() != len(shape) or any(b is not None and a != b for a, b in zip(t.shape, shape)):
+                raise ValueError(f"{name} must be int32 of shape {shape}, got {t.dtype} {tuple(t.shape)}")
+            if not t.is_cuda or t.device != lengths.device or (t.numel() > 0 and t.stride(-1) != 1):
+                raise ValueError(f"{name} must be a device tensor with contiguous rows, all three on one device")
+        for name, v in (("n_tokens", n_tokens), ("max_new", max_new), ("max_length", max_length)):
+            if not 0 <= v < 2 ** 31:
+                raise ValueError(f"{name} must lie in [0, 2^31)")
+        self.tensors = (page_table, lengths, starts)       # the kernels read them
+        self.device, self.n_seqs, self.n_tokens = lengths.device, n, n_tokens
+        self.struct = scalekv_paged_batch(page_table.data_ptr(), lengths.data_ptr(), starts.data_ptr(), page_table.stride(0),
+                                          page_table.shape[1], n, n_tokens, max_new, max_length)
+        self.address = C.addressof(self.struct)
+
+
+class PagedKV:
+    """Owns the pool and the workspace of a paged token cache (torch tensors; `pool`: a uint8 tensor of the caller's instead) and one
+    library handle.  Every call runs on PyTorch's current stream of the device."""
+
+    def __init__(self, n_layers, n_pages, n_kv_heads, head_dim, store="q8", page_tokens=64, device=0, pool=None):
+        if not torch.cuda.is_available():
+            raise RuntimeError("PagedKV needs a CUDA device (sm_100a); there is no CPU path")
+        self.lib, self._call = load_library(), load_call()
+        self._fn = {f: C.cast(getattr(self.lib, "scalekv_paged_" + f), C.c_void_p).value for f in ("write", "read", "attend")}
+        self.device, self.device_index = torch.device("cuda", device), device
+        self.n_layers, self.n_pages, self.n_kv_heads, self.head_dim = n_layers, n_pages, n_kv_heads, head_dim
+        self.store, self.page_tokens = store, page_tokens
+        cfg = scalekv_paged_config(n_layers, n_pages, page_tokens, n_kv_heads, head_dim, STORES[store])
+        cfg.device = device
+        pb, wb = C.c_size_t(0), C.c_size_t(0)
+        st = self.lib.scalekv_paged_query_sizes(C.byref(cfg), C.byref(pb), C.byref(wb))
+        if st:
+            raise ScaleKVError(st, "scalekv_paged_query_sizes")
+        self.pool_bytes, self.workspace_bytes = pb.value, wb.value
+        if pool is None:
+            pool = torch.empty(pb.value, dtype=torch.uint8, device=self.device)
+        elif pool.device != self.device or pool.dtype != torch.uint8 or not pool.is_contiguous():
+            raise ValueError(f"pool must be a contiguous uint8 tensor on {self.device}")
+        self.pool = pool
+        self.workspace = torch.empty(wb.value, dtype=torch.uint8, device=self.device)
+        cfg.pool, cfg.pool_bytes = pool.data_ptr(), pool.numel()
+        cfg.workspace, cfg.workspace_bytes = self.workspace.data_ptr(), wb.value
+        self.handle = C.c_void_p(None)
+        with torch.cuda.device(self.device):
+            st = self.lib.scalekv_paged_init(C.byref(cfg), C.byref(self.handle))
+        if st:
+            raise ScaleKVError(st, "scalekv_paged_init")
+        self._handle = self.handle.value
+
+    def _check(self, st):
+        if st:
+            raise ScaleKVError(st, self.lib.scalekv_paged_error_string(self.handle).decode())
+
+    def _stream(self):
+        return torch._C._cuda_getCurrentRawStream(self.device_index)
+
+    def close(self):
+        if getattr(self, "handle", None) and self.handle.value:
+            self.lib.scalekv_paged_destroy(self.handle)
+            self.handle = C.c_void_p(None)
+            self._handle = 0
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _batch(self, batch):
+        if batch.device != self.device:
+            raise ValueError(f"the batch is on {batch.device}, the cache on {self.device}")
+        return batch.address
+
+    # -- C ABI, same names
+    def scalekv_paged_write(self, layer, batch, K, V):
+        """The new tokens' rows, K and V [n_tokens, n_kv_heads, head_dim] in bf16 or f32, join the cache."""
+        self._check(self._call.paged_move(self._fn["write"], self._handle, layer, self._batch(batch), batch.n_tokens, self.n_kv_heads,
+                                          self.head_dim, self.device_index, K, V, self._stream()))
+
+    def scalekv_paged_read(self, layer, batch, K=None, V=None, dtype=torch.bfloat16):
+        """The cached rows of the batch's new tokens as numbers -> (K, V), which are made of `dtype` where not given."""
+        shape = (batch.n_tokens, self.n_kv_heads, self.head_dim)
+        K = torch.empty(shape, dtype=dtype, device=self.device) if K is None else K
+        V = torch.empty(shape, dtype=dtype, device=self.device) if V is None else V
+        self._check(self._call.paged_move(self._fn["read"], self._handle, layer, self._batch(batch), batch.n_tokens, self.n_kv_heads,
+                                          self.head_dim, self.device_index, K, V, self._stream()))
+        return K, V
+
+    def scalekv_paged_attend(self, layer, batch, Q, O=None, lse=None, causal=True, window=0, n_sink=0, softmax_scale=0.0):
+        """Attention of the queries Q [n_tokens, heads, head_dim] (bf16) over the cache -> O; lse: a float32 [n_tokens, heads] to fill."""
+        if O is None:
+            O = torch.empty_like(Q)
+        self._check(self._call.paged_attend(self._fn["attend"], self._handle, layer, self._batch(batch), batch.n_tokens, self.head_dim,
+                                            self.device_index, Q, O, lse, causal, window, n_sink, softmax_scale, self._stream()))
+        return O
+
+    def scalekv_paged_sync(self):
+        self._check(self.lib.scalekv_paged_sync(self.handle, self._stream()))
+
+    def scalekv_paged_launch_count(self):
+        n = C.c_int64(0)
+        self._check(self.lib.scalekv_paged_launch_count(self.handle, C.byref(n)))
+        return n.value

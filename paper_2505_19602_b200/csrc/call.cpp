@@ -193,8 +193,96 @@ PyObject *layer_stats_ex(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return nullptr;
 }
 
+// ---- the paged token cache: [tokens][heads][head_dim] tensors, whose type, device and sizes are checked here, since the library sees addresses
+// only.  What does not fit is a ValueError that names the argument.
+bool rows(PyObject *obj, const char *name, long tokens, long heads, long dim, int device, scalekv_rows *out, at::ScalarType *type, long *got_heads) {
+  if (!THPVariable_Check(obj)) {
+    PyErr_Format(PyExc_TypeError, "%s: expected a tensor, got %s", name, Py_TYPE(obj)->tp_name);
+    return false;
+  }
+  return guarded([&] {
+    const at::Tensor &t = THPVariable_Unpack(obj);
+    const char *wrong = nullptr;
+    if (t.dim() != 3 || t.size(0) != tokens || (heads > 0 && t.size(1) != heads) || t.size(2) != dim) wrong = "has another shape than [tokens, heads, head_dim]";
+    else if (!t.is_cuda() || t.get_device() != device) wrong = "is not on the cache's device";
+    else if (t.scalar_type() != at::kBFloat16 && t.scalar_type() != at::kFloat) wrong = "is neither bfloat16 nor float32";
+    else if (*type != at::ScalarType::Undefined && t.scalar_type() != *type) wrong = "has another type than it should";
+    else if (t.numel() > 0 && t.stride(2) != 1) wrong = "must have contiguous head_dim";
+    if (wrong) {
+      PyErr_Format(PyExc_ValueError, "%s %s", name, wrong);
+      return false;
+    }
+    *type = t.scalar_type();
+    if (got_heads) *got_heads = t.size(1);
+    *out = {t.data_ptr(), t.stride(0), t.stride(1)};
+    // (the stride of an axis of one entry says nothing and need not keep rows on 16 bytes)
+    if (t.size(0) <= 1) out->stride_t = 0;
+    if (t.size(1) <= 1) out->stride_h = 0;
+    return true;
+  });
+}
+
+// move(function, handle, layer, batch address, tokens, kv heads, head_dim, device, K, V, stream): paged_write and paged_read
+PyObject *paged_move(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arguments(n, 11)) return nullptr;
+  const auto fn = address<decltype(&scalekv_paged_write)>(a[0]);
+  const auto kv = address<scalekv_paged *>(a[1]);
+  const int layer = (int)PyLong_AsLong(a[2]);
+  const auto batch = address<const scalekv_paged_batch *>(a[3]);
+  const long tokens = PyLong_AsLong(a[4]), heads = PyLong_AsLong(a[5]), dim = PyLong_AsLong(a[6]), device = PyLong_AsLong(a[7]);
+  const auto stream = address<void *>(a[10]);
+  if (PyErr_Occurred()) return nullptr;
+  scalekv_rows k, v;
+  at::ScalarType type = at::ScalarType::Undefined;
+  if (!rows(a[8], "K", tokens, heads, dim, (int)device, &k, &type, nullptr) || !rows(a[9], "V", tokens, heads, dim, (int)device, &v, &type, nullptr)) return nullptr;
+  CALL(fn(kv, layer, batch, k, v, type == at::kFloat ? SCALEKV_F32 : SCALEKV_BF16, stream));
+}
+
+// paged_attend(function, handle, layer, batch address, tokens, head_dim, device, Q, O, lse or None, causal, window, sinks, scale, stream)
+PyObject *paged_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arguments(n, 15)) return nullptr;
+  const auto fn = address<decltype(&scalekv_paged_attend)>(a[0]);
+  const auto kv = address<scalekv_paged *>(a[1]);
+  const int layer = (int)PyLong_AsLong(a[2]);
+  const auto batch = address<const scalekv_paged_batch *>(a[3]);
+  const long tokens = PyLong_AsLong(a[4]), dim = PyLong_AsLong(a[5]), device = PyLong_AsLong(a[6]);
+  const long window = PyLong_AsLong(a[11]), sinks = PyLong_AsLong(a[12]);
+  const int causal = PyObject_IsTrue(a[10]);
+  const double scale = PyFloat_AsDouble(a[13]);
+  const auto stream = address<void *>(a[14]);
+  if (PyErr_Occurred()) return nullptr;
+  if (window > 0x7fffffff || sinks > 0x7fffffff || window < 0 || sinks < 0) {
+    PyErr_SetString(PyExc_ValueError, "window and n_sink must lie in [0, 2^31)");
+    return nullptr;
+  }
+  const scalekv_paged_mask mask = {causal, (int32_t)window, (int32_t)sinks};
+  scalekv_rows q, o;
+  at::ScalarType type = at::kBFloat16;
+  long heads = 0;
+  float *lse = nullptr;
+  if (!rows(a[7], "Q", tokens, 0, dim, (int)device, &q, &type, &heads) || !rows(a[8], "O", tokens, heads, dim, (int)device, &o, &type, nullptr)) return nullptr;
+  if (a[9] != Py_None) {
+    if (!THPVariable_Check(a[9])) {
+      PyErr_SetString(PyExc_TypeError, "lse: expected a tensor");
+      return nullptr;
+    }
+    if (!guarded([&] {
+          const at::Tensor &t = THPVariable_Unpack(a[9]);
+          if (t.dim() != 2 || t.size(0) != tokens || t.size(1) != heads || t.scalar_type() != at::kFloat || !t.is_contiguous() || !t.is_cuda() ||
+              t.get_device() != device) {
+            PyErr_SetString(PyExc_ValueError, "lse must be a contiguous float32 [tokens, heads] on the cache's device");
+            return false;
+          }
+          lse = static_cast<float *>(t.data_ptr());
+          return true;
+        })) return nullptr;
+  }
+  CALL(fn(kv, layer, batch, (int32_t)heads, q, o, lse, &mask, (float)scale, stream));
+}
+
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {METHOD(step), METHOD(step_ex), METHOD(append), METHOD(attend), METHOD(compress_ex), METHOD(layer_stats_ex),
+PyMethodDef methods[] = {METHOD(step), METHOD(step_ex), METHOD(append), METHOD(attend), METHOD(compress_ex), METHOD(layer_stats_ex), METHOD(paged_move),
+                         METHOD(paged_attend),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_scalekv_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,281 @@
+// Host runtime and C ABI of the paged token cache (see include/scalekv.h for the contract): checks arguments, cuts launches.
+#include <cuda_runtime.h>
+#include <nvtx3/nvToolsExt.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdarg>
+#include <cstdio>
+#include <new>
+#include <string>
+
+#include "../../include/scalekv.h"
+#include "paged_store.cuh"
+#include "paged_stream.cuh"
+
+using namespace scalekv;
+using namespace scalekv::paged;
+
+namespace {
+
+// Rows of partial results that a launch may leave (rows of the call times CTAs that share a row's keys).
+constexpr long long kPartRows = 148 * 256;
+constexpr size_t kStatusBytes = 256;
+constexpr int kMaxLength = 1 << 30;      // tokens that a sequence's pages may hold: sums of a position and a window stay in 32 bits
+
+struct Layout {
+  size_t rows_bytes, scale_bytes;        // of K, and of V, over all layers
+  size_t pool_bytes, ws_bytes;
+};
+
+scalekv_status make_layout(const scalekv_paged_config *c, Layout &y, std::string &err) {
+  if (!c) { err = "null config"; return SCALEKV_ERR_INVALID_ARG; }
+  if (c->n_layers < 1 || c->n_pages < 1 || c->n_kv_heads < 1) { err = "n_layers, n_pages and n_kv_heads must be >= 1"; return SCALEKV_ERR_INVALID_ARG; }
+  if (c->page_tokens < 16 || (c->page_tokens & (c->page_tokens - 1))) { err = "page_tokens must be a power of two >= 16"; return SCALEKV_ERR_INVALID_ARG; }
+  if (c->head_dim != 64 && c->head_dim != 128) { err = "unsupported head_dim: 64 and 128 are built"; return SCALEKV_ERR_UNSUPPORTED; }
+  if (c->store != SCALEKV_STORE_BF16 && c->store != SCALEKV_STORE_Q8) { err = "unknown store"; return SCALEKV_ERR_INVALID_ARG; }
+  const double rows = (double)c->n_layers * c->n_pages * c->n_kv_heads * c->page_tokens;
+  if (rows > 1e14 || (long long)c->n_pages * c->page_tokens > 0x7fffffffLL) { err = "more than 2^31 - 1 tokens in a layer's pages"; return SCALEKV_ERR_CAPACITY; }
+  const size_t n = (size_t)c->n_layers * c->n_pages * c->n_kv_heads * c->page_tokens;
+  y.rows_bytes = n * c->head_dim * (c->store == SCALEKV_STORE_Q8 ? 1 : 2);
+  y.scale_bytes = c->store == SCALEKV_STORE_Q8 ? n * 4 : 0;
+  y.pool_bytes = 2 * (y.rows_bytes + y.scale_bytes);
+  y.ws_bytes = kStatusBytes + (size_t)kPartRows * (c->head_dim + 2) * 4;
+  return SCALEKV_OK;
+}
+
+}  // namespace
+
+struct scalekv_paged {
+  scalekv_paged_config cfg;
+  Layout lay;
+  int n_sm = 148, page_shift = 0;
+  int64_t launches = 0;
+  std::string err = "ok";
+};
+
+namespace {
+
+scalekv_status fail(scalekv_paged *c, scalekv_status st, const char *fmt, ...) {
+  char buf[512];
+  va_list ap; va_start(ap, fmt); vsnprintf(buf, sizeof buf, fmt, ap); va_end(ap);
+  if (c) c->err = buf;
+  return st;
+}
+
+Store layer_store(const scalekv_paged *c, int layer) {
+  const scalekv_paged_config &g = c->cfg;
+  const size_t rows = c->lay.rows_bytes / g.n_layers, scales = c->lay.scale_bytes / g.n_layers;
+  char *pool = static_cast<char *>(g.pool);
+  Store s;
+  s.k_rows = pool + rows * layer;
+  s.v_rows = pool + c->lay.rows_bytes + rows * layer;
+  s.k_scales = reinterpret_cast<float *>(pool + 2 * c->lay.rows_bytes + scales * layer);
+  s.v_scales = reinterpret_cast<float *>(pool + 2 * c->lay.rows_bytes + c->lay.scale_bytes + scales * layer);
+  s.n_pages = g.n_pages; s.heads = g.n_kv_heads; s.page_shift = c->page_shift;
+  s.status = static_cast<int *>(g.workspace);
+  return s;
+}
+
+bool rows_ok(const scalekv_rows &x, int esize) {
+  return x.ptr != nullptr && !(reinterpret_cast<uintptr_t>(x.ptr) & 15) && (x.stride_t * esize) % 16 == 0 && (x.stride_h * esize) % 16 == 0;
+}
+
+Rows view(const scalekv_rows &x, int esize) { return {static_cast<char *>(const_cast<void *>(x.ptr)), x.stride_t * esize, x.stride_h * esize}; }
+
+scalekv_status check_batch(scalekv_paged *c, int layer, const scalekv_paged_batch *b, Batch &out) {
+  if (layer < 0 || layer >= c->cfg.n_layers) return fail(c, SCALEKV_ERR_INVALID_ARG, "layer %d out of range", layer);
+  if (!b || b->n_seqs < 0 || b->n_tokens < 0 || b->max_new < 0 || b->max_length < 0)
+    return fail(c, SCALEKV_ERR_INVALID_ARG, "batch null, or a negative size in it");
+  if (b->n_seqs == 0 && b->n_tokens > 0) return fail(c, SCALEKV_ERR_INVALID_ARG, "tokens without sequences");
+  if (b->n_tokens > 0 && (!b->page_table || !b->lengths || !b->starts)) return fail(c, SCALEKV_ERR_INVALID_ARG, "batch array null");
+  if (b->n_tokens > 0 && b->max_new < 1) return fail(c, SCALEKV_ERR_INVALID_ARG, "max_new must be >= 1 when there are tokens");
+  if (b->table_stride < 0 || b->table_pages < 0 || ((long long)b->table_pages << c->page_shift) > kMaxLength)
+    return fail(c, SCALEKV_ERR_INVALID_ARG, "table_stride or table_pages negative, or a sequence's pages hold more than 2^30 tokens");
+  out = {b->page_table, b->lengths, b->starts, b->table_stride, b->table_pages, b->n_seqs, b->n_tokens};
+  return SCALEKV_OK;
+}
+
+scalekv_status launched(scalekv_paged *c, const char *what) {
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return fail(c, SCALEKV_ERR_CUDA, "launch of %s failed: %s", what, cudaGetErrorString(e));
+  ++c->launches;
+  return SCALEKV_OK;
+}
+
+struct Range {  // an NVTX range around one call
+  explicit Range(const char *name) { nvtxRangePushA(name); }
+  ~Range() { nvtxRangePop(); }
+};
+
+template <bool kWrite, typename T, int D, bool kQ8>
+void launch_store(const Store &s, const Batch &bt, const Rows &K, const Rows &V, int n_rows, cudaStream_t stream) {
+  const int per_block = kStoreThreads / (D / 8) * kRowsPerLane, blocks = (n_rows + per_block - 1) / per_block;
+  const Divisor per_token = Divisor::of(2 * s.heads);
+  if constexpr (kWrite) paged_write_kernel<T, D, kQ8><<<blocks, kStoreThreads, 0, stream>>>(s, bt, K, V, per_token, n_rows);
+  else paged_read_kernel<T, D, kQ8><<<blocks, kStoreThreads, 0, stream>>>(s, bt, K, V, per_token, n_rows);
+}
+
+template <bool kWrite>
+scalekv_status move_rows(scalekv_paged *c, int layer, const scalekv_paged_batch *batch, scalekv_rows K, scalekv_rows V, int dtype, void *stream) {
+  if (!c) return SCALEKV_ERR_INVALID_ARG;
+  Range range(kWrite ? "scalekv.paged_write" : "scalekv.paged_read");
+  Batch bt;
+  if (scalekv_status st = check_batch(c, layer, batch, bt)) return st;
+  if (dtype != SCALEKV_BF16 && dtype != SCALEKV_F32) return fail(c, SCALEKV_ERR_UNSUPPORTED, "rows are bf16 or f32");
+  if (bt.n_tokens == 0) return SCALEKV_OK;
+  const int esize = dtype == SCALEKV_BF16 ? 2 : 4;
+  if (!rows_ok(K, esize) || !rows_ok(V, esize)) return fail(c, SCALEKV_ERR_INVALID_ARG, "K/V null or rows not 16-byte aligned");
+  const long long n_rows = 2ll * c->cfg.n_kv_heads * bt.n_tokens;
+  if (n_rows > 0x7fff0000LL) return fail(c, SCALEKV_ERR_UNSUPPORTED, "more than 2^31 rows in a call");
+  const Store s = layer_store(c, layer);
+  const Rows k = view(K, esize), v = view(V, esize);
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  auto go = [&](auto t, auto dim) {
+    using T = decltype(t);
+    constexpr int D = decltype(dim)::value;
+    if (c->cfg.store == SCALEKV_STORE_Q8) launch_store<kWrite, T, D, true>(s, bt, k, v, (int)n_rows, st);
+    else launch_store<kWrite, T, D, false>(s, bt, k, v, (int)n_rows, st);
+  };
+  auto typed = [&](auto t) {
+    if (c->cfg.head_dim == 128) go(t, std::integral_constant<int, 128>{});
+    else go(t, std::integral_constant<int, 64>{});
+  };
+  if (dtype == SCALEKV_BF16) typed(__nv_bfloat16{}); else typed(float{});
+  return launched(c, kWrite ? "paged_write" : "paged_read");
+}
+
+}  // namespace
+
+extern "C" {
+
+scalekv_status scalekv_paged_query_sizes(const scalekv_paged_config *cfg, size_t *pool_bytes, size_t *workspace_bytes) {
+  Layout y;
+  std::string err;
+  if (scalekv_status st = make_layout(cfg, y, err)) return st;
+  if (pool_bytes) *pool_bytes = y.pool_bytes;
+  if (workspace_bytes) *workspace_bytes = y.ws_bytes;
+  return SCALEKV_OK;
+}
+
+scalekv_status scalekv_paged_init(const scalekv_paged_config *cfg, scalekv_paged **out) {
+  if (!out) return SCALEKV_ERR_INVALID_ARG;
+  *out = nullptr;
+  Layout y;
+  std::string err;
+  scalekv_status st = make_layout(cfg, y, err);
+  if (st) { fprintf(stderr, "scalekv_paged_init: %s\n", err.c_str()); return st; }
+  if (!cfg->pool || !cfg->workspace || (reinterpret_cast<uintptr_t>(cfg->pool) & 255) || (reinterpret_cast<uintptr_t>(cfg->workspace) & 255)) {
+    fprintf(stderr, "scalekv_paged_init: pool and workspace must be 256-byte aligned device pointers\n");
+    return SCALEKV_ERR_INVALID_ARG;
+  }
+  if (cfg->pool_bytes < y.pool_bytes || cfg->workspace_bytes < y.ws_bytes) {
+    fprintf(stderr, "scalekv_paged_init: pool needs %zu bytes, workspace %zu\n", y.pool_bytes, y.ws_bytes);
+    return SCALEKV_ERR_CAPACITY;
+  }
+  scalekv_paged *c = new (std::nothrow) scalekv_paged;
+  if (!c) return SCALEKV_ERR_CAPACITY;
+  c->cfg = *cfg;
+  c->lay = y;
+  while ((1 << c->page_shift) < cfg->page_tokens) ++c->page_shift;
+  if (cudaSetDevice(cfg->device) != cudaSuccess ||
+      cudaDeviceGetAttribute(&c->n_sm, cudaDevAttrMultiProcessorCount, cfg->device) != cudaSuccess ||
+      cudaMemset(cfg->workspace, 0, kStatusBytes) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
+    fprintf(stderr, "scalekv_paged_init: %s\n", cudaGetErrorString(cudaGetLastError()));
+    delete c;
+    return SCALEKV_ERR_CUDA;
+  }
+  *out = c;
+  return SCALEKV_OK;
+}
+
+scalekv_status scalekv_paged_destroy(scalekv_paged *kv) {
+  if (!kv) return SCALEKV_ERR_INVALID_ARG;
+  delete kv;
+  return SCALEKV_OK;
+}
+
+scalekv_status scalekv_paged_write(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, scalekv_rows K, scalekv_rows V, int32_t dtype,
+                                   void *stream) {
+  return move_rows<true>(kv, layer, batch, K, V, dtype, stream);
+}
+
+scalekv_status scalekv_paged_read(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, scalekv_rows K, scalekv_rows V, int32_t dtype,
+                                  void *stream) {
+  return move_rows<false>(kv, layer, batch, K, V, dtype, stream);
+}
+
+scalekv_status scalekv_paged_attend(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, int32_t n_heads, scalekv_rows Q, scalekv_rows O,
+                                    float *lse, const scalekv_paged_mask *mask, float softmax_scale, void *stream) {
+  if (!kv) return SCALEKV_ERR_INVALID_ARG;
+  scalekv_paged *c = kv;
+  Range range("scalekv.paged_attend");
+  AttendArgs a;
+  if (scalekv_status st = check_batch(c, layer, batch, a.bt)) return st;
+  const int H = c->cfg.n_kv_heads, D = c->cfg.head_dim;
+  if (n_heads < 1 || n_heads % H) return fail(c, SCALEKV_ERR_INVALID_ARG, "%d query heads are not a multiple of %d kv heads", n_heads, H);
+  if (!mask || mask->window < 0 || mask->n_sink < 0) return fail(c, SCALEKV_ERR_INVALID_ARG, "mask null, or a negative size in it");
+  if (!std::isfinite(softmax_scale) || softmax_scale < 0.f) return fail(c, SCALEKV_ERR_INVALID_ARG, "softmax_scale must be finite and >= 0");
+  if (a.bt.n_tokens == 0) return SCALEKV_OK;
+  if (!rows_ok(Q, 2) || !rows_ok(O, 2)) return fail(c, SCALEKV_ERR_INVALID_ARG, "Q/O null or rows not 16-byte aligned");
+  const long long all_rows = (long long)a.bt.n_tokens * n_heads;
+  const int G = n_heads / H;
+  const long long max_rows = (long long)std::min(batch->max_new, a.bt.n_tokens) * G;      // query rows of a sequence and kv head
+  if (all_rows > kMaxLength) return fail(c, SCALEKV_ERR_UNSUPPORTED, "more than 2^30 query rows in a call");
+  const long long tiles = (max_rows + kTileRows - 1) / kTileRows;
+  if (tiles * a.bt.n_seqs > 0x7fffffffLL || H > 65535) return fail(c, SCALEKV_ERR_UNSUPPORTED, "too many row tiles in a call");
+  a.s = layer_store(c, layer);
+  a.Q = view(Q, 2); a.O = view(O, 2);
+  a.lse = lse;
+  a.part_o = reinterpret_cast<float *>(static_cast<char *>(c->cfg.workspace) + kStatusBytes);
+  a.part_ml = a.part_o + (size_t)kPartRows * D;
+  a.mask = {mask->causal != 0, std::min(mask->window, kMaxLength), mask->n_sink};
+  a.group = Divisor::of(G);
+  a.n_heads = n_heads;
+  a.max_new = batch->max_new;
+  a.scale_log2e = (softmax_scale > 0.f ? softmax_scale : 1.f / std::sqrt((float)D)) * kLog2e;
+  const long long items = tiles * a.bt.n_seqs * H;
+  long long keys = std::max(batch->max_length, 1);
+  if (a.mask.window > 0) keys = std::min<long long>(keys, (long long)a.mask.window + batch->max_new + a.mask.n_sink);
+  const int steps = (int)((keys + 15) / 16);
+  long long split = std::min<long long>((3ll * c->n_sm + items - 1) / items, (steps + 2 * kStreamWarps - 1) / (2 * kStreamWarps));
+  split = std::max<long long>(1, std::min<long long>(split, kPartRows / all_rows));
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const dim3 grid((unsigned)(tiles * a.bt.n_seqs), H, (unsigned)split);
+  const bool q8 = c->cfg.store == SCALEKV_STORE_Q8;
+  if (D == 128) {
+    if (q8) paged_stream_kernel<128, true><<<grid, kStreamThreads, 0, st>>>(a, (int)tiles);
+    else paged_stream_kernel<128, false><<<grid, kStreamThreads, 0, st>>>(a, (int)tiles);
+  } else {
+    if (q8) paged_stream_kernel<64, true><<<grid, kStreamThreads, 0, st>>>(a, (int)tiles);
+    else paged_stream_kernel<64, false><<<grid, kStreamThreads, 0, st>>>(a, (int)tiles);
+  }
+  if (scalekv_status s = launched(c, "paged_attend")) return s;
+  if (split == 1) return SCALEKV_OK;
+  const unsigned blocks = (unsigned)((all_rows + 7) / 8);
+  if (D == 128) paged_join_kernel<128><<<blocks, 256, 0, st>>>(a, (int)split);
+  else paged_join_kernel<64><<<blocks, 256, 0, st>>>(a, (int)split);
+  return launched(c, "paged_join");
+}
+
+scalekv_status scalekv_paged_sync(scalekv_paged *kv, void *stream) {
+  if (!kv) return SCALEKV_ERR_INVALID_ARG;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int status = 0;
+  cudaError_t e = cudaMemcpyAsync(&status, kv->cfg.workspace, sizeof status, cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e != cudaSuccess) return fail(kv, SCALEKV_ERR_CUDA, "sync: %s", cudaGetErrorString(e));
+  if (status == 0) return SCALEKV_OK;
+  return fail(kv, (scalekv_status)status, status == SCALEKV_ERR_TIMEOUT ? "a device-side wait gave up"
+                                                                        : "a page, length or start of a batch was out of range: its rows were left out");
+}
+
+scalekv_status scalekv_paged_launch_count(scalekv_paged *kv, int64_t *count) {
+  if (!kv || !count) return SCALEKV_ERR_INVALID_ARG;
+  *count = kv->launches;
+  return SCALEKV_OK;
+}
+
+const char *scalekv_paged_error_string(scalekv_paged *kv) { return kv ? kv->err.c_str() : "null handle"; }
+
+}  // extern "C"
