@@ -12,6 +12,7 @@
 #include "../../include/scalekv.h"
 #include "paged_store.cuh"
 #include "paged_stream.cuh"
+#include "paged_tile.cuh"
 
 using namespace scalekv;
 using namespace scalekv::paged;
@@ -114,6 +115,16 @@ void launch_store(const Store &s, const Batch &bt, const Rows &K, const Rows &V,
   const Divisor per_token = Divisor::of(2 * s.heads);
   if constexpr (kWrite) paged_write_kernel<T, D, kQ8><<<blocks, kStoreThreads, 0, stream>>>(s, bt, K, V, per_token, n_rows);
   else paged_read_kernel<T, D, kQ8><<<blocks, kStoreThreads, 0, stream>>>(s, bt, K, V, per_token, n_rows);
+}
+
+template <int D, bool kQ8>
+scalekv_status launch_tile(scalekv_paged *c, const AttendArgs &a, int items, int split, cudaStream_t stream) {
+  constexpr uint32_t smem = TileLayout<D, kQ8>::kSmem;
+  // (per device and process; the answer is the same every time)
+  if (cudaFuncSetAttribute(paged_tile_kernel<D, kQ8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+    return fail(c, SCALEKV_ERR_CUDA, "cannot raise the dynamic shared memory limit");
+  paged_tile_kernel<D, kQ8><<<dim3((unsigned)(items * a.s.heads), (unsigned)split), kTileThreads, smem, stream>>>(a, Divisor::of(a.s.heads), items);
+  return launched(c, "paged_attend");
 }
 
 template <bool kWrite>
@@ -234,23 +245,37 @@ scalekv_status scalekv_paged_attend(scalekv_paged *kv, int32_t layer, const scal
   a.n_heads = n_heads;
   a.max_new = batch->max_new;
   a.scale_log2e = (softmax_scale > 0.f ? softmax_scale : 1.f / std::sqrt((float)D)) * kLog2e;
-  const long long items = tiles * a.bt.n_seqs * H;
   long long keys = std::max(batch->max_length, 1);
   if (a.mask.window > 0) keys = std::min<long long>(keys, (long long)a.mask.window + batch->max_new + a.mask.n_sink);
-  const int steps = (int)((keys + 15) / 16);
-  long long split = std::min<long long>((3ll * c->n_sm + items - 1) / items, (steps + 2 * kStreamWarps - 1) / (2 * kStreamWarps));
-  split = std::max<long long>(1, std::min<long long>(split, kPartRows / all_rows));
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const dim3 grid((unsigned)(tiles * a.bt.n_seqs), H, (unsigned)split);
   const bool q8 = c->cfg.store == SCALEKV_STORE_Q8;
-  if (D == 128) {
-    if (q8) paged_stream_kernel<128, true><<<grid, kStreamThreads, 0, st>>>(a, (int)tiles);
-    else paged_stream_kernel<128, false><<<grid, kStreamThreads, 0, st>>>(a, (int)tiles);
+  long long split;
+  scalekv_status done;
+  if (max_rows <= kTileRows) {
+    const long long items = tiles * a.bt.n_seqs * H;
+    const int steps = (int)((keys + 15) / 16);
+    split = std::min<long long>((3ll * c->n_sm + items - 1) / items, (steps + 2 * kStreamWarps - 1) / (2 * kStreamWarps));
+    split = std::max<long long>(1, std::min<long long>(split, kPartRows / all_rows));
+    const dim3 grid((unsigned)(tiles * a.bt.n_seqs), H, (unsigned)split);
+    if (D == 128) {
+      if (q8) paged_stream_kernel<128, true><<<grid, kStreamThreads, 0, st>>>(a, (int)tiles);
+      else paged_stream_kernel<128, false><<<grid, kStreamThreads, 0, st>>>(a, (int)tiles);
+    } else {
+      if (q8) paged_stream_kernel<64, true><<<grid, kStreamThreads, 0, st>>>(a, (int)tiles);
+      else paged_stream_kernel<64, false><<<grid, kStreamThreads, 0, st>>>(a, (int)tiles);
+    }
+    done = launched(c, "paged_attend");
   } else {
-    if (q8) paged_stream_kernel<64, true><<<grid, kStreamThreads, 0, st>>>(a, (int)tiles);
-    else paged_stream_kernel<64, false><<<grid, kStreamThreads, 0, st>>>(a, (int)tiles);
+    // no more items than this, whatever the starts say
+    const long long items = std::min<long long>((long long)a.bt.n_tokens * G / kItemRows + a.bt.n_seqs, (max_rows + kItemRows - 1) / kItemRows * a.bt.n_seqs);
+    if (items * H > 0x7fffffffLL) return fail(c, SCALEKV_ERR_UNSUPPORTED, "too many row tiles in a call");
+    const long long tiles_k = (keys + kTileKeys - 1) / kTileKeys;
+    split = std::min<long long>(c->n_sm / (items * H), tiles_k / 2);
+    split = std::max<long long>(1, std::min<long long>(split, kPartRows / all_rows));
+    if (D == 128) done = q8 ? launch_tile<128, true>(c, a, (int)items, (int)split, st) : launch_tile<128, false>(c, a, (int)items, (int)split, st);
+    else done = q8 ? launch_tile<64, true>(c, a, (int)items, (int)split, st) : launch_tile<64, false>(c, a, (int)items, (int)split, st);
   }
-  if (scalekv_status s = launched(c, "paged_attend")) return s;
+  if (done) return done;
   if (split == 1) return SCALEKV_OK;
   const unsigned blocks = (unsigned)((all_rows + 7) / 8);
   if (D == 128) paged_join_kernel<128><<<blocks, 256, 0, st>>>(a, (int)split);

@@ -225,13 +225,14 @@ __global__ void __launch_bounds__(kStreamThreads, 3) paged_stream_kernel(const A
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[n][e] *= kQ8 ? a.scale_log2e * ks[2 * n + (e & 1)] : a.scale_log2e;
     const bool whole = page >= 0 && key0 >= lo_full && key0 + 16 <= hi_full;
+    uint32_t hidden = 0;
     if (!whole) {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int pos = key0 + n * 8 + 2 * quad + (e & 1), i = e >> 1;
-          if (page < 0 || pos >= row_hi[i] || (pos < row_lo[i] && pos >= n_sink)) x[n][e] = -INFINITY;
+          if (page < 0 || pos >= row_hi[i] || (pos < row_lo[i] && pos >= n_sink)) { x[n][e] = -INFINITY; hidden |= 1u << (4 * n + e); }
         }
     }
     const int page_next = next;
@@ -272,7 +273,7 @@ __global__ void __launch_bounds__(kStreamThreads, 3) paged_stream_kernel(const A
       if constexpr (kQ8) {
         // (a hidden key counts for nothing even where its scale is no number)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[n][e] = x[n][e] == 0.f ? 0.f : x[n][e] * vs[2 * n + (e & 1)];
+        for (int e = 0; e < 4; ++e) x[n][e] = (hidden >> (4 * n + e)) & 1u ? 0.f : x[n][e] * vs[2 * n + (e & 1)];
       }
       asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[2 * n]) : "f"(x[n][1]), "f"(x[n][0]));
       asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[2 * n + 1]) : "f"(x[n][3]), "f"(x[n][2]));

@@ -1,0 +1,716 @@
+// Attention of many query rows over the paged token cache: chunks of new tokens, on tcgen05.
+//
+// The query rows of a kv head (row r: head r mod G of the group, token r / G) are cut into items of 256, a pair of 128-row tiles A and B;
+// every 128-key tile is brought into shared memory once for both.  An item of 128 rows or fewer is a single: A and B are then the
+// same queries against the even and the odd key tiles, combined at the end.  gridDim.y CTAs share an item's key tiles where there are
+// few items; paged_join_kernel combines what they leave.
+//
+// Roles in a CTA of 512 threads (four warpgroups, registers dealt out by setmaxnreg):
+//   warp 0        : tcgen05.mma issuer.  S_A(0), S_B(0), then per step j  PV_A(j), S_A(j+1), PV_B(j), S_B(j+1): the tensor pipe works
+//                   for one tile while the other's softmax runs.
+//   warps 4-7     : loaders.  Rows go through registers or cp.async, not TMA: a row that no query of the item sees is not read but
+//                   zeroed (unwritten rows and pages given back may hold NaN, and 0 x NaN would reach the accumulators), and codes become bf16 on the way:
+//                   exactly, by integer and one subtract instruction for a pair, into the 128-byte-swizzled tile that the
+//                   products read.  A thread holds the next tile's 16-byte pieces in registers while it converts this one's.
+//   warps 8-15    : softmax, a warpgroup for each tile, a thread for each row (TMEM lane): one sweep over the row's 128 products in
+//                   four chunks of 32, exponentials against a lazy reference (raised when a chunk's sum leaves 2^13), P as bf16 over the products already
+//                   read.  With codes a key's scale is a factor of its column: K's is part of the factor of the exponent's FMA, V's multiplies P
+//                   before it is rounded; both come from shared memory, a broadcast load for four columns.
+// Every wait is bounded; one that gives up raises the sticky status and all roles fall through to the end.
+#pragma once
+#include <type_traits>
+
+#include "paged_stream.cuh"
+#include "tc.cuh"
+
+namespace scalekv {
+namespace paged {
+
+using namespace scalekv::tc;
+
+constexpr int kTileThreads = 512;
+constexpr int kItemRows = 256;
+constexpr int kTileKeys = 128;
+constexpr int kSweepChunks = 4;
+constexpr int kEarly = 3;                         // chunks whose part of the PV product is issued under the rest of the sweep
+constexpr int kScaleSlots = 4;                    // key tiles whose scales are held (see the loaders)
+
+template <int D, bool kQ8>
+struct TileLayout {
+  static constexpr int kStages = kQ8 ? 4 : 5;
+  static constexpr uint32_t kTile = 128 * D * 2, kHalf = 128 * 128;      // an operand tile; 64 columns of it: one 128-byte swizzle span
+  static constexpr uint32_t kOffQ = 0, kOffRing = 2 * kTile, kOffScale = kOffRing + kStages * kTile;
+  static constexpr uint32_t kOffHoles = kOffScale + (kQ8 ? kScaleSlots * 2 * 512 : 0);
+  static constexpr uint32_t kOffBar = kOffHoles + kScaleSlots * 4;
+  enum { bQFull = 0, bFull = 2, bEmpty = bFull + kStages, bSFull = bEmpty + kStages, bPFull = bSFull + 2, bPvDone = bPFull + 2,
+         bFinal = bPvDone + 2, bPEarly = bFinal + 2, bPvEarly = bPEarly + 2, bCount = bPvEarly + 2 };
+  static_assert(bCount <= 32, "one lane of a warp initialises each barrier");
+  static constexpr uint32_t kOffItem = kOffBar + 8 * bCount;             // TMEM address, abort flag, the item
+  static constexpr uint32_t kSmem = kOffItem + 64;
+  static_assert(kSmem <= 232448, "more shared memory than a CTA can have");
+  static_assert(kOffBar % 8 == 0, "barriers are 8 bytes");
+};
+
+// Instruction descriptor: bf16 x bf16 -> fp32, M = 128, N = n, A K-major; B K-major or MN-major.
+__host__ __device__ constexpr uint32_t tile_desc(bool b_mn_major, int n) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
+}
+// The four products of a K-major operand of 64 columns (tc_mma_ss_x8: of 128).
+__device__ __forceinline__ void mma_ss_x4(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc) {
+  asm volatile(
+      "{\n\t.reg .pred e, pf, pt;\n\t.reg .b64 da, db;\n\t.reg .b32 al, bl;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 pf, 0, 0;\n\tsetp.eq.b32 pt, 0, 0;\n\t"
+      "mov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, pf;\n\t"
+      "add.u32 al, %1, 2;\n\tadd.u32 bl, %2, 2;\n\tmov.b64 da, {al, %3};\n\tmov.b64 db, {bl, %3};\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, pt;\n\t"
+      "add.u32 al, %1, 4;\n\tadd.u32 bl, %2, 4;\n\tmov.b64 da, {al, %3};\n\tmov.b64 db, {bl, %3};\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, pt;\n\t"
+      "add.u32 al, %1, 6;\n\tadd.u32 bl, %2, 6;\n\tmov.b64 da, {al, %3};\n\tmov.b64 db, {bl, %3};\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, pt;\n\t"
+      "}" ::"r"(d_tmem),
+      "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc)
+      : "memory");
+}
+template <int kRegs> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs)); }
+template <int kRegs> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs)); }
+__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void store_shared(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ float4 load_shared4(uint32_t at) {
+  float4 x;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(at));
+  return x;
+}
+// 16 bytes from global memory, or zeros
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool on) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+
+// The bounded wait of tc.cuh, without a call: a kernel that deals out its registers by setmaxnreg makes none.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *status) {
+  bool ok = mbar_try(bar, parity);
+  if (!ok) {
+    const unsigned long long t0 = globaltimer();
+    for (int i = 0;; ++i) {
+      if (mbar_try(bar, parity)) { ok = true; break; }
+      if ((i & 63) != 63) continue;
+      if (*abort_flag || *reinterpret_cast<volatile int *>(status) == kDevTimeout) break;
+      if (globaltimer() - t0 > kWaitLimitNs) {
+        *abort_flag = 1;
+        atomicExch(status, kDevTimeout);
+        break;
+      }
+    }
+  }
+  return __all_sync(0xffffffffu, ok);
+}
+
+// What a row sees of a key tile, relative to the tile's first key: columns [lo, hi) and [0, sink), less those of `holes` (a bit for
+// each 16: their page is out of range).
+struct Seen {
+  int lo, hi, sink;
+  uint32_t holes;
+  __device__ __forceinline__ bool operator()(int col) const {
+    return col < hi && (col >= lo || col < sink) && !((holes >> (col >> 4)) & 1u);
+  }
+};
+
+// A chunk whose sum shows that an exponent left the lazy band, or that some row had no reference yet: taken again by the whole warp, from the
+// raw products in columns 32 cc .. of s_addr (P covers columns below 16 cc only).  The reference rises to the chunk's largest exponent
+// where that is larger; the chunk's P is stored against it, and what was accumulated under the old one is multiplied by f = 2^(old - new): the
+// sum, P of the chunks p_first .. cc - 1, and O, once the product that pv_bar stands for has landed.
+struct Risen { float m, l; int o_landed, ok; };
+template <int D, bool kQ8>
+__device__ __forceinline__ Risen raise_row(Seen seen, float c, float m, float l, uint32_t s_addr, uint32_t scales, int cc, int p_first, uint32_t o_addr, int with_o,
+                                        int o_landed, uint32_t pv_bar, uint32_t pv_parity, volatile int *abort_flag, int *status) {
+  float x[32];
+  tc_ld32(s_addr + cc * 32, x);
+  tc_wait_ld();
+  float top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < 32; i += 4) {
+    const float4 k = kQ8 ? load_shared4(scales + (cc * 32 + i) * 4) : make_float4(c, c, c, c);
+    x[i] *= k.x; x[i + 1] *= k.y; x[i + 2] *= k.z; x[i + 3] *= k.w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (!seen(cc * 32 + i + e)) x[i + e] = -INFINITY;
+      top = fmaxf(top, x[i + e]);
+    }
+  }
+  const float m_new = fmaxf(m, top), f = ex2(m - m_new);
+  float sum = 0.f;
+  uint32_t pk[16];
+#pragma unroll
+  for (int i = 0; i < 32; i += 4) {
+    const float4 v = kQ8 ? load_shared4(scales + 512 + (cc * 32 + i) * 4) : make_float4(1.f, 1.f, 1.f, 1.f);
+    float p[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      p[e] = ex2(x[i + e] - m_new);
+      sum += p[e];
+      const float ve = e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w;
+      if (kQ8) p[e] = seen(cc * 32 + i + e) ? p[e] * ve : 0.f;
+    }
+    pk[i / 2] = pack_bf16(p[0], p[1]);
+    pk[i / 2 + 1] = pack_bf16(p[2], p[3]);
+  }
+  tc_st16(s_addr + cc * 16, pk);
+#pragma unroll 1
+  for (int e = p_first; e < cc; ++e) {
+    uint32_t r[16];
+    tc_ld16(s_addr + e * 16, r);
+    tc_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r[i] = pack_bf16(__uint_as_float(r[i] << 16) * f, __uint_as_float(r[i] & 0xffff0000u) * f);
+    tc_st16(s_addr + e * 16, r);
+  }
+  if (with_o) {
+    if (!o_landed) {
+      if (!mbar_wait_warp(pv_bar, pv_parity, abort_flag, status)) return {m_new, l * f + sum, 0, 0};
+      tc_fence_after();
+      o_landed = 1;
+    }
+#pragma unroll 1
+    for (int e = 0; e < D / 32; ++e) {
+      float o[32];
+      tc_ld32(o_addr + e * 32, o);
+      tc_wait_ld();
+#pragma unroll
+      for (int i = 0; i < 32; ++i) o[i] *= f;
+      tc_st32(o_addr + e * 32, o);
+    }
+  }
+  tc_wait_st();
+  return {m_new, l * f + sum, o_landed, 1};
+}
+
+template <int D, bool kQ8>
+__global__ void __launch_bounds__(kTileThreads, 1) paged_tile_kernel(const __grid_constant__ AttendArgs a, const Divisor per_heads, int n_items) {
+  using Y = TileLayout<D, kQ8>;
+  constexpr int kStages = Y::kStages;
+  constexpr uint32_t kTile = Y::kTile, kHalf = Y::kHalf;
+  constexpr uint32_t kColS = 0, kColO = 256;      // S/P buffers at 0 and 128, O accumulators at 256 and 384
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  const uint32_t base = smem_u32(smem_raw);
+  const uint32_t bars = base + Y::kOffBar;
+  auto bar = [&](int i) { return bars + 8u * (uint32_t)i; };
+  volatile int *item = reinterpret_cast<volatile int *>(smem_raw + Y::kOffItem);
+  volatile int *abort_flag = item + 1;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x & 127;
+  const Store &s = a.s;
+  int *status = s.status;
+  const int e = per_heads.div(blockIdx.x), head = (int)blockIdx.x - e * per_heads.d;
+
+  // ---- set-up: barriers, TMEM, and the item.  Items are counted through the sequences, and taken from the end: of a causal chunk the
+  // last rows see most.
+  if (warp == 0) {
+    const int want = n_items - 1 - e;
+    int before = 0, seq = -1, tile = 0;
+    for (int b0 = 0; b0 < a.bt.n_seqs && seq < 0; b0 += 32) {
+      const int b = b0 + lane;
+      int n = 0;
+      if (b < a.bt.n_seqs) {
+        const int st = __ldg(a.bt.starts + b), en = min(__ldg(a.bt.starts + b + 1), a.bt.n_tokens);
+        if (st >= 0 && en > st) n = (int)(((long long)(en - st) * a.group.d + kItemRows - 1) / kItemRows);
+      }
+      int incl = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += up;
+      }
+      const unsigned behind = __ballot_sync(0xffffffffu, before + incl > want);
+      if (behind) {
+        const int src = __ffs(behind) - 1;
+        seq = b0 + src;
+        tile = want - before - (__shfl_sync(0xffffffffu, incl - n, src));
+      }
+      before += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    if (lane == 0) {
+      int start = 0, n_new = 0, length = 0;
+      if (seq >= 0) {
+        start = __ldg(a.bt.starts + seq);
+        n_new = min(__ldg(a.bt.starts + seq + 1), a.bt.n_tokens) - start;
+        length = __ldg(a.bt.lengths + seq);
+        const int room = a.bt.table_pages << s.page_shift;
+        if ((unsigned)length > (unsigned)room || n_new > a.max_new) report(status);
+        length = max(min(length, room), 0);
+      }
+      if (*reinterpret_cast<volatile int *>(status) == kDevTimeout) seq = -1;      // an earlier CTA gave up: do not pile on
+      if (base & 1023u) { report(status); seq = -1; }
+      item[1] = 0;
+      item[2] = seq; item[3] = tile; item[4] = start; item[5] = n_new; item[6] = length;
+    }
+  } else if (warp == 1) {
+    if (lane < Y::bCount) {
+      const bool four = lane < 2 || (lane >= Y::bFull && lane < Y::bFull + kStages) || (lane >= Y::bPFull && lane < Y::bPFull + 2) ||
+                        (lane >= Y::bPEarly && lane < Y::bPEarly + 2);
+      mbar_init(bar(lane), four ? 4u : 1u);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  } else if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + Y::kOffItem), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = (uint32_t)item[0];
+  const int seq = item[2], row0 = item[3] * kItemRows, start = item[4], n_new = item[5], length = item[6];
+  const int first = length - n_new, all = n_new * a.group.d, rows = seq < 0 ? 0 : min(kItemRows, all - row0);
+  const bool pair = rows > 128;
+  // the key tiles that some row of the item sees: the sinks', then those of [lo, hi); this CTA's are lo .. lo + nt - 1 of them
+  int lo_all = 0, hi_all = 0;
+  if (rows > 0) {
+    lo_all = min(seen_lo(a.mask, first + a.group.div(row0)), length);
+    hi_all = seen_hi(a.mask, first + a.group.div(row0 + rows - 1), length);
+  }
+  const int n_sink = a.mask.window > 0 ? a.mask.n_sink : 0;
+  const int lo_tile = lo_all >> 7, hi_tile = max((hi_all + 127) >> 7, lo_tile);
+  const int sink_tiles = min((min(n_sink, hi_all) + 127) >> 7, lo_tile);
+  const int n_tiles = sink_tiles + hi_tile - lo_tile;
+  const int lo = (int)((long long)n_tiles * blockIdx.y / gridDim.y), nt = (int)((long long)n_tiles * (blockIdx.y + 1) / gridDim.y) - lo;
+  auto key_of = [&](int i) { i += lo; return (i < sink_tiles ? i : i - sink_tiles + lo_tile) << 7; };     // first position of key tile i of this CTA
+  const bool shared = !pair && nt > 1;
+  auto n_steps = [&](int qt) { return shared ? (nt + 1 - qt) >> 1 : (pair || qt == 0 ? nt : 0); };
+  auto ring_of = [&](int j, int qt) { return shared ? 4 * j + 2 * qt : 2 * j; };      // ring tile of tile qt's K in step j (its V is the next)
+
+  if (warp < 4) {
+    registers_down<56>();
+    if (warp == 0 && rows > 0) {
+      // -------------------------------------------------------------- MMA issuer (the whole warp walks, one elected lane issues)
+      constexpr uint32_t idesc_qk = tile_desc(false, 128), idesc_pv = tile_desc(true, D), dhi = desc_hi(1024);
+      const bool leader = elect_one();
+      auto mma_s = [&](int kt, int qt) {
+        const uint32_t q = desc_lo(base + Y::kOffQ + (pair && qt ? kTile : 0u), 16), k = desc_lo(base + Y::kOffRing + (kt % kStages) * kTile, 16);
+        if constexpr (D == 128) tc_mma_ss_x8(tmem + kColS + qt * 128, q, k, dhi, idesc_qk);
+        else mma_ss_x4(tmem + kColS + qt * 128, q, k, dhi, idesc_qk);
+      };
+      auto ring_full = [&](int t) { return mbar_wait_warp(bar(Y::bFull + t % kStages), (t / kStages) & 1, abort_flag, status); };
+      const int steps[2] = {n_steps(0), n_steps(1)};
+      bool ok = true;
+      for (int qt = 0; qt < 2 && ok && steps[qt] > 0; ++qt) {
+        const int kt = ring_of(0, qt);
+        ok = mbar_wait_warp(bar(Y::bQFull + (pair ? qt : 0)), 0, abort_flag, status) && ring_full(kt);
+        if (!ok) break;
+        tc_fence_after();
+        mma_s(kt, qt);
+        if (leader) {
+          tc_commit(bar(Y::bSFull + qt));
+          if (!pair || qt == 1) tc_commit(bar(Y::bEmpty + kt % kStages));
+        }
+        __syncwarp();
+      }
+      for (int j = 0; j < steps[0] && ok; ++j) {
+        for (int qt = 0; qt < 2 && ok; ++qt) {
+          if (j >= steps[qt]) break;
+          const bool more = j + 1 < steps[qt];
+          const int vt = ring_of(j, qt) + 1, kt = ring_of(j + 1, qt);
+          const uint32_t vd = desc_lo(base + Y::kOffRing + (vt % kStages) * kTile, kHalf), pa = tmem + kColS + qt * 128, oa = tmem + kColO + qt * 128;
+          ok = ring_full(vt) && mbar_wait_warp(bar(Y::bPEarly + qt), j & 1, abort_flag, status);
+          if (!ok) break;
+          tc_fence_after();
+          tc_mma_ts_n<2 * kEarly>(oa, pa, vd, dhi, idesc_pv, j > 0 ? 1u : 0u);
+          if (leader) tc_commit(bar(Y::bPvEarly + qt));
+          __syncwarp();
+          ok = (!more || ring_full(kt)) && mbar_wait_warp(bar(Y::bPFull + qt), j & 1, abort_flag, status);
+          if (!ok) break;
+          tc_fence_after();
+          tc_mma_ts_n<8 - 2 * kEarly>(oa, pa + p_col(2 * kEarly), vd + 128 * 2 * kEarly, dhi, idesc_pv, 1u);
+          if (more) mma_s(kt, qt);
+          if (leader) {
+            tc_commit(bar((more ? Y::bSFull : Y::bFinal) + qt));
+            tc_commit(bar(Y::bPvDone + qt));
+            if (!pair || qt == 1) {
+              tc_commit(bar(Y::bEmpty + vt % kStages));
+              if (more) tc_commit(bar(Y::bEmpty + kt % kStages));
+            }
+          }
+          __syncwarp();
+        }
+      }
+    }
+  } else if (warp < 8) {
+    registers_down<104>();
+    // ---------------------------------------------------------------- loaders
+    // Ring tile t holds K (even) or V (odd) of key tile t / 2.  The scales of both and the holes go with K, into slot (t / 2) mod
+    // kScaleSlots; that slot's last readers are done: its K tile's stage was released behind a product that was issued after their P.
+    const int w = warp - 4;
+    auto in_use = [&](int pos) { return pos < hi_all && (pos >= lo_all || pos < n_sink); };
+    // pages of key tile i: lane g < 8 has that of keys 16 g .. of the tile, which lie in one
+    auto group_in_use = [&](int i) {
+      const int pos = key_of(i) + 16 * (lane & 7);
+      return pos < hi_all && (pos + 16 > lo_all || pos < n_sink);
+    };
+    auto pages = [&](int i) { return i < nt && group_in_use(i) ? page_of(s, a.bt, seq, key_of(i) + 16 * (lane & 7)) : -1; };
+    auto row_of = [&](int page, int pos) { return store_row(s, max(page, 0), head, pos); };
+    constexpr int kPieces = D / (kQ8 ? 16 : 8), kRowsAtOnce = 128 / kPieces, kIters = 128 / kRowsAtOnce;      // 16-byte pieces of a row
+    const int piece = tid % kPieces, sub = tid / kPieces;
+    constexpr int kRowBytes = D * (kQ8 ? 1 : 2);
+    auto stage_at = [&](int t) { return base + Y::kOffRing + (t % kStages) * kTile; };
+    bool ok = true;
+    auto wait_empty = [&](int t) { return mbar_wait_warp(bar(Y::bEmpty + t % kStages), ((t / kStages) & 1) ^ 1, abort_flag, status); };
+    auto announce = [&](int t) {
+      fence_async_proxy();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(Y::bFull + t % kStages));
+    };
+    int page = pages(0), page_next = pages(1);
+    auto put_holes = [&](int i, int pg) {
+      const uint32_t holes = __ballot_sync(0xffffffffu, lane < 8 && pg < 0 && group_in_use(i));
+      if (w == 0 && lane == 0) asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + Y::kOffHoles + (i % kScaleSlots) * 4), "r"(holes) : "memory");
+    };
+    if constexpr (kQ8) {
+      uint4 buf[2][kIters];
+      float sc[2] = {0.f, 0.f};
+      auto fetch = [&](int t, int pg, uint4 *to) {
+        const char *pool = (t & 1) ? s.v_rows : s.k_rows;
+        const int key0 = key_of(t >> 1);
+#pragma unroll
+        for (int it = 0; it < kIters; ++it) {
+          const int r = it * kRowsAtOnce + sub;
+          const int p = __shfl_sync(0xffffffffu, pg, r >> 4);
+          const bool on = p >= 0 && in_use(key0 + r);
+          to[it] = on ? load_stream(pool + row_of(p, key0 + r) * kRowBytes + piece * 16) : make_uint4(0u, 0u, 0u, 0u);
+        }
+        if (!(t & 1)) {
+          const int p = __shfl_sync(0xffffffffu, pg, tid >> 4);
+          const bool on = p >= 0 && in_use(key0 + tid);
+          const size_t row = row_of(p, key0 + tid);
+          sc[0] = on ? __ldg(s.k_scales + row) * a.scale_log2e : 0.f;
+          sc[1] = on ? __ldg(s.v_scales + row) : 0.f;
+        }
+      };
+      auto convert = [&](int t, const uint4 *from) {
+        if (!(t & 1)) {
+          const uint32_t at = base + Y::kOffScale + ((t >> 1) % kScaleSlots) * 1024 + tid * 4;
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(sc[0]) : "memory");
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 512), "f"(sc[1]) : "memory");
+        }
+        // 16 codes become two 16-byte pieces of a row's 128-byte span; lanes of the second half of a row write theirs the other way
+        // round, so that eight lanes' stores meet all banks
+        const int half = piece >> 2, flip = half;
+        const uint32_t to = stage_at(t) + half * kHalf;
+#pragma unroll
+        for (int it = 0; it < kIters; ++it) {
+          const int r = it * kRowsAtOnce + sub;
+          uint32_t u[8];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            u[2 * k] = codes_bf16(word(from[it], k), 0u, 0x4140);
+            u[2 * k + 1] = codes_bf16(word(from[it], k), 0u, 0x4342);
+          }
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const int q = k ^ flip;
+            const uint32_t at = to + r * 128 + ((((piece & 3) * 2 + q) ^ (r & 7)) << 4);
+            store_shared(at, q ? u[4] : u[0], q ? u[5] : u[1], q ? u[6] : u[2], q ? u[7] : u[3]);
+          }
+        }
+      };
+      if (nt > 0 && rows > 0) fetch(0, page, buf[0]);
+      for (int t = 0; t < 2 * nt && rows > 0 && ok; t += 2) {
+        // K of the tile, while V's pieces are on their way; then V, while the next K's are
+        fetch(t + 1, page, buf[1]);
+        ok = wait_empty(t);
+        if (!ok) break;
+        put_holes(t >> 1, page);
+        convert(t, buf[0]);
+        announce(t);
+        page = page_next;
+        page_next = pages((t >> 1) + 2);
+        if (t + 2 < 2 * nt) fetch(t + 2, page, buf[0]);
+        ok = wait_empty(t + 1);
+        if (!ok) break;
+        convert(t + 1, buf[1]);
+        announce(t + 1);
+      }
+    } else {
+      constexpr int kLag = 2;                     // ring tiles under way before the oldest is waited for
+      int t = 0, told = 0;                        // ring tiles asked for, announced
+      for (; t < 2 * nt && rows > 0; ++t) {
+        if (!__all_sync(0xffffffffu, mbar_try(bar(Y::bEmpty + t % kStages), ((t / kStages) & 1) ^ 1))) {
+          // no stage is free: what is under way is announced first, since the release may be waiting for it
+          asm volatile("cp.async.wait_all;" ::: "memory");
+          for (; told < t; ++told) announce(told);
+          ok = wait_empty(t);
+          if (!ok) break;
+        }
+        if (!(t & 1)) put_holes(t >> 1, page);
+        const char *pool = (t & 1) ? s.v_rows : s.k_rows;
+        const int key0 = key_of(t >> 1);
+        const uint32_t to = stage_at(t) + (piece >> 3) * kHalf;
+#pragma unroll 4
+        for (int it = 0; it < kIters; ++it) {
+          const int r = it * kRowsAtOnce + sub;
+          const int p = __shfl_sync(0xffffffffu, page, r >> 4);
+          const bool on = p >= 0 && in_use(key0 + r);
+          copy16(to + r * 128 + (((piece & 7) ^ (r & 7)) << 4), pool + (on ? row_of(p, key0 + r) * kRowBytes + piece * 16 : 0), on);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (t & 1) {
+          page = page_next;
+          page_next = pages((t >> 1) + 2);
+        }
+        if (t - told >= kLag) {
+          asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
+          announce(told++);
+        }
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");       // (also where this CTA gives up: nothing may land later)
+      if (ok)
+        for (; told < t; ++told) announce(told);
+    }
+  } else {
+    registers_up<176>();
+    // ---------------------------------------------------------------- softmax
+    const int qt = (warp - 8) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+    const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
+    const int tile_row0 = row0 + (pair ? qt * 128 : 0);
+    if (rows > 0 && (pair || qt == 0)) {
+      // the tile's queries: 16 or 8 pieces of 16 bytes a row, swizzled as the products read them; zeros beyond the last row
+      constexpr int kPieces = D / 8, kAtOnce = 128 / kPieces;
+      const int piece = tid % kPieces, sub = tid / kPieces;
+      const uint32_t to = base + Y::kOffQ + qt * kTile + (piece >> 3) * kHalf;
+#pragma unroll 4
+      for (int it = 0; it < kPieces; ++it) {
+        const int r = it * kAtOnce + sub, i = tile_row0 + r;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (i < all) {
+          const int t = a.group.div(i), g = i - t * a.group.d;
+          v = __ldg(reinterpret_cast<const uint4 *>(a.Q.ptr + (start + t) * a.Q.st + (head * a.group.d + g) * a.Q.sh) + piece);
+        }
+        store_shared(to + r * 128 + (((piece & 7) ^ (r & 7)) << 4), v.x, v.y, v.z, v.w);
+      }
+      fence_async_proxy();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(Y::bQFull + qt));
+    }
+    // this row's limits, and those of the warp's rows together
+    const int i_own = tile_row0 + row;
+    const int t_own = a.group.div(max(min(i_own, all - 1), 0));
+    const int row_lo = seen_lo(a.mask, first + t_own), row_hi = seen_hi(a.mask, first + t_own, length);
+    const int warp_lo = __reduce_min_sync(0xffffffffu, row_lo), warp_lo_full = __reduce_max_sync(0xffffffffu, row_lo);
+    const int warp_hi = __reduce_max_sync(0xffffffffu, row_hi), warp_hi_full = __reduce_min_sync(0xffffffffu, row_hi);
+    const float c = a.scale_log2e;
+    const uint64_t c2 = pack2(c, c);
+    float m = -INFINITY, l = 0.f;
+    const uint32_t o_addr = lane_addr + kColO + qt * 128, s_addr = lane_addr + kColS + qt * 128;
+    const int steps = rows > 0 ? n_steps(qt) : 0;
+    bool ok = true;
+    for (int j = 0; j < steps && ok; ++j) {
+      const int i_tile = shared ? 2 * j + qt : j, key0 = key_of(i_tile);
+      ok = mbar_wait_warp(bar(Y::bSFull + qt), j & 1, abort_flag, status);
+      if (!ok) break;
+      tc_fence_after();
+      uint32_t holes;
+      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(holes) : "r"(base + Y::kOffHoles + (i_tile % kScaleSlots) * 4));
+      const uint32_t scales = base + Y::kOffScale + (i_tile % kScaleSlots) * 1024;
+      const Seen seen = {row_lo - key0, row_hi - key0, n_sink - key0, holes};
+      int o_landed = 0;
+      float v[2][32];
+      // p = 2^(x - m) of a chunk in place of its products
+      auto front = [&](float *x, int cc, auto masked) {
+        const uint64_t negm2 = pack2(-m, -m);
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+          uint64_t k0 = c2, k1 = c2;
+          if constexpr (kQ8) {
+            const float4 k = load_shared4(scales + (cc * 32 + i) * 4);
+            k0 = pack2(k.x, k.y);
+            k1 = pack2(k.z, k.w);
+          }
+          float y[4];
+          unpack2(fma2(pack2(x[i], x[i + 1]), k0, negm2), y[0], y[1]);
+          unpack2(fma2(pack2(x[i + 2], x[i + 3]), k1, negm2), y[2], y[3]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if constexpr (decltype(masked)::value)
+              if (!seen(cc * 32 + i + e)) y[e] = -INFINITY;
+            x[i + e] = ex2(y[e]);
+          }
+        }
+      };
+      // 32 values of at most 2^8 sum to at most 2^13; a larger, infinite or NaN sum means that some exponent left the band
+      auto back = [&](const float *p, uint32_t *pk, int cc, auto masked) {
+        uint64_t sum_a = pack2(0.f, 0.f), sum_b = sum_a;
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+          uint64_t p0 = pack2(p[i], p[i + 1]), p1 = pack2(p[i + 2], p[i + 3]);
+          sum_a = add2(sum_a, p0);
+          sum_b = add2(sum_b, p1);
+          float y[4] = {p[i], p[i + 1], p[i + 2], p[i + 3]};
+          if constexpr (kQ8) {
+            const float4 k = load_shared4(scales + 512 + (cc * 32 + i) * 4);
+            unpack2(mul2(p0, pack2(k.x, k.y)), y[0], y[1]);
+            unpack2(mul2(p1, pack2(k.z, k.w)), y[2], y[3]);
+            if constexpr (decltype(masked)::value) {       // (a hidden value's scale may be no number)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (!seen(cc * 32 + i + e)) y[e] = 0.f;
+            }
+          }
+          pk[i / 2] = pack_bf16(y[0], y[1]);
+          pk[i / 2 + 1] = pack_bf16(y[2], y[3]);
+        }
+        float s0, s1, s2, s3;
+        unpack2(sum_a, s0, s1);
+        unpack2(sum_b, s2, s3);
+        return (s0 + s1) + (s2 + s3);
+      };
+      auto sweep = [&](auto masked) {
+        constexpr bool kMasked = decltype(masked)::value;
+        // a chunk that no row of the warp sees: zeros, and no exponentials
+        auto empty = [&](int cc) {
+          const int at = key0 + cc * 32;
+          return kMasked && (at >= warp_hi || (at + 32 <= warp_lo && at >= n_sink));
+        };
+        tc_ld32(s_addr, v[0]);
+        tc_ld32(s_addr + 32, v[1]);
+        tc_wait_ld();
+        if (j == 0) {
+          // no reference yet: the largest of the row's first 32 exponents, or the lowest number where all are hidden
+          float top = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            const float4 k = kQ8 ? load_shared4(scales + i * 4) : make_float4(c, c, c, c);
+            float y[4] = {v[0][i] * k.x, v[0][i + 1] * k.y, v[0][i + 2] * k.z, v[0][i + 3] * k.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (!kMasked || seen(i + e)) top = fmaxf(top, y[e]);
+          }
+          m = fmaxf(top, -FLT_MAX);
+        }
+        if (!empty(0)) front(v[0], 0, masked);
+#pragma unroll
+        for (int cc = 0; cc < kSweepChunks; ++cc) {
+          uint32_t pk[16];
+          const bool next = cc + 1 < kSweepChunks && !empty(cc + 1);
+          if (empty(cc)) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) pk[i] = 0u;
+            if (next) front(v[(cc + 1) & 1], cc + 1, masked);
+            if (cc + 2 < kSweepChunks) tc_ld32(s_addr + (cc + 2) * 32, v[cc & 1]);
+            tc_st16(s_addr + cc * 16, pk);
+          } else {
+            if (next) front(v[(cc + 1) & 1], cc + 1, masked);
+            const float sum = back(v[cc & 1], pk, cc, masked);
+            if (cc + 2 < kSweepChunks) tc_ld32(s_addr + (cc + 2) * 32, v[cc & 1]);
+            if (__any_sync(0xffffffffu, !(sum <= 8192.f))) {
+              const bool late = cc >= kEarly;
+              const Risen r = raise_row<D, kQ8>(seen, c, m, l, s_addr, scales, cc, late ? kEarly : 0, o_addr, (late || j > 0) ? 1 : 0,
+                                                late ? (o_landed == 2) : (o_landed >= 1), bar((late ? Y::bPvEarly : Y::bPvDone) + qt),
+                                                (late ? j : j - 1) & 1, abort_flag, status);
+              ok = __all_sync(0xffffffffu, r.ok != 0);
+              if (!ok) return;
+              m = r.m; l = r.l;
+              if (r.o_landed) o_landed = late ? 2 : 1;
+              if (next) {
+                tc_ld32(s_addr + (cc + 1) * 32, v[(cc + 1) & 1]);
+                tc_wait_ld();
+                front(v[(cc + 1) & 1], cc + 1, masked);
+              }
+            } else {
+              tc_st16(s_addr + cc * 16, pk);
+              l += sum;
+            }
+          }
+          if (cc == kEarly - 1) {
+            tc_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(Y::bPEarly + qt));
+          }
+          if (cc + 2 < kSweepChunks) tc_wait_ld();
+        }
+      };
+      if (holes != 0 || key0 < warp_lo_full || key0 + kTileKeys > warp_hi_full) sweep(std::true_type{}); else sweep(std::false_type{});
+      if (!ok) break;
+      tc_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(Y::bPFull + qt));
+    }
+    // ---- the rows go out: normalised, or, where CTAs share them, as they are with their reference and sum
+    if (steps > 0 && ok) ok = mbar_wait_warp(bar(Y::bFinal + qt), 0, abort_flag, status);
+    tc_fence_after();
+    const bool mine = i_own < all && rows > 0;
+    const int g = i_own - a.group.div(max(i_own, 0)) * a.group.d;
+    const int h = head * a.group.d + g;
+    const size_t all_rows = (size_t)a.bt.n_tokens * a.n_heads, out_row = mine ? (size_t)(start + t_own) * a.n_heads + h : 0;
+    const bool split = gridDim.y > 1;
+    const size_t part = (size_t)blockIdx.y * all_rows + out_row;
+    auto put = [&](float *o, int col0, float f) {          // 32 columns of this row
+      if (!mine) return;
+      if (split) {
+        float4 *to = reinterpret_cast<float4 *>(a.part_o + part * D + col0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) to[i] = make_float4(o[4 * i] * f, o[4 * i + 1] * f, o[4 * i + 2] * f, o[4 * i + 3] * f);
+      } else {
+        uint4 *to = reinterpret_cast<uint4 *>(a.O.ptr + (start + t_own) * a.O.st + h * a.O.sh + col0 * 2);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          to[i] = make_uint4(pack_bf16(o[8 * i] * f, o[8 * i + 1] * f), pack_bf16(o[8 * i + 2] * f, o[8 * i + 3] * f),
+                             pack_bf16(o[8 * i + 4] * f, o[8 * i + 5] * f), pack_bf16(o[8 * i + 6] * f, o[8 * i + 7] * f));
+      }
+    };
+    auto put_sums = [&](float mr, float lr) {
+      if (!mine) return;
+      if (split) *reinterpret_cast<float2 *>(a.part_ml + part * 2) = make_float2(lr == 0.f ? -INFINITY : mr, lr);
+      else if (a.lse != nullptr) a.lse[out_row] = lr == 0.f ? -INFINITY : (mr + log2f(lr)) * kLn2;
+    };
+    if (rows > 0 && ok && !shared && (pair || qt == 0)) {
+      // (a row that saw nothing has a sum of 0 and an accumulator of zeros, or none at all)
+      const float f = split ? 1.f : (l == 0.f ? 0.f : 1.f / l);
+#pragma unroll 1
+      for (int cc = 0; cc < D / 32; ++cc) {
+        float o[32];
+        if (steps > 0) {
+          tc_ld32(o_addr + cc * 32, o);
+          tc_wait_ld();
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] = 0.f;
+        }
+        put(o, cc * 32, f);
+      }
+      put_sums(m, l);
+    } else if (shared) {
+      // the two halves of the keys: both accumulators lie in the same lanes, so only references and sums are handed over (through the
+      // second query tile's place, which a single does not use); each warpgroup finishes half of the columns
+      const uint32_t stat = base + Y::kOffQ + kTile + (uint32_t)row * 8;
+      if (!ok) l = -1.f;                                   // (no sum is negative)
+      asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(stat + (uint32_t)qt * 1024), "f"(m), "f"(l) : "memory");
+      tc_fence_before();
+      asm volatile("bar.sync 2, 256;" ::: "memory");
+      tc_fence_after();
+      float m2, l2;
+      asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(m2), "=f"(l2) : "r"(stat + (uint32_t)(qt ^ 1) * 1024) : "memory");
+      const float top = fmaxf(m, m2);
+      const float f1 = l == 0.f ? 0.f : ex2(m - top), f2 = l2 == 0.f ? 0.f : ex2(m2 - top), sum = l * f1 + l2 * f2;
+      const float f = split ? 1.f : (sum == 0.f ? 0.f : 1.f / sum);
+      if (__all_sync(0xffffffffu, !(l < 0.f || l2 < 0.f))) {
+#pragma unroll 1
+        for (int cc = 0; cc < D / 64; ++cc) {
+          const int col = qt * (D / 2) + cc * 32;
+          float x[32], y[32];
+          tc_ld32(o_addr + col, x);
+          tc_ld32(lane_addr + kColO + (qt ^ 1) * 128 + col, y);
+          tc_wait_ld();
+#pragma unroll
+          for (int i = 0; i < 32; ++i) x[i] = x[i] * f1 + y[i] * f2;
+          put(x, col, f);
+        }
+        if (qt == 0) put_sums(top, sum);
+      }
+    }
+    tc_fence_before();
+  }
+  __syncthreads();
+  if (warp == 2) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
+}
+
+}  // namespace paged
+}  // namespace scalekv

@@ -28,7 +28,8 @@ struct Rows {
   long long st, sh;
 };
 
-__device__ __forceinline__ void report(int *status) { atomicExch(status, kDevCheck); }
+// (a wait that gave up stays on record)
+__device__ __forceinline__ void report(int *status) { atomicCAS(status, 0, kDevCheck); }
 
 // Page of position pos of sequence b, or -1 (reported) where the table has none.
 __device__ __forceinline__ int page_of(const Store &s, const Batch &bt, int b, int pos) {

@@ -41,7 +41,7 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
   return ok != 0;
 }
 // Bounded wait: false when the CTA is aborting or the time limit ran out (status raised).
-__device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *status,
+__device__ __noinline__ inline bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *status,
                                             unsigned long long limit_ns = kWaitLimitNs) {
   const unsigned long long t0 = globaltimer();
   while (true) {
@@ -60,7 +60,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   return mbar_wait_slow(bar, parity, abort_flag, status);
 }
 // For a CTA that gives up: waits for a copy of its own that is still under way, whatever the status, a second at most.
-__device__ __noinline__ void mbar_drain(uint32_t bar, uint32_t parity) {
+__device__ __noinline__ inline void mbar_drain(uint32_t bar, uint32_t parity) {
   const unsigned long long t0 = globaltimer();
   while (!mbar_try(bar, parity) && globaltimer() - t0 < kWaitLimitNs / 2) {}
 }
