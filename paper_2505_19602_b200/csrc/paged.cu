@@ -36,7 +36,11 @@ scalekv_status make_layout(const scalekv_paged_config *c, Layout &y, std::string
   if (c->head_dim != 64 && c->head_dim != 128) { err = "unsupported head_dim: 64 and 128 are built"; return SCALEKV_ERR_UNSUPPORTED; }
   if (c->store != SCALEKV_STORE_BF16 && c->store != SCALEKV_STORE_Q8) { err = "unknown store"; return SCALEKV_ERR_INVALID_ARG; }
   const double rows = (double)c->n_layers * c->n_pages * c->n_kv_heads * c->page_tokens;
-  if (rows > 1e14 || (long long)c->n_pages * c->page_tokens > 0x7fffffffLL) { err = "more than 2^31 - 1 tokens in a layer's pages"; return SCALEKV_ERR_CAPACITY; }
+  if (rows > 1e14 || (long long)c->n_pages * c->page_tokens > 0x7fffffffLL || (long long)c->n_layers * c->n_pages > 0x7fffffffLL ||
+      (long long)c->n_kv_heads * c->page_tokens > 0x7fffffffLL) {
+    err = "more than 2^31 - 1 tokens in a layer's pages, pages in all layers or rows in a page";
+    return SCALEKV_ERR_CAPACITY;
+  }
   const size_t n = (size_t)c->n_layers * c->n_pages * c->n_kv_heads * c->page_tokens;
   y.rows_bytes = n * c->head_dim * (c->store == SCALEKV_STORE_Q8 ? 1 : 2);
   y.scale_bytes = c->store == SCALEKV_STORE_Q8 ? n * 4 : 0;
@@ -52,6 +56,7 @@ struct scalekv_paged {
   Layout lay;
   int n_sm = 148, page_shift = 0;
   int64_t launches = 0;
+  TileMaps maps;
   std::string err = "ok";
 };
 
@@ -118,12 +123,13 @@ void launch_store(const Store &s, const Batch &bt, const Rows &K, const Rows &V,
 }
 
 template <int D, bool kQ8>
-scalekv_status launch_tile(scalekv_paged *c, const AttendArgs &a, int items, int split, cudaStream_t stream) {
+scalekv_status launch_tile(scalekv_paged *c, int layer, const AttendArgs &a, int items, int split, cudaStream_t stream) {
   constexpr uint32_t smem = TileLayout<D, kQ8>::kSmem;
   // (per device and process; the answer is the same every time)
   if (cudaFuncSetAttribute(paged_tile_kernel<D, kQ8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
     return fail(c, SCALEKV_ERR_CUDA, "cannot raise the dynamic shared memory limit");
-  paged_tile_kernel<D, kQ8><<<dim3((unsigned)(items * a.s.heads), (unsigned)split), kTileThreads, smem, stream>>>(a, Divisor::of(a.s.heads), items);
+  paged_tile_kernel<D, kQ8><<<dim3((unsigned)(items * a.s.heads), (unsigned)split), TileLayout<D, kQ8>::kThreads, smem, stream>>>(
+      c->maps.k, c->maps.v, a, Divisor::of(a.s.heads), items, layer * c->cfg.n_pages);
   return launched(c, "paged_attend");
 }
 
@@ -193,6 +199,12 @@ scalekv_status scalekv_paged_init(const scalekv_paged_config *cfg, scalekv_paged
       cudaDeviceGetAttribute(&c->n_sm, cudaDevAttrMultiProcessorCount, cfg->device) != cudaSuccess ||
       cudaMemset(cfg->workspace, 0, kStatusBytes) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
     fprintf(stderr, "scalekv_paged_init: %s\n", cudaGetErrorString(cudaGetLastError()));
+    delete c;
+    return SCALEKV_ERR_CUDA;
+  }
+  if (!c->maps.make(cfg->pool, static_cast<char *>(cfg->pool) + y.rows_bytes, (long long)cfg->n_layers * cfg->n_pages, cfg->n_kv_heads, cfg->page_tokens,
+                    cfg->head_dim, cfg->store == SCALEKV_STORE_Q8, err)) {
+    fprintf(stderr, "scalekv_paged_init: %s\n", err.c_str());
     delete c;
     return SCALEKV_ERR_CUDA;
   }
@@ -272,8 +284,8 @@ scalekv_status scalekv_paged_attend(scalekv_paged *kv, int32_t layer, const scal
     const long long tiles_k = (keys + kTileKeys - 1) / kTileKeys;
     split = std::min<long long>(c->n_sm / (items * H), tiles_k / 2);
     split = std::max<long long>(1, std::min<long long>(split, kPartRows / all_rows));
-    if (D == 128) done = q8 ? launch_tile<128, true>(c, a, (int)items, (int)split, st) : launch_tile<128, false>(c, a, (int)items, (int)split, st);
-    else done = q8 ? launch_tile<64, true>(c, a, (int)items, (int)split, st) : launch_tile<64, false>(c, a, (int)items, (int)split, st);
+    if (D == 128) done = q8 ? launch_tile<128, true>(c, layer, a, (int)items, (int)split, st) : launch_tile<128, false>(c, layer, a, (int)items, (int)split, st);
+    else done = q8 ? launch_tile<64, true>(c, layer, a, (int)items, (int)split, st) : launch_tile<64, false>(c, layer, a, (int)items, (int)split, st);
   }
   if (done) return done;
   if (split == 1) return SCALEKV_OK;

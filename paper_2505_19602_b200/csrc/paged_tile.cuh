@@ -5,19 +5,22 @@
 // same queries against the even and the odd key tiles, combined at the end.  gridDim.y CTAs share an item's key tiles where there are
 // few items; paged_join_kernel combines what they leave.
 //
-// Roles in a CTA of 512 threads (four warpgroups, registers dealt out by setmaxnreg):
+// Roles in a CTA, by warpgroup (registers dealt out by setmaxnreg):
 //   warp 0        : tcgen05.mma issuer.  S_A(0), S_B(0), then per step j  PV_A(j), S_A(j+1), PV_B(j), S_B(j+1): the tensor pipe works
 //                   for one tile while the other's softmax runs.
-//   warps 4-7     : loaders.  Rows go through registers or cp.async, not TMA: a row that no query of the item sees is not read but
-//                   zeroed (unwritten rows and pages given back may hold NaN, and 0 x NaN would reach the accumulators), and codes become bf16 on the way:
-//                   exactly, by integer and one subtract instruction for a pair, into the 128-byte-swizzled tile that the
-//                   products read.  A thread holds the next tile's 16-byte pieces in registers while it converts this one's.
-//   warps 8-15    : softmax, a warpgroup for each tile, a thread for each row (TMEM lane): one sweep over the row's 128 products in
+//   warp 1        : TMA producer: the tile's rows, page by page, into a ring of operand tiles K_0, V_0, K_1, V_1, ...  bf16 rows land as the
+//                   products read them (128-byte swizzle), codes in the first half of their stage.
+//   warps 4-7     : with codes only, converters.  A thread takes its codes out of the stage, waits for the others' and puts them back as bf16: exactly, by
+//                   integer instructions and one subtraction for a pair.  They also bring the scales.
+//   the last eight: softmax, a warpgroup for each tile, a thread for each row (TMEM lane): one sweep over the row's 128 products in
 //                   four chunks of 32, exponentials against a lazy reference (raised when a chunk's sum leaves 2^13), P as bf16 over the products already
 //                   read.  With codes a key's scale is a factor of its column: K's is part of the factor of the exponent's FMA, V's multiplies P
 //                   before it is rounded; both come from shared memory, a broadcast load for four columns.
+// Rows that no query of the item sees (behind the length, ahead of the window, on a page out of range) may hold anything.  Their products are hidden one
+// by one; as values codes are numbers whatever they are, and bf16 rows are zeroed by the issuer before the product reads them.
 // Every wait is bounded; one that gives up raises the sticky status and all roles fall through to the end.
 #pragma once
+#include <string>
 #include <type_traits>
 
 #include "paged_stream.cuh"
@@ -28,7 +31,6 @@ namespace paged {
 
 using namespace scalekv::tc;
 
-constexpr int kTileThreads = 512;
 constexpr int kItemRows = 256;
 constexpr int kTileKeys = 128;
 constexpr int kSweepChunks = 4;
@@ -37,13 +39,17 @@ constexpr int kScaleSlots = 4;                    // key tiles whose scales are 
 
 template <int D, bool kQ8>
 struct TileLayout {
+  static constexpr int kThreads = kQ8 ? 512 : 384, kSoftmaxWarp = kQ8 ? 8 : 4;
+  // registers of a thread of the first warpgroup, of the converters, of softmax: shares of what the block was launched with
+  static constexpr int kRegs0 = kQ8 ? 56 : 72, kRegs1 = 104, kRegsS = kQ8 ? 176 : 216, kRegsLaunch = kQ8 ? 128 : 168;
+  static_assert(kRegs0 + (kQ8 ? kRegs1 : 0) + 2 * kRegsS <= kRegsLaunch * (kThreads / 128), "a share would wait for registers that nobody returns");
   static constexpr int kStages = kQ8 ? 4 : 5;
   static constexpr uint32_t kTile = 128 * D * 2, kHalf = 128 * 128;      // an operand tile; 64 columns of it: one 128-byte swizzle span
   static constexpr uint32_t kOffQ = 0, kOffRing = 2 * kTile, kOffScale = kOffRing + kStages * kTile;
   static constexpr uint32_t kOffHoles = kOffScale + (kQ8 ? kScaleSlots * 2 * 512 : 0);
   static constexpr uint32_t kOffBar = kOffHoles + kScaleSlots * 4;
   enum { bQFull = 0, bFull = 2, bEmpty = bFull + kStages, bSFull = bEmpty + kStages, bPFull = bSFull + 2, bPvDone = bPFull + 2,
-         bFinal = bPvDone + 2, bPEarly = bFinal + 2, bPvEarly = bPEarly + 2, bCount = bPvEarly + 2 };
+         bFinal = bPvDone + 2, bPEarly = bFinal + 2, bPvEarly = bPEarly + 2, bRaw = bPvEarly + 2, bCount = bRaw + (kQ8 ? kStages : 0) };
   static_assert(bCount <= 32, "one lane of a warp initialises each barrier");
   static constexpr uint32_t kOffItem = kOffBar + 8 * bCount;             // TMEM address, abort flag, the item
   static constexpr uint32_t kSmem = kOffItem + 64;
@@ -79,9 +85,15 @@ __device__ __forceinline__ float4 load_shared4(uint32_t at) {
   asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(at));
   return x;
 }
-// 16 bytes from global memory, or zeros
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool on) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+__device__ __forceinline__ uint4 load_shared16(uint32_t at) {
+  uint4 x;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(at));
+  return x;
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *tm, int x, int y, int z, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+               "l"(tm), "r"(x), "r"(y), "r"(z), "r"(bar)
+               : "memory");
 }
 
 // The bounded wait of tc.cuh, without a call: a kernel that deals out its registers by setmaxnreg makes none.
@@ -182,8 +194,11 @@ __device__ __forceinline__ Risen raise_row(Seen seen, float c, float m, float l,
   return {m_new, l * f + sum, o_landed, 1};
 }
 
+// tmK, tmV: the K and V rows of all layers, [layer * pages + page][kv head * page_tokens + row][head_dim]; page0: layer * pages
 template <int D, bool kQ8>
-__global__ void __launch_bounds__(kTileThreads, 1) paged_tile_kernel(const __grid_constant__ AttendArgs a, const Divisor per_heads, int n_items) {
+__global__ void __launch_bounds__(TileLayout<D, kQ8>::kThreads, 1)
+paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ AttendArgs a,
+                  const Divisor per_heads, int n_items, int page0) {
   using Y = TileLayout<D, kQ8>;
   constexpr int kStages = Y::kStages;
   constexpr uint32_t kTile = Y::kTile, kHalf = Y::kHalf;
@@ -242,7 +257,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tile_kernel(const __gri
     }
   } else if (warp == 1) {
     if (lane < Y::bCount) {
-      const bool four = lane < 2 || (lane >= Y::bFull && lane < Y::bFull + kStages) || (lane >= Y::bPFull && lane < Y::bPFull + 2) ||
+      // arrivals a phase: one lane of each of four warps for what a warpgroup hands over, else the producer or a commit
+      const bool four = lane < 2 || (kQ8 && lane >= Y::bFull && lane < Y::bFull + kStages) || (lane >= Y::bPFull && lane < Y::bPFull + 2) ||
                         (lane >= Y::bPEarly && lane < Y::bPEarly + 2);
       mbar_init(bar(lane), four ? 4u : 1u);
     }
@@ -274,8 +290,16 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tile_kernel(const __gri
   auto n_steps = [&](int qt) { return shared ? (nt + 1 - qt) >> 1 : (pair || qt == 0 ? nt : 0); };
   auto ring_of = [&](int j, int qt) { return shared ? 4 * j + 2 * qt : 2 * j; };      // ring tile of tile qt's K in step j (its V is the next)
 
+  auto in_use = [&](int pos) { return pos < hi_all && (pos >= lo_all || pos < n_sink); };       // some row of the item sees it
+  // pages of key tile i: lane g (mod 8) has that of keys 16 g .. of the tile, which lie in one; -1: nobody looks there, or it is out of range
+  auto group_in_use = [&](int i) {
+    const int pos = key_of(i) + 16 * (lane & 7);
+    return pos < hi_all && (pos + 16 > lo_all || pos < n_sink);
+  };
+  auto pages = [&](int i) { return i < nt && group_in_use(i) ? page_of(s, a.bt, seq, key_of(i) + 16 * (lane & 7)) : -1; };
+
   if (warp < 4) {
-    registers_down<56>();
+    registers_down<Y::kRegs0>();
     if (warp == 0 && rows > 0) {
       // -------------------------------------------------------------- MMA issuer (the whole warp walks, one elected lane issues)
       constexpr uint32_t idesc_qk = tile_desc(false, 128), idesc_pv = tile_desc(true, D), dhi = desc_hi(1024);
@@ -287,6 +311,21 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tile_kernel(const __gri
       };
       auto ring_full = [&](int t) { return mbar_wait_warp(bar(Y::bFull + t % kStages), (t / kStages) & 1, abort_flag, status); };
       const int steps[2] = {n_steps(0), n_steps(1)};
+      // hidden rows of a tile of bf16 values become zeros before a product reads them: P is 0 there, and 0 x NaN is NaN
+      auto clean = [&](int vt) {
+        const int key0 = key_of(vt >> 1);
+        uint32_t holes;
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(holes) : "r"(base + Y::kOffHoles + ((vt >> 1) % kScaleSlots) * 4));
+        if (key0 >= lo_all && key0 + kTileKeys <= hi_all && holes == 0) return;
+        const uint32_t tile = base + Y::kOffRing + (vt % kStages) * kTile;
+        for (int r = lane; r < kTileKeys; r += 32) {
+          if (in_use(key0 + r) && !((holes >> (r >> 4)) & 1u)) continue;
+#pragma unroll 1
+          for (int x = 0; x < D / 8; ++x) store_shared(tile + (x >> 3) * kHalf + r * 128 + (x & 7) * 16, 0u, 0u, 0u, 0u);
+        }
+        fence_async_proxy();
+        __syncwarp();
+      };
       bool ok = true;
       for (int qt = 0; qt < 2 && ok && steps[qt] > 0; ++qt) {
         const int kt = ring_of(0, qt);
@@ -306,7 +345,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tile_kernel(const __gri
           const bool more = j + 1 < steps[qt];
           const int vt = ring_of(j, qt) + 1, kt = ring_of(j + 1, qt);
           const uint32_t vd = desc_lo(base + Y::kOffRing + (vt % kStages) * kTile, kHalf), pa = tmem + kColS + qt * 128, oa = tmem + kColO + qt * 128;
-          ok = ring_full(vt) && mbar_wait_warp(bar(Y::bPEarly + qt), j & 1, abort_flag, status);
+          ok = ring_full(vt);
+          if (!ok) break;
+          if (!kQ8 && (!pair || qt == 0)) clean(vt);
+          ok = mbar_wait_warp(bar(Y::bPEarly + qt), j & 1, abort_flag, status);
           if (!ok) break;
           tc_fence_after();
           tc_mma_ts_n<2 * kEarly>(oa, pa, vd, dhi, idesc_pv, j > 0 ? 1u : 0u);
@@ -328,142 +370,104 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tile_kernel(const __gri
           __syncwarp();
         }
       }
-    }
-  } else if (warp < 8) {
-    registers_down<104>();
-    // ---------------------------------------------------------------- loaders
-    // Ring tile t holds K (even) or V (odd) of key tile t / 2.  The scales of both and the holes go with K, into slot (t / 2) mod
-    // kScaleSlots; that slot's last readers are done: its K tile's stage was released behind a product that was issued after their P.
-    const int w = warp - 4;
-    auto in_use = [&](int pos) { return pos < hi_all && (pos >= lo_all || pos < n_sink); };
-    // pages of key tile i: lane g < 8 has that of keys 16 g .. of the tile, which lie in one
-    auto group_in_use = [&](int i) {
-      const int pos = key_of(i) + 16 * (lane & 7);
-      return pos < hi_all && (pos + 16 > lo_all || pos < n_sink);
-    };
-    auto pages = [&](int i) { return i < nt && group_in_use(i) ? page_of(s, a.bt, seq, key_of(i) + 16 * (lane & 7)) : -1; };
-    auto row_of = [&](int page, int pos) { return store_row(s, max(page, 0), head, pos); };
-    constexpr int kPieces = D / (kQ8 ? 16 : 8), kRowsAtOnce = 128 / kPieces, kIters = 128 / kRowsAtOnce;      // 16-byte pieces of a row
-    const int piece = tid % kPieces, sub = tid / kPieces;
-    constexpr int kRowBytes = D * (kQ8 ? 1 : 2);
-    auto stage_at = [&](int t) { return base + Y::kOffRing + (t % kStages) * kTile; };
-    bool ok = true;
-    auto wait_empty = [&](int t) { return mbar_wait_warp(bar(Y::bEmpty + t % kStages), ((t / kStages) & 1) ^ 1, abort_flag, status); };
-    auto announce = [&](int t) {
-      fence_async_proxy();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(Y::bFull + t % kStages));
-    };
-    int page = pages(0), page_next = pages(1);
-    auto put_holes = [&](int i, int pg) {
-      const uint32_t holes = __ballot_sync(0xffffffffu, lane < 8 && pg < 0 && group_in_use(i));
-      if (w == 0 && lane == 0) asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + Y::kOffHoles + (i % kScaleSlots) * 4), "r"(holes) : "memory");
-    };
-    if constexpr (kQ8) {
-      uint4 buf[2][kIters];
-      float sc[2] = {0.f, 0.f};
-      auto fetch = [&](int t, int pg, uint4 *to) {
-        const char *pool = (t & 1) ? s.v_rows : s.k_rows;
-        const int key0 = key_of(t >> 1);
-#pragma unroll
-        for (int it = 0; it < kIters; ++it) {
-          const int r = it * kRowsAtOnce + sub;
-          const int p = __shfl_sync(0xffffffffu, pg, r >> 4);
-          const bool on = p >= 0 && in_use(key0 + r);
-          to[it] = on ? load_stream(pool + row_of(p, key0 + r) * kRowBytes + piece * 16) : make_uint4(0u, 0u, 0u, 0u);
-        }
-        if (!(t & 1)) {
-          const int p = __shfl_sync(0xffffffffu, pg, tid >> 4);
-          const bool on = p >= 0 && in_use(key0 + tid);
-          const size_t row = row_of(p, key0 + tid);
-          sc[0] = on ? __ldg(s.k_scales + row) * a.scale_log2e : 0.f;
-          sc[1] = on ? __ldg(s.v_scales + row) : 0.f;
-        }
-      };
-      auto convert = [&](int t, const uint4 *from) {
-        if (!(t & 1)) {
-          const uint32_t at = base + Y::kOffScale + ((t >> 1) % kScaleSlots) * 1024 + tid * 4;
-          asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(sc[0]) : "memory");
-          asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 512), "f"(sc[1]) : "memory");
-        }
-        // 16 codes become two 16-byte pieces of a row's 128-byte span; lanes of the second half of a row write theirs the other way
-        // round, so that eight lanes' stores meet all banks
-        const int half = piece >> 2, flip = half;
-        const uint32_t to = stage_at(t) + half * kHalf;
-#pragma unroll
-        for (int it = 0; it < kIters; ++it) {
-          const int r = it * kRowsAtOnce + sub;
-          uint32_t u[8];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            u[2 * k] = codes_bf16(word(from[it], k), 0u, 0x4140);
-            u[2 * k + 1] = codes_bf16(word(from[it], k), 0u, 0x4342);
-          }
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const int q = k ^ flip;
-            const uint32_t at = to + r * 128 + ((((piece & 3) * 2 + q) ^ (r & 7)) << 4);
-            store_shared(at, q ? u[4] : u[0], q ? u[5] : u[1], q ? u[6] : u[2], q ? u[7] : u[3]);
-          }
-        }
-      };
-      if (nt > 0 && rows > 0) fetch(0, page, buf[0]);
-      for (int t = 0; t < 2 * nt && rows > 0 && ok; t += 2) {
-        // K of the tile, while V's pieces are on their way; then V, while the next K's are
-        fetch(t + 1, page, buf[1]);
-        ok = wait_empty(t);
+    } else if (warp == 1 && rows > 0) {
+      // -------------------------------------------------------------- TMA producer (the whole warp walks, one elected lane issues)
+      // Ring tile t holds K (even) or V (odd) of key tile t / 2, which bRaw (codes) or bFull says.  A tile's holes go with its K.
+      const int box = min(1 << s.page_shift, kTileKeys), in_page = (1 << s.page_shift) - 1;
+      constexpr int kLanded = kQ8 ? Y::bRaw : Y::bFull;
+      constexpr uint32_t kRowBytes = D * (kQ8 ? 1 : 2);
+      int page = pages(0), page_next = pages(1), t = 0;
+      bool ok = true;
+      for (; t < 2 * nt; ++t) {
+        const int st = t % kStages, key0 = key_of(t >> 1);
+        ok = mbar_wait_warp(bar(Y::bEmpty + st), ((t / kStages) & 1) ^ 1, abort_flag, status);
         if (!ok) break;
-        put_holes(t >> 1, page);
-        convert(t, buf[0]);
-        announce(t);
-        page = page_next;
-        page_next = pages((t >> 1) + 2);
-        if (t + 2 < 2 * nt) fetch(t + 2, page, buf[0]);
-        ok = wait_empty(t + 1);
-        if (!ok) break;
-        convert(t + 1, buf[1]);
-        announce(t + 1);
-      }
-    } else {
-      constexpr int kLag = 2;                     // ring tiles under way before the oldest is waited for
-      int t = 0, told = 0;                        // ring tiles asked for, announced
-      for (; t < 2 * nt && rows > 0; ++t) {
-        if (!__all_sync(0xffffffffu, mbar_try(bar(Y::bEmpty + t % kStages), ((t / kStages) & 1) ^ 1))) {
-          // no stage is free: what is under way is announced first, since the release may be waiting for it
-          asm volatile("cp.async.wait_all;" ::: "memory");
-          for (; told < t; ++told) announce(told);
-          ok = wait_empty(t);
-          if (!ok) break;
+        const uint32_t there = __ballot_sync(0xffffffffu, page >= 0) & 0xffu, used = __ballot_sync(0xffffffffu, group_in_use(t >> 1)) & 0xffu;
+        if (!(t & 1) && lane == 0)
+          asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + Y::kOffHoles + ((t >> 1) % kScaleSlots) * 4), "r"(used & ~there) : "memory");
+        // boxes whose first group in use has a page (the groups of a box share it)
+        const CUtensorMap *tm = (t & 1) ? &tmV : &tmK;
+        uint32_t boxes = 0;
+        for (int r0 = 0; r0 < kTileKeys; r0 += box)
+          if ((there >> (r0 >> 4)) & ((1u << (box >> 4)) - 1u)) ++boxes;
+        if (elect_one()) mbar_expect_tx(bar(kLanded + st), boxes * box * kRowBytes);
+        __syncwarp();
+        for (int r0 = 0; r0 < kTileKeys; r0 += box) {
+          const uint32_t mine = (there >> (r0 >> 4)) & ((1u << (box >> 4)) - 1u);
+          if (!mine) continue;
+          const int pg = __shfl_sync(0xffffffffu, page, (r0 >> 4) + __ffs(mine) - 1);
+          if (elect_one()) {
+            const int y = (head << s.page_shift) + ((key0 + r0) & in_page), z = page0 + pg;
+            const uint32_t dst = base + Y::kOffRing + st * kTile + r0 * (kQ8 ? D : 128);
+            tma_load_3d(dst, tm, 0, y, z, bar(kLanded + st));
+            if constexpr (!kQ8 && D == 128) tma_load_3d(dst + kHalf, tm, 64, y, z, bar(kLanded + st));
+          }
+          __syncwarp();
         }
-        if (!(t & 1)) put_holes(t >> 1, page);
-        const char *pool = (t & 1) ? s.v_rows : s.k_rows;
-        const int key0 = key_of(t >> 1);
-        const uint32_t to = stage_at(t) + (piece >> 3) * kHalf;
-#pragma unroll 4
-        for (int it = 0; it < kIters; ++it) {
-          const int r = it * kRowsAtOnce + sub;
-          const int p = __shfl_sync(0xffffffffu, page, r >> 4);
-          const bool on = p >= 0 && in_use(key0 + r);
-          copy16(to + r * 128 + (((piece & 7) ^ (r & 7)) << 4), pool + (on ? row_of(p, key0 + r) * kRowBytes + piece * 16 : 0), on);
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
         if (t & 1) {
           page = page_next;
           page_next = pages((t >> 1) + 2);
         }
-        if (t - told >= kLag) {
-          asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
-          announce(told++);
+      }
+      if (!ok) {
+        // this CTA gives up: nothing may land in its shared memory once it is gone (a second at most)
+        for (int k = max(t - kStages, 0); k < t; ++k) {
+          const unsigned long long t0 = globaltimer();
+          while (!mbar_try(bar(kLanded + k % kStages), (k / kStages) & 1) && globaltimer() - t0 < kWaitLimitNs / 2) {}
         }
       }
-      asm volatile("cp.async.wait_all;" ::: "memory");       // (also where this CTA gives up: nothing may land later)
-      if (ok)
-        for (; told < t; ++told) announce(told);
+    }
+  } else if (kQ8 && warp < 8) {
+    registers_down<Y::kRegs1>();
+    // ---------------------------------------------------------------- converters
+    // The scales of both go with K, into slot (t / 2) mod kScaleSlots; that slot's last readers are done: the stage of this K was
+    // released behind a product that was issued after their P.
+    constexpr int kPieces = D / 16, kRowsAtOnce = 128 / kPieces, kIters = 128 / kRowsAtOnce;      // 16 codes a piece
+    const int piece = tid % kPieces, sub = tid / kPieces, half = piece >> 2;
+    float k_scale = 0.f, v_scale = 0.f;
+    auto fetch_scales = [&](int i) {
+      const int page = __shfl_sync(0xffffffffu, pages(i), tid >> 4), pos = key_of(i) + tid;
+      const bool on = page >= 0 && in_use(pos);
+      const size_t row = store_row(s, max(page, 0), head, pos);
+      k_scale = on ? __ldg(s.k_scales + row) * a.scale_log2e : 0.f;
+      v_scale = on ? __ldg(s.v_scales + row) : 0.f;
+    };
+    bool ok = true;
+    if (nt > 0 && rows > 0) fetch_scales(0);
+    for (int t = 0; t < 2 * nt && rows > 0; ++t) {
+      const uint32_t stage = base + Y::kOffRing + (t % kStages) * kTile;
+      ok = mbar_wait_warp(bar(Y::bRaw + t % kStages), (t / kStages) & 1, abort_flag, status);
+      if (!ok) break;
+      uint4 raw[kIters];
+#pragma unroll
+      for (int it = 0; it < kIters; ++it) raw[it] = load_shared16(stage + (it * kRowsAtOnce + sub) * D + piece * 16);
+      if (!(t & 1)) {
+        const uint32_t at = base + Y::kOffScale + ((t >> 1) % kScaleSlots) * 1024 + tid * 4;
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(k_scale) : "memory");
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 512), "f"(v_scale) : "memory");
+        if ((t >> 1) + 1 < nt) fetch_scales((t >> 1) + 1);
+      }
+      asm volatile("bar.sync 3, 128;" ::: "memory");          // all codes are out of the stage
+      // 16 codes become two 16-byte pieces of a row's 128-byte span; lanes of the second half of a row write theirs the other way
+      // round, so that eight lanes' stores meet all banks
+      const uint32_t to = stage + half * kHalf;
+#pragma unroll
+      for (int it = 0; it < kIters; ++it) {
+        const int r = it * kRowsAtOnce + sub;
+        const uint32_t w[4] = {half ? raw[it].z : raw[it].x, half ? raw[it].w : raw[it].y, half ? raw[it].x : raw[it].z, half ? raw[it].y : raw[it].w};
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          store_shared(to + r * 128 + ((((piece & 3) * 2 + (k ^ half)) ^ (r & 7)) << 4), codes_bf16(w[2 * k], 0u, 0x4140), codes_bf16(w[2 * k], 0u, 0x4342),
+                       codes_bf16(w[2 * k + 1], 0u, 0x4140), codes_bf16(w[2 * k + 1], 0u, 0x4342));
+      }
+      fence_async_proxy();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(Y::bFull + t % kStages));
     }
   } else {
-    registers_up<176>();
+    registers_up<Y::kRegsS>();
     // ---------------------------------------------------------------- softmax
-    const int qt = (warp - 8) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+    const int qt = (warp - Y::kSoftmaxWarp) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
     const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
     const int tile_row0 = row0 + (pair ? qt * 128 : 0);
     if (rows > 0 && (pair || qt == 0)) {
@@ -711,6 +715,36 @@ __global__ void __launch_bounds__(kTileThreads, 1) paged_tile_kernel(const __gri
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
   }
 }
+
+// The tensor maps of a pool's rows, made once.
+struct TileMaps {
+  CUtensorMap k, v;
+  bool make(void *k_rows, void *v_rows, long long pages, int heads, int page_tokens, int head_dim, bool q8, std::string &err) {
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess || !fn) {
+      err = "cuTensorMapEncodeTiled not available";
+      return false;
+    }
+    const auto encode = reinterpret_cast<CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                                      const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                                      CUtensorMapL2promotion, CUtensorMapFloatOOBfill)>(fn);
+    const size_t row = (size_t)head_dim * (q8 ? 1 : 2);
+    const cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)heads * page_tokens, (cuuint64_t)pages};
+    const cuuint64_t strides[2] = {row, row * heads * page_tokens};
+    const cuuint32_t box[3] = {(cuuint32_t)(q8 ? head_dim : 64), (cuuint32_t)(page_tokens < kTileKeys ? page_tokens : kTileKeys), 1}, step[3] = {1, 1, 1};
+    for (int i = 0; i < 2; ++i) {
+      const CUresult r = encode(i ? &v : &k, q8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, i ? v_rows : k_rows, dims, strides, box,
+                                step, CU_TENSOR_MAP_INTERLEAVE_NONE, q8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+      if (r != CUDA_SUCCESS) {
+        err = "cuTensorMapEncodeTiled(pool) failed with code " + std::to_string((int)r);
+        return false;
+      }
+    }
+    return true;
+  }
+};
 
 }  // namespace paged
 }  // namespace scalekv
