@@ -125,54 +125,76 @@ struct Seen {
   }
 };
 
+// 8 consecutive 32-bit columns of this thread's TMEM lane
+__device__ __forceinline__ void tc_ld8(uint32_t at, uint32_t *r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ void tc_st8(uint32_t at, const uint32_t *r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+               "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+
 // A chunk whose sum shows that an exponent left the lazy band, or that some row had no reference yet: taken again by the whole warp, from the
 // raw products in columns 32 cc .. of s_addr (P covers columns below 16 cc only).  The reference rises to the chunk's largest exponent
 // where that is larger; the chunk's P is stored against it, and what was accumulated under the old one is multiplied by f = 2^(old - new): the
 // sum, P of the chunks p_first .. cc - 1, and O, once the product that pv_bar stands for has landed.
+// Rare, and written into the sweep four times (a kernel that deals out its registers makes no calls), so its loops stay loops.
 struct Risen { float m, l; int o_landed, ok; };
 template <int D, bool kQ8>
-__device__ __forceinline__ Risen raise_row(Seen seen, float c, float m, float l, uint32_t s_addr, uint32_t scales, int cc, int p_first, uint32_t o_addr, int with_o,
-                                        int o_landed, uint32_t pv_bar, uint32_t pv_parity, volatile int *abort_flag, int *status) {
-  float x[32];
-  tc_ld32(s_addr + cc * 32, x);
-  tc_wait_ld();
+__device__ __forceinline__ Risen raise_row(const Seen &seen, float c, float m, float l, uint32_t s_addr, uint32_t scales, int cc, int p_first, uint32_t o_addr,
+                                           int with_o, int o_landed, uint32_t pv_bar, uint32_t pv_parity, volatile int *abort_flag, int *status) {
+  uint32_t r[8];
   float top = -INFINITY;
+  // eight exponents of the chunk, from column `at` of the tile
+  auto exponents = [&](int at) {
+    tc_ld8(s_addr + at, r);
+    tc_wait_ld();
 #pragma unroll
-  for (int i = 0; i < 32; i += 4) {
-    const float4 k = kQ8 ? load_shared4(scales + (cc * 32 + i) * 4) : make_float4(c, c, c, c);
-    x[i] *= k.x; x[i + 1] *= k.y; x[i + 2] *= k.z; x[i + 3] *= k.w;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (!seen(cc * 32 + i + e)) x[i + e] = -INFINITY;
-      top = fmaxf(top, x[i + e]);
+    for (int i = 0; i < 8; ++i) {
+      float k = c;
+      if constexpr (kQ8) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(k) : "r"(scales + (at + i) * 4));
+      r[i] = __float_as_uint(seen(at + i) ? __uint_as_float(r[i]) * k : -INFINITY);
     }
+  };
+#pragma unroll 1
+  for (int at = cc * 32; at < cc * 32 + 32; at += 8) {
+    exponents(at);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, __uint_as_float(r[i]));
   }
   const float m_new = fmaxf(m, top), f = ex2(m - m_new);
   float sum = 0.f;
+  // (the first chunk's P lies over its own products: it is stored when all have been read)
   uint32_t pk[16];
 #pragma unroll
-  for (int i = 0; i < 32; i += 4) {
-    const float4 v = kQ8 ? load_shared4(scales + 512 + (cc * 32 + i) * 4) : make_float4(1.f, 1.f, 1.f, 1.f);
-    float p[4];
+  for (int q = 0; q < 4; ++q) {
+    exponents(cc * 32 + q * 8);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      p[e] = ex2(x[i + e] - m_new);
-      sum += p[e];
-      const float ve = e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w;
-      if (kQ8) p[e] = seen(cc * 32 + i + e) ? p[e] * ve : 0.f;
+    for (int i = 0; i < 8; i += 2) {
+      float p0 = ex2(__uint_as_float(r[i]) - m_new), p1 = ex2(__uint_as_float(r[i + 1]) - m_new);
+      sum += p0 + p1;
+      if constexpr (kQ8) {
+        const int at = cc * 32 + q * 8 + i;
+        float v0, v1;
+        asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v0), "=f"(v1) : "r"(scales + 512 + at * 4));
+        p0 = seen(at) ? p0 * v0 : 0.f;
+        p1 = seen(at + 1) ? p1 * v1 : 0.f;
+      }
+      pk[q * 4 + i / 2] = pack_bf16(p0, p1);
     }
-    pk[i / 2] = pack_bf16(p[0], p[1]);
-    pk[i / 2 + 1] = pack_bf16(p[2], p[3]);
   }
   tc_st16(s_addr + cc * 16, pk);
 #pragma unroll 1
-  for (int e = p_first; e < cc; ++e) {
-    uint32_t r[16];
-    tc_ld16(s_addr + e * 16, r);
+  for (int e = p_first * 2; e < cc * 2; ++e) {
+    tc_ld8(s_addr + e * 8, r);
     tc_wait_ld();
 #pragma unroll
-    for (int i = 0; i < 16; ++i) r[i] = pack_bf16(__uint_as_float(r[i] << 16) * f, __uint_as_float(r[i] & 0xffff0000u) * f);
-    tc_st16(s_addr + e * 16, r);
+    for (int i = 0; i < 8; ++i) r[i] = pack_bf16(__uint_as_float(r[i] << 16) * f, __uint_as_float(r[i] & 0xffff0000u) * f);
+    tc_st8(s_addr + e * 8, r);
   }
   if (with_o) {
     if (!o_landed) {
@@ -181,13 +203,12 @@ __device__ __forceinline__ Risen raise_row(Seen seen, float c, float m, float l,
       o_landed = 1;
     }
 #pragma unroll 1
-    for (int e = 0; e < D / 32; ++e) {
-      float o[32];
-      tc_ld32(o_addr + e * 32, o);
+    for (int e = 0; e < D / 8; ++e) {
+      tc_ld8(o_addr + e * 8, r);
       tc_wait_ld();
 #pragma unroll
-      for (int i = 0; i < 32; ++i) o[i] *= f;
-      tc_st32(o_addr + e * 32, o);
+      for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
+      tc_st8(o_addr + e * 8, r);
     }
   }
   tc_wait_st();
@@ -304,10 +325,12 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       // -------------------------------------------------------------- MMA issuer (the whole warp walks, one elected lane issues)
       constexpr uint32_t idesc_qk = tile_desc(false, 128), idesc_pv = tile_desc(true, D), dhi = desc_hi(1024);
       const bool leader = elect_one();
-      auto mma_s = [&](int kt, int qt) {
-        const uint32_t q = desc_lo(base + Y::kOffQ + (pair && qt ? kTile : 0u), 16), k = desc_lo(base + Y::kOffRing + (kt % kStages) * kTile, 16);
-        if constexpr (D == 128) tc_mma_ss_x8(tmem + kColS + qt * 128, q, k, dhi, idesc_qk);
-        else mma_ss_x4(tmem + kColS + qt * 128, q, k, dhi, idesc_qk);
+      // What stands between the arrival of P and the tile's next S product is issue alone: descriptors and barriers' addresses are formed before the wait.
+      const uint32_t q_lo[2] = {desc_lo(base + Y::kOffQ, 16), desc_lo(base + Y::kOffQ + (pair ? kTile : 0u), 16)};
+      auto k_desc = [&](int kt) { return desc_lo(base + Y::kOffRing + (kt % kStages) * kTile, 16); };
+      auto mma_s = [&](uint32_t k, int qt) {
+        if constexpr (D == 128) tc_mma_ss_x8(tmem + kColS + qt * 128, q_lo[qt], k, dhi, idesc_qk);
+        else mma_ss_x4(tmem + kColS + qt * 128, q_lo[qt], k, dhi, idesc_qk);
       };
       auto ring_full = [&](int t) { return mbar_wait_warp(bar(Y::bFull + t % kStages), (t / kStages) & 1, abort_flag, status); };
       const int steps[2] = {n_steps(0), n_steps(1)};
@@ -332,7 +355,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         ok = mbar_wait_warp(bar(Y::bQFull + (pair ? qt : 0)), 0, abort_flag, status) && ring_full(kt);
         if (!ok) break;
         tc_fence_after();
-        mma_s(kt, qt);
+        mma_s(k_desc(kt), qt);
         if (leader) {
           tc_commit(bar(Y::bSFull + qt));
           if (!pair || qt == 1) tc_commit(bar(Y::bEmpty + kt % kStages));
@@ -345,6 +368,8 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           const bool more = j + 1 < steps[qt];
           const int vt = ring_of(j, qt) + 1, kt = ring_of(j + 1, qt);
           const uint32_t vd = desc_lo(base + Y::kOffRing + (vt % kStages) * kTile, kHalf), pa = tmem + kColS + qt * 128, oa = tmem + kColO + qt * 128;
+          const uint32_t kd = k_desc(kt), v_empty = bar(Y::bEmpty + vt % kStages), k_empty = bar(Y::bEmpty + kt % kStages);
+          const uint32_t done = bar((more ? Y::bSFull : Y::bFinal) + qt);
           ok = ring_full(vt);
           if (!ok) break;
           if (!kQ8 && (!pair || qt == 0)) clean(vt);
@@ -358,13 +383,13 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           if (!ok) break;
           tc_fence_after();
           tc_mma_ts_n<8 - 2 * kEarly>(oa, pa + p_col(2 * kEarly), vd + 128 * 2 * kEarly, dhi, idesc_pv, 1u);
-          if (more) mma_s(kt, qt);
+          if (more) mma_s(kd, qt);
           if (leader) {
-            tc_commit(bar((more ? Y::bSFull : Y::bFinal) + qt));
+            tc_commit(done);
             tc_commit(bar(Y::bPvDone + qt));
             if (!pair || qt == 1) {
-              tc_commit(bar(Y::bEmpty + vt % kStages));
-              if (more) tc_commit(bar(Y::bEmpty + kt % kStages));
+              tc_commit(v_empty);
+              if (more) tc_commit(k_empty);
             }
           }
           __syncwarp();
