@@ -9,13 +9,13 @@
 //   warp 0        : tcgen05.mma issuer.  S_A(0), S_B(0), then per step j  PV_A(j), S_A(j+1), PV_B(j), S_B(j+1): the tensor pipe works
 //                   for one tile while the other's softmax runs.
 //   warp 1        : TMA producer: the tile's rows, page by page, into a ring of operand tiles K_0, V_0, K_1, V_1, ...  bf16 rows land as the
-//                   products read them (128-byte swizzle), codes in the first half of their stage.
-//   warps 4-7     : with codes only, converters.  A thread takes its codes out of the stage, waits for the others' and puts them back as bf16: exactly, by
+//                   products read them (128-byte swizzle), codes in the second half of their stage.
+//   warps 4-7     : with codes only, converters, which put the codes of a stage back into it as bf16: exactly, by
 //                   integer instructions and one subtraction for a pair.  They also bring the scales.
-//   the last eight: softmax, a warpgroup for each tile, a thread for each row (TMEM lane): one sweep over the row's 128 products in
-//                   four chunks of 32, exponentials against a lazy reference (raised when a chunk's sum leaves 2^13), P as bf16 over the products already
+//   the last eight: softmax, a warpgroup for each tile, a warp for each 32 rows (TMEM lanes): one sweep over their 128 products in
+//                   four chunks of 32, exponentials against a lazy reference, which rises when one exceeds it by more than 2^8, P as bf16 over the products already
 //                   read.  With codes a key's scale is a factor of its column: K's is part of the factor of the exponent's FMA, V's multiplies P
-//                   before it is rounded; both come from shared memory, a broadcast load for four columns.
+//                   before it is rounded; both come from shared memory.
 // Rows that no query of the item sees (behind the length, ahead of the window, on a page out of range) may hold anything.  Their products are hidden one
 // by one; as values codes are numbers whatever they are, and bf16 rows are zeroed by the issuer before the product reads them.
 // Every wait is bounded; one that gives up raises the sticky status and all roles fall through to the end.
@@ -34,7 +34,7 @@ using namespace scalekv::tc;
 constexpr int kItemRows = 256;
 constexpr int kTileKeys = 128;
 constexpr int kSweepChunks = 4;
-constexpr int kEarly = 3;                         // chunks whose part of the PV product is issued under the rest of the sweep
+constexpr int kEarly = 3;                         // (the sweep's loop counts on it) chunks whose part of the PV product is issued under the rest of the sweep
 constexpr int kScaleSlots = 4;                    // key tiles whose scales are held (see the loaders)
 
 template <int D, bool kQ8>
@@ -115,16 +115,37 @@ __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, vo
   return __all_sync(0xffffffffu, ok);
 }
 
-// What a row sees of a key tile, relative to the tile's first key: columns [lo, hi) and [0, sink), less those of `holes` (a bit for
-// each 16: their page is out of range).
-struct Seen {
-  int lo, hi, sink;
-  uint32_t holes;
-  __device__ __forceinline__ bool operator()(int col) const {
-    return col < hi && (col >= lo || col < sink) && !((holes >> (col >> 4)) & 1u);
-  }
-};
-
+// TMEM as the softmax threads read it: 16 lanes (query rows) x 8 columns at a time, of which a thread has columns 2 c, 2 c + 1 of rows r and r + 8
+// (c = lane mod 4, r = lane / 4).  So a thread has a quarter of the columns of four rows, r + 8 k, and not one row's whole: the
+// scales of columns, which it loads from shared memory, are a quarter as many for the same number of products.  With all 128 columns' scales loaded by
+// each thread of a row's own, those loads alone were 2 048 of 8 900 cycles a step (a 16-byte load takes a warp four cycles, the same address or not).
+// 32 columns: x[16 h + 4 j + 2 b + e] is column 8 j + 2 c + e of row r + 16 h + 8 b.
+__device__ __forceinline__ void ld_rows(uint32_t at, float *x) {
+  uint32_t r[32];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[16 * h + 0]), "=r"(r[16 * h + 1]), "=r"(r[16 * h + 2]), "=r"(r[16 * h + 3]), "=r"(r[16 * h + 4]), "=r"(r[16 * h + 5]),
+                   "=r"(r[16 * h + 6]), "=r"(r[16 * h + 7]), "=r"(r[16 * h + 8]), "=r"(r[16 * h + 9]), "=r"(r[16 * h + 10]), "=r"(r[16 * h + 11]),
+                   "=r"(r[16 * h + 12]), "=r"(r[16 * h + 13]), "=r"(r[16 * h + 14]), "=r"(r[16 * h + 15])
+                 : "r"(at + (uint32_t)((16 * h) << 16))
+                 : "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
+}
+// P of those 32 columns, pairs of bf16: p[8 h + 2 j + b]
+__device__ __forceinline__ void st_rows(uint32_t at, const uint32_t *p) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at + (uint32_t)((16 * h) << 16)), "r"(p[8 * h + 0]),
+                 "r"(p[8 * h + 1]), "r"(p[8 * h + 2]), "r"(p[8 * h + 3]), "r"(p[8 * h + 4]), "r"(p[8 * h + 5]), "r"(p[8 * h + 6]), "r"(p[8 * h + 7])
+                 : "memory");
+}
+__device__ __forceinline__ float2 load_shared2(uint32_t at) {
+  float2 x;
+  asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(at));
+  return x;
+}
 // 8 consecutive 32-bit columns of this thread's TMEM lane
 __device__ __forceinline__ void tc_ld8(uint32_t at, uint32_t *r) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
@@ -137,83 +158,30 @@ __device__ __forceinline__ void tc_st8(uint32_t at, const uint32_t *r) {
                "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
 }
-
-// A chunk whose sum shows that an exponent left the lazy band, or that some row had no reference yet: taken again by the whole warp, from the
-// raw products in columns 32 cc .. of s_addr (P covers columns below 16 cc only).  The reference rises to the chunk's largest exponent
-// where that is larger; the chunk's P is stored against it, and what was accumulated under the old one is multiplied by f = 2^(old - new): the
-// sum, P of the chunks p_first .. cc - 1, and O, once the product that pv_bar stands for has landed.
-// Rare, and written into the sweep four times (a kernel that deals out its registers makes no calls), so its loops stay loops.
-struct Risen { float m, l; int o_landed, ok; };
-template <int D, bool kQ8>
-__device__ __forceinline__ Risen raise_row(const Seen &seen, float c, float m, float l, uint32_t s_addr, uint32_t scales, int cc, int p_first, uint32_t o_addr,
-                                           int with_o, int o_landed, uint32_t pv_bar, uint32_t pv_parity, volatile int *abort_flag, int *status) {
-  uint32_t r[8];
-  float top = -INFINITY;
-  // eight exponents of the chunk, from column `at` of the tile
-  auto exponents = [&](int at) {
-    tc_ld8(s_addr + at, r);
-    tc_wait_ld();
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float k = c;
-      if constexpr (kQ8) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(k) : "r"(scales + (at + i) * 4));
-      r[i] = __float_as_uint(seen(at + i) ? __uint_as_float(r[i]) * k : -INFINITY);
-    }
-  };
-#pragma unroll 1
-  for (int at = cc * 32; at < cc * 32 + 32; at += 8) {
-    exponents(at);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = fmaxf(top, __uint_as_float(r[i]));
-  }
-  const float m_new = fmaxf(m, top), f = ex2(m - m_new);
-  float sum = 0.f;
-  // (the first chunk's P lies over its own products: it is stored when all have been read)
-  uint32_t pk[16];
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    exponents(cc * 32 + q * 8);
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      float p0 = ex2(__uint_as_float(r[i]) - m_new), p1 = ex2(__uint_as_float(r[i + 1]) - m_new);
-      sum += p0 + p1;
-      if constexpr (kQ8) {
-        const int at = cc * 32 + q * 8 + i;
-        float v0, v1;
-        asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v0), "=f"(v1) : "r"(scales + 512 + at * 4));
-        p0 = seen(at) ? p0 * v0 : 0.f;
-        p1 = seen(at + 1) ? p1 * v1 : 0.f;
-      }
-      pk[q * 4 + i / 2] = pack_bf16(p0, p1);
-    }
-  }
-  tc_st16(s_addr + cc * 16, pk);
-#pragma unroll 1
-  for (int e = p_first * 2; e < cc * 2; ++e) {
-    tc_ld8(s_addr + e * 8, r);
-    tc_wait_ld();
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = pack_bf16(__uint_as_float(r[i] << 16) * f, __uint_as_float(r[i] & 0xffff0000u) * f);
-    tc_st8(s_addr + e * 8, r);
-  }
-  if (with_o) {
-    if (!o_landed) {
-      if (!mbar_wait_warp(pv_bar, pv_parity, abort_flag, status)) return {m_new, l * f + sum, 0, 0};
-      tc_fence_after();
-      o_landed = 1;
-    }
-#pragma unroll 1
-    for (int e = 0; e < D / 8; ++e) {
-      tc_ld8(o_addr + e * 8, r);
-      tc_wait_ld();
-#pragma unroll
-      for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
-      tc_st8(o_addr + e * 8, r);
-    }
-  }
-  tc_wait_st();
-  return {m_new, l * f + sum, o_landed, 1};
+__device__ __forceinline__ float quad_max(float x) {
+  x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+  return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
 }
+// Of the four rows of a thread the value of row `lane` of its warp
+__device__ __forceinline__ float own_row(const float *x, int lane) {
+  float y = 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float z = __shfl_sync(0xffffffffu, x[k], (lane & 7) * 4);
+    if (lane >> 3 == k) y = z;
+  }
+  return y;
+}
+
+// What this thread's rows see of a key tile, relative to the tile's first key: columns [lo[k], hi[k]) and [0, sink), less those of `holes` (a
+// bit for each 16: their page is out of range).
+struct Seen {
+  int lo[4], hi[4], sink;
+  uint32_t holes;
+  __device__ __forceinline__ bool operator()(int k, int col) const {
+    return col < hi[k] && (col >= lo[k] || col < sink) && !((holes >> (col >> 4)) & 1u);
+  }
+};
 
 // tmK, tmV: the K and V rows of all layers, [layer * pages + page][kv head * page_tokens + row][head_dim]; page0: layer * pages
 template <int D, bool kQ8>
@@ -329,8 +297,8 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       const uint32_t q_lo[2] = {desc_lo(base + Y::kOffQ, 16), desc_lo(base + Y::kOffQ + (pair ? kTile : 0u), 16)};
       auto k_desc = [&](int kt) { return desc_lo(base + Y::kOffRing + (kt % kStages) * kTile, 16); };
       auto mma_s = [&](uint32_t k, int qt) {
-        if constexpr (D == 128) tc_mma_ss_x8(tmem + kColS + qt * 128, q_lo[qt], k, dhi, idesc_qk);
-        else mma_ss_x4(tmem + kColS + qt * 128, q_lo[qt], k, dhi, idesc_qk);
+        if constexpr (D == 128) tc_mma_ss_x8(tmem + kColS + qt * 128, qt ? q_lo[1] : q_lo[0], k, dhi, idesc_qk);
+        else mma_ss_x4(tmem + kColS + qt * 128, qt ? q_lo[1] : q_lo[0], k, dhi, idesc_qk);
       };
       auto ring_full = [&](int t) { return mbar_wait_warp(bar(Y::bFull + t % kStages), (t / kStages) & 1, abort_flag, status); };
       const int steps[2] = {n_steps(0), n_steps(1)};
@@ -363,9 +331,11 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         __syncwarp();
       }
       for (int j = 0; j < steps[0] && ok; ++j) {
+#pragma unroll 1
         for (int qt = 0; qt < 2 && ok; ++qt) {
-          if (j >= steps[qt]) break;
-          const bool more = j + 1 < steps[qt];
+          const int mine = qt ? steps[1] : steps[0];
+          if (j >= mine) break;
+          const bool more = j + 1 < mine;
           const int vt = ring_of(j, qt) + 1, kt = ring_of(j + 1, qt);
           const uint32_t vd = desc_lo(base + Y::kOffRing + (vt % kStages) * kTile, kHalf), pa = tmem + kColS + qt * 128, oa = tmem + kColO + qt * 128;
           const uint32_t kd = k_desc(kt), v_empty = bar(Y::bEmpty + vt % kStages), k_empty = bar(Y::bEmpty + kt % kStages);
@@ -423,7 +393,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           const int pg = __shfl_sync(0xffffffffu, page, (r0 >> 4) + __ffs(mine) - 1);
           if (elect_one()) {
             const int y = (head << s.page_shift) + ((key0 + r0) & in_page), z = page0 + pg;
-            const uint32_t dst = base + Y::kOffRing + st * kTile + r0 * (kQ8 ? D : 128);
+            const uint32_t dst = base + Y::kOffRing + st * kTile + (kQ8 ? kTile - 128 * D : 0u) + r0 * (kQ8 ? D : 128);
             tma_load_3d(dst, tm, 0, y, z, bar(kLanded + st));
             if constexpr (!kQ8 && D == 128) tma_load_3d(dst + kHalf, tm, 64, y, z, bar(kLanded + st));
           }
@@ -447,8 +417,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     // ---------------------------------------------------------------- converters
     // The scales of both go with K, into slot (t / 2) mod kScaleSlots; that slot's last readers are done: the stage of this K was
     // released behind a product that was issued after their P.
-    constexpr int kPieces = D / 16, kRowsAtOnce = 128 / kPieces, kIters = 128 / kRowsAtOnce;      // 16 codes a piece
-    const int piece = tid % kPieces, sub = tid / kPieces, half = piece >> 2;
+    const int piece = tid & 3, sub = tid >> 2;      // 16 codes a piece, 64 columns at a time
     float k_scale = 0.f, v_scale = 0.f;
     auto fetch_scales = [&](int i) {
       const int page = __shfl_sync(0xffffffffu, pages(i), tid >> 4), pos = key_of(i) + tid;
@@ -463,28 +432,34 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       const uint32_t stage = base + Y::kOffRing + (t % kStages) * kTile;
       ok = mbar_wait_warp(bar(Y::bRaw + t % kStages), (t / kStages) & 1, abort_flag, status);
       if (!ok) break;
-      uint4 raw[kIters];
-#pragma unroll
-      for (int it = 0; it < kIters; ++it) raw[it] = load_shared16(stage + (it * kRowsAtOnce + sub) * D + piece * 16);
       if (!(t & 1)) {
         const uint32_t at = base + Y::kOffScale + ((t >> 1) % kScaleSlots) * 1024 + tid * 4;
         asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(k_scale) : "memory");
         asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 512), "f"(v_scale) : "memory");
         if ((t >> 1) + 1 < nt) fetch_scales((t >> 1) + 1);
       }
-      asm volatile("bar.sync 3, 128;" ::: "memory");          // all codes are out of the stage
-      // 16 codes become two 16-byte pieces of a row's 128-byte span; lanes of the second half of a row write theirs the other way
-      // round, so that eight lanes' stores meet all banks
-      const uint32_t to = stage + half * kHalf;
-#pragma unroll
-      for (int it = 0; it < kIters; ++it) {
-        const int r = it * kRowsAtOnce + sub;
-        const uint32_t w[4] = {half ? raw[it].z : raw[it].x, half ? raw[it].w : raw[it].y, half ? raw[it].x : raw[it].z, half ? raw[it].y : raw[it].w};
+      // 16 codes become two 16-byte pieces of a row's 128-byte span of 64 columns.  Eight lanes' stores, of two
+      // neighbouring rows, meet all banks.
+      auto convert = [&](const uint4 &raw, uint32_t span, int r) {
+        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
         for (int k = 0; k < 2; ++k)
-          store_shared(to + r * 128 + ((((piece & 3) * 2 + (k ^ half)) ^ (r & 7)) << 4), codes_bf16(w[2 * k], 0u, 0x4140), codes_bf16(w[2 * k], 0u, 0x4342),
+          store_shared(span + r * 128 + (((piece * 2 + k) ^ (r & 7)) << 4), codes_bf16(w[2 * k], 0u, 0x4140), codes_bf16(w[2 * k], 0u, 0x4342),
                        codes_bf16(w[2 * k + 1], 0u, 0x4140), codes_bf16(w[2 * k + 1], 0u, 0x4342));
+      };
+      // The codes lie in the stage's last quarter or half.  What becomes its first half can go there at once; what becomes the half that they
+      // lie in is taken out by all threads before any puts it back.
+      const uint32_t raw_at = stage + kTile - 128 * D + piece * 16;
+      uint4 last[4];
+#pragma unroll
+      for (int it = 0; it < 4; ++it) last[it] = load_shared16(raw_at + (it * 32 + sub) * D + (D - 64));
+      if constexpr (D == 128) {
+#pragma unroll 1
+        for (int r = sub; r < 128; r += 32) convert(load_shared16(raw_at + r * D), stage, r);
       }
+      asm volatile("bar.sync 3, 128;" ::: "memory");
+#pragma unroll
+      for (int it = 0; it < 4; ++it) convert(last[it], stage + (D == 128 ? kHalf : 0u), it * 32 + sub);
       fence_async_proxy();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(Y::bFull + t % kStages));
@@ -514,17 +489,25 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(Y::bQFull + qt));
     }
-    // this row's limits, and those of the warp's rows together
-    const int i_own = tile_row0 + row;
-    const int t_own = a.group.div(max(min(i_own, all - 1), 0));
-    const int row_lo = seen_lo(a.mask, first + t_own), row_hi = seen_hi(a.mask, first + t_own, length);
-    const int warp_lo = __reduce_min_sync(0xffffffffu, row_lo), warp_lo_full = __reduce_max_sync(0xffffffffu, row_lo);
-    const int warp_hi = __reduce_max_sync(0xffffffffu, row_hi), warp_hi_full = __reduce_min_sync(0xffffffffu, row_hi);
+    // the limits of this thread's rows (lane / 4 + 8 k of the warp's), and those of the warp's rows together
+    auto token_of = [&](int i) { return a.group.div(max(min(i, all - 1), 0)); };
+    int row_lo[4], row_hi[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int p = first + token_of(tile_row0 + quarter * 32 + (lane >> 2) + 8 * k);
+      row_lo[k] = seen_lo(a.mask, p);
+      row_hi[k] = seen_hi(a.mask, p, length);
+    }
+    const int p_top = first + token_of(tile_row0 + quarter * 32), p_end = first + token_of(tile_row0 + quarter * 32 + 31);
+    const int warp_lo = seen_lo(a.mask, p_top), warp_lo_full = seen_lo(a.mask, p_end);
+    const int warp_hi = seen_hi(a.mask, p_end, length), warp_hi_full = seen_hi(a.mask, p_top, length);
     const float c = a.scale_log2e;
     const uint64_t c2 = pack2(c, c);
-    float m = -INFINITY, l = 0.f;
+    // references start at the lowest number: differences from it are numbers
+    float m[4] = {-FLT_MAX, -FLT_MAX, -FLT_MAX, -FLT_MAX}, l[4] = {0.f, 0.f, 0.f, 0.f};
     const uint32_t o_addr = lane_addr + kColO + qt * 128, s_addr = lane_addr + kColS + qt * 128;
     const int steps = rows > 0 ? n_steps(qt) : 0;
+    const int quad = lane & 3;
     bool ok = true;
     for (int j = 0; j < steps && ok; ++j) {
       const int i_tile = shared ? 2 * j + qt : j, key0 = key_of(i_tile);
@@ -533,131 +516,204 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       tc_fence_after();
       uint32_t holes;
       asm volatile("ld.shared.b32 %0, [%1];" : "=r"(holes) : "r"(base + Y::kOffHoles + (i_tile % kScaleSlots) * 4));
-      const uint32_t scales = base + Y::kOffScale + (i_tile % kScaleSlots) * 1024;
-      const Seen seen = {row_lo - key0, row_hi - key0, n_sink - key0, holes};
-      int o_landed = 0;
-      float v[2][32];
-      // p = 2^(x - m) of a chunk in place of its products
-      auto front = [&](float *x, int cc, auto masked) {
-        const uint64_t negm2 = pack2(-m, -m);
+      const uint32_t scales = base + Y::kOffScale + (i_tile % kScaleSlots) * 1024, my_scales = scales + 8 * quad;
+      Seen seen;
 #pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-          uint64_t k0 = c2, k1 = c2;
+      for (int k = 0; k < 4; ++k) { seen.lo[k] = row_lo[k] - key0; seen.hi[k] = row_hi[k] - key0; }
+      seen.sink = n_sink - key0;
+      seen.holes = holes;
+      auto hand_over = [&](int which) {
+        tc_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(which + qt));
+      };
+      // ---- tiles that every row of the warp sees whole.  p = 2^(x - m) of a chunk in place of its products:
+      auto front = [&](float *x, int cc) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          uint64_t k2 = c2;
           if constexpr (kQ8) {
-            const float4 k = load_shared4(scales + (cc * 32 + i) * 4);
-            k0 = pack2(k.x, k.y);
-            k1 = pack2(k.z, k.w);
+            const float2 two = load_shared2(my_scales + (cc * 32 + 8 * g) * 4);
+            k2 = pack2(two.x, two.y);
           }
-          float y[4];
-          unpack2(fma2(pack2(x[i], x[i + 1]), k0, negm2), y[0], y[1]);
-          unpack2(fma2(pack2(x[i + 2], x[i + 3]), k1, negm2), y[2], y[3]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if constexpr (decltype(masked)::value)
-              if (!seen(cc * 32 + i + e)) y[e] = -INFINITY;
-            x[i + e] = ex2(y[e]);
+          for (int k = 0; k < 4; ++k) {
+            float *y = x + 16 * (k >> 1) + 4 * g + 2 * (k & 1);
+            unpack2(fma2(pack2(y[0], y[1]), k2, pack2(-m[k], -m[k])), y[0], y[1]);
+            y[0] = ex2(y[0]);
+            y[1] = ex2(y[1]);
           }
         }
       };
-      // 32 values of at most 2^8 sum to at most 2^13; a larger, infinite or NaN sum means that some exponent left the band
-      auto back = [&](const float *p, uint32_t *pk, int cc, auto masked) {
-        uint64_t sum_a = pack2(0.f, 0.f), sum_b = sum_a;
+      // P of a chunk, and its rows' sums.  8 values of at most 2^8 sum to at most 2^11; a larger, infinite or NaN sum means that some exponent
+      // left the band.
+      auto back = [&](const float *x, uint32_t *pk, float *sum, int cc) {
+        uint64_t sums[4];
 #pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-          uint64_t p0 = pack2(p[i], p[i + 1]), p1 = pack2(p[i + 2], p[i + 3]);
-          sum_a = add2(sum_a, p0);
-          sum_b = add2(sum_b, p1);
-          float y[4] = {p[i], p[i + 1], p[i + 2], p[i + 3]};
+        for (int g = 0; g < 4; ++g) {
+          [[maybe_unused]] uint64_t v2 = 0;
           if constexpr (kQ8) {
-            const float4 k = load_shared4(scales + 512 + (cc * 32 + i) * 4);
-            unpack2(mul2(p0, pack2(k.x, k.y)), y[0], y[1]);
-            unpack2(mul2(p1, pack2(k.z, k.w)), y[2], y[3]);
-            if constexpr (decltype(masked)::value) {       // (a hidden value's scale may be no number)
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (!seen(cc * 32 + i + e)) y[e] = 0.f;
-            }
+            const float2 two = load_shared2(my_scales + 512 + (cc * 32 + 8 * g) * 4);
+            v2 = pack2(two.x, two.y);
           }
-          pk[i / 2] = pack_bf16(y[0], y[1]);
-          pk[i / 2 + 1] = pack_bf16(y[2], y[3]);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float *y = x + 16 * (k >> 1) + 4 * g + 2 * (k & 1);
+            const uint64_t p2 = pack2(y[0], y[1]);
+            sums[k] = g == 0 ? p2 : add2(sums[k], p2);
+            float p0 = y[0], p1 = y[1];
+            if constexpr (kQ8) unpack2(mul2(p2, v2), p0, p1);
+            pk[8 * (k >> 1) + 2 * g + (k & 1)] = pack_bf16(p0, p1);
+          }
         }
-        float s0, s1, s2, s3;
-        unpack2(sum_a, s0, s1);
-        unpack2(sum_b, s2, s3);
-        return (s0 + s1) + (s2 + s3);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          float s0, s1;
+          unpack2(sums[k], s0, s1);
+          sum[k] = s0 + s1;
+        }
+        return !(sum[0] <= 2048.f && sum[1] <= 2048.f && sum[2] <= 2048.f && sum[3] <= 2048.f);
       };
-      auto sweep = [&](auto masked) {
-        constexpr bool kMasked = decltype(masked)::value;
-        // a chunk that no row of the warp sees: zeros, and no exponentials
-        auto empty = [&](int cc) {
-          const int at = key0 + cc * 32;
-          return kMasked && (at >= warp_hi || (at + 32 <= warp_lo && at >= n_sink));
-        };
-        tc_ld32(s_addr, v[0]);
-        tc_ld32(s_addr + 32, v[1]);
+      int cc = 0;                                  // the first chunk that is not finished
+      if (holes == 0 && key0 >= warp_lo_full && key0 + kTileKeys <= warp_hi_full) {
+        // Software-pipelined: the exponentials of the next chunk are under way while this one is summed, checked and stored.  Two chunks to an
+        // iteration, since the roles' loops together have to stay in the SM's instruction cache: with all four unrolled a step in codes, which
+        // has the converters' loop beside it, missed it 28 times in a hundred and took 7 700 cycles instead of XXXX.
+        float v[2][32];
+        ld_rows(s_addr, v[0]);
+        ld_rows(s_addr + 32, v[1]);
         tc_wait_ld();
-        if (j == 0) {
-          // no reference yet: the largest of the row's first 32 exponents, or the lowest number where all are hidden
-          float top = -INFINITY;
-#pragma unroll
-          for (int i = 0; i < 32; i += 4) {
-            const float4 k = kQ8 ? load_shared4(scales + i * 4) : make_float4(c, c, c, c);
-            float y[4] = {v[0][i] * k.x, v[0][i + 1] * k.y, v[0][i + 2] * k.z, v[0][i + 3] * k.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (!kMasked || seen(i + e)) top = fmaxf(top, y[e]);
-          }
-          m = fmaxf(top, -FLT_MAX);
-        }
-        if (!empty(0)) front(v[0], 0, masked);
-#pragma unroll
-        for (int cc = 0; cc < kSweepChunks; ++cc) {
+        front(v[0], 0);
+        auto finish = [&](int q, const float *x) {         // false: chunk q has to be taken again
           uint32_t pk[16];
-          const bool next = cc + 1 < kSweepChunks && !empty(cc + 1);
-          if (empty(cc)) {
+          float sum[4];
+          if (__any_sync(0xffffffffu, back(x, pk, sum, q))) return false;
+          st_rows(s_addr + q * 16, pk);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) pk[i] = 0u;
-            if (next) front(v[(cc + 1) & 1], cc + 1, masked);
-            if (cc + 2 < kSweepChunks) tc_ld32(s_addr + (cc + 2) * 32, v[cc & 1]);
-            tc_st16(s_addr + cc * 16, pk);
-          } else {
-            if (next) front(v[(cc + 1) & 1], cc + 1, masked);
-            const float sum = back(v[cc & 1], pk, cc, masked);
-            if (cc + 2 < kSweepChunks) tc_ld32(s_addr + (cc + 2) * 32, v[cc & 1]);
-            if (__any_sync(0xffffffffu, !(sum <= 8192.f))) {
-              const bool late = cc >= kEarly;
-              const Risen r = raise_row<D, kQ8>(seen, c, m, l, s_addr, scales, cc, late ? kEarly : 0, o_addr, (late || j > 0) ? 1 : 0,
-                                                late ? (o_landed == 2) : (o_landed >= 1), bar((late ? Y::bPvEarly : Y::bPvDone) + qt),
-                                                (late ? j : j - 1) & 1, abort_flag, status);
-              ok = __all_sync(0xffffffffu, r.ok != 0);
-              if (!ok) return;
-              m = r.m; l = r.l;
-              if (r.o_landed) o_landed = late ? 2 : 1;
-              if (next) {
-                tc_ld32(s_addr + (cc + 1) * 32, v[(cc + 1) & 1]);
-                tc_wait_ld();
-                front(v[(cc + 1) & 1], cc + 1, masked);
-              }
-            } else {
-              tc_st16(s_addr + cc * 16, pk);
-              l += sum;
+          for (int k = 0; k < 4; ++k) l[k] += sum[k];
+          cc = q + 1;
+          return true;
+        };
+#pragma unroll 1
+        for (int q = 0; q < kSweepChunks; q += 2) {
+          front(v[1], q + 1);
+          if (!finish(q, v[0])) break;
+          if (q == 0) ld_rows(s_addr + 64, v[0]);
+          else hand_over(Y::bPEarly);
+          if (q == 0) {
+            tc_wait_ld();
+            front(v[0], 2);
+          }
+          if (!finish(q + 1, v[1])) break;
+          if (q == 0) {
+            ld_rows(s_addr + 96, v[1]);
+            tc_wait_ld();
+          }
+        }
+      }
+      // ---- chunk by chunk, from the raw products in columns 32 cc .. (P covers columns below 16 cc only): tiles of which some rows see a part, and what is
+      // left of a tile once an exponent has left the band.  Where one is more than 2^8 above a row's reference, the references of all the warp's rows rise
+      // to their chunk's largest, and what was accumulated under the old one is multiplied by f = 2^(old - new): the sum, P of the chunks that the
+      // tensor core has not been given yet, and O, once the last product given to it has landed.
+      int landed = 0;                              // 1: the last step's product has; 2: the early part of this one's, too
+#pragma unroll 1
+      for (; cc < kSweepChunks && ok; ++cc) {
+        const int col0 = cc * 32 + 2 * quad, at = key0 + cc * 32;
+        uint32_t pk[16];
+        if (at >= warp_hi || (at + 32 <= warp_lo && at >= n_sink)) {       // no row of the warp sees it
+#pragma unroll
+          for (int i = 0; i < 16; ++i) pk[i] = 0u;
+        } else {
+          float x[32], top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          ld_rows(s_addr + cc * 32, x);
+          tc_wait_ld();
+          uint32_t hidden = 0;
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const float2 k2 = kQ8 ? load_shared2(scales + (col0 + 8 * g) * 4) : make_float2(c, c);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              float *y = x + 16 * (k >> 1) + 4 * g + 2 * (k & 1);
+              const bool s0 = seen(k, col0 + 8 * g), s1 = seen(k, col0 + 8 * g + 1);
+              y[0] = s0 ? y[0] * k2.x : -INFINITY;
+              y[1] = s1 ? y[1] * k2.y : -INFINITY;
+              hidden |= (s0 ? 0u : 1u << (8 * g + 2 * k)) | (s1 ? 0u : 2u << (8 * g + 2 * k));
+              top[k] = max3(top[k], y[0], y[1]);
             }
           }
-          if (cc == kEarly - 1) {
+          if (__any_sync(0xffffffffu, top[0] > m[0] + 8.f || top[1] > m[1] + 8.f || top[2] > m[2] + 8.f || top[3] > m[3] + 8.f)) {
+            float f[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float raised = fmaxf(m[k], quad_max(top[k]));
+              f[k] = ex2(m[k] - raised);
+              m[k] = raised;
+              l[k] *= f[k];
+            }
+            // P and O are scaled a lane's row at a time
+            const float f_own = own_row(f, lane);
+            const bool late = cc >= kEarly;
+            uint32_t r[8];
             tc_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(Y::bPEarly + qt));
+#pragma unroll 1
+            for (int e = late ? 2 * kEarly : 0; e < cc * 2; ++e) {
+              tc_ld8(s_addr + e * 8, r);
+              tc_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 8; ++i) r[i] = pack_bf16(__uint_as_float(r[i] << 16) * f_own, __uint_as_float(r[i] & 0xffff0000u) * f_own);
+              tc_st8(s_addr + e * 8, r);
+            }
+            if (late || j > 0) {
+              if (landed < (late ? 2 : 1)) {
+                ok = mbar_wait_warp(bar((late ? Y::bPvEarly : Y::bPvDone) + qt), (late ? j : j - 1) & 1, abort_flag, status);
+                if (!ok) break;
+                tc_fence_after();
+                landed = late ? 2 : 1;
+              }
+#pragma unroll 1
+              for (int e = 0; e < D / 8; ++e) {
+                tc_ld8(o_addr + e * 8, r);
+                tc_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f_own);
+                tc_st8(o_addr + e * 8, r);
+              }
+            }
           }
-          if (cc + 2 < kSweepChunks) tc_wait_ld();
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const float2 v2 = kQ8 ? load_shared2(scales + 512 + (col0 + 8 * g) * 4) : make_float2(1.f, 1.f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float *y = x + 16 * (k >> 1) + 4 * g + 2 * (k & 1);
+              float p0 = ex2(y[0] - m[k]), p1 = ex2(y[1] - m[k]);
+              l[k] += p0 + p1;
+              if constexpr (kQ8) {                 // (a hidden value's scale may be no number)
+                p0 = (hidden >> (8 * g + 2 * k)) & 1u ? 0.f : p0 * v2.x;
+                p1 = (hidden >> (8 * g + 2 * k)) & 2u ? 0.f : p1 * v2.y;
+              }
+              pk[8 * (k >> 1) + 2 * g + (k & 1)] = pack_bf16(p0, p1);
+            }
+          }
         }
-      };
-      if (holes != 0 || key0 < warp_lo_full || key0 + kTileKeys > warp_hi_full) sweep(std::true_type{}); else sweep(std::false_type{});
+        st_rows(s_addr + cc * 16, pk);
+        if (cc == kEarly - 1) hand_over(Y::bPEarly);
+      }
       if (!ok) break;
-      tc_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(Y::bPFull + qt));
+      hand_over(Y::bPFull);
+    }
+    // from here on a thread has a row of its own, i_own of the sequence's
+    const int i_own = tile_row0 + row, t_own = token_of(i_own);
+    float m_own = -INFINITY, l_own = 0.f;
+    if (steps > 0) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        l[k] += __shfl_xor_sync(0xffffffffu, l[k], 1);
+        l[k] += __shfl_xor_sync(0xffffffffu, l[k], 2);
+      }
+      m_own = own_row(m, lane);
+      l_own = own_row(l, lane);
     }
     // ---- the rows go out: normalised, or, where CTAs share them, as they are with their reference and sum
     if (steps > 0 && ok) ok = mbar_wait_warp(bar(Y::bFinal + qt), 0, abort_flag, status);
@@ -689,7 +745,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     };
     if (rows > 0 && ok && !shared && (pair || qt == 0)) {
       // (a row that saw nothing has a sum of 0 and an accumulator of zeros, or none at all)
-      const float f = split ? 1.f : (l == 0.f ? 0.f : 1.f / l);
+      const float f = split ? 1.f : (l_own == 0.f ? 0.f : 1.f / l_own);
 #pragma unroll 1
       for (int cc = 0; cc < D / 32; ++cc) {
         float o[32];
@@ -702,22 +758,22 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         }
         put(o, cc * 32, f);
       }
-      put_sums(m, l);
+      put_sums(m_own, l_own);
     } else if (shared) {
       // the two halves of the keys: both accumulators lie in the same lanes, so only references and sums are handed over (through the
       // second query tile's place, which a single does not use); each warpgroup finishes half of the columns
       const uint32_t stat = base + Y::kOffQ + kTile + (uint32_t)row * 8;
-      if (!ok) l = -1.f;                                   // (no sum is negative)
-      asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(stat + (uint32_t)qt * 1024), "f"(m), "f"(l) : "memory");
+      if (!ok) l_own = -1.f;                                   // (no sum is negative)
+      asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(stat + (uint32_t)qt * 1024), "f"(m_own), "f"(l_own) : "memory");
       tc_fence_before();
       asm volatile("bar.sync 2, 256;" ::: "memory");
       tc_fence_after();
       float m2, l2;
       asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(m2), "=f"(l2) : "r"(stat + (uint32_t)(qt ^ 1) * 1024) : "memory");
-      const float top = fmaxf(m, m2);
-      const float f1 = l == 0.f ? 0.f : ex2(m - top), f2 = l2 == 0.f ? 0.f : ex2(m2 - top), sum = l * f1 + l2 * f2;
+      const float top = fmaxf(m_own, m2);
+      const float f1 = l_own == 0.f ? 0.f : ex2(m_own - top), f2 = l2 == 0.f ? 0.f : ex2(m2 - top), sum = l_own * f1 + l2 * f2;
       const float f = split ? 1.f : (sum == 0.f ? 0.f : 1.f / sum);
-      if (__all_sync(0xffffffffu, !(l < 0.f || l2 < 0.f))) {
+      if (__all_sync(0xffffffffu, !(l_own < 0.f || l2 < 0.f))) {
 #pragma unroll 1
         for (int cc = 0; cc < D / 64; ++cc) {
           const int col = qt * (D / 2) + cc * 32;
