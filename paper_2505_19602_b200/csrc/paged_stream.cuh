@@ -10,8 +10,7 @@
 //     since a product's sum may run in any order, a lane takes whichever dims make its loads 16 bytes long; the query operand is read
 //     in the same order.
 //   - V's pairs of keys are interleaved from rows held by the lane, and its dims are dealt to the n-tiles so that those rows are 16 bytes long, too.
-//   - Codes become bf16 exactly: 128 + (c mod 128), less 128 or 256 by the sign.  The key's scale multiplies the product, the value's
-//     scale multiplies P, both in fp32; P is rounded to bf16 for its product with V, as it is where rows are bf16.
+//   - Codes become bf16 exactly (codes_bf16).  The key's scale multiplies the product, the value's scale multiplies P, both in fp32; P is rounded to bf16 for its product with V, as it is where rows are bf16.
 //   - While one half (K or V) of a step is computed with, the other half's loads are under way.
 // The running maximum of a row is raised when a step exceeds it by more than 2^3, and the sums with it: P stays below 2^8.
 // A CTA's four warps take the steps in turn and are combined in shared memory; gridDim.z CTAs share a row tile's keys where there
@@ -57,13 +56,19 @@ __device__ __forceinline__ float exp2_approx(float x) {
   return y;
 }
 
-// Two codes, in the bytes that `sel` picks for the low and the high half, as two bf16 numbers.
-__device__ __forceinline__ uint32_t codes_bf16(uint32_t a, uint32_t b, uint32_t sel) {
-  const uint32_t t = __byte_perm(a, b, sel);
-  const uint32_t low = (t & 0x007f007fu) | 0x43004300u, base = (t & 0x00800080u) | 0x43004300u;
+// Codes as bf16, exactly and without a conversion instruction: a byte u = c + 128 (the code with its sign bit turned) alone in 16 bits is the
+// subnormal u 2^-133, so one fused multiply-add gives u 2^-133 2^127 - 2 = c 2^-6.  The 2^6 goes into the factor that the scale is anyway.
+constexpr float kCodeUnit = 64.f;
+__device__ __forceinline__ uint32_t turn_signs(uint32_t w) { return w ^ 0x80808080u; }
+__device__ __forceinline__ uint32_t codes_bf16(uint32_t two) {                    // two such bytes, each in 16 bits
   uint32_t r;
-  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(low), "r"(base));
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(two), "r"(0x7f007f00u), "r"(0xc000c000u));
   return r;
+}
+__device__ __forceinline__ uint32_t codes_low(uint32_t w) { return codes_bf16(__byte_perm(w, 0u, 0x4140)); }      // of a word's four the first two
+__device__ __forceinline__ uint32_t codes_high(uint32_t w) { return codes_bf16(__byte_perm(w, 0u, 0x4342)); }
+template <int kByte> __device__ __forceinline__ uint32_t codes_across(uint32_t a, uint32_t b) {                   // the same byte of two words
+  return codes_bf16(__byte_perm(a, b, 0x0400 + kByte * 0x0101) & 0x00ff00ffu);
 }
 
 __device__ __forceinline__ void mma_16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
@@ -203,9 +208,9 @@ __global__ void __launch_bounds__(kStreamThreads, 3) paged_stream_kernel(const A
           const uint32_t f0[4] = {a0.x, a1.x, a0.y, a1.y}, f1[4] = {a0.z, a1.z, a0.w, a1.w};
 #pragma unroll
           for (int n = 0; n < 2; ++n) {
-            const uint32_t w0 = word(kq[n][i], 2 * h), w1 = word(kq[n][i], 2 * h + 1);
-            mma_16816(x[n], f0, codes_bf16(w0, 0u, 0x4140), codes_bf16(w0, 0u, 0x4342));
-            mma_16816(x[n], f1, codes_bf16(w1, 0u, 0x4140), codes_bf16(w1, 0u, 0x4342));
+            const uint32_t w0 = turn_signs(word(kq[n][i], 2 * h)), w1 = turn_signs(word(kq[n][i], 2 * h + 1));
+            mma_16816(x[n], f0, codes_low(w0), codes_high(w0));
+            mma_16816(x[n], f1, codes_low(w1), codes_high(w1));
           }
         }
       } else {
@@ -223,7 +228,7 @@ __global__ void __launch_bounds__(kStreamThreads, 3) paged_stream_kernel(const A
 #pragma unroll
     for (int n = 0; n < 2; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[n][e] *= kQ8 ? a.scale_log2e * ks[2 * n + (e & 1)] : a.scale_log2e;
+      for (int e = 0; e < 4; ++e) x[n][e] *= kQ8 ? a.scale_log2e * kCodeUnit * ks[2 * n + (e & 1)] : a.scale_log2e;
     const bool whole = page >= 0 && key0 >= lo_full && key0 + 16 <= hi_full;
     uint32_t hidden = 0;
     if (!whole) {
@@ -273,7 +278,7 @@ __global__ void __launch_bounds__(kStreamThreads, 3) paged_stream_kernel(const A
       if constexpr (kQ8) {
         // (a hidden key counts for nothing even where its scale is no number)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[n][e] = (hidden >> (4 * n + e)) & 1u ? 0.f : x[n][e] * vs[2 * n + (e & 1)];
+        for (int e = 0; e < 4; ++e) x[n][e] = (hidden >> (4 * n + e)) & 1u ? 0.f : x[n][e] * (kCodeUnit * vs[2 * n + (e & 1)]);
       }
       asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[2 * n]) : "f"(x[n][1]), "f"(x[n][0]));
       asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[2 * n + 1]) : "f"(x[n][3]), "f"(x[n][2]));
@@ -281,11 +286,14 @@ __global__ void __launch_bounds__(kStreamThreads, 3) paged_stream_kernel(const A
     // O += P V
     if constexpr (kQ8) {
 #pragma unroll
-      for (int j = 0; j < D / 8; ++j) {
-        const int w = j >> 2;
-        // byte j & 3 of two keys' words into the low byte of either half (what else a half holds is masked off)
-        const uint32_t sel = 0x0400 + (j & 3) * 0x0101;
-        mma_16816(o[j], p, codes_bf16(word(vq[0][0], w), word(vq[1][0], w), sel), codes_bf16(word(vq[2][0], w), word(vq[3][0], w), sel));
+      for (int w = 0; w < D / 32; ++w) {
+        uint32_t c[4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) c[n] = turn_signs(word(vq[n][0], w));
+        mma_16816(o[4 * w], p, codes_across<0>(c[0], c[1]), codes_across<0>(c[2], c[3]));
+        mma_16816(o[4 * w + 1], p, codes_across<1>(c[0], c[1]), codes_across<1>(c[2], c[3]));
+        mma_16816(o[4 * w + 2], p, codes_across<2>(c[0], c[1]), codes_across<2>(c[2], c[3]));
+        mma_16816(o[4 * w + 3], p, codes_across<3>(c[0], c[1]), codes_across<3>(c[2], c[3]));
       }
     } else {
 #pragma unroll

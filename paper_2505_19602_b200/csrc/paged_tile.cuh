@@ -10,8 +10,7 @@
 //                   for one tile while the other's softmax runs.
 //   warp 1        : TMA producer: the tile's rows, page by page, into a ring of operand tiles K_0, V_0, K_1, V_1, ...  bf16 rows land as the
 //                   products read them (128-byte swizzle), codes in the second half of their stage.
-//   warps 4-7     : with codes only, converters, which put the codes of a stage back into it as bf16: exactly, by
-//                   integer instructions and one subtraction for a pair.  They also bring the scales.
+//   warps 4-7     : with codes only, converters, which put the codes of a stage back into it as bf16 (exactly: codes_bf16) and bring the scales.
 //   the last eight: softmax, a warpgroup for each tile, a warp for each 32 rows (TMEM lanes): one sweep over their 128 products in
 //                   four chunks of 32, exponentials against a lazy reference, which rises when one exceeds it by more than 2^8, P as bf16 over the products already
 //                   read.  With codes a key's scale is a factor of its column: K's is part of the factor of the exponent's FMA, V's multiplies P
@@ -44,6 +43,7 @@ struct TileLayout {
   static constexpr int kRegs0 = kQ8 ? 56 : 72, kRegs1 = 104, kRegsS = kQ8 ? 176 : 216, kRegsLaunch = kQ8 ? 128 : 168;
   static_assert(kRegs0 + (kQ8 ? kRegs1 : 0) + 2 * kRegsS <= kRegsLaunch * (kThreads / 128), "a share would wait for registers that nobody returns");
   static constexpr int kStages = kQ8 ? 4 : 5;
+  static constexpr int kRows = kQ8 ? 4 : 1;       // rows that a softmax thread has columns of (see ld_rows)
   static constexpr uint32_t kTile = 128 * D * 2, kHalf = 128 * 128;      // an operand tile; 64 columns of it: one 128-byte swizzle span
   static constexpr uint32_t kOffQ = 0, kOffRing = 2 * kTile, kOffScale = kOffRing + kStages * kTile;
   static constexpr uint32_t kOffHoles = kOffScale + (kQ8 ? kScaleSlots * 2 * 512 : 0);
@@ -115,12 +115,14 @@ __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, vo
   return __all_sync(0xffffffffu, ok);
 }
 
-// TMEM as the softmax threads read it: 16 lanes (query rows) x 8 columns at a time, of which a thread has columns 2 c, 2 c + 1 of rows r and r + 8
+// TMEM as the softmax threads read it where rows are codes: 16 lanes (query rows) x 8 columns at a time, of which a thread has columns 2 c, 2 c + 1 of rows r and r + 8
 // (c = lane mod 4, r = lane / 4).  So a thread has a quarter of the columns of four rows, r + 8 k, and not one row's whole: the
 // scales of columns, which it loads from shared memory, are a quarter as many for the same number of products.  With all 128 columns' scales loaded by
 // each thread of a row's own, those loads alone were 2 048 of 8 900 cycles a step (a 16-byte load takes a warp four cycles, the same address or not).
 // 32 columns: x[16 h + 4 j + 2 b + e] is column 8 j + 2 c + e of row r + 16 h + 8 b.
-__device__ __forceinline__ void ld_rows(uint32_t at, float *x) {
+// R = 1: a thread has a row's 32 columns, x[i] is column i.
+template <int R> __device__ __forceinline__ void ld_rows(uint32_t at, float *x) {
+  if constexpr (R == 1) { tc_ld32(at, x); return; }
   uint32_t r[32];
 #pragma unroll
   for (int h = 0; h < 2; ++h)
@@ -133,8 +135,9 @@ __device__ __forceinline__ void ld_rows(uint32_t at, float *x) {
 #pragma unroll
   for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
 }
-// P of those 32 columns, pairs of bf16: p[8 h + 2 j + b]
-__device__ __forceinline__ void st_rows(uint32_t at, const uint32_t *p) {
+// P of those 32 columns, pairs of bf16: p[8 h + 2 j + b], or p[i / 2]
+template <int R> __device__ __forceinline__ void st_rows(uint32_t at, const uint32_t *p) {
+  if constexpr (R == 1) { tc_st16(at, p); return; }
 #pragma unroll
   for (int h = 0; h < 2; ++h)
     asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at + (uint32_t)((16 * h) << 16)), "r"(p[8 * h + 0]),
@@ -158,12 +161,19 @@ __device__ __forceinline__ void tc_st8(uint32_t at, const uint32_t *r) {
                "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
 }
-__device__ __forceinline__ float quad_max(float x) {
+// Of a thread's pairs of columns number g (of 16 / R), in its k-th row: where the pair lies in x, and P in p
+template <int R> __device__ __forceinline__ constexpr int pair_at(int g, int k) { return R == 1 ? 2 * g : 16 * (k >> 1) + 4 * g + 2 * (k & 1); }
+template <int R> __device__ __forceinline__ constexpr int p_at(int g, int k) { return R == 1 ? g : 8 * (k >> 1) + 2 * g + (k & 1); }
+template <int R> __device__ __forceinline__ constexpr int pair_col(int g) { return R == 1 ? 2 * g : 8 * g; }      // its column, less 2 c
+// The largest of what the threads of a row have
+template <int R> __device__ __forceinline__ float row_max(float x) {
+  if constexpr (R == 1) return x;
   x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
   return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
 }
-// Of the four rows of a thread the value of row `lane` of its warp
-__device__ __forceinline__ float own_row(const float *x, int lane) {
+// Of the R rows of a thread the value of row `lane` of its warp
+template <int R> __device__ __forceinline__ float own_row(const float *x, int lane) {
+  if constexpr (R == 1) return x[0];
   float y = 0.f;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -175,8 +185,8 @@ __device__ __forceinline__ float own_row(const float *x, int lane) {
 
 // What this thread's rows see of a key tile, relative to the tile's first key: columns [lo[k], hi[k]) and [0, sink), less those of `holes` (a
 // bit for each 16: their page is out of range).
-struct Seen {
-  int lo[4], hi[4], sink;
+template <int R> struct Seen {
+  int lo[R], hi[R], sink;
   uint32_t holes;
   __device__ __forceinline__ bool operator()(int k, int col) const {
     return col < hi[k] && (col >= lo[k] || col < sink) && !((holes >> (col >> 4)) & 1u);
@@ -423,8 +433,8 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       const int page = __shfl_sync(0xffffffffu, pages(i), tid >> 4), pos = key_of(i) + tid;
       const bool on = page >= 0 && in_use(pos);
       const size_t row = store_row(s, max(page, 0), head, pos);
-      k_scale = on ? __ldg(s.k_scales + row) * a.scale_log2e : 0.f;
-      v_scale = on ? __ldg(s.v_scales + row) : 0.f;
+      k_scale = on ? __ldg(s.k_scales + row) * (a.scale_log2e * kCodeUnit) : 0.f;
+      v_scale = on ? __ldg(s.v_scales + row) * kCodeUnit : 0.f;
     };
     bool ok = true;
     if (nt > 0 && rows > 0) fetch_scales(0);
@@ -441,11 +451,11 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       // 16 codes become two 16-byte pieces of a row's 128-byte span of 64 columns.  Eight lanes' stores, of two
       // neighbouring rows, meet all banks.
       auto convert = [&](const uint4 &raw, uint32_t span, int r) {
-        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+        const uint32_t w[4] = {turn_signs(raw.x), turn_signs(raw.y), turn_signs(raw.z), turn_signs(raw.w)};
 #pragma unroll
         for (int k = 0; k < 2; ++k)
-          store_shared(span + r * 128 + (((piece * 2 + k) ^ (r & 7)) << 4), codes_bf16(w[2 * k], 0u, 0x4140), codes_bf16(w[2 * k], 0u, 0x4342),
-                       codes_bf16(w[2 * k + 1], 0u, 0x4140), codes_bf16(w[2 * k + 1], 0u, 0x4342));
+          store_shared(span + r * 128 + (((piece * 2 + k) ^ (r & 7)) << 4), codes_low(w[2 * k]), codes_high(w[2 * k]), codes_low(w[2 * k + 1]),
+                       codes_high(w[2 * k + 1]));
       };
       // The codes lie in the stage's last quarter or half.  What becomes its first half can go there at once; what becomes the half that they
       // lie in is taken out by all threads before any puts it back.
@@ -454,7 +464,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 #pragma unroll
       for (int it = 0; it < 4; ++it) last[it] = load_shared16(raw_at + (it * 32 + sub) * D + (D - 64));
       if constexpr (D == 128) {
-#pragma unroll 1
+#pragma unroll 2
         for (int r = sub; r < 128; r += 32) convert(load_shared16(raw_at + r * D), stage, r);
       }
       asm volatile("bar.sync 3, 128;" ::: "memory");
@@ -489,12 +499,13 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(Y::bQFull + qt));
     }
-    // the limits of this thread's rows (lane / 4 + 8 k of the warp's), and those of the warp's rows together
+    // the limits of this thread's rows (lane / 4 + 8 k of the warp's, or its lane's own), and those of the warp's rows together
     auto token_of = [&](int i) { return a.group.div(max(min(i, all - 1), 0)); };
-    int row_lo[4], row_hi[4];
+    constexpr int R = Y::kRows, kPairs = 16 / R;           // rows of a thread, and its pairs of columns in 32
+    int row_lo[R], row_hi[R];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int p = first + token_of(tile_row0 + quarter * 32 + (lane >> 2) + 8 * k);
+    for (int k = 0; k < R; ++k) {
+      const int p = first + token_of(tile_row0 + quarter * 32 + (R == 1 ? lane : (lane >> 2) + 8 * k));
       row_lo[k] = seen_lo(a.mask, p);
       row_hi[k] = seen_hi(a.mask, p, length);
     }
@@ -504,10 +515,12 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     const float c = a.scale_log2e;
     const uint64_t c2 = pack2(c, c);
     // references start at the lowest number: differences from it are numbers
-    float m[4] = {-FLT_MAX, -FLT_MAX, -FLT_MAX, -FLT_MAX}, l[4] = {0.f, 0.f, 0.f, 0.f};
+    float m[R], l[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) { m[k] = -FLT_MAX; l[k] = 0.f; }
     const uint32_t o_addr = lane_addr + kColO + qt * 128, s_addr = lane_addr + kColS + qt * 128;
     const int steps = rows > 0 ? n_steps(qt) : 0;
-    const int quad = lane & 3;
+    const int quad = R == 1 ? 0 : lane & 3;
     bool ok = true;
     for (int j = 0; j < steps && ok; ++j) {
       const int i_tile = shared ? 2 * j + qt : j, key0 = key_of(i_tile);
@@ -517,9 +530,9 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       uint32_t holes;
       asm volatile("ld.shared.b32 %0, [%1];" : "=r"(holes) : "r"(base + Y::kOffHoles + (i_tile % kScaleSlots) * 4));
       const uint32_t scales = base + Y::kOffScale + (i_tile % kScaleSlots) * 1024, my_scales = scales + 8 * quad;
-      Seen seen;
+      Seen<R> seen;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) { seen.lo[k] = row_lo[k] - key0; seen.hi[k] = row_hi[k] - key0; }
+      for (int k = 0; k < R; ++k) { seen.lo[k] = row_lo[k] - key0; seen.hi[k] = row_hi[k] - key0; }
       seen.sink = n_sink - key0;
       seen.holes = holes;
       auto hand_over = [&](int which) {
@@ -531,49 +544,51 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       // ---- tiles that every row of the warp sees whole.  p = 2^(x - m) of a chunk in place of its products:
       auto front = [&](float *x, int cc) {
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
+        for (int g = 0; g < kPairs; ++g) {
           uint64_t k2 = c2;
           if constexpr (kQ8) {
-            const float2 two = load_shared2(my_scales + (cc * 32 + 8 * g) * 4);
+            const float2 two = load_shared2(my_scales + (cc * 32 + pair_col<R>(g)) * 4);
             k2 = pack2(two.x, two.y);
           }
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            float *y = x + 16 * (k >> 1) + 4 * g + 2 * (k & 1);
+          for (int k = 0; k < R; ++k) {
+            float *y = x + pair_at<R>(g, k);
             unpack2(fma2(pack2(y[0], y[1]), k2, pack2(-m[k], -m[k])), y[0], y[1]);
             y[0] = ex2(y[0]);
             y[1] = ex2(y[1]);
           }
         }
       };
-      // P of a chunk, and its rows' sums.  8 values of at most 2^8 sum to at most 2^11; a larger, infinite or NaN sum means that some exponent
-      // left the band.
+      // P of a chunk, and its rows' sums.  A sum above that of as many times 2^8, an infinite one or NaN means that some exponent left the band.
       auto back = [&](const float *x, uint32_t *pk, float *sum, int cc) {
-        uint64_t sums[4];
+        uint64_t sums[2][R];                       // of even and odd pairs
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
+        for (int g = 0; g < kPairs; ++g) {
           [[maybe_unused]] uint64_t v2 = 0;
           if constexpr (kQ8) {
-            const float2 two = load_shared2(my_scales + 512 + (cc * 32 + 8 * g) * 4);
+            const float2 two = load_shared2(my_scales + 512 + (cc * 32 + pair_col<R>(g)) * 4);
             v2 = pack2(two.x, two.y);
           }
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float *y = x + 16 * (k >> 1) + 4 * g + 2 * (k & 1);
+          for (int k = 0; k < R; ++k) {
+            const float *y = x + pair_at<R>(g, k);
             const uint64_t p2 = pack2(y[0], y[1]);
-            sums[k] = g == 0 ? p2 : add2(sums[k], p2);
+            sums[g & 1][k] = g < 2 ? p2 : add2(sums[g & 1][k], p2);
             float p0 = y[0], p1 = y[1];
             if constexpr (kQ8) unpack2(mul2(p2, v2), p0, p1);
-            pk[8 * (k >> 1) + 2 * g + (k & 1)] = pack_bf16(p0, p1);
+            pk[p_at<R>(g, k)] = pack_bf16(p0, p1);
           }
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < R; ++k) {
           float s0, s1;
-          unpack2(sums[k], s0, s1);
+          unpack2(add2(sums[0][k], sums[1][k]), s0, s1);
           sum[k] = s0 + s1;
         }
-        return !(sum[0] <= 2048.f && sum[1] <= 2048.f && sum[2] <= 2048.f && sum[3] <= 2048.f);
+        bool inside = true;
+#pragma unroll
+        for (int k = 0; k < R; ++k) inside = inside && sum[k] <= 256.f * (32 / R);
+        return !inside;
       };
       int cc = 0;                                  // the first chunk that is not finished
       if (holes == 0 && key0 >= warp_lo_full && key0 + kTileKeys <= warp_hi_full) {
@@ -581,25 +596,25 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         // iteration, since the roles' loops together have to stay in the SM's instruction cache: with all four unrolled a step in codes, which
         // has the converters' loop beside it, missed it 28 times in a hundred and took 7 700 cycles instead of XXXX.
         float v[2][32];
-        ld_rows(s_addr, v[0]);
-        ld_rows(s_addr + 32, v[1]);
+        ld_rows<R>(s_addr, v[0]);
+        ld_rows<R>(s_addr + 32, v[1]);
         tc_wait_ld();
         front(v[0], 0);
         auto finish = [&](int q, const float *x) {         // false: chunk q has to be taken again
           uint32_t pk[16];
-          float sum[4];
+          float sum[R];
           if (__any_sync(0xffffffffu, back(x, pk, sum, q))) return false;
-          st_rows(s_addr + q * 16, pk);
+          st_rows<R>(s_addr + q * 16, pk);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) l[k] += sum[k];
+          for (int k = 0; k < R; ++k) l[k] += sum[k];
           cc = q + 1;
           return true;
         };
-#pragma unroll 1
+#pragma unroll(kQ8 ? 1 : 2)
         for (int q = 0; q < kSweepChunks; q += 2) {
           front(v[1], q + 1);
           if (!finish(q, v[0])) break;
-          if (q == 0) ld_rows(s_addr + 64, v[0]);
+          if (q == 0) ld_rows<R>(s_addr + 64, v[0]);
           else hand_over(Y::bPEarly);
           if (q == 0) {
             tc_wait_ld();
@@ -607,7 +622,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           }
           if (!finish(q + 1, v[1])) break;
           if (q == 0) {
-            ld_rows(s_addr + 96, v[1]);
+            ld_rows<R>(s_addr + 96, v[1]);
             tc_wait_ld();
           }
         }
@@ -625,34 +640,39 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 #pragma unroll
           for (int i = 0; i < 16; ++i) pk[i] = 0u;
         } else {
-          float x[32], top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-          ld_rows(s_addr + cc * 32, x);
+          float x[32], top[R];
+#pragma unroll
+          for (int k = 0; k < R; ++k) top[k] = -INFINITY;
+          ld_rows<R>(s_addr + cc * 32, x);
           tc_wait_ld();
           uint32_t hidden = 0;
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const float2 k2 = kQ8 ? load_shared2(scales + (col0 + 8 * g) * 4) : make_float2(c, c);
+          for (int g = 0; g < kPairs; ++g) {
+            const float2 k2 = kQ8 ? load_shared2(scales + (col0 + pair_col<R>(g)) * 4) : make_float2(c, c);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              float *y = x + 16 * (k >> 1) + 4 * g + 2 * (k & 1);
-              const bool s0 = seen(k, col0 + 8 * g), s1 = seen(k, col0 + 8 * g + 1);
+            for (int k = 0; k < R; ++k) {
+              float *y = x + pair_at<R>(g, k);
+              const bool s0 = seen(k, col0 + pair_col<R>(g)), s1 = seen(k, col0 + pair_col<R>(g) + 1);
               y[0] = s0 ? y[0] * k2.x : -INFINITY;
               y[1] = s1 ? y[1] * k2.y : -INFINITY;
-              hidden |= (s0 ? 0u : 1u << (8 * g + 2 * k)) | (s1 ? 0u : 2u << (8 * g + 2 * k));
+              hidden |= (s0 ? 0u : 1u << (2 * (g * R + k))) | (s1 ? 0u : 2u << (2 * (g * R + k)));
               top[k] = max3(top[k], y[0], y[1]);
             }
           }
-          if (__any_sync(0xffffffffu, top[0] > m[0] + 8.f || top[1] > m[1] + 8.f || top[2] > m[2] + 8.f || top[3] > m[3] + 8.f)) {
-            float f[4];
+          bool rise = false;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float raised = fmaxf(m[k], quad_max(top[k]));
+          for (int k = 0; k < R; ++k) rise = rise || top[k] > m[k] + 8.f;
+          if (__any_sync(0xffffffffu, rise)) {
+            float f[R];
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+              const float raised = fmaxf(m[k], row_max<R>(top[k]));
               f[k] = ex2(m[k] - raised);
               m[k] = raised;
               l[k] *= f[k];
             }
             // P and O are scaled a lane's row at a time
-            const float f_own = own_row(f, lane);
+            const float f_own = own_row<R>(f, lane);
             const bool late = cc >= kEarly;
             uint32_t r[8];
             tc_wait_st();
@@ -682,22 +702,22 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             }
           }
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const float2 v2 = kQ8 ? load_shared2(scales + 512 + (col0 + 8 * g) * 4) : make_float2(1.f, 1.f);
+          for (int g = 0; g < kPairs; ++g) {
+            const float2 v2 = kQ8 ? load_shared2(scales + 512 + (col0 + pair_col<R>(g)) * 4) : make_float2(1.f, 1.f);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float *y = x + 16 * (k >> 1) + 4 * g + 2 * (k & 1);
+            for (int k = 0; k < R; ++k) {
+              const float *y = x + pair_at<R>(g, k);
               float p0 = ex2(y[0] - m[k]), p1 = ex2(y[1] - m[k]);
               l[k] += p0 + p1;
               if constexpr (kQ8) {                 // (a hidden value's scale may be no number)
-                p0 = (hidden >> (8 * g + 2 * k)) & 1u ? 0.f : p0 * v2.x;
-                p1 = (hidden >> (8 * g + 2 * k)) & 2u ? 0.f : p1 * v2.y;
+                p0 = (hidden >> (2 * (g * R + k))) & 1u ? 0.f : p0 * v2.x;
+                p1 = (hidden >> (2 * (g * R + k))) & 2u ? 0.f : p1 * v2.y;
               }
-              pk[8 * (k >> 1) + 2 * g + (k & 1)] = pack_bf16(p0, p1);
+              pk[p_at<R>(g, k)] = pack_bf16(p0, p1);
             }
           }
         }
-        st_rows(s_addr + cc * 16, pk);
+        st_rows<R>(s_addr + cc * 16, pk);
         if (cc == kEarly - 1) hand_over(Y::bPEarly);
       }
       if (!ok) break;
@@ -708,12 +728,13 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     float m_own = -INFINITY, l_own = 0.f;
     if (steps > 0) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < R; ++k) {
+        if (R == 1) break;
         l[k] += __shfl_xor_sync(0xffffffffu, l[k], 1);
         l[k] += __shfl_xor_sync(0xffffffffu, l[k], 2);
       }
-      m_own = own_row(m, lane);
-      l_own = own_row(l, lane);
+      m_own = own_row<R>(m, lane);
+      l_own = own_row<R>(l, lane);
     }
     // ---- the rows go out: normalised, or, where CTAs share them, as they are with their reference and sum
     if (steps > 0 && ok) ok = mbar_wait_warp(bar(Y::bFinal + qt), 0, abort_flag, status);
