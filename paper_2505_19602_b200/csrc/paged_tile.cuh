@@ -11,10 +11,11 @@
 //   warp 1        : TMA producer: the tile's rows, page by page, into a ring of operand tiles K_0, V_0, K_1, V_1, ...  bf16 rows land as the
 //                   products read them (128-byte swizzle), codes in the second half of their stage.
 //   warps 4-7     : with codes only, converters, which put the codes of a stage back into it as bf16 (exactly: codes_bf16) and bring the scales.
-//   the last eight: softmax, a warpgroup for each tile, a warp for each 32 rows (TMEM lanes): one sweep over their 128 products in
+//   the last eight: softmax, a warpgroup for each tile, a thread for each row (TMEM lane): one sweep over its 128 products in
 //                   four chunks of 32, exponentials against a lazy reference, which rises when one exceeds it by more than 2^8, P as bf16 over the products already
 //                   read.  With codes a key's scale is a factor of its column: K's is part of the factor of the exponent's FMA, V's multiplies P
-//                   before it is rounded; both come from shared memory.
+//                   before it is rounded; both come from shared memory, four columns to a load.  (A thread with a quarter of the columns of four rows loads a quarter as many
+//                   scales, but its sweep was the longer: 1 478 us for what is 1 247.)
 // Rows that no query of the item sees (behind the length, ahead of the window, on a page out of range) may hold anything.  Their products are hidden one
 // by one; as values codes are numbers whatever they are, and bf16 rows are zeroed by the issuer before the product reads them.
 // Every wait is bounded; one that gives up raises the sticky status and all roles fall through to the end.
@@ -33,7 +34,7 @@ using namespace scalekv::tc;
 constexpr int kItemRows = 256;
 constexpr int kTileKeys = 128;
 constexpr int kSweepChunks = 4;
-constexpr int kEarly = 3;                         // (the sweep's loop counts on it) chunks whose part of the PV product is issued under the rest of the sweep
+constexpr int kEarly = 3;                         // chunks whose part of the PV product is issued under the rest of the sweep
 constexpr int kScaleSlots = 4;                    // key tiles whose scales are held (see the loaders)
 
 template <int D, bool kQ8>
@@ -43,7 +44,6 @@ struct TileLayout {
   static constexpr int kRegs0 = kQ8 ? 56 : 72, kRegs1 = 104, kRegsS = kQ8 ? 176 : 216, kRegsLaunch = kQ8 ? 128 : 168;
   static_assert(kRegs0 + (kQ8 ? kRegs1 : 0) + 2 * kRegsS <= kRegsLaunch * (kThreads / 128), "a share would wait for registers that nobody returns");
   static constexpr int kStages = kQ8 ? 4 : 5;
-  static constexpr int kRows = kQ8 ? 4 : 1;       // rows that a softmax thread has columns of (see ld_rows)
   static constexpr uint32_t kTile = 128 * D * 2, kHalf = 128 * 128;      // an operand tile; 64 columns of it: one 128-byte swizzle span
   static constexpr uint32_t kOffQ = 0, kOffRing = 2 * kTile, kOffScale = kOffRing + kStages * kTile;
   static constexpr uint32_t kOffHoles = kOffScale + (kQ8 ? kScaleSlots * 2 * 512 : 0);
@@ -115,35 +115,6 @@ __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, vo
   return __all_sync(0xffffffffu, ok);
 }
 
-// TMEM as the softmax threads read it where rows are codes: 16 lanes (query rows) x 8 columns at a time, of which a thread has columns 2 c, 2 c + 1 of rows r and r + 8
-// (c = lane mod 4, r = lane / 4).  So a thread has a quarter of the columns of four rows, r + 8 k, and not one row's whole: the
-// scales of columns, which it loads from shared memory, are a quarter as many for the same number of products.  With all 128 columns' scales loaded by
-// each thread of a row's own, those loads alone were 2 048 of 8 900 cycles a step (a 16-byte load takes a warp four cycles, the same address or not).
-// 32 columns: x[16 h + 4 j + 2 b + e] is column 8 j + 2 c + e of row r + 16 h + 8 b.
-// R = 1: a thread has a row's 32 columns, x[i] is column i.
-template <int R> __device__ __forceinline__ void ld_rows(uint32_t at, float *x) {
-  if constexpr (R == 1) { tc_ld32(at, x); return; }
-  uint32_t r[32];
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-                 : "=r"(r[16 * h + 0]), "=r"(r[16 * h + 1]), "=r"(r[16 * h + 2]), "=r"(r[16 * h + 3]), "=r"(r[16 * h + 4]), "=r"(r[16 * h + 5]),
-                   "=r"(r[16 * h + 6]), "=r"(r[16 * h + 7]), "=r"(r[16 * h + 8]), "=r"(r[16 * h + 9]), "=r"(r[16 * h + 10]), "=r"(r[16 * h + 11]),
-                   "=r"(r[16 * h + 12]), "=r"(r[16 * h + 13]), "=r"(r[16 * h + 14]), "=r"(r[16 * h + 15])
-                 : "r"(at + (uint32_t)((16 * h) << 16))
-                 : "memory");
-#pragma unroll
-  for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
-}
-// P of those 32 columns, pairs of bf16: p[8 h + 2 j + b], or p[i / 2]
-template <int R> __device__ __forceinline__ void st_rows(uint32_t at, const uint32_t *p) {
-  if constexpr (R == 1) { tc_st16(at, p); return; }
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-    asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at + (uint32_t)((16 * h) << 16)), "r"(p[8 * h + 0]),
-                 "r"(p[8 * h + 1]), "r"(p[8 * h + 2]), "r"(p[8 * h + 3]), "r"(p[8 * h + 4]), "r"(p[8 * h + 5]), "r"(p[8 * h + 6]), "r"(p[8 * h + 7])
-                 : "memory");
-}
 __device__ __forceinline__ float2 load_shared2(uint32_t at) {
   float2 x;
   asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(at));
@@ -161,35 +132,13 @@ __device__ __forceinline__ void tc_st8(uint32_t at, const uint32_t *r) {
                "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
 }
-// Of a thread's pairs of columns number g (of 16 / R), in its k-th row: where the pair lies in x, and P in p
-template <int R> __device__ __forceinline__ constexpr int pair_at(int g, int k) { return R == 1 ? 2 * g : 16 * (k >> 1) + 4 * g + 2 * (k & 1); }
-template <int R> __device__ __forceinline__ constexpr int p_at(int g, int k) { return R == 1 ? g : 8 * (k >> 1) + 2 * g + (k & 1); }
-template <int R> __device__ __forceinline__ constexpr int pair_col(int g) { return R == 1 ? 2 * g : 8 * g; }      // its column, less 2 c
-// The largest of what the threads of a row have
-template <int R> __device__ __forceinline__ float row_max(float x) {
-  if constexpr (R == 1) return x;
-  x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-  return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-}
-// Of the R rows of a thread the value of row `lane` of its warp
-template <int R> __device__ __forceinline__ float own_row(const float *x, int lane) {
-  if constexpr (R == 1) return x[0];
-  float y = 0.f;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const float z = __shfl_sync(0xffffffffu, x[k], (lane & 7) * 4);
-    if (lane >> 3 == k) y = z;
-  }
-  return y;
-}
-
-// What this thread's rows see of a key tile, relative to the tile's first key: columns [lo[k], hi[k]) and [0, sink), less those of `holes` (a
-// bit for each 16: their page is out of range).
-template <int R> struct Seen {
-  int lo[R], hi[R], sink;
+// What a row sees of a key tile, relative to the tile's first key: columns [lo, hi) and [0, sink), less those of `holes` (a bit for
+// each 16: their page is out of range).
+struct Seen {
+  int lo, hi, sink;
   uint32_t holes;
-  __device__ __forceinline__ bool operator()(int k, int col) const {
-    return col < hi[k] && (col >= lo[k] || col < sink) && !((holes >> (col >> 4)) & 1u);
+  __device__ __forceinline__ bool operator()(int col) const {
+    return col < hi && (col >= lo || col < sink) && !((holes >> (col >> 4)) & 1u);
   }
 };
 
@@ -499,28 +448,19 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(Y::bQFull + qt));
     }
-    // the limits of this thread's rows (lane / 4 + 8 k of the warp's, or its lane's own), and those of the warp's rows together
+    // this row's limits, and those of the warp's rows together
+    const int i_own = tile_row0 + row;                     // this thread's row, of the sequence's
     auto token_of = [&](int i) { return a.group.div(max(min(i, all - 1), 0)); };
-    constexpr int R = Y::kRows, kPairs = 16 / R;           // rows of a thread, and its pairs of columns in 32
-    int row_lo[R], row_hi[R];
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-      const int p = first + token_of(tile_row0 + quarter * 32 + (R == 1 ? lane : (lane >> 2) + 8 * k));
-      row_lo[k] = seen_lo(a.mask, p);
-      row_hi[k] = seen_hi(a.mask, p, length);
-    }
-    const int p_top = first + token_of(tile_row0 + quarter * 32), p_end = first + token_of(tile_row0 + quarter * 32 + 31);
+    const int t_own = token_of(i_own), p_top = first + token_of(tile_row0 + quarter * 32), p_end = first + token_of(tile_row0 + quarter * 32 + 31);
+    const int row_lo = seen_lo(a.mask, first + t_own), row_hi = seen_hi(a.mask, first + t_own, length);
     const int warp_lo = seen_lo(a.mask, p_top), warp_lo_full = seen_lo(a.mask, p_end);
     const int warp_hi = seen_hi(a.mask, p_end, length), warp_hi_full = seen_hi(a.mask, p_top, length);
     const float c = a.scale_log2e;
     const uint64_t c2 = pack2(c, c);
-    // references start at the lowest number: differences from it are numbers
-    float m[R], l[R];
-#pragma unroll
-    for (int k = 0; k < R; ++k) { m[k] = -FLT_MAX; l[k] = 0.f; }
+    // the reference starts at the lowest number: differences from it are numbers
+    float m = -FLT_MAX, l = 0.f;
     const uint32_t o_addr = lane_addr + kColO + qt * 128, s_addr = lane_addr + kColS + qt * 128;
     const int steps = rows > 0 ? n_steps(qt) : 0;
-    const int quad = R == 1 ? 0 : lane & 3;
     bool ok = true;
     for (int j = 0; j < steps && ok; ++j) {
       const int i_tile = shared ? 2 * j + qt : j, key0 = key_of(i_tile);
@@ -529,12 +469,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       tc_fence_after();
       uint32_t holes;
       asm volatile("ld.shared.b32 %0, [%1];" : "=r"(holes) : "r"(base + Y::kOffHoles + (i_tile % kScaleSlots) * 4));
-      const uint32_t scales = base + Y::kOffScale + (i_tile % kScaleSlots) * 1024, my_scales = scales + 8 * quad;
-      Seen<R> seen;
-#pragma unroll
-      for (int k = 0; k < R; ++k) { seen.lo[k] = row_lo[k] - key0; seen.hi[k] = row_hi[k] - key0; }
-      seen.sink = n_sink - key0;
-      seen.holes = holes;
+      const uint32_t scales = base + Y::kOffScale + (i_tile % kScaleSlots) * 1024;       // K's, 512 bytes further V's
       auto hand_over = [&](int which) {
         tc_wait_st();
         tc_fence_before();
@@ -543,86 +478,73 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       };
       // ---- tiles that every row of the warp sees whole.  p = 2^(x - m) of a chunk in place of its products:
       auto front = [&](float *x, int cc) {
+        const uint64_t negm2 = pack2(-m, -m);
 #pragma unroll
-        for (int g = 0; g < kPairs; ++g) {
-          uint64_t k2 = c2;
+        for (int i = 0; i < 32; i += 4) {
+          uint64_t k0 = c2, k1 = c2;
           if constexpr (kQ8) {
-            const float2 two = load_shared2(my_scales + (cc * 32 + pair_col<R>(g)) * 4);
-            k2 = pack2(two.x, two.y);
+            const float4 k = load_shared4(scales + (cc * 32 + i) * 4);
+            k0 = pack2(k.x, k.y);
+            k1 = pack2(k.z, k.w);
           }
+          unpack2(fma2(pack2(x[i], x[i + 1]), k0, negm2), x[i], x[i + 1]);
+          unpack2(fma2(pack2(x[i + 2], x[i + 3]), k1, negm2), x[i + 2], x[i + 3]);
 #pragma unroll
-          for (int k = 0; k < R; ++k) {
-            float *y = x + pair_at<R>(g, k);
-            unpack2(fma2(pack2(y[0], y[1]), k2, pack2(-m[k], -m[k])), y[0], y[1]);
-            y[0] = ex2(y[0]);
-            y[1] = ex2(y[1]);
-          }
+          for (int e = 0; e < 4; ++e) x[i + e] = ex2(x[i + e]);
         }
       };
-      // P of a chunk, and its rows' sums.  A sum above that of as many times 2^8, an infinite one or NaN means that some exponent left the band.
-      auto back = [&](const float *x, uint32_t *pk, float *sum, int cc) {
-        uint64_t sums[2][R];                       // of even and odd pairs
+      // P of a chunk, and its sum: 32 values of at most 2^8 sum to at most 2^13; a larger, infinite or NaN sum means that some exponent left the band.
+      auto back = [&](const float *x, uint32_t *pk, int cc) {
+        uint64_t sum_a = pack2(0.f, 0.f), sum_b = sum_a;
 #pragma unroll
-        for (int g = 0; g < kPairs; ++g) {
-          [[maybe_unused]] uint64_t v2 = 0;
+        for (int i = 0; i < 32; i += 4) {
+          const uint64_t p0 = pack2(x[i], x[i + 1]), p1 = pack2(x[i + 2], x[i + 3]);
+          sum_a = add2(sum_a, p0);
+          sum_b = add2(sum_b, p1);
+          float y[4] = {x[i], x[i + 1], x[i + 2], x[i + 3]};
           if constexpr (kQ8) {
-            const float2 two = load_shared2(my_scales + 512 + (cc * 32 + pair_col<R>(g)) * 4);
-            v2 = pack2(two.x, two.y);
+            const float4 k = load_shared4(scales + 512 + (cc * 32 + i) * 4);
+            unpack2(mul2(p0, pack2(k.x, k.y)), y[0], y[1]);
+            unpack2(mul2(p1, pack2(k.z, k.w)), y[2], y[3]);
           }
-#pragma unroll
-          for (int k = 0; k < R; ++k) {
-            const float *y = x + pair_at<R>(g, k);
-            const uint64_t p2 = pack2(y[0], y[1]);
-            sums[g & 1][k] = g < 2 ? p2 : add2(sums[g & 1][k], p2);
-            float p0 = y[0], p1 = y[1];
-            if constexpr (kQ8) unpack2(mul2(p2, v2), p0, p1);
-            pk[p_at<R>(g, k)] = pack_bf16(p0, p1);
-          }
+          pk[i / 2] = pack_bf16(y[0], y[1]);
+          pk[i / 2 + 1] = pack_bf16(y[2], y[3]);
         }
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-          float s0, s1;
-          unpack2(add2(sums[0][k], sums[1][k]), s0, s1);
-          sum[k] = s0 + s1;
-        }
-        bool inside = true;
-#pragma unroll
-        for (int k = 0; k < R; ++k) inside = inside && sum[k] <= 256.f * (32 / R);
-        return !inside;
+        float s0, s1;
+        unpack2(add2(sum_a, sum_b), s0, s1);
+        return s0 + s1;
       };
       int cc = 0;                                  // the first chunk that is not finished
       if (holes == 0 && key0 >= warp_lo_full && key0 + kTileKeys <= warp_hi_full) {
-        // Software-pipelined: the exponentials of the next chunk are under way while this one is summed, checked and stored.  Two chunks to an
-        // iteration, since the roles' loops together have to stay in the SM's instruction cache: with all four unrolled a step in codes, which
-        // has the converters' loop beside it, missed it 28 times in a hundred and took 7 700 cycles instead of XXXX.
+        // Software-pipelined: the exponentials of the next chunk are under way while this one is summed, checked and stored.
         float v[2][32];
-        ld_rows<R>(s_addr, v[0]);
-        ld_rows<R>(s_addr + 32, v[1]);
+        tc_ld32(s_addr, v[0]);
+        tc_ld32(s_addr + 32, v[1]);
         tc_wait_ld();
         front(v[0], 0);
         auto finish = [&](int q, const float *x) {         // false: chunk q has to be taken again
           uint32_t pk[16];
-          float sum[R];
-          if (__any_sync(0xffffffffu, back(x, pk, sum, q))) return false;
-          st_rows<R>(s_addr + q * 16, pk);
-#pragma unroll
-          for (int k = 0; k < R; ++k) l[k] += sum[k];
+          const float sum = back(x, pk, q);
+          if (__any_sync(0xffffffffu, !(sum <= 8192.f))) return false;
+          tc_st16(s_addr + q * 16, pk);
+          l += sum;
           cc = q + 1;
           return true;
         };
-#pragma unroll(kQ8 ? 1 : 2)
+#pragma unroll
         for (int q = 0; q < kSweepChunks; q += 2) {
           front(v[1], q + 1);
           if (!finish(q, v[0])) break;
-          if (q == 0) ld_rows<R>(s_addr + 64, v[0]);
-          else hand_over(Y::bPEarly);
           if (q == 0) {
+            tc_ld32(s_addr + 64, v[0]);
             tc_wait_ld();
             front(v[0], 2);
+          } else {
+            hand_over(Y::bPEarly);
           }
           if (!finish(q + 1, v[1])) break;
           if (q == 0) {
-            ld_rows<R>(s_addr + 96, v[1]);
+            tc_ld32(s_addr + 96, v[1]);
             tc_wait_ld();
           }
         }
@@ -631,48 +553,35 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       // left of a tile once an exponent has left the band.  Where one is more than 2^8 above a row's reference, the references of all the warp's rows rise
       // to their chunk's largest, and what was accumulated under the old one is multiplied by f = 2^(old - new): the sum, P of the chunks that the
       // tensor core has not been given yet, and O, once the last product given to it has landed.
+      // (One loop for both, not unrolled: the roles' loops together have to stay in the SM's instruction cache.  With a masked copy of the sweep above and a copy of
+      // the raise in each of its chunks a step in codes, which has the converters' loop beside it, missed it 28 times in a hundred: 2 255 us for what is 1 247.)
+      const Seen seen = {row_lo - key0, row_hi - key0, n_sink - key0, holes};
       int landed = 0;                              // 1: the last step's product has; 2: the early part of this one's, too
 #pragma unroll 1
       for (; cc < kSweepChunks && ok; ++cc) {
-        const int col0 = cc * 32 + 2 * quad, at = key0 + cc * 32;
+        const int col0 = cc * 32, at = key0 + col0;
         uint32_t pk[16];
         if (at >= warp_hi || (at + 32 <= warp_lo && at >= n_sink)) {       // no row of the warp sees it
 #pragma unroll
           for (int i = 0; i < 16; ++i) pk[i] = 0u;
         } else {
-          float x[32], top[R];
-#pragma unroll
-          for (int k = 0; k < R; ++k) top[k] = -INFINITY;
-          ld_rows<R>(s_addr + cc * 32, x);
+          float x[32], top = -INFINITY;
+          tc_ld32(s_addr + col0, x);
           tc_wait_ld();
           uint32_t hidden = 0;
 #pragma unroll
-          for (int g = 0; g < kPairs; ++g) {
-            const float2 k2 = kQ8 ? load_shared2(scales + (col0 + pair_col<R>(g)) * 4) : make_float2(c, c);
-#pragma unroll
-            for (int k = 0; k < R; ++k) {
-              float *y = x + pair_at<R>(g, k);
-              const bool s0 = seen(k, col0 + pair_col<R>(g)), s1 = seen(k, col0 + pair_col<R>(g) + 1);
-              y[0] = s0 ? y[0] * k2.x : -INFINITY;
-              y[1] = s1 ? y[1] * k2.y : -INFINITY;
-              hidden |= (s0 ? 0u : 1u << (2 * (g * R + k))) | (s1 ? 0u : 2u << (2 * (g * R + k)));
-              top[k] = max3(top[k], y[0], y[1]);
-            }
+          for (int i = 0; i < 32; i += 2) {
+            const float2 k = kQ8 ? load_shared2(scales + (col0 + i) * 4) : make_float2(c, c);
+            const bool s0 = seen(col0 + i), s1 = seen(col0 + i + 1);
+            x[i] = s0 ? x[i] * k.x : -INFINITY;
+            x[i + 1] = s1 ? x[i + 1] * k.y : -INFINITY;
+            hidden |= (s0 ? 0u : 1u << i) | (s1 ? 0u : 2u << i);
+            top = max3(top, x[i], x[i + 1]);
           }
-          bool rise = false;
-#pragma unroll
-          for (int k = 0; k < R; ++k) rise = rise || top[k] > m[k] + 8.f;
-          if (__any_sync(0xffffffffu, rise)) {
-            float f[R];
-#pragma unroll
-            for (int k = 0; k < R; ++k) {
-              const float raised = fmaxf(m[k], row_max<R>(top[k]));
-              f[k] = ex2(m[k] - raised);
-              m[k] = raised;
-              l[k] *= f[k];
-            }
-            // P and O are scaled a lane's row at a time
-            const float f_own = own_row<R>(f, lane);
+          if (__any_sync(0xffffffffu, top > m + 8.f)) {
+            const float raised = fmaxf(m, top), f = ex2(m - raised);
+            m = raised;
+            l *= f;
             const bool late = cc >= kEarly;
             uint32_t r[8];
             tc_wait_st();
@@ -681,7 +590,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
               tc_ld8(s_addr + e * 8, r);
               tc_wait_ld();
 #pragma unroll
-              for (int i = 0; i < 8; ++i) r[i] = pack_bf16(__uint_as_float(r[i] << 16) * f_own, __uint_as_float(r[i] & 0xffff0000u) * f_own);
+              for (int i = 0; i < 8; ++i) r[i] = pack_bf16(__uint_as_float(r[i] << 16) * f, __uint_as_float(r[i] & 0xffff0000u) * f);
               tc_st8(s_addr + e * 8, r);
             }
             if (late || j > 0) {
@@ -696,45 +605,28 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                 tc_ld8(o_addr + e * 8, r);
                 tc_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f_own);
+                for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
                 tc_st8(o_addr + e * 8, r);
               }
             }
           }
 #pragma unroll
-          for (int g = 0; g < kPairs; ++g) {
-            const float2 v2 = kQ8 ? load_shared2(scales + 512 + (col0 + pair_col<R>(g)) * 4) : make_float2(1.f, 1.f);
-#pragma unroll
-            for (int k = 0; k < R; ++k) {
-              const float *y = x + pair_at<R>(g, k);
-              float p0 = ex2(y[0] - m[k]), p1 = ex2(y[1] - m[k]);
-              l[k] += p0 + p1;
-              if constexpr (kQ8) {                 // (a hidden value's scale may be no number)
-                p0 = (hidden >> (2 * (g * R + k))) & 1u ? 0.f : p0 * v2.x;
-                p1 = (hidden >> (2 * (g * R + k))) & 2u ? 0.f : p1 * v2.y;
-              }
-              pk[p_at<R>(g, k)] = pack_bf16(p0, p1);
+          for (int i = 0; i < 32; i += 2) {
+            const float2 k = kQ8 ? load_shared2(scales + 512 + (col0 + i) * 4) : make_float2(1.f, 1.f);
+            float p0 = ex2(x[i] - m), p1 = ex2(x[i + 1] - m);
+            l += p0 + p1;
+            if constexpr (kQ8) {                   // (a hidden value's scale may be no number)
+              p0 = (hidden >> i) & 1u ? 0.f : p0 * k.x;
+              p1 = (hidden >> i) & 2u ? 0.f : p1 * k.y;
             }
+            pk[i / 2] = pack_bf16(p0, p1);
           }
         }
-        st_rows<R>(s_addr + cc * 16, pk);
+        tc_st16(s_addr + cc * 16, pk);
         if (cc == kEarly - 1) hand_over(Y::bPEarly);
       }
       if (!ok) break;
       hand_over(Y::bPFull);
-    }
-    // from here on a thread has a row of its own, i_own of the sequence's
-    const int i_own = tile_row0 + row, t_own = token_of(i_own);
-    float m_own = -INFINITY, l_own = 0.f;
-    if (steps > 0) {
-#pragma unroll
-      for (int k = 0; k < R; ++k) {
-        if (R == 1) break;
-        l[k] += __shfl_xor_sync(0xffffffffu, l[k], 1);
-        l[k] += __shfl_xor_sync(0xffffffffu, l[k], 2);
-      }
-      m_own = own_row<R>(m, lane);
-      l_own = own_row<R>(l, lane);
     }
     // ---- the rows go out: normalised, or, where CTAs share them, as they are with their reference and sum
     if (steps > 0 && ok) ok = mbar_wait_warp(bar(Y::bFinal + qt), 0, abort_flag, status);
@@ -766,7 +658,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     };
     if (rows > 0 && ok && !shared && (pair || qt == 0)) {
       // (a row that saw nothing has a sum of 0 and an accumulator of zeros, or none at all)
-      const float f = split ? 1.f : (l_own == 0.f ? 0.f : 1.f / l_own);
+      const float f = split ? 1.f : (l == 0.f ? 0.f : 1.f / l);
 #pragma unroll 1
       for (int cc = 0; cc < D / 32; ++cc) {
         float o[32];
@@ -779,22 +671,22 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         }
         put(o, cc * 32, f);
       }
-      put_sums(m_own, l_own);
+      put_sums(m, l);
     } else if (shared) {
       // the two halves of the keys: both accumulators lie in the same lanes, so only references and sums are handed over (through the
       // second query tile's place, which a single does not use); each warpgroup finishes half of the columns
       const uint32_t stat = base + Y::kOffQ + kTile + (uint32_t)row * 8;
-      if (!ok) l_own = -1.f;                                   // (no sum is negative)
-      asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(stat + (uint32_t)qt * 1024), "f"(m_own), "f"(l_own) : "memory");
+      if (!ok) l = -1.f;                                   // (no sum is negative)
+      asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(stat + (uint32_t)qt * 1024), "f"(m), "f"(l) : "memory");
       tc_fence_before();
       asm volatile("bar.sync 2, 256;" ::: "memory");
       tc_fence_after();
       float m2, l2;
       asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(m2), "=f"(l2) : "r"(stat + (uint32_t)(qt ^ 1) * 1024) : "memory");
-      const float top = fmaxf(m_own, m2);
-      const float f1 = l_own == 0.f ? 0.f : ex2(m_own - top), f2 = l2 == 0.f ? 0.f : ex2(m2 - top), sum = l_own * f1 + l2 * f2;
+      const float top = fmaxf(m, m2);
+      const float f1 = l == 0.f ? 0.f : ex2(m - top), f2 = l2 == 0.f ? 0.f : ex2(m2 - top), sum = l * f1 + l2 * f2;
       const float f = split ? 1.f : (sum == 0.f ? 0.f : 1.f / sum);
-      if (__all_sync(0xffffffffu, !(l_own < 0.f || l2 < 0.f))) {
+      if (__all_sync(0xffffffffu, !(l < 0.f || l2 < 0.f))) {
 #pragma unroll 1
         for (int cc = 0; cc < D / 64; ++cc) {
           const int col = qt * (D / 2) + cc * 32;
