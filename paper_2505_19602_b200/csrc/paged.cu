@@ -22,6 +22,7 @@ namespace {
 // Rows of partial results that a launch may leave (rows of the call times CTAs that share a row's keys).
 constexpr long long kPartRows = 148 * 256;
 constexpr size_t kStatusBytes = 256;
+constexpr int kMaxCounts = 4096;         // sequences times kv heads of a launch whose keys are shared
 constexpr int kMaxLength = 1 << 30;      // tokens that a sequence's pages may hold: sums of a position and a window stay in 32 bits
 
 struct Layout {
@@ -45,7 +46,7 @@ scalekv_status make_layout(const scalekv_paged_config *c, Layout &y, std::string
   y.rows_bytes = n * c->head_dim * (c->store == SCALEKV_STORE_Q8 ? 1 : 2);
   y.scale_bytes = c->store == SCALEKV_STORE_Q8 ? n * 4 : 0;
   y.pool_bytes = 2 * (y.rows_bytes + y.scale_bytes);
-  y.ws_bytes = kStatusBytes + (size_t)kPartRows * (c->head_dim + 2) * 4;
+  y.ws_bytes = kStatusBytes + kMaxCounts * 4 + (size_t)kPartRows * (c->head_dim + 2) * 4;
   return SCALEKV_OK;
 }
 
@@ -123,6 +124,15 @@ void launch_store(const Store &s, const Batch &bt, const Rows &K, const Rows &V,
 }
 
 template <int D, bool kQ8>
+scalekv_status launch_stream(scalekv_paged *c, const AttendArgs &a, int split, cudaStream_t stream) {
+  constexpr int smem = StreamLayout<D, kQ8>::kSmem;
+  if (cudaFuncSetAttribute(paged_stream_kernel<D, kQ8>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+    return fail(c, SCALEKV_ERR_CUDA, "cannot raise the dynamic shared memory limit");
+  paged_stream_kernel<D, kQ8><<<dim3(a.bt.n_seqs, a.s.heads, split), kStreamThreads, smem, stream>>>(a);
+  return launched(c, "paged_attend");
+}
+
+template <int D, bool kQ8>
 scalekv_status launch_tile(scalekv_paged *c, int layer, const AttendArgs &a, int items, int split, cudaStream_t stream) {
   constexpr uint32_t smem = TileLayout<D, kQ8>::kSmem;
   // (per device and process; the answer is the same every time)
@@ -197,7 +207,7 @@ scalekv_status scalekv_paged_init(const scalekv_paged_config *cfg, scalekv_paged
   while ((1 << c->page_shift) < cfg->page_tokens) ++c->page_shift;
   if (cudaSetDevice(cfg->device) != cudaSuccess ||
       cudaDeviceGetAttribute(&c->n_sm, cudaDevAttrMultiProcessorCount, cfg->device) != cudaSuccess ||
-      cudaMemset(cfg->workspace, 0, kStatusBytes) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
+      cudaMemset(cfg->workspace, 0, kStatusBytes + kMaxCounts * 4) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
     fprintf(stderr, "scalekv_paged_init: %s\n", cudaGetErrorString(cudaGetLastError()));
     delete c;
     return SCALEKV_ERR_CUDA;
@@ -245,12 +255,12 @@ scalekv_status scalekv_paged_attend(scalekv_paged *kv, int32_t layer, const scal
   const int G = n_heads / H;
   const long long max_rows = (long long)std::min(batch->max_new, a.bt.n_tokens) * G;      // query rows of a sequence and kv head
   if (all_rows > kMaxLength) return fail(c, SCALEKV_ERR_UNSUPPORTED, "more than 2^30 query rows in a call");
-  const long long tiles = (max_rows + kTileRows - 1) / kTileRows;
-  if (tiles * a.bt.n_seqs > 0x7fffffffLL || H > 65535) return fail(c, SCALEKV_ERR_UNSUPPORTED, "too many row tiles in a call");
+  if (H > 65535) return fail(c, SCALEKV_ERR_UNSUPPORTED, "more than 65535 kv heads");
   a.s = layer_store(c, layer);
   a.Q = view(Q, 2); a.O = view(O, 2);
   a.lse = lse;
-  a.part_o = reinterpret_cast<float *>(static_cast<char *>(c->cfg.workspace) + kStatusBytes);
+  a.counts = reinterpret_cast<int *>(static_cast<char *>(c->cfg.workspace) + kStatusBytes);
+  a.part_o = reinterpret_cast<float *>(a.counts + kMaxCounts);
   a.part_ml = a.part_o + (size_t)kPartRows * D;
   a.mask = {mask->causal != 0, std::min(mask->window, kMaxLength), mask->n_sink};
   a.group = Divisor::of(G);
@@ -264,19 +274,15 @@ scalekv_status scalekv_paged_attend(scalekv_paged *kv, int32_t layer, const scal
   long long split;
   scalekv_status done;
   if (max_rows <= kTileRows) {
-    const long long items = tiles * a.bt.n_seqs * H;
+    const long long items = a.bt.n_seqs * H;
     const int steps = (int)((keys + 15) / 16);
-    split = std::min<long long>((3ll * c->n_sm + items - 1) / items, (steps + 2 * kStreamWarps - 1) / (2 * kStreamWarps));
+    const int slots = c->n_sm * (q8 || D == 64 ? 4 : 2);
+    split = std::min<long long>((slots + items - 1) / items, (steps + 2 * kStreamWarps - 1) / (2 * kStreamWarps));
     split = std::max<long long>(1, std::min<long long>(split, kPartRows / all_rows));
-    const dim3 grid((unsigned)(tiles * a.bt.n_seqs), H, (unsigned)split);
-    if (D == 128) {
-      if (q8) paged_stream_kernel<128, true><<<grid, kStreamThreads, 0, st>>>(a, (int)tiles);
-      else paged_stream_kernel<128, false><<<grid, kStreamThreads, 0, st>>>(a, (int)tiles);
-    } else {
-      if (q8) paged_stream_kernel<64, true><<<grid, kStreamThreads, 0, st>>>(a, (int)tiles);
-      else paged_stream_kernel<64, false><<<grid, kStreamThreads, 0, st>>>(a, (int)tiles);
-    }
-    done = launched(c, "paged_attend");
+    if (items > kMaxCounts) split = 1;
+    if (D == 128) done = q8 ? launch_stream<128, true>(c, a, (int)split, st) : launch_stream<128, false>(c, a, (int)split, st);
+    else done = q8 ? launch_stream<64, true>(c, a, (int)split, st) : launch_stream<64, false>(c, a, (int)split, st);
+    return done;
   } else {
     // no more items than this, whatever the starts say
     const long long items = std::min<long long>((long long)a.bt.n_tokens * G / kItemRows + a.bt.n_seqs, (max_rows + kItemRows - 1) / kItemRows * a.bt.n_seqs);

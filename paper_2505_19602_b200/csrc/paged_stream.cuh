@@ -2,30 +2,51 @@
 //
 //   y_j = scale <q, k_j>,  lse = log sum_j exp(y_j),  O = sum_j exp(y_j - lse) v_j   over the keys j that the row sees.
 //
-// A kv head's query rows, the group's heads of every new token, share its keys: row r is head r mod G of token r / G, 16 rows a tile.
+// A kv head's query rows, the group's heads of every new token, share its keys: row r is head r mod G of token r / G, up to 16 of them.
 // What bounds it is reading the keys and values once: 2 (d + 4) bytes a key as codes, 4 d as bf16, against 8 d products a key and row.
-// So a warp streams its share of the cache from global memory straight into the registers of the matrix instructions (m16n8k16, rows x keys x
-// dims), with nothing staged in shared memory and no barrier before the end:
-//   - 16 keys at a time, which lie in one page.  The eight keys of an n-tile are one to each four lanes, as the B operand has them, and
-//     since a product's sum may run in any order, a lane takes whichever dims make its loads 16 bytes long; the query operand is read
-//     in the same order.
-//   - V's pairs of keys are interleaved from rows held by the lane, and its dims are dealt to the n-tiles so that those rows are 16 bytes long, too.
-//   - Codes become bf16 exactly (codes_bf16).  The key's scale multiplies the product, the value's scale multiplies P, both in fp32; P is rounded to bf16 for its product with V, as it is where rows are bf16.
-//   - While one half (K or V) of a step is computed with, the other half's loads are under way.
+// So every warp streams its own share of the cache, 16 keys (which lie in one page) at a time, through a ring of stages in shared memory that it
+// fills with asynchronous copies and shares with nobody: no barrier before the end, and the loads of a few steps are always under way.
+// (With the loads in registers, half a step ahead, a step took a loaded DRAM latency: 32 sequences of up to 10 521 entries, 8 kv heads in codes, 285 us for
+// what is XXXX.)  Products are m16n8k16, rows x keys x dims:
+//   - K's eight keys of an n-tile are one to each four lanes, as the B operand has them, and since a product's sum may run in any order, a lane
+//     takes the dims that lie in its 16-byte piece; the query operand is read in the same order.
+//   - V's pairs of keys are interleaved from two rows' pieces, and its dims are dealt to the n-tiles so that those are 16 bytes long, too.
+//   - Pieces are placed in a stage so that eight lanes' loads meet all banks, K's (two rows, four pieces) and V's (four rows, two pieces).
+//   - Codes become bf16 exactly (codes_bf16).  The key's scale multiplies the product, the value's scale multiplies P, both in fp32; P is rounded to bf16
+//     for its product with V, as it is where rows are bf16.
 // The running maximum of a row is raised when a step exceeds it by more than 2^3, and the sums with it: P stays below 2^8.
-// A CTA's four warps take the steps in turn and are combined in shared memory; gridDim.z CTAs share a row tile's keys where there
-// are few, and paged_join_kernel combines what they leave.
+// A CTA's four warps take the steps in turn and are combined in shared memory.  Where a sequence's heads are few, gridDim.z CTAs share its
+// keys; each leaves its part in the workspace, and the last one to do so, by a counter that it sets back, combines them in their order.
 #pragma once
 #include <cfloat>
 #include <cmath>
 
-#include "paged_view.cuh"
+#include "paged_store.cuh"
 
 namespace scalekv {
 namespace paged {
 
 constexpr int kStreamThreads = 128, kStreamWarps = kStreamThreads / 32;
 constexpr int kTileRows = 16;
+
+template <int D, bool kQ8>
+struct StreamLayout {
+  static constexpr int kRowBytes = D * (kQ8 ? 1 : 2);
+  static constexpr int kStages = kRowBytes >= 128 ? 3 : 4;
+  static constexpr int kCtas = kRowBytes >= 256 ? 2 : 4;                          // CTAs that an SM has room for
+  static constexpr int kScales = 32 * kRowBytes;                                  // offsets in a stage: K rows, V rows, the scales of both
+  static constexpr int kStage = kScales + (kQ8 ? 128 : 0);
+  static constexpr int kQLd = D + 8;                                              // a row of queries: 16 bytes more against bank conflicts
+  static constexpr int kOffRing = kTileRows * kQLd * 2;
+  static constexpr int kRing = kStreamWarps * kStages * kStage;
+  static constexpr int kParts = kStreamWarps * kTileRows * (D + 2) * 4;           // the warps' sums, over the ring once that is done with
+  static constexpr int kSmem = kOffRing + (kRing > kParts ? kRing : kParts);
+  // where piece x (16 bytes) of row r lies
+  static __device__ __forceinline__ int piece(int r, int x) {
+    if (kRowBytes == 64) return r * 64 + ((x ^ ((r >> 1) & 3)) << 4);
+    return r * kRowBytes + ((x ^ ((r & 6) ^ ((r & 1) << 2))) << 4);
+  }
+};
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 3.f;
 
@@ -39,6 +60,7 @@ struct AttendArgs {
   Rows Q, O;                       // [tokens][heads][head_dim] bf16
   float *lse;                      // [tokens][heads] or null
   float *part_o, *part_ml;         // [split][tokens * heads][head_dim], [split][tokens * heads][2]: base-2 reference and sum
+  int *counts;                     // parts left so far, one for each sequence and kv head of a split launch; zero between launches
   Mask mask;
   Divisor group;                   // query heads of a kv head
   int n_heads;                     // query heads
@@ -77,128 +99,120 @@ __device__ __forceinline__ void mma_16816(float *c, const uint32_t *a, uint32_t 
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ uint4 load_stream(const void *p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
-}
 __device__ __forceinline__ uint32_t word(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+// 16 bytes from global to shared memory, or zeros
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool on) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
 
 template <int D, bool kQ8>
-__global__ void __launch_bounds__(kStreamThreads, 3) paged_stream_kernel(const AttendArgs a, int tiles) {
-  constexpr int kRowBytes = D * (kQ8 ? 1 : 2);
-  constexpr int kPieces = kRowBytes / 64;                // 16-byte pieces of a K row that a lane holds
+__global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8>::kCtas) paged_stream_kernel(const __grid_constant__ AttendArgs a) {
+  using Y = StreamLayout<D, kQ8>;
+  constexpr int kRowBytes = Y::kRowBytes, kStages = Y::kStages, kQLd = Y::kQLd;
+  constexpr int kPieces = kRowBytes / 64;                // 16-byte pieces of a K row that a lane takes
   constexpr int kValPieces = kRowBytes >= 128 ? kRowBytes / 128 : 1;   // ... of a V row (half of one: 64 codes)
-  constexpr int kQLd = D + 8;                            // a row of queries in shared memory: 16 bytes more against bank conflicts
-  __shared__ __align__(16) __nv_bfloat16 q_smem[kTileRows * kQLd];
-  __shared__ float o_smem[kStreamWarps][kTileRows][D];
-  __shared__ float ml_smem[kStreamWarps][kTileRows][2];
+  extern __shared__ __align__(16) char smem[];
+  __nv_bfloat16 *q_smem = reinterpret_cast<__nv_bfloat16 *>(smem);
+  __shared__ int last_one;
 
-  const int seq = blockIdx.x / tiles, tile = blockIdx.x - seq * tiles, head = blockIdx.y;
+  const int seq = blockIdx.x, head = blockIdx.y;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = lane & 3, oct = lane >> 2;
   const Store &s = a.s;
   const int start = __ldg(a.bt.starts + seq), n_new = min(__ldg(a.bt.starts + seq + 1), a.bt.n_tokens) - start;
-  const int rows = n_new * a.group.d - tile * kTileRows;   // query rows of this tile (beyond 16: of later ones too)
+  int length = __ldg(a.bt.lengths + seq);
+  const int rows = min(n_new * a.group.d, kTileRows);      // query rows
   if (n_new > a.max_new && threadIdx.x == 0) report(s.status);
   if (rows <= 0 || start < 0) return;
-  int length = __ldg(a.bt.lengths + seq);
   if ((unsigned)length > (unsigned)(a.bt.table_pages << s.page_shift)) {       // (what lies behind the table counts as hidden)
     length = length < 0 ? 0 : a.bt.table_pages << s.page_shift;
     report(s.status);
   }
   const int first = length - n_new;                        // position of the sequence's first new token
 
+  // the keys that some row sees, in steps of 16: the sinks' steps, then those of [lo, hi)
+  const int t_last = a.group.div(rows - 1);
+  const int lo_all = min(seen_lo(a.mask, first), length), hi_all = seen_hi(a.mask, first + t_last, length);
+  const int lo_step = lo_all >> 4, hi_step = max((hi_all + 15) >> 4, lo_step);
+  const int sink_steps = a.mask.window > 0 ? min((min(a.mask.n_sink, hi_all) + 15) >> 4, lo_step) : 0;
+  const int steps = sink_steps + hi_step - lo_step;
+  const int step_lo = (int)((long long)steps * blockIdx.z / gridDim.z), step_hi = (int)((long long)steps * (blockIdx.z + 1) / gridDim.z);
+  const int n_sink = a.mask.window > 0 ? a.mask.n_sink : 0;
+  auto in_use = [&](int pos) { return pos < hi_all && (pos >= lo_all || pos < n_sink); };
+  auto key_of = [&](int step) { return (step < sink_steps ? step : step - sink_steps + lo_step) << 4; };
+  auto page_at = [&](int step) { return step < step_hi ? page_of(s, a.bt, seq, key_of(step)) : -1; };
+
+  // ---- the ring: this warp's steps are step_lo + warp, + 4, ..
+  char *ring = smem + Y::kOffRing + warp * kStages * Y::kStage;
+  const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+  auto fetch = [&](int step, int page, int stage) {
+    if (page >= 0) {
+      constexpr int kRowPieces = kRowBytes / 16, kRowsAtOnce = 32 / kRowPieces;
+      const int key0 = key_of(step), x = lane % kRowPieces, r0 = lane / kRowPieces;
+      const size_t row0 = store_row(s, page, head, key0);
+      const char *k = s.k_rows + (row0 + r0) * kRowBytes + x * 16, *v = s.v_rows + (row0 + r0) * kRowBytes + x * 16;
+      const uint32_t to = ring_at + stage * Y::kStage;
+#pragma unroll
+      for (int i = 0; i < 16 / kRowsAtOnce; ++i) {
+        const int r = r0 + i * kRowsAtOnce;
+        // (hidden keys' products are hidden one by one, and codes are numbers whatever they are; hidden rows of bf16 values must be)
+        copy16(to + Y::piece(r, x), k + i * kRowsAtOnce * kRowBytes, true);
+        copy16(to + 16 * kRowBytes + Y::piece(r, x), v + i * kRowsAtOnce * kRowBytes, kQ8 || in_use(key0 + r));
+      }
+      if (kQ8 && lane < 8) copy16(to + Y::kScales + lane * 16, (lane < 4 ? s.k_scales : s.v_scales) + row0 + (lane & 3) * 4, true);
+    } else if (!kQ8 && step < step_hi) {
+      for (int i = lane; i < 32 * kRowBytes / 16; i += 32) *reinterpret_cast<uint4 *>(ring + stage * Y::kStage + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  int step = step_lo + warp, pages[kStages];               // of this step and those behind it
+#pragma unroll
+  for (int i = 0; i < kStages; ++i) pages[i] = page_at(step + i * kStreamWarps);
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) fetch(step + i * kStreamWarps, pages[i], i);
+
   // query rows, zeros beyond the last one
   for (int i = threadIdx.x; i < kTileRows * (D / 8); i += kStreamThreads) {
     const int r = i / (D / 8), piece = i % (D / 8);
     uint4 v = make_uint4(0u, 0u, 0u, 0u);
     if (r < rows) {
-      const int t = a.group.div(tile * kTileRows + r), g = tile * kTileRows + r - t * a.group.d;
+      const int t = a.group.div(r), g = r - t * a.group.d;
       v = __ldg(reinterpret_cast<const uint4 *>(a.Q.ptr + (start + t) * a.Q.st + (head * a.group.d + g) * a.Q.sh) + piece);
     }
     *reinterpret_cast<uint4 *>(q_smem + r * kQLd + piece * 8) = v;
   }
-
-  // the keys that some row of the tile sees, in steps of 16: the sinks' steps, then those of [lo, hi)
-  const int t_first = a.group.div(tile * kTileRows), t_last = a.group.div(tile * kTileRows + min(rows, kTileRows) - 1);
-  const int lo_all = min(seen_lo(a.mask, first + t_first), length), hi_all = seen_hi(a.mask, first + t_last, length);
-  const int lo_step = lo_all >> 4, hi_step = max((hi_all + 15) >> 4, lo_step);
-  const int sink_steps = a.mask.window > 0 ? min((min(a.mask.n_sink, hi_all) + 15) >> 4, lo_step) : 0;
-  const int steps = sink_steps + hi_step - lo_step;
-  const int step_lo = (int)((long long)steps * blockIdx.z / gridDim.z), step_hi = (int)((long long)steps * (blockIdx.z + 1) / gridDim.z);
   // a step all of whose keys every row sees: [lo_full, hi_full)
-  const int lo_full = seen_lo(a.mask, first + t_last), hi_full = seen_hi(a.mask, first + t_first, length);
+  const int lo_full = seen_lo(a.mask, first + t_last), hi_full = seen_hi(a.mask, first, length);
   // limits of this lane's rows, oct and oct + 8
   int row_lo[2], row_hi[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int p = first + a.group.div(tile * kTileRows + min(oct + 8 * i, rows - 1));
+    const int p = first + a.group.div(min(oct + 8 * i, rows - 1));
     row_lo[i] = seen_lo(a.mask, p);
     row_hi[i] = seen_hi(a.mask, p, length);
   }
-  const int n_sink = a.mask.window > 0 ? a.mask.n_sink : 0;
-  auto in_use = [&](int pos) { return pos < hi_all && (pos >= lo_all || pos < n_sink); };
-  auto key_of = [&](int step) { return (step < sink_steps ? step : step - sink_steps + lo_step) << 4; };
-
-  uint4 kq[2][kPieces], vq[4][kValPieces];
-  float ks[4], vs[4];
-  auto load_k = [&](int key0, int page) {
-    const size_t row0 = store_row(s, max(page, 0), head, key0);
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      const int k = n * 8 + oct;
-      const bool on = page >= 0 && in_use(key0 + k);
-      const char *p = s.k_rows + (row0 + k) * kRowBytes + quad * 16;
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i) kq[n][i] = on ? load_stream(p + i * 64) : make_uint4(0u, 0u, 0u, 0u);
-      if constexpr (kQ8) {
-        const float2 two = __ldg(reinterpret_cast<const float2 *>(s.k_scales + row0 + n * 8 + 2 * quad));
-        ks[2 * n] = two.x; ks[2 * n + 1] = two.y;
-      }
-    }
-  };
-  auto load_v = [&](int key0, int page) {
-    const size_t row0 = store_row(s, max(page, 0), head, key0);
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const int k = (n >> 1) * 8 + 2 * quad + (n & 1);
-      const bool on = page >= 0 && in_use(key0 + k);
-      const char *p = s.v_rows + (row0 + k) * kRowBytes;
-      if constexpr (kRowBytes >= 128) {
-#pragma unroll
-        for (int i = 0; i < kValPieces; ++i) vq[n][i] = on ? load_stream(p + i * 128 + oct * 16) : make_uint4(0u, 0u, 0u, 0u);
-      } else {
-        const uint2 two = on ? __ldg(reinterpret_cast<const uint2 *>(p + oct * 8)) : make_uint2(0u, 0u);
-        vq[n][0] = make_uint4(two.x, two.y, 0u, 0u);
-      }
-    }
-    if constexpr (kQ8) {
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const float2 two = __ldg(reinterpret_cast<const float2 *>(s.v_scales + row0 + n * 8 + 2 * quad));
-        vs[2 * n] = two.x; vs[2 * n + 1] = two.y;
-      }
-    }
-  };
-  auto page_at = [&](int step) { return step < step_hi ? page_of(s, a.bt, seq, key_of(step)) : -1; };
 
   float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
   __syncthreads();
 
-  int step = step_lo + warp, page = page_at(step);
-  int next = page_at(step + kStreamWarps);
-  if (step < step_hi) {
-    load_k(key_of(step), page);
-    load_v(key_of(step), page);
-  }
-  for (; step < step_hi; step += kStreamWarps) {
-    const int key0 = key_of(step);
+  for (int stage = 0; step < step_hi; step += kStreamWarps) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+    __syncwarp();                                          // everybody's copies of this step are there, and the stage before it is done with
+    fetch(step + (kStages - 1) * kStreamWarps, pages[kStages - 1], stage == 0 ? kStages - 1 : stage - 1);
+    const int key0 = key_of(step), page = pages[0];
+#pragma unroll
+    for (int i = 0; i + 1 < kStages; ++i) pages[i] = pages[i + 1];
+    pages[kStages - 1] = page_at(step + kStages * kStreamWarps);
+    const char *k_at = ring + stage * Y::kStage, *v_at = k_at + 16 * kRowBytes;
+    stage = stage + 1 == kStages ? 0 : stage + 1;
     // S = Q K^T
     float x[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
+      uint4 k[2];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) k[n] = *reinterpret_cast<const uint4 *>(k_at + Y::piece(n * 8 + oct, i * 4 + quad));
       if constexpr (kQ8) {
         // a piece is 16 dims: four products, each of four of this lane's dims
 #pragma unroll
@@ -208,7 +222,7 @@ __global__ void __launch_bounds__(kStreamThreads, 3) paged_stream_kernel(const A
           const uint32_t f0[4] = {a0.x, a1.x, a0.y, a1.y}, f1[4] = {a0.z, a1.z, a0.w, a1.w};
 #pragma unroll
           for (int n = 0; n < 2; ++n) {
-            const uint32_t w0 = turn_signs(word(kq[n][i], 2 * h)), w1 = turn_signs(word(kq[n][i], 2 * h + 1));
+            const uint32_t w0 = turn_signs(word(k[n], 2 * h)), w1 = turn_signs(word(k[n], 2 * h + 1));
             mma_16816(x[n], f0, codes_low(w0), codes_high(w0));
             mma_16816(x[n], f1, codes_low(w1), codes_high(w1));
           }
@@ -219,16 +233,24 @@ __global__ void __launch_bounds__(kStreamThreads, 3) paged_stream_kernel(const A
         const uint32_t f0[4] = {a0.x, a1.x, a0.y, a1.y}, f1[4] = {a0.z, a1.z, a0.w, a1.w};
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
-          mma_16816(x[n], f0, kq[n][i].x, kq[n][i].y);
-          mma_16816(x[n], f1, kq[n][i].z, kq[n][i].w);
+          mma_16816(x[n], f0, k[n].x, k[n].y);
+          mma_16816(x[n], f1, k[n].z, k[n].w);
         }
       }
     }
     // base-2 exponents; hidden keys at -inf, whatever their rows and scales hold
+    float vs[2][2];
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[n][e] *= kQ8 ? a.scale_log2e * kCodeUnit * ks[2 * n + (e & 1)] : a.scale_log2e;
+    for (int n = 0; n < 2; ++n) {
+      float2 ks = make_float2(a.scale_log2e, a.scale_log2e);
+      if constexpr (kQ8) {
+        ks = *reinterpret_cast<const float2 *>(k_at + Y::kScales + (n * 8 + 2 * quad) * 4);
+        ks.x *= a.scale_log2e * kCodeUnit; ks.y *= a.scale_log2e * kCodeUnit;
+        const float2 two = *reinterpret_cast<const float2 *>(k_at + Y::kScales + 64 + (n * 8 + 2 * quad) * 4);
+        vs[n][0] = two.x * kCodeUnit; vs[n][1] = two.y * kCodeUnit;
+      }
+      x[n][0] *= ks.x; x[n][1] *= ks.y; x[n][2] *= ks.x; x[n][3] *= ks.y;
+    }
     const bool whole = page >= 0 && key0 >= lo_full && key0 + 16 <= hi_full;
     uint32_t hidden = 0;
     if (!whole) {
@@ -240,21 +262,18 @@ __global__ void __launch_bounds__(kStreamThreads, 3) paged_stream_kernel(const A
           if (page < 0 || pos >= row_hi[i] || (pos < row_lo[i] && pos >= n_sink)) { x[n][e] = -INFINITY; hidden |= 1u << (4 * n + e); }
         }
     }
-    const int page_next = next;
-    if (step + kStreamWarps < step_hi) load_k(key_of(step + kStreamWarps), page_next);
-    next = page_at(step + 2 * kStreamWarps);
     // the rows' references
     float top[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       top[i] = fmaxf(fmaxf(x[0][2 * i], x[0][2 * i + 1]), fmaxf(x[1][2 * i], x[1][2 * i + 1]));
-      top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
-      top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
     }
     if (__any_sync(0xffffffffu, top[0] > m[0] + kRaise || top[1] > m[1] + kRaise)) {
       float f[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
+        top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+        top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
         const float raised = fmaxf(m[i], top[i]);
         f[i] = raised == -INFINITY ? 1.f : exp2_approx(m[i] - raised);      // (from no reference at all: 0)
         m[i] = raised;
@@ -278,18 +297,29 @@ __global__ void __launch_bounds__(kStreamThreads, 3) paged_stream_kernel(const A
       if constexpr (kQ8) {
         // (a hidden key counts for nothing even where its scale is no number)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[n][e] = (hidden >> (4 * n + e)) & 1u ? 0.f : x[n][e] * (kCodeUnit * vs[2 * n + (e & 1)]);
+        for (int e = 0; e < 4; ++e) x[n][e] = (hidden >> (4 * n + e)) & 1u ? 0.f : x[n][e] * vs[n][e & 1];
       }
-      asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[2 * n]) : "f"(x[n][1]), "f"(x[n][0]));
-      asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[2 * n + 1]) : "f"(x[n][3]), "f"(x[n][2]));
+      p[2 * n] = pair_bf16(x[n][0], x[n][1]);
+      p[2 * n + 1] = pair_bf16(x[n][2], x[n][3]);
     }
     // O += P V
     if constexpr (kQ8) {
+      uint4 v[4];
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const int r = (n >> 1) * 8 + 2 * quad + (n & 1);
+        if constexpr (kRowBytes >= 128) {
+          v[n] = *reinterpret_cast<const uint4 *>(v_at + Y::piece(r, oct));
+        } else {
+          const uint2 two = *reinterpret_cast<const uint2 *>(v_at + Y::piece(r, oct >> 1) + (oct & 1) * 8);
+          v[n] = make_uint4(two.x, two.y, 0u, 0u);
+        }
+      }
 #pragma unroll
       for (int w = 0; w < D / 32; ++w) {
         uint32_t c[4];
 #pragma unroll
-        for (int n = 0; n < 4; ++n) c[n] = turn_signs(word(vq[n][0], w));
+        for (int n = 0; n < 4; ++n) c[n] = turn_signs(word(v[n], w));
         mma_16816(o[4 * w], p, codes_across<0>(c[0], c[1]), codes_across<0>(c[2], c[3]));
         mma_16816(o[4 * w + 1], p, codes_across<1>(c[0], c[1]), codes_across<1>(c[2], c[3]));
         mma_16816(o[4 * w + 2], p, codes_across<2>(c[0], c[1]), codes_across<2>(c[2], c[3]));
@@ -297,68 +327,111 @@ __global__ void __launch_bounds__(kStreamThreads, 3) paged_stream_kernel(const A
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < kValPieces; ++i)
+      for (int i = 0; i < kValPieces; ++i) {
+        uint4 v[4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) v[n] = *reinterpret_cast<const uint4 *>(v_at + Y::piece((n >> 1) * 8 + 2 * quad + (n & 1), i * 8 + oct));
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const uint32_t sel = (e & 1) ? 0x7632 : 0x5410;
-          mma_16816(o[i * 8 + e], p, __byte_perm(word(vq[0][i], e >> 1), word(vq[1][i], e >> 1), sel),
-                    __byte_perm(word(vq[2][i], e >> 1), word(vq[3][i], e >> 1), sel));
+          mma_16816(o[i * 8 + e], p, __byte_perm(word(v[0], e >> 1), word(v[1], e >> 1), sel), __byte_perm(word(v[2], e >> 1), word(v[3], e >> 1), sel));
         }
+      }
     }
-    if (step + kStreamWarps < step_hi) load_v(key_of(step + kStreamWarps), page_next);
-    page = page_next;
   }
 
-  // ---- the warps' parts, combined
+  // ---- the warps' parts, combined over what was the ring
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();
+  float *o_smem = reinterpret_cast<float *>(smem + Y::kOffRing), *ml_smem = o_smem + kStreamWarps * kTileRows * D;      // [warp][row][dim], [warp][row][2]
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
     l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-    if (quad == 0) { ml_smem[warp][oct + 8 * i][0] = m[i]; ml_smem[warp][oct + 8 * i][1] = l[i]; }
+    if (quad == 0) *reinterpret_cast<float2 *>(ml_smem + (warp * kTileRows + oct + 8 * i) * 2) = make_float2(m[i], l[i]);
   }
 #pragma unroll
   for (int j = 0; j < D / 8; ++j)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       // column n = 2 quad + (e & 1) of n-tile j
-      const int n = 2 * quad + (e & 1);
-      const int dim = kQ8 ? n * (D / 8) + j : (j >> 3) * 64 + n * 8 + (j & 7);
-      o_smem[warp][oct + 8 * (e >> 1)][dim] = o[j][e];
+      const int n = 2 * quad + (e & 1), dim = kQ8 ? n * (D / 8) + j : (j >> 3) * 64 + n * 8 + (j & 7);
+      o_smem[(warp * kTileRows + oct + 8 * (e >> 1)) * D + dim] = o[j][e];
     }
   __syncthreads();
   const size_t all_rows = (size_t)a.bt.n_tokens * a.n_heads;
-  for (int i = threadIdx.x; i < min(rows, kTileRows) * (D / 8); i += kStreamThreads) {
+  auto place = [&](int r, int &t, int &h) {
+    t = a.group.div(r);
+    h = head * a.group.d + r - t * a.group.d;
+    t += start;
+  };
+  auto put = [&](int t, int h, int piece, const float *acc, float2 ml) {
+    const float inv = ml.y == 0.f ? 0.f : 1.f / ml.y;
+    *(reinterpret_cast<uint4 *>(a.O.ptr + t * a.O.st + h * a.O.sh) + piece) =
+        make_uint4(pair_bf16(acc[0] * inv, acc[1] * inv), pair_bf16(acc[2] * inv, acc[3] * inv), pair_bf16(acc[4] * inv, acc[5] * inv), pair_bf16(acc[6] * inv, acc[7] * inv));
+    if (piece == 0 && a.lse != nullptr) a.lse[(size_t)t * a.n_heads + h] = ml.y == 0.f ? -INFINITY : (ml.x + log2f(ml.y)) * kLn2;
+  };
+  for (int i = threadIdx.x; i < rows * (D / 8); i += kStreamThreads) {
     const int r = i / (D / 8), piece = i % (D / 8);
-    float top = -INFINITY;
+    float acc[8], top = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kStreamWarps; ++w) top = fmaxf(top, ml_smem[w][r][0]);
-    float sum = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int w = 0; w < kStreamWarps; ++w) top = fmaxf(top, ml_smem[(w * kTileRows + r) * 2]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
 #pragma unroll
     for (int w = 0; w < kStreamWarps; ++w) {
-      if (ml_smem[w][r][0] == -INFINITY) continue;
-      const float f = exp2_approx(ml_smem[w][r][0] - top);
-      sum += f * ml_smem[w][r][1];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += f * o_smem[w][r][piece * 8 + e];
+      const float2 x = *reinterpret_cast<const float2 *>(ml_smem + (w * kTileRows + r) * 2);
+      const float f = x.x == -INFINITY ? 0.f : exp2_approx(x.x - top);
+      sum += f * x.y;
+      const float4 *v = reinterpret_cast<const float4 *>(o_smem + (w * kTileRows + r) * D + piece * 8);
+      const float4 lo = v[0], hi = v[1];
+      acc[0] += f * lo.x; acc[1] += f * lo.y; acc[2] += f * lo.z; acc[3] += f * lo.w;
+      acc[4] += f * hi.x; acc[5] += f * hi.y; acc[6] += f * hi.z; acc[7] += f * hi.w;
     }
-    const int t = a.group.div(tile * kTileRows + r), g = tile * kTileRows + r - t * a.group.d;
-    const int h = head * a.group.d + g;
-    const size_t row = (size_t)(start + t) * a.n_heads + h;
+    const float2 ml = make_float2(top, sum);
+    int t, h;
+    place(r, t, h);
     if (gridDim.z == 1) {
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      uint32_t u[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u[e]) : "f"(acc[2 * e + 1] * inv), "f"(acc[2 * e] * inv));
-      *(reinterpret_cast<uint4 *>(a.O.ptr + (start + t) * a.O.st + h * a.O.sh) + piece) = make_uint4(u[0], u[1], u[2], u[3]);
-      if (piece == 0 && a.lse != nullptr) a.lse[row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+      put(t, h, piece, acc, ml);
     } else {
-      const size_t part = (size_t)blockIdx.z * all_rows + row;
+      const size_t part = (size_t)blockIdx.z * all_rows + (size_t)t * a.n_heads + h;
       float4 *dst = reinterpret_cast<float4 *>(a.part_o + part * D + piece * 8);
       dst[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
       dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
-      if (piece == 0) *reinterpret_cast<float2 *>(a.part_ml + part * 2) = make_float2(top, sum);
+      if (piece == 0) *reinterpret_cast<float2 *>(a.part_ml + part * 2) = ml;
     }
+  }
+  if (gridDim.z == 1) return;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    int *count = a.counts + blockIdx.x * gridDim.y + blockIdx.y;
+    last_one = atomicAdd(count, 1) == (int)gridDim.z - 1;
+    if (last_one) *count = 0;
+  }
+  __syncthreads();
+  if (!last_one) return;
+  __threadfence();
+  for (int i = threadIdx.x; i < rows * (D / 8); i += kStreamThreads) {
+    const int r = i / (D / 8), piece = i % (D / 8);
+    int t, h;
+    place(r, t, h);
+    const size_t row = (size_t)t * a.n_heads + h;
+    auto ml_of = [&](int e) { return __ldcg(reinterpret_cast<const float2 *>(a.part_ml + ((size_t)e * all_rows + row) * 2)); };
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, top = -INFINITY, sum = 0.f;
+#pragma unroll 4
+    for (int e = 0; e < (int)gridDim.z; ++e) top = fmaxf(top, ml_of(e).x);
+#pragma unroll 4
+    for (int e = 0; e < (int)gridDim.z; ++e) {
+      const float2 x = ml_of(e);
+      const float4 *v = reinterpret_cast<const float4 *>(a.part_o + ((size_t)e * all_rows + row) * D + piece * 8);
+      const float4 lo = __ldcg(v), hi = __ldcg(v + 1);
+      const float f = x.x == -INFINITY ? 0.f : exp2_approx(x.x - top);
+      sum += f * x.y;
+      acc[0] += f * lo.x; acc[1] += f * lo.y; acc[2] += f * lo.z; acc[3] += f * lo.w;
+      acc[4] += f * hi.x; acc[5] += f * hi.y; acc[6] += f * hi.z; acc[7] += f * hi.w;
+    }
+    put(t, h, piece, acc, make_float2(top, sum));
   }
 }
 
