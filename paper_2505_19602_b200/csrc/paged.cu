@@ -115,12 +115,25 @@ struct Range {  // an NVTX range around one call
   ~Range() { nvtxRangePop(); }
 };
 
+// Every kernel here may be set up while the one before it in the stream is finishing: all of them wait for that one's end (griddepcontrol.wait)
+// before they read or write anything.
+template <typename... P, typename... A>
+cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t stream, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = grid; cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
+  cfg.attrs = &attr; cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+
 template <bool kWrite, typename T, int D, bool kQ8>
 void launch_store(const Store &s, const Batch &bt, const Rows &K, const Rows &V, int n_rows, cudaStream_t stream) {
   const int per_block = kStoreThreads / (D / 8) * kRowsPerLane, blocks = (n_rows + per_block - 1) / per_block;
   const Divisor per_token = Divisor::of(2 * s.heads);
-  if constexpr (kWrite) paged_write_kernel<T, D, kQ8><<<blocks, kStoreThreads, 0, stream>>>(s, bt, K, V, per_token, n_rows);
-  else paged_read_kernel<T, D, kQ8><<<blocks, kStoreThreads, 0, stream>>>(s, bt, K, V, per_token, n_rows);
+  if constexpr (kWrite) launch(paged_write_kernel<T, D, kQ8>, dim3(blocks), kStoreThreads, 0, stream, s, bt, K, V, per_token, n_rows);
+  else launch(paged_read_kernel<T, D, kQ8>, dim3(blocks), kStoreThreads, 0, stream, s, bt, K, V, per_token, n_rows);
 }
 
 template <int D, bool kQ8>
@@ -128,7 +141,7 @@ scalekv_status launch_stream(scalekv_paged *c, const AttendArgs &a, int split, c
   constexpr int smem = StreamLayout<D, kQ8>::kSmem;
   if (cudaFuncSetAttribute(paged_stream_kernel<D, kQ8>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
     return fail(c, SCALEKV_ERR_CUDA, "cannot raise the dynamic shared memory limit");
-  paged_stream_kernel<D, kQ8><<<dim3(a.bt.n_seqs, a.s.heads, split), kStreamThreads, smem, stream>>>(a);
+  launch(paged_stream_kernel<D, kQ8>, dim3(a.bt.n_seqs, a.s.heads, split), kStreamThreads, smem, stream, a);
   return launched(c, "paged_attend");
 }
 
@@ -138,8 +151,8 @@ scalekv_status launch_tile(scalekv_paged *c, int layer, const AttendArgs &a, int
   // (per device and process; the answer is the same every time)
   if (cudaFuncSetAttribute(paged_tile_kernel<D, kQ8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
     return fail(c, SCALEKV_ERR_CUDA, "cannot raise the dynamic shared memory limit");
-  paged_tile_kernel<D, kQ8><<<dim3((unsigned)(items * a.s.heads), (unsigned)split), TileLayout<D, kQ8>::kThreads, smem, stream>>>(
-      c->maps.k, c->maps.v, a, Divisor::of(a.s.heads), items, layer * c->cfg.n_pages);
+  launch(paged_tile_kernel<D, kQ8>, dim3((unsigned)(items * a.s.heads), (unsigned)split), TileLayout<D, kQ8>::kThreads, smem, stream, c->maps.k, c->maps.v, a,
+         Divisor::of(a.s.heads), items, layer * c->cfg.n_pages);
   return launched(c, "paged_attend");
 }
 
@@ -274,10 +287,11 @@ scalekv_status scalekv_paged_attend(scalekv_paged *kv, int32_t layer, const scal
   long long split;
   scalekv_status done;
   if (max_rows <= kTileRows) {
-    const long long items = a.bt.n_seqs * H;
-    const int steps = (int)((keys + 15) / 16);
-    const int slots = c->n_sm * (q8 || D == 64 ? 4 : 2);
-    split = std::min<long long>((slots + items - 1) / items, (steps + 2 * kStreamWarps - 1) / (2 * kStreamWarps));
+    // CTAs that share a sequence's keys: within one wave down to 8 steps of 16 keys each (one sequence of 1 999 entries, 8 kv heads, 1 / 4 / 8 / 16 / 32
+    // CTAs for a head: 34.9 / 15.5 / 12.3 / 12.3 / 16.4 us); beyond it, for lengths that differ, up to two waves of 64 steps or more (32 x up to 10 521, 256 pairs of
+    // sequence and head, 1 / 2 / 4 / 8 / 16: 197 / 157 / 143 / 144 / 163; 64 x 1 028 keys of a window, 1 / 2 / 4: 45 / 54 / 64).
+    const long long items = (long long)a.bt.n_seqs * H, slots = (long long)c->n_sm * (q8 || D == 64 ? 4 : 2), steps = (keys + 15) / 16;
+    split = std::max(std::min(slots / items, steps / 8), std::min(2 * slots / items, steps / 64));
     split = std::max<long long>(1, std::min<long long>(split, kPartRows / all_rows));
     if (items > kMaxCounts) split = 1;
     if (D == 128) done = q8 ? launch_stream<128, true>(c, a, (int)split, st) : launch_stream<128, false>(c, a, (int)split, st);
@@ -296,8 +310,8 @@ scalekv_status scalekv_paged_attend(scalekv_paged *kv, int32_t layer, const scal
   if (done) return done;
   if (split == 1) return SCALEKV_OK;
   const unsigned blocks = (unsigned)((all_rows + 7) / 8);
-  if (D == 128) paged_join_kernel<128><<<blocks, 256, 0, st>>>(a, (int)split);
-  else paged_join_kernel<64><<<blocks, 256, 0, st>>>(a, (int)split);
+  if (D == 128) launch(paged_join_kernel<128>, dim3(blocks), 256, 0, st, a, (int)split);
+  else launch(paged_join_kernel<64>, dim3(blocks), 256, 0, st, a, (int)split);
   return launched(c, "paged_join");
 }
 

@@ -56,6 +56,8 @@ __global__ void __launch_bounds__(kStoreThreads) paged_write_kernel(const Store 
                                                                     int n_rows) {
   constexpr int kLanes = D / 8, kGroups = kStoreThreads / kLanes;
   const int lane = threadIdx.x % kLanes, r0 = blockIdx.x * kGroups * kRowsPerLane + threadIdx.x / kLanes;
+  wait_for_grid();
+  next_grid();
   float x[kRowsPerLane][8];
 #pragma unroll
   for (int i = 0; i < kRowsPerLane; ++i) {
@@ -111,6 +113,8 @@ __global__ void __launch_bounds__(kStoreThreads) paged_read_kernel(const Store s
                                                                    int n_rows) {
   constexpr int kLanes = D / 8, kGroups = kStoreThreads / kLanes;
   const int lane = threadIdx.x % kLanes, r0 = blockIdx.x * kGroups * kRowsPerLane + threadIdx.x / kLanes;
+  wait_for_grid();
+  next_grid();
   int seq = block_seq_of(bt, per_token.div(blockIdx.x * kGroups * kRowsPerLane));
   uint4 w[kRowsPerLane];
   float scale[kRowsPerLane];

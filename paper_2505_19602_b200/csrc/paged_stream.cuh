@@ -118,6 +118,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8>::kCtas) p
   const int seq = blockIdx.x, head = blockIdx.y;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = lane & 3, oct = lane >> 2;
   const Store &s = a.s;
+  wait_for_grid();
   const int start = __ldg(a.bt.starts + seq), n_new = min(__ldg(a.bt.starts + seq + 1), a.bt.n_tokens) - start;
   int length = __ldg(a.bt.lengths + seq);
   const int rows = min(n_new * a.group.d, kTileRows);      // query rows
@@ -340,6 +341,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8>::kCtas) p
     }
   }
 
+  next_grid();
   // ---- the warps' parts, combined over what was the ring
   asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
@@ -440,6 +442,8 @@ template <int D>
 __global__ void __launch_bounds__(256) paged_join_kernel(const AttendArgs a, int n_split) {
   constexpr int kPer = D / 32;
   const int lane = threadIdx.x & 31, row = blockIdx.x * 8 + (threadIdx.x >> 5), all_rows = a.bt.n_tokens * a.n_heads;
+  wait_for_grid();
+  next_grid();
   if (row >= all_rows) return;
   float m = -INFINITY, sum = 0.f, acc[kPer];
 #pragma unroll

@@ -165,6 +165,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   // ---- set-up: barriers, TMEM, and the item.  Items are counted through the sequences, and taken from the end: of a causal chunk the
   // last rows see most.
   if (warp == 0) {
+    wait_for_grid();
     const int want = n_items - 1 - e;
     int before = 0, seq = -1, tile = 0;
     for (int b0 = 0; b0 < a.bt.n_seqs && seq < 0; b0 += 32) {
@@ -215,6 +216,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + Y::kOffItem), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  wait_for_grid();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -324,6 +326,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           __syncwarp();
         }
       }
+      next_grid();
     } else if (warp == 1 && rows > 0) {
       // -------------------------------------------------------------- TMA producer (the whole warp walks, one elected lane issues)
       // Ring tile t holds K (even) or V (odd) of key tile t / 2, which bRaw (codes) or bFull says.  A tile's holes go with its K.

@@ -28,6 +28,11 @@ struct Rows {
   long long st, sh;
 };
 
+// The grid before this one in the stream has ended, and all that it wrote is there.  First of all in every kernel but for what needs no memory.
+__device__ __forceinline__ void wait_for_grid() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// The grid behind this one may be set up where it finds room.
+__device__ __forceinline__ void next_grid() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // (a wait that gave up stays on record)
 __device__ __forceinline__ void report(int *status) { atomicCAS(status, 0, kDevCheck); }
 
