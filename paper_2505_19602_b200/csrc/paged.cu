@@ -136,12 +136,19 @@ void launch_store(const Store &s, const Batch &bt, const Rows &K, const Rows &V,
   else launch(paged_read_kernel<T, D, kQ8>, dim3(blocks), kStoreThreads, 0, stream, s, bt, K, V, per_token, n_rows);
 }
 
-template <int D, bool kQ8>
-scalekv_status launch_stream(scalekv_paged *c, const AttendArgs &a, int split, cudaStream_t stream) {
-  constexpr int smem = StreamLayout<D, kQ8>::kSmem;
-  if (cudaFuncSetAttribute(paged_stream_kernel<D, kQ8>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+template <int D, bool kQ8, int kN>
+scalekv_status launch_stream(scalekv_paged *c, const AttendArgs &a, long long keys, cudaStream_t stream) {
+  using Y = StreamLayout<D, kQ8, kN>;
+  // CTAs that share a sequence's keys: within one wave down to 8 steps of 16 keys each (one sequence of 1 999 entries, 8 kv heads, 1 / 4 / 8 / 16 / 32
+  // CTAs for a head: 34.9 / 15.5 / 12.3 / 12.3 / 16.4 us); beyond it, for lengths that differ, up to two waves of 64 steps or more (32 x up to 10 521, 256 pairs of
+  // sequence and head, 1 / 2 / 4 / 8 / 16: 197 / 157 / 143 / 144 / 163; 64 x 1 028 keys of a window, 1 / 2 / 4: 45 / 54 / 64).
+  const long long items = (long long)a.bt.n_seqs * a.s.heads, slots = (long long)c->n_sm * Y::kCtas, steps = (keys + 15) / 16;
+  long long split = std::max(std::min(slots / items, steps / 8), std::min(2 * slots / items, steps / 64));
+  split = std::max<long long>(1, std::min<long long>(split, kPartRows / ((long long)a.bt.n_tokens * a.n_heads)));
+  if (items > kMaxCounts) split = 1;
+  if (cudaFuncSetAttribute(paged_stream_kernel<D, kQ8, kN>, cudaFuncAttributeMaxDynamicSharedMemorySize, Y::kSmem) != cudaSuccess)
     return fail(c, SCALEKV_ERR_CUDA, "cannot raise the dynamic shared memory limit");
-  launch(paged_stream_kernel<D, kQ8>, dim3(a.bt.n_seqs, a.s.heads, split), kStreamThreads, smem, stream, a);
+  launch(paged_stream_kernel<D, kQ8, kN>, dim3(a.bt.n_seqs, a.s.heads, (unsigned)split), kStreamThreads, Y::kSmem, stream, a);
   return launched(c, "paged_attend");
 }
 
@@ -286,17 +293,16 @@ scalekv_status scalekv_paged_attend(scalekv_paged *kv, int32_t layer, const scal
   const bool q8 = c->cfg.store == SCALEKV_STORE_Q8;
   long long split;
   scalekv_status done;
-  if (max_rows <= kTileRows) {
-    // CTAs that share a sequence's keys: within one wave down to 8 steps of 16 keys each (one sequence of 1 999 entries, 8 kv heads, 1 / 4 / 8 / 16 / 32
-    // CTAs for a head: 34.9 / 15.5 / 12.3 / 12.3 / 16.4 us); beyond it, for lengths that differ, up to two waves of 64 steps or more (32 x up to 10 521, 256 pairs of
-    // sequence and head, 1 / 2 / 4 / 8 / 16: 197 / 157 / 143 / 144 / 163; 64 x 1 028 keys of a window, 1 / 2 / 4: 45 / 54 / 64).
-    const long long items = (long long)a.bt.n_seqs * H, slots = (long long)c->n_sm * (q8 || D == 64 ? 4 : 2), steps = (keys + 15) / 16;
-    split = std::max(std::min(slots / items, steps / 8), std::min(2 * slots / items, steps / 64));
-    split = std::max<long long>(1, std::min<long long>(split, kPartRows / all_rows));
-    if (items > kMaxCounts) split = 1;
-    if (D == 128) done = q8 ? launch_stream<128, true>(c, a, (int)split, st) : launch_stream<128, false>(c, a, (int)split, st);
-    else done = q8 ? launch_stream<64, true>(c, a, (int)split, st) : launch_stream<64, false>(c, a, (int)split, st);
-    return done;
+  if (max_rows <= kStreamRows) {
+    auto go = [&](auto dim, auto codes) {
+      constexpr int kD = decltype(dim)::value;
+      constexpr bool kQ8 = decltype(codes)::value;
+      return max_rows <= 8 ? launch_stream<kD, kQ8, 1>(c, a, keys, st) : launch_stream<kD, kQ8, 2>(c, a, keys, st);
+    };
+    using D64 = std::integral_constant<int, 64>;
+    using D128 = std::integral_constant<int, 128>;
+    if (D == 128) return q8 ? go(D128{}, std::true_type{}) : go(D128{}, std::false_type{});
+    return q8 ? go(D64{}, std::true_type{}) : go(D64{}, std::false_type{});
   } else {
     // no more items than this, whatever the starts say
     const long long items = std::min<long long>((long long)a.bt.n_tokens * G / kItemRows + a.bt.n_seqs, (max_rows + kItemRows - 1) / kItemRows * a.bt.n_seqs);

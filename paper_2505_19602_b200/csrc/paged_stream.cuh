@@ -7,10 +7,12 @@
 // So every warp streams its own share of the cache, 16 keys (which lie in one page) at a time, through a ring of stages in shared memory that it
 // fills with asynchronous copies and shares with nobody: no barrier before the end, and the loads of a few steps are always under way.
 // (With the loads in registers, half a step ahead, a step took a loaded DRAM latency: 32 sequences of up to 10 521 entries, 8 kv heads in codes, 285 us for
-// what is XXXX.)  Products are m16n8k16, rows x keys x dims:
-//   - K's eight keys of an n-tile are one to each four lanes, as the B operand has them, and since a product's sum may run in any order, a lane
-//     takes the dims that lie in its 16-byte piece; the query operand is read in the same order.
-//   - V's pairs of keys are interleaved from two rows' pieces, and its dims are dealt to the n-tiles so that those are 16 bytes long, too.
+// what is XXXX.)  Products are m16n8k16 with the few query rows as the n-tiles of eight, S^T = K Q^T (keys x rows x dims) and O^T = V^T P^T
+// (dims x rows x keys): of an m-tile of query rows most would be padding, in the products and in the exponentials.
+//   - A lane has keys r and r + 8 (r = lane / 4) of K, as the A operand does, and since a product's sum may run in any order, it takes the dims that lie in its
+//     16-byte pieces; the queries, which stay in registers, are read in the same order.
+//   - P is transposed from where the first product leaves it to where the second wants it by movmatrix.
+//   - V's pairs of keys are interleaved from two rows' pieces, and its dims are dealt to the m-tiles so that those are 16 bytes long, too.
 //   - Pieces are placed in a stage so that eight lanes' loads meet all banks, K's (two rows, four pieces) and V's (four rows, two pieces).
 //   - Codes become bf16 exactly (codes_bf16).  The key's scale multiplies the product, the value's scale multiplies P, both in fp32; P is rounded to bf16
 //     for its product with V, as it is where rows are bf16.
@@ -27,20 +29,19 @@ namespace scalekv {
 namespace paged {
 
 constexpr int kStreamThreads = 128, kStreamWarps = kStreamThreads / 32;
-constexpr int kTileRows = 16;
+constexpr int kStreamRows = 16;                   // query rows of a sequence and kv head that go this way
 
-template <int D, bool kQ8>
+// kN: n-tiles of eight query rows
+template <int D, bool kQ8, int kN>
 struct StreamLayout {
   static constexpr int kRowBytes = D * (kQ8 ? 1 : 2);
   static constexpr int kStages = kRowBytes >= 128 ? 3 : 4;
-  static constexpr int kCtas = kRowBytes >= 256 ? 2 : 4;                          // CTAs that an SM has room for
+  static constexpr int kCtas = kRowBytes >= 256 ? 2 : kN == 2 && D == 128 ? 3 : 4;            // CTAs that an SM has room for
   static constexpr int kScales = 32 * kRowBytes;                                  // offsets in a stage: K rows, V rows, the scales of both
   static constexpr int kStage = kScales + (kQ8 ? 128 : 0);
-  static constexpr int kQLd = D + 8;                                              // a row of queries: 16 bytes more against bank conflicts
-  static constexpr int kOffRing = kTileRows * kQLd * 2;
   static constexpr int kRing = kStreamWarps * kStages * kStage;
-  static constexpr int kParts = kStreamWarps * kTileRows * (D + 2) * 4;           // the warps' sums, over the ring once that is done with
-  static constexpr int kSmem = kOffRing + (kRing > kParts ? kRing : kParts);
+  static constexpr int kParts = kStreamWarps * 8 * kN * (D + 2) * 4;              // the warps' sums, over the ring once that is done with
+  static constexpr int kSmem = kRing > kParts ? kRing : kParts;
   // where piece x (16 bytes) of row r lies
   static __device__ __forceinline__ int piece(int r, int x) {
     if (kRowBytes == 64) return r * 64 + ((x ^ ((r >> 1) & 3)) << 4);
@@ -89,8 +90,8 @@ __device__ __forceinline__ uint32_t codes_bf16(uint32_t two) {                  
 }
 __device__ __forceinline__ uint32_t codes_low(uint32_t w) { return codes_bf16(__byte_perm(w, 0u, 0x4140)); }      // of a word's four the first two
 __device__ __forceinline__ uint32_t codes_high(uint32_t w) { return codes_bf16(__byte_perm(w, 0u, 0x4342)); }
-template <int kByte> __device__ __forceinline__ uint32_t codes_across(uint32_t a, uint32_t b) {                   // the same byte of two words
-  return codes_bf16(__byte_perm(a, b, 0x0400 + kByte * 0x0101) & 0x00ff00ffu);
+template <int kByte> __device__ __forceinline__ uint32_t codes_across(uint32_t a, uint32_t b) {                   // the same byte of two words, signs as they are
+  return codes_bf16((__byte_perm(a, b, 0x0400 + kByte * 0x0101) ^ 0x00800080u) & 0x00ff00ffu);
 }
 
 __device__ __forceinline__ void mma_16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
@@ -99,20 +100,23 @@ __device__ __forceinline__ void mma_16816(float *c, const uint32_t *a, uint32_t 
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// [row of 8][pair of columns] in the lanes -> [column][pair of rows]
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
 __device__ __forceinline__ uint32_t word(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 // 16 bytes from global to shared memory, or zeros
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool on) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
 }
 
-template <int D, bool kQ8>
-__global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8>::kCtas) paged_stream_kernel(const __grid_constant__ AttendArgs a) {
-  using Y = StreamLayout<D, kQ8>;
-  constexpr int kRowBytes = Y::kRowBytes, kStages = Y::kStages, kQLd = Y::kQLd;
-  constexpr int kPieces = kRowBytes / 64;                // 16-byte pieces of a K row that a lane takes
-  constexpr int kValPieces = kRowBytes >= 128 ? kRowBytes / 128 : 1;   // ... of a V row (half of one: 64 codes)
+template <int D, bool kQ8, int kN>
+__global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8, kN>::kCtas) paged_stream_kernel(const __grid_constant__ AttendArgs a) {
+  using Y = StreamLayout<D, kQ8, kN>;
+  constexpr int kRowBytes = Y::kRowBytes, kStages = Y::kStages;
   extern __shared__ __align__(16) char smem[];
-  __nv_bfloat16 *q_smem = reinterpret_cast<__nv_bfloat16 *>(smem);
   __shared__ int last_one;
 
   const int seq = blockIdx.x, head = blockIdx.y;
@@ -121,7 +125,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8>::kCtas) p
   wait_for_grid();
   const int start = __ldg(a.bt.starts + seq), n_new = min(__ldg(a.bt.starts + seq + 1), a.bt.n_tokens) - start;
   int length = __ldg(a.bt.lengths + seq);
-  const int rows = min(n_new * a.group.d, kTileRows);      // query rows
+  const int rows = min(n_new * a.group.d, 8 * kN);         // query rows
   if (n_new > a.max_new && threadIdx.x == 0) report(s.status);
   if (rows <= 0 || start < 0) return;
   if ((unsigned)length > (unsigned)(a.bt.table_pages << s.page_shift)) {       // (what lies behind the table counts as hidden)
@@ -134,16 +138,16 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8>::kCtas) p
   const int t_last = a.group.div(rows - 1);
   const int lo_all = min(seen_lo(a.mask, first), length), hi_all = seen_hi(a.mask, first + t_last, length);
   const int lo_step = lo_all >> 4, hi_step = max((hi_all + 15) >> 4, lo_step);
-  const int sink_steps = a.mask.window > 0 ? min((min(a.mask.n_sink, hi_all) + 15) >> 4, lo_step) : 0;
+  const int n_sink = a.mask.window > 0 ? a.mask.n_sink : 0;
+  const int sink_steps = min((min(n_sink, hi_all) + 15) >> 4, lo_step);
   const int steps = sink_steps + hi_step - lo_step;
   const int step_lo = (int)((long long)steps * blockIdx.z / gridDim.z), step_hi = (int)((long long)steps * (blockIdx.z + 1) / gridDim.z);
-  const int n_sink = a.mask.window > 0 ? a.mask.n_sink : 0;
   auto in_use = [&](int pos) { return pos < hi_all && (pos >= lo_all || pos < n_sink); };
   auto key_of = [&](int step) { return (step < sink_steps ? step : step - sink_steps + lo_step) << 4; };
   auto page_at = [&](int step) { return step < step_hi ? page_of(s, a.bt, seq, key_of(step)) : -1; };
 
   // ---- the ring: this warp's steps are step_lo + warp, + 4, ..
-  char *ring = smem + Y::kOffRing + warp * kStages * Y::kStage;
+  char *ring = smem + warp * kStages * Y::kStage;
   const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
   auto fetch = [&](int step, int page, int stage) {
     if (page >= 0) {
@@ -171,31 +175,30 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8>::kCtas) p
 #pragma unroll
   for (int i = 0; i < kStages - 1; ++i) fetch(step + i * kStreamWarps, pages[i], i);
 
-  // query rows, zeros beyond the last one
-  for (int i = threadIdx.x; i < kTileRows * (D / 8); i += kStreamThreads) {
-    const int r = i / (D / 8), piece = i % (D / 8);
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (r < rows) {
-      const int t = a.group.div(r), g = r - t * a.group.d;
-      v = __ldg(reinterpret_cast<const uint4 *>(a.Q.ptr + (start + t) * a.Q.st + (head * a.group.d + g) * a.Q.sh) + piece);
+  // the queries of row oct of every n-tile, zeros beyond the last one, in the order in which a lane has K's dims: four for each product
+  uint2 q[kN][D / 16];
+#pragma unroll
+  for (int n = 0; n < kN; ++n) {
+    const int r = n * 8 + oct, t = a.group.div(r), g = r - t * a.group.d;
+    const char *row = a.Q.ptr + (start + t) * a.Q.st + (head * a.group.d + g) * a.Q.sh;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      const int dim = kQ8 ? (k >> 2) * 64 + quad * 16 + (k & 3) * 4 : (k >> 1) * 32 + quad * 8 + (k & 1) * 4;
+      q[n][k] = r < rows ? __ldg(reinterpret_cast<const uint2 *>(row + dim * 2)) : make_uint2(0u, 0u);
     }
-    *reinterpret_cast<uint4 *>(q_smem + r * kQLd + piece * 8) = v;
   }
   // a step all of whose keys every row sees: [lo_full, hi_full)
   const int lo_full = seen_lo(a.mask, first + t_last), hi_full = seen_hi(a.mask, first, length);
-  // limits of this lane's rows, oct and oct + 8
-  int row_lo[2], row_hi[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int p = first + a.group.div(min(oct + 8 * i, rows - 1));
-    row_lo[i] = seen_lo(a.mask, p);
-    row_hi[i] = seen_hi(a.mask, p, length);
-  }
 
-  float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  // O^T: rows 2 quad, 2 quad + 1 of every n-tile; references and sums of those rows (the sum over this lane's keys)
+  float o[D / 16][kN][4], m[kN][2], l[kN][2];
 #pragma unroll
-  for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-  __syncthreads();
+  for (int n = 0; n < kN; ++n) {
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.f;
+    m[n][0] = m[n][1] = -FLT_MAX;                          // (the lowest number: differences from it are numbers)
+    l[n][0] = l[n][1] = 0.f;
+  }
 
   for (int stage = 0; step < step_hi; step += kStreamWarps) {
     asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
@@ -207,135 +210,122 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8>::kCtas) p
     pages[kStages - 1] = page_at(step + kStages * kStreamWarps);
     const char *k_at = ring + stage * Y::kStage, *v_at = k_at + 16 * kRowBytes;
     stage = stage + 1 == kStages ? 0 : stage + 1;
-    // S = Q K^T
-    float x[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    // S^T = K Q^T
+    float x[kN][4];
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      uint4 k[2];
+    for (int n = 0; n < kN; ++n) x[n][0] = x[n][1] = x[n][2] = x[n][3] = 0.f;
 #pragma unroll
-      for (int n = 0; n < 2; ++n) k[n] = *reinterpret_cast<const uint4 *>(k_at + Y::piece(n * 8 + oct, i * 4 + quad));
+    for (int i = 0; i < kRowBytes / 64; ++i) {
+      const uint4 lo = *reinterpret_cast<const uint4 *>(k_at + Y::piece(oct, i * 4 + quad)), hi = *reinterpret_cast<const uint4 *>(k_at + Y::piece(oct + 8, i * 4 + quad));
       if constexpr (kQ8) {
-        // a piece is 16 dims: four products, each of four of this lane's dims
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const __nv_bfloat16 *q0 = q_smem + oct * kQLd + i * 64 + quad * 16 + h * 8;
-          const uint4 a0 = *reinterpret_cast<const uint4 *>(q0), a1 = *reinterpret_cast<const uint4 *>(q0 + 8 * kQLd);
-          const uint32_t f0[4] = {a0.x, a1.x, a0.y, a1.y}, f1[4] = {a0.z, a1.z, a0.w, a1.w};
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t w0 = turn_signs(word(lo, w)), w1 = turn_signs(word(hi, w));
+          const uint32_t f[4] = {codes_low(w0), codes_low(w1), codes_high(w0), codes_high(w1)};
 #pragma unroll
-          for (int n = 0; n < 2; ++n) {
-            const uint32_t w0 = turn_signs(word(k[n], 2 * h)), w1 = turn_signs(word(k[n], 2 * h + 1));
-            mma_16816(x[n], f0, codes_low(w0), codes_high(w0));
-            mma_16816(x[n], f1, codes_low(w1), codes_high(w1));
-          }
+          for (int n = 0; n < kN; ++n) mma_16816(x[n], f, q[n][4 * i + w].x, q[n][4 * i + w].y);
         }
       } else {
-        const __nv_bfloat16 *q0 = q_smem + oct * kQLd + i * 32 + quad * 8;
-        const uint4 a0 = *reinterpret_cast<const uint4 *>(q0), a1 = *reinterpret_cast<const uint4 *>(q0 + 8 * kQLd);
-        const uint32_t f0[4] = {a0.x, a1.x, a0.y, a1.y}, f1[4] = {a0.z, a1.z, a0.w, a1.w};
+        const uint32_t f0[4] = {lo.x, hi.x, lo.y, hi.y}, f1[4] = {lo.z, hi.z, lo.w, hi.w};
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          mma_16816(x[n], f0, k[n].x, k[n].y);
-          mma_16816(x[n], f1, k[n].z, k[n].w);
+        for (int n = 0; n < kN; ++n) {
+          mma_16816(x[n], f0, q[n][2 * i].x, q[n][2 * i].y);
+          mma_16816(x[n], f1, q[n][2 * i + 1].x, q[n][2 * i + 1].y);
         }
       }
     }
     // base-2 exponents; hidden keys at -inf, whatever their rows and scales hold
-    float vs[2][2];
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      float2 ks = make_float2(a.scale_log2e, a.scale_log2e);
-      if constexpr (kQ8) {
-        ks = *reinterpret_cast<const float2 *>(k_at + Y::kScales + (n * 8 + 2 * quad) * 4);
-        ks.x *= a.scale_log2e * kCodeUnit; ks.y *= a.scale_log2e * kCodeUnit;
-        const float2 two = *reinterpret_cast<const float2 *>(k_at + Y::kScales + 64 + (n * 8 + 2 * quad) * 4);
-        vs[n][0] = two.x * kCodeUnit; vs[n][1] = two.y * kCodeUnit;
-      }
-      x[n][0] *= ks.x; x[n][1] *= ks.y; x[n][2] *= ks.x; x[n][3] *= ks.y;
+    float ks0 = a.scale_log2e, ks1 = a.scale_log2e, vs0 = 1.f, vs1 = 1.f;
+    if constexpr (kQ8) {
+      const float *scales = reinterpret_cast<const float *>(k_at + Y::kScales) + oct;
+      ks0 *= kCodeUnit * scales[0]; ks1 *= kCodeUnit * scales[8];
+      vs0 = kCodeUnit * scales[16]; vs1 = kCodeUnit * scales[24];
     }
+#pragma unroll
+    for (int n = 0; n < kN; ++n) { x[n][0] *= ks0; x[n][1] *= ks0; x[n][2] *= ks1; x[n][3] *= ks1; }
     const bool whole = page >= 0 && key0 >= lo_full && key0 + 16 <= hi_full;
     uint32_t hidden = 0;
     if (!whole) {
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+      for (int n = 0; n < kN; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int pos = key0 + n * 8 + 2 * quad + (e & 1), i = e >> 1;
-          if (page < 0 || pos >= row_hi[i] || (pos < row_lo[i] && pos >= n_sink)) { x[n][e] = -INFINITY; hidden |= 1u << (4 * n + e); }
+          const int t = first + a.group.div(min(n * 8 + 2 * quad + (e & 1), rows - 1)), pos = key0 + oct + 8 * (e >> 1);
+          if (page < 0 || pos >= seen_hi(a.mask, t, length) || (pos < seen_lo(a.mask, t) && pos >= n_sink)) {
+            x[n][e] = -INFINITY;
+            hidden |= 1u << (4 * n + e);
+          }
         }
     }
     // the rows' references
-    float top[2];
+    bool rise = false;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      top[i] = fmaxf(fmaxf(x[0][2 * i], x[0][2 * i + 1]), fmaxf(x[1][2 * i], x[1][2 * i + 1]));
+    for (int n = 0; n < kN; ++n) rise = rise || fmaxf(x[n][0], x[n][2]) > m[n][0] + kRaise || fmaxf(x[n][1], x[n][3]) > m[n][1] + kRaise;
+    if (__any_sync(0xffffffffu, rise)) {
+#pragma unroll
+      for (int n = 0; n < kN; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float raised = fmaxf(fmaxf(x[n][e], x[n][2 + e]), m[n][e]);
+#pragma unroll
+          for (int d = 4; d < 32; d *= 2) raised = fmaxf(raised, __shfl_xor_sync(0xffffffffu, raised, d));
+          const float f = exp2_approx(m[n][e] - raised);
+          m[n][e] = raised;
+          l[n][e] *= f;
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) { o[i][n][e] *= f; o[i][n][2 + e] *= f; }
+        }
     }
-    if (__any_sync(0xffffffffu, top[0] > m[0] + kRaise || top[1] > m[1] + kRaise)) {
-      float f[2];
+    uint32_t p[kN][2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
-        top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
-        const float raised = fmaxf(m[i], top[i]);
-        f[i] = raised == -INFINITY ? 1.f : exp2_approx(m[i] - raised);      // (from no reference at all: 0)
-        m[i] = raised;
-        l[i] *= f[i];
-      }
-#pragma unroll
-      for (int j = 0; j < D / 8; ++j) {
-        o[j][0] *= f[0]; o[j][1] *= f[0];
-        o[j][2] *= f[1]; o[j][3] *= f[1];
-      }
-    }
-    const float ref[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
-    uint32_t p[4];
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
+    for (int n = 0; n < kN; ++n) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        x[n][e] = exp2_approx(x[n][e] - ref[e >> 1]);
-        l[e >> 1] += x[n][e];
+        x[n][e] = exp2_approx(x[n][e] - m[n][e & 1]);
+        l[n][e & 1] += x[n][e];
       }
-      if constexpr (kQ8) {
-        // (a hidden key counts for nothing even where its scale is no number)
+      float y[4] = {x[n][0] * vs0, x[n][1] * vs0, x[n][2] * vs1, x[n][3] * vs1};
+      if (kQ8 && !whole) {                                 // (a hidden value counts for nothing even where its scale is no number)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[n][e] = (hidden >> (4 * n + e)) & 1u ? 0.f : x[n][e] * vs[n][e & 1];
+        for (int e = 0; e < 4; ++e)
+          if ((hidden >> (4 * n + e)) & 1u) y[e] = 0.f;
       }
-      p[2 * n] = pair_bf16(x[n][0], x[n][1]);
-      p[2 * n + 1] = pair_bf16(x[n][2], x[n][3]);
+      p[n][0] = transpose_8x8(pair_bf16(y[0], y[1]));
+      p[n][1] = transpose_8x8(pair_bf16(y[2], y[3]));
     }
-    // O += P V
-    if constexpr (kQ8) {
+    // O^T += V^T P^T
+#pragma unroll
+    for (int i = 0; i < (kRowBytes >= 128 ? kRowBytes / 128 : 1); ++i) {
       uint4 v[4];
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
         const int r = (n >> 1) * 8 + 2 * quad + (n & 1);
         if constexpr (kRowBytes >= 128) {
-          v[n] = *reinterpret_cast<const uint4 *>(v_at + Y::piece(r, oct));
+          v[n] = *reinterpret_cast<const uint4 *>(v_at + Y::piece(r, i * 8 + oct));
         } else {
           const uint2 two = *reinterpret_cast<const uint2 *>(v_at + Y::piece(r, oct >> 1) + (oct & 1) * 8);
           v[n] = make_uint4(two.x, two.y, 0u, 0u);
         }
       }
+      if constexpr (kQ8) {
 #pragma unroll
-      for (int w = 0; w < D / 32; ++w) {
-        uint32_t c[4];
+        for (int w = 0; w < D / 32; ++w) {
+          const uint32_t c0 = word(v[0], w), c1 = word(v[1], w), c2 = word(v[2], w), c3 = word(v[3], w);
+          const uint32_t f0[4] = {codes_across<0>(c0, c1), codes_across<1>(c0, c1), codes_across<0>(c2, c3), codes_across<1>(c2, c3)};
+          const uint32_t f1[4] = {codes_across<2>(c0, c1), codes_across<3>(c0, c1), codes_across<2>(c2, c3), codes_across<3>(c2, c3)};
 #pragma unroll
-        for (int n = 0; n < 4; ++n) c[n] = turn_signs(word(v[n], w));
-        mma_16816(o[4 * w], p, codes_across<0>(c[0], c[1]), codes_across<0>(c[2], c[3]));
-        mma_16816(o[4 * w + 1], p, codes_across<1>(c[0], c[1]), codes_across<1>(c[2], c[3]));
-        mma_16816(o[4 * w + 2], p, codes_across<2>(c[0], c[1]), codes_across<2>(c[2], c[3]));
-        mma_16816(o[4 * w + 3], p, codes_across<3>(c[0], c[1]), codes_across<3>(c[2], c[3]));
-      }
-    } else {
+          for (int n = 0; n < kN; ++n) {
+            mma_16816(o[2 * w][n], f0, p[n][0], p[n][1]);
+            mma_16816(o[2 * w + 1][n], f1, p[n][0], p[n][1]);
+          }
+        }
+      } else {
 #pragma unroll
-      for (int i = 0; i < kValPieces; ++i) {
-        uint4 v[4];
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t c0 = word(v[0], w), c1 = word(v[1], w), c2 = word(v[2], w), c3 = word(v[3], w);
+          const uint32_t f[4] = {__byte_perm(c0, c1, 0x5410), __byte_perm(c0, c1, 0x7632), __byte_perm(c2, c3, 0x5410), __byte_perm(c2, c3, 0x7632)};
 #pragma unroll
-        for (int n = 0; n < 4; ++n) v[n] = *reinterpret_cast<const uint4 *>(v_at + Y::piece((n >> 1) * 8 + 2 * quad + (n & 1), i * 8 + oct));
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint32_t sel = (e & 1) ? 0x7632 : 0x5410;
-          mma_16816(o[i * 8 + e], p, __byte_perm(word(v[0], e >> 1), word(v[1], e >> 1), sel), __byte_perm(word(v[2], e >> 1), word(v[3], e >> 1), sel));
+          for (int n = 0; n < kN; ++n) mma_16816(o[4 * i + w][n], f, p[n][0], p[n][1]);
         }
       }
     }
@@ -345,20 +335,23 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8>::kCtas) p
   // ---- the warps' parts, combined over what was the ring
   asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
-  float *o_smem = reinterpret_cast<float *>(smem + Y::kOffRing), *ml_smem = o_smem + kStreamWarps * kTileRows * D;      // [warp][row][dim], [warp][row][2]
+  constexpr int kRows = 8 * kN;
+  float *o_smem = reinterpret_cast<float *>(smem), *ml_smem = o_smem + kStreamWarps * kRows * D;      // [warp][row][dim], [warp][row][2]
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-    if (quad == 0) *reinterpret_cast<float2 *>(ml_smem + (warp * kTileRows + oct + 8 * i) * 2) = make_float2(m[i], l[i]);
-  }
+  for (int n = 0; n < kN; ++n)
 #pragma unroll
-  for (int j = 0; j < D / 8; ++j)
+    for (int e = 0; e < 2; ++e) {
+      float sum = l[n][e];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      // column n = 2 quad + (e & 1) of n-tile j
-      const int n = 2 * quad + (e & 1), dim = kQ8 ? n * (D / 8) + j : (j >> 3) * 64 + n * 8 + (j & 7);
-      o_smem[(warp * kTileRows + oct + 8 * (e >> 1)) * D + dim] = o[j][e];
+      for (int d = 4; d < 32; d *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      const int r = n * 8 + 2 * quad + e;
+      if (oct == 0) *reinterpret_cast<float2 *>(ml_smem + (warp * kRows + r) * 2) = make_float2(m[n][e], sum);
+      // an m-tile's rows oct and oct + 8 are neighbouring dims of the lane's piece
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        const int dim = kQ8 ? oct * (D / 8) + 2 * i : (i >> 2) * 64 + oct * 8 + 2 * (i & 3);
+        *reinterpret_cast<float2 *>(o_smem + (warp * kRows + r) * D + dim) = make_float2(o[i][n][e], o[i][n][2 + e]);
+      }
     }
   __syncthreads();
   const size_t all_rows = (size_t)a.bt.n_tokens * a.n_heads;
@@ -377,15 +370,15 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8>::kCtas) p
     const int r = i / (D / 8), piece = i % (D / 8);
     float acc[8], top = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kStreamWarps; ++w) top = fmaxf(top, ml_smem[(w * kTileRows + r) * 2]);
+    for (int w = 0; w < kStreamWarps; ++w) top = fmaxf(top, ml_smem[(w * kRows + r) * 2]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] = 0.f;
 #pragma unroll
     for (int w = 0; w < kStreamWarps; ++w) {
-      const float2 x = *reinterpret_cast<const float2 *>(ml_smem + (w * kTileRows + r) * 2);
-      const float f = x.x == -INFINITY ? 0.f : exp2_approx(x.x - top);
+      const float2 x = *reinterpret_cast<const float2 *>(ml_smem + (w * kRows + r) * 2);
+      const float f = exp2_approx(x.x - top);
       sum += f * x.y;
-      const float4 *v = reinterpret_cast<const float4 *>(o_smem + (w * kTileRows + r) * D + piece * 8);
+      const float4 *v = reinterpret_cast<const float4 *>(o_smem + (w * kRows + r) * D + piece * 8);
       const float4 lo = v[0], hi = v[1];
       acc[0] += f * lo.x; acc[1] += f * lo.y; acc[2] += f * lo.z; acc[3] += f * lo.w;
       acc[4] += f * hi.x; acc[5] += f * hi.y; acc[6] += f * hi.z; acc[7] += f * hi.w;
@@ -428,7 +421,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8>::kCtas) p
       const float2 x = ml_of(e);
       const float4 *v = reinterpret_cast<const float4 *>(a.part_o + ((size_t)e * all_rows + row) * D + piece * 8);
       const float4 lo = __ldcg(v), hi = __ldcg(v + 1);
-      const float f = x.x == -INFINITY ? 0.f : exp2_approx(x.x - top);
+      const float f = exp2_approx(x.x - top);
       sum += f * x.y;
       acc[0] += f * lo.x; acc[1] += f * lo.y; acc[2] += f * lo.z; acc[3] += f * lo.w;
       acc[4] += f * hi.x; acc[5] += f * hi.y; acc[6] += f * hi.z; acc[7] += f * hi.w;
