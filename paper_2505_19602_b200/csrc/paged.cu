@@ -143,12 +143,15 @@ scalekv_status launch_stream(scalekv_paged *c, const AttendArgs &a, long long ke
   // CTAs for a head: 34.9 / 15.5 / 12.3 / 12.3 / 16.4 us); beyond it, for lengths that differ, up to two waves of 64 steps or more (32 x up to 10 521, 256 pairs of
   // sequence and head, 1 / 2 / 4 / 8 / 16: 197 / 157 / 143 / 144 / 163; 64 x 1 028 keys of a window, 1 / 2 / 4: 45 / 54 / 64).
   const long long items = (long long)a.bt.n_seqs * a.s.heads, slots = (long long)c->n_sm * Y::kCtas, steps = (keys + 15) / 16;
-  long long split = std::max(std::min(slots / items, steps / 8), std::min(2 * slots / items, steps / 64));
-  split = std::max<long long>(1, std::min<long long>(split, kPartRows / ((long long)a.bt.n_tokens * a.n_heads)));
+  // Otherwise the steps of all of them are dealt out evenly, where that gives a CTA 64 or more.
+  const long long room = std::min<long long>(kPartRows / ((long long)a.bt.n_tokens * a.n_heads), 256);      // parts that the workspace holds
+  long long split = std::max<long long>(1, std::min(std::min(slots / items, steps / 8), room));
+  const bool by_length = a.bt.n_seqs > 1 && a.bt.n_seqs <= 512 && items <= std::min<long long>(kMaxCounts, 3 * slots) && room >= 3 && items * steps >= slots * 64;
   if (items > kMaxCounts) split = 1;
   if (cudaFuncSetAttribute(paged_stream_kernel<D, kQ8, kN>, cudaFuncAttributeMaxDynamicSharedMemorySize, Y::kSmem) != cudaSuccess)
     return fail(c, SCALEKV_ERR_CUDA, "cannot raise the dynamic shared memory limit");
-  launch(paged_stream_kernel<D, kQ8, kN>, dim3(a.bt.n_seqs, a.s.heads, (unsigned)split), kStreamThreads, Y::kSmem, stream, a);
+  launch(paged_stream_kernel<D, kQ8, kN>, by_length ? dim3((unsigned)slots) : dim3(a.bt.n_seqs, a.s.heads, (unsigned)split), kStreamThreads, Y::kSmem, stream, a,
+         by_length ? (int)room : 0);
   return launched(c, "paged_attend");
 }
 

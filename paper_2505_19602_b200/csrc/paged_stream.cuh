@@ -50,6 +50,7 @@ struct StreamLayout {
 };
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 3.f;
+constexpr int kSecond = 40;
 
 struct Mask {
   int causal, window, n_sink;      // window 0: none
@@ -100,6 +101,28 @@ __device__ __forceinline__ void mma_16816(float *c, const uint32_t *a, uint32_t 
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// What a sequence has to do with a launch: its query rows of a kv head, and the keys that some of them sees, in steps of 16: the sinks' steps,
+// then those of [lo, hi).
+struct Span {
+  int start, rows, length, first, lo, hi, n_sink, lo_step, sink_steps, steps;
+  __device__ __forceinline__ Span(const AttendArgs &a, int seq, int most_rows, bool tell) {
+    start = __ldg(a.bt.starts + seq);
+    length = __ldg(a.bt.lengths + seq);
+    const int n_new = min(__ldg(a.bt.starts + seq + 1), a.bt.n_tokens) - start, room = a.bt.table_pages << a.s.page_shift;
+    if (tell && (n_new > a.max_new || (unsigned)length > (unsigned)room)) report(a.s.status);
+    length = max(min(length, room), 0);                    // (what lies behind the table counts as hidden)
+    first = length - n_new;                                // position of the sequence's first new token
+    rows = start < 0 || n_new <= 0 ? 0 : min(n_new * a.group.d, most_rows);
+    const int t_last = a.group.div(max(rows - 1, 0));
+    lo = min(seen_lo(a.mask, first), length);
+    hi = seen_hi(a.mask, first + t_last, length);
+    n_sink = a.mask.window > 0 ? a.mask.n_sink : 0;
+    lo_step = lo >> 4;
+    sink_steps = min((min(n_sink, hi) + 15) >> 4, lo_step);
+    steps = rows > 0 ? sink_steps + max((hi + 15) >> 4, lo_step) - lo_step : 0;
+  }
+};
+
 // [row of 8][pair of columns] in the lanes -> [column][pair of rows]
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
   uint32_t y;
@@ -112,38 +135,18 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool on) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
 }
 
+// One part of a sequence and kv head: steps step_lo .. step_hi - 1 of it, as part number `part` of `parts`.  All threads of the CTA.
 template <int D, bool kQ8, int kN>
-__global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8, kN>::kCtas) paged_stream_kernel(const __grid_constant__ AttendArgs a) {
+__device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp, char *smem, int *shared_word, int seq, int head, int step_lo, int step_hi, int part,
+                                            int parts) {
   using Y = StreamLayout<D, kQ8, kN>;
   constexpr int kRowBytes = Y::kRowBytes, kStages = Y::kStages;
-  extern __shared__ __align__(16) char smem[];
-  __shared__ int last_one;
-
-  const int seq = blockIdx.x, head = blockIdx.y;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = lane & 3, oct = lane >> 2;
   const Store &s = a.s;
-  wait_for_grid();
-  const int start = __ldg(a.bt.starts + seq), n_new = min(__ldg(a.bt.starts + seq + 1), a.bt.n_tokens) - start;
-  int length = __ldg(a.bt.lengths + seq);
-  const int rows = min(n_new * a.group.d, 8 * kN);         // query rows
-  if (n_new > a.max_new && threadIdx.x == 0) report(s.status);
-  if (rows <= 0 || start < 0) return;
-  if ((unsigned)length > (unsigned)(a.bt.table_pages << s.page_shift)) {       // (what lies behind the table counts as hidden)
-    length = length < 0 ? 0 : a.bt.table_pages << s.page_shift;
-    report(s.status);
-  }
-  const int first = length - n_new;                        // position of the sequence's first new token
-
-  // the keys that some row sees, in steps of 16: the sinks' steps, then those of [lo, hi)
+  const int item = seq * s.heads + head, start = sp.start, rows = sp.rows, length = sp.length, first = sp.first, n_sink = sp.n_sink;
   const int t_last = a.group.div(rows - 1);
-  const int lo_all = min(seen_lo(a.mask, first), length), hi_all = seen_hi(a.mask, first + t_last, length);
-  const int lo_step = lo_all >> 4, hi_step = max((hi_all + 15) >> 4, lo_step);
-  const int n_sink = a.mask.window > 0 ? a.mask.n_sink : 0;
-  const int sink_steps = min((min(n_sink, hi_all) + 15) >> 4, lo_step);
-  const int steps = sink_steps + hi_step - lo_step;
-  const int step_lo = (int)((long long)steps * blockIdx.z / gridDim.z), step_hi = (int)((long long)steps * (blockIdx.z + 1) / gridDim.z);
-  auto in_use = [&](int pos) { return pos < hi_all && (pos >= lo_all || pos < n_sink); };
-  auto key_of = [&](int step) { return (step < sink_steps ? step : step - sink_steps + lo_step) << 4; };
+  auto in_use = [&](int pos) { return pos < sp.hi && (pos >= sp.lo || pos < n_sink); };
+  auto key_of = [&](int step) { return (step < sp.sink_steps ? step : step - sp.sink_steps + sp.lo_step) << 4; };
   auto page_at = [&](int step) { return step < step_hi ? page_of(s, a.bt, seq, key_of(step)) : -1; };
 
   // ---- the ring: this warp's steps are step_lo + warp, + 4, ..
@@ -331,7 +334,6 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8, kN>::kCta
     }
   }
 
-  next_grid();
   // ---- the warps' parts, combined over what was the ring
   asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
@@ -386,26 +388,28 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8, kN>::kCta
     const float2 ml = make_float2(top, sum);
     int t, h;
     place(r, t, h);
-    if (gridDim.z == 1) {
+    if (parts == 1) {
       put(t, h, piece, acc, ml);
     } else {
-      const size_t part = (size_t)blockIdx.z * all_rows + (size_t)t * a.n_heads + h;
-      float4 *dst = reinterpret_cast<float4 *>(a.part_o + part * D + piece * 8);
+      const size_t at = (size_t)part * all_rows + (size_t)t * a.n_heads + h;
+      float4 *dst = reinterpret_cast<float4 *>(a.part_o + at * D + piece * 8);
       dst[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
       dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
-      if (piece == 0) *reinterpret_cast<float2 *>(a.part_ml + part * 2) = ml;
+      if (piece == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = ml;
     }
   }
-  if (gridDim.z == 1) return;
-  __threadfence();
-  __syncthreads();
+  if (parts > 1) __threadfence();
+  __syncthreads();                                         // (also: what was the ring may be one again)
+  if (parts == 1) return;
   if (threadIdx.x == 0) {
-    int *count = a.counts + blockIdx.x * gridDim.y + blockIdx.y;
-    last_one = atomicAdd(count, 1) == (int)gridDim.z - 1;
-    if (last_one) *count = 0;
+    const int last = atomicAdd(a.counts + item, 1) == parts - 1;
+    if (last) a.counts[item] = 0;
+    *shared_word = last;
   }
   __syncthreads();
-  if (!last_one) return;
+  const bool last = *shared_word != 0;
+  __syncthreads();
+  if (!last) return;
   __threadfence();
   for (int i = threadIdx.x; i < rows * (D / 8); i += kStreamThreads) {
     const int r = i / (D / 8), piece = i % (D / 8);
@@ -415,9 +419,9 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8, kN>::kCta
     auto ml_of = [&](int e) { return __ldcg(reinterpret_cast<const float2 *>(a.part_ml + ((size_t)e * all_rows + row) * 2)); };
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, top = -INFINITY, sum = 0.f;
 #pragma unroll 4
-    for (int e = 0; e < (int)gridDim.z; ++e) top = fmaxf(top, ml_of(e).x);
+    for (int e = 0; e < parts; ++e) top = fmaxf(top, ml_of(e).x);
 #pragma unroll 4
-    for (int e = 0; e < (int)gridDim.z; ++e) {
+    for (int e = 0; e < parts; ++e) {
       const float2 x = ml_of(e);
       const float4 *v = reinterpret_cast<const float4 *>(a.part_o + ((size_t)e * all_rows + row) * D + piece * 8);
       const float4 lo = __ldcg(v), hi = __ldcg(v + 1);
@@ -428,6 +432,92 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8, kN>::kCta
     }
     put(t, h, piece, acc, make_float2(top, sum));
   }
+}
+
+template <int D, bool kQ8, int kN>
+__global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8, kN>::kCtas) paged_stream_kernel(const __grid_constant__ AttendArgs a, int most_parts) {
+  using Y = StreamLayout<D, kQ8, kN>;
+  extern __shared__ __align__(16) char smem[];
+  __shared__ int shared_word;
+  const int lane = threadIdx.x & 31;
+  wait_for_grid();
+  // Either a CTA to each part of a sequence and kv head, as the grid says, or (most_parts > 0) by what the lengths turn out to be: as many equal parts of
+  // each as there are CTAs for; or, where that would leave the longest ones' parts too long, the steps of all of them one behind the other and an equal share to
+  // every CTA, which may begin and end within a sequence.  That costs a CTA a second beginning and end: kSecond steps.  (At least one step to whoever has
+  // rows, so that it is met; no more than most_parts shares to a sequence and head.)
+  const int heads = a.s.heads;
+  auto weight = [&](int b, bool tell) {
+    if (b >= a.bt.n_seqs) return 0;
+    const Span sp(a, b, 8 * kN, tell);
+    return sp.rows > 0 ? max(sp.steps, 1) : 0;
+  };
+  long long at = 0, end = 1;
+  int share = 0, split = gridDim.z;                        // share 0: parts
+  int seq = blockIdx.x, head = blockIdx.y, part = blockIdx.z;
+  if (most_parts > 0) {
+    long long total = 0;
+    int longest = 1;
+    for (int b0 = 0; b0 < a.bt.n_seqs; b0 += 32) {
+      const int w = weight(b0 + lane, blockIdx.x == 0 && threadIdx.x < 32);
+      total += __reduce_add_sync(0xffffffffu, w);
+      longest = max(longest, __reduce_max_sync(0xffffffffu, w));
+    }
+    total *= heads;
+    const int ctas = gridDim.x, items = a.bt.n_seqs * heads;
+    split = max(1, min(min(ctas / items, longest / 8), most_parts));
+    share = max((int)((total + ctas - 1) / ctas), (longest + most_parts - 2) / (most_parts - 1));
+    if (share + kSecond >= (items + ctas - 1) / ctas * ((longest + split - 1) / split)) {
+      share = 0;
+      at = blockIdx.x;
+      end = (long long)items * split;
+    } else {
+      at = (long long)blockIdx.x * share;
+      end = min(at + share, total);
+    }
+  }
+  while (at < end) {
+    int parts = split, lo, hi;
+    long long next = at + gridDim.x, from = 0;             // where this CTA goes on; of the sequence and head the first step
+    if (share > 0) {
+      long long before = 0;                                // steps of the sequences ahead of b0
+      int w = 0, incl = 0, b0 = 0;
+      unsigned behind = 0;
+      for (; b0 < a.bt.n_seqs; b0 += 32) {
+        incl = w = weight(b0 + lane, false);
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const int up = __shfl_up_sync(0xffffffffu, incl, d);
+          if (lane >= d) incl += up;
+        }
+        behind = __ballot_sync(0xffffffffu, before + (long long)incl * heads > at);
+        if (behind) break;
+        before += (long long)__shfl_sync(0xffffffffu, incl, 31) * heads;
+      }
+      const int src = __ffs(behind) - 1, steps = __shfl_sync(0xffffffffu, w, src);
+      from = before + (long long)__shfl_sync(0xffffffffu, incl - w, src) * heads;
+      seq = b0 + src;
+      head = (int)((at - from) / steps);
+      from += (long long)head * steps;
+      next = min(from + steps, end);
+      part = (int)(at / share - from / share);
+      parts = (int)((from + steps - 1) / share - from / share) + 1;
+    } else if (most_parts > 0) {
+      part = (int)at % split;
+      head = (int)at / split % heads;
+      seq = (int)at / split / heads;
+    }
+    const Span sp(a, seq, 8 * kN, most_parts == 0 && threadIdx.x == 0);
+    if (share > 0) {
+      lo = (int)(at - from);
+      hi = min((int)(next - from), sp.steps);
+    } else {
+      lo = (int)((long long)sp.steps * part / parts);
+      hi = (int)((long long)sp.steps * (part + 1) / parts);
+    }
+    if (sp.rows > 0) stream_part<D, kQ8, kN>(a, sp, smem, &shared_word, seq, head, lo, hi, part, parts);
+    at = next;
+  }
+  next_grid();
 }
 
 // O = sum_e 2^(m_e - M) O_e / sum_e 2^(m_e - M) l_e, M the largest reference: a warp to each row.
