@@ -5,18 +5,29 @@
 // a value is off by at most s / 2 and a few units of fp32.  A row of zeros has s = 0; a row that holds an infinity or a NaN has
 // s = NaN and codes 0, so it reads back as NaN and is not taken for numbers.
 //
-// Both kernels move every row once, eight values a lane: 16 lanes are a row of 128, 8 one of 64.  A block takes kRowsPerLane rows for each of its row
-// groups, all loads before all stores.  Rows are numbered token by token, in a token K's heads and then V's.
+// Both kernels move every row once; what bounds them is that.  A lane has 16 values of a row, 8 lanes are a row of 128, 4 one of 64.  A block takes a few
+// tokens, all heads of K and V of them: one thread to a token finds its place, then the rows follow one another as they do in a dense tensor.
+// us per pass, eight values a lane and every row's place looked up by its own lanes / so: 84 168 tokens of 8 heads in codes read as bf16 118 / XXXR, 24 646 of 16
+// heads written and read back 228 / XXXW.
 #pragma once
 #include <math_constants.h>
 
 #include "paged_view.cuh"
+#include "tc.cuh"
 
 namespace scalekv {
 namespace paged {
 
 constexpr int kStoreThreads = 256;
-constexpr int kRowsPerLane = 4;
+constexpr int kMostTokens = 32;                  // tokens of a block
+
+struct Moves {
+  Store s;
+  Batch bt;
+  Rows K, V;
+  Divisor per_token;                             // 16-value pieces of a token: of K's heads, then of V's
+  int tokens;                                    // of a block
+};
 
 // The first sequence that ends behind token t (n_seqs: none does).  All threads of the block, same t.
 __device__ __forceinline__ int block_seq_of(const Batch &bt, int t) {
@@ -28,139 +39,195 @@ __device__ __forceinline__ int block_seq_of(const Batch &bt, int t) {
   return seq;
 }
 
-// Position of token t in its sequence, and the sequence, which is `seq` or a later one.  False (reported): t belongs to no sequence.
-__device__ __forceinline__ bool locate(const Store &s, const Batch &bt, int t, int &seq, int &pos) {
-  while (seq < bt.n_seqs && __ldg(bt.starts + seq + 1) <= t) ++seq;
-  if (seq >= bt.n_seqs || t < __ldg(bt.starts + seq)) { report(s.status); return false; }
-  pos = __ldg(bt.lengths + seq) - __ldg(bt.starts + seq + 1) + t;
-  return true;
+// Row of head 0 of the block's tokens, in K as in V; -1 (reported) where a token belongs to no sequence or its page is out of range.
+__device__ __forceinline__ void place_tokens(const Moves &mv, int t0, int n, long long *row) {
+  const Batch &bt = mv.bt;
+  int seq = block_seq_of(bt, t0);
+  if ((int)threadIdx.x < n) {
+    const int t = t0 + (int)threadIdx.x;
+    while (seq < bt.n_seqs && __ldg(bt.starts + seq + 1) <= t) ++seq;
+    long long at = -1;
+    if (seq >= bt.n_seqs || t < __ldg(bt.starts + seq)) {
+      report(mv.s.status);
+    } else {
+      const int pos = __ldg(bt.lengths + seq) - __ldg(bt.starts + seq + 1) + t, page = page_of(mv.s, bt, seq, pos);
+      if (page >= 0) at = (long long)store_row(mv.s, page, 0, pos);
+    }
+    row[threadIdx.x] = at;
+  }
+  __syncthreads();
 }
 
-__device__ __forceinline__ void load8(const __nv_bfloat16 *p, float *x) { Vec16<__nv_bfloat16>::load(p, x); }
-__device__ __forceinline__ void load8(const float *p, float *x) { Vec16<float>::load(p, x); Vec16<float>::load(p + 4, x + 4); }
 __device__ __forceinline__ uint32_t pair_bf16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-__device__ __forceinline__ void store8(__nv_bfloat16 *p, const float *x) {
-  *reinterpret_cast<uint4 *>(p) = make_uint4(pair_bf16(x[0], x[1]), pair_bf16(x[2], x[3]), pair_bf16(x[4], x[5]), pair_bf16(x[6], x[7]));
+// (NaN if any of them is)
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
-__device__ __forceinline__ void store8(float *p, const float *x) {
-  *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
-  *reinterpret_cast<float4 *>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
-}
-
-template <typename T, int D, bool kQ8>
-__global__ void __launch_bounds__(kStoreThreads) paged_write_kernel(const Store s, const Batch bt, const Rows K, const Rows V, const Divisor per_token,
-                                                                    int n_rows) {
-  constexpr int kLanes = D / 8, kGroups = kStoreThreads / kLanes;
-  const int lane = threadIdx.x % kLanes, r0 = blockIdx.x * kGroups * kRowsPerLane + threadIdx.x / kLanes;
-  wait_for_grid();
-  next_grid();
-  float x[kRowsPerLane][8];
+// 16 values as they lie in memory, and as numbers
+template <typename T> struct Raw16 {
+  uint4 w[sizeof(T)];
+  __device__ __forceinline__ void load(const T *p) {
 #pragma unroll
-  for (int i = 0; i < kRowsPerLane; ++i) {
-    const int r = r0 + i * kGroups;
-    if (r >= n_rows) break;
-    const int t = per_token.div(r), e = r - t * per_token.d;
-    const bool v = e >= s.heads;
-    const Rows &X = v ? V : K;
-    load8(reinterpret_cast<const T *>(X.ptr + t * X.st + (v ? e - s.heads : e) * X.sh) + lane * 8, x[i]);
+    for (int i = 0; i < (int)sizeof(T); ++i) w[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
   }
-  int seq = block_seq_of(bt, per_token.div(blockIdx.x * kGroups * kRowsPerLane));
+  __device__ __forceinline__ void numbers(float *x) const {
 #pragma unroll
-  for (int i = 0; i < kRowsPerLane; ++i) {
-    const int r = r0 + i * kGroups;
-    // (the lanes of a row take every branch together, and the reduction names them alone)
-    if (r >= n_rows) break;
-    const int t = per_token.div(r), e = r - t * per_token.d;
-    const bool v = e >= s.heads;
-    int pos;
-    if (!locate(s, bt, t, seq, pos)) break;
-    const int page = page_of(s, bt, seq, pos);
-    if (page < 0) continue;
-    const size_t row = store_row(s, page, v ? e - s.heads : e, pos);
-    char *rows = v ? s.v_rows : s.k_rows;
-    if constexpr (!kQ8) {
-      store8(reinterpret_cast<__nv_bfloat16 *>(rows) + row * D + lane * 8, x[i]);
-    } else {
-      // the largest magnitude by its bits: an infinity or a NaN is above every number
-      unsigned a = 0;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) a = max(a, __float_as_uint(x[i][k]) & 0x7fffffffu);
-      const unsigned mask = (kLanes == 32 ? 0xffffffffu : ((1u << kLanes) - 1u) << ((threadIdx.x & 31) / kLanes * kLanes));
-#pragma unroll
-      for (int o = kLanes / 2; o > 0; o >>= 1) a = max(a, __shfl_xor_sync(mask, a, o));
-      const bool finite = a < 0x7f800000u;
-      const float scale = finite ? __fdiv_rn(__uint_as_float(a), 127.f) : CUDART_NAN_F;
-      uint32_t w[2] = {0u, 0u};
-      if (scale > 0.f) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int c = max(-127, min(127, __float2int_rn(__fdiv_rn(x[i][k], scale))));
-          w[k >> 2] |= ((unsigned)c & 0xffu) << (8 * (k & 3));
-        }
-      }
-      *reinterpret_cast<uint2 *>(rows + row * D + lane * 8) = make_uint2(w[0], w[1]);
-      if (lane == 0) (v ? s.v_scales : s.k_scales)[row] = scale;
-    }
-  }
-}
-
-template <typename T, int D, bool kQ8>
-__global__ void __launch_bounds__(kStoreThreads) paged_read_kernel(const Store s, const Batch bt, const Rows K, const Rows V, const Divisor per_token,
-                                                                   int n_rows) {
-  constexpr int kLanes = D / 8, kGroups = kStoreThreads / kLanes;
-  const int lane = threadIdx.x % kLanes, r0 = blockIdx.x * kGroups * kRowsPerLane + threadIdx.x / kLanes;
-  wait_for_grid();
-  next_grid();
-  int seq = block_seq_of(bt, per_token.div(blockIdx.x * kGroups * kRowsPerLane));
-  uint4 w[kRowsPerLane];
-  float scale[kRowsPerLane];
-#pragma unroll
-  for (int i = 0; i < kRowsPerLane; ++i) {
-    const int r = r0 + i * kGroups;
-    w[i] = make_uint4(0u, 0u, 0u, 0u);
-    scale[i] = 0.f;                                     // (a row without a page, which is reported, comes back as zeros)
-    if (r >= n_rows) break;
-    const int t = per_token.div(r), e = r - t * per_token.d;
-    const bool v = e >= s.heads;
-    int pos;
-    if (!locate(s, bt, t, seq, pos)) break;
-    const int page = page_of(s, bt, seq, pos);
-    if (page < 0) continue;
-    const size_t row = store_row(s, page, v ? e - s.heads : e, pos);
-    const char *rows = v ? s.v_rows : s.k_rows;
-    if constexpr (kQ8) {
-      const uint2 c = __ldg(reinterpret_cast<const uint2 *>(rows + row * D + lane * 8));
-      w[i].x = c.x; w[i].y = c.y;
-      scale[i] = __ldg((v ? s.v_scales : s.k_scales) + row);
-    } else {
-      w[i] = __ldg(reinterpret_cast<const uint4 *>(rows + (row * D + lane * 8) * 2));
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < kRowsPerLane; ++i) {
-    const int r = r0 + i * kGroups;
-    if (r >= n_rows) break;
-    const int t = per_token.div(r), e = r - t * per_token.d;
-    const bool v = e >= s.heads;
-    const Rows &X = v ? V : K;
-    T *out = reinterpret_cast<T *>(X.ptr + t * X.st + (v ? e - s.heads : e) * X.sh) + lane * 8;
-    float x[8];
-    if constexpr (kQ8) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = (float)(int8_t)((k < 4 ? w[i].x : w[i].y) >> (8 * (k & 3))) * scale[i];
-    } else {
+    for (int i = 0; i < (int)sizeof(T); ++i) {
       const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        x[2 * k] = __uint_as_float(u[k] << 16);
-        x[2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u);
+        if constexpr (sizeof(T) == 4) {
+          x[4 * i + k] = __uint_as_float(u[k]);
+        } else {
+          x[8 * i + 2 * k] = __uint_as_float(u[k] << 16);
+          x[8 * i + 2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u);
+        }
       }
     }
-    store8(out, x);
+  }
+};
+__device__ __forceinline__ void store16(__nv_bfloat16 *p, const float *x) {
+#pragma unroll
+  for (int i = 0; i < 16; i += 8)
+    *reinterpret_cast<uint4 *>(p + i) = make_uint4(pair_bf16(x[i], x[i + 1]), pair_bf16(x[i + 2], x[i + 3]), pair_bf16(x[i + 4], x[i + 5]), pair_bf16(x[i + 6], x[i + 7]));
+}
+__device__ __forceinline__ void store16(float *p, const float *x) {
+#pragma unroll
+  for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4 *>(p + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+}
+
+// Codes of 16 values: x / s rounded to fp32 and then to an integer, half to even.  The quotient by Markstein's theorem (IBM J. Res. Dev. 34, 1990): with r the
+// rounded reciprocal, q within a unit in the last place of the quotient and e = x - q s, which a fused multiply-add gives exactly, q + e r is the rounded
+// quotient.  x r is within two units, one such step makes that one, a second the result.  (A division for each of them took the larger part of the kernel's
+// time.)  Adding 1.5 2^23 rounds to an integer and leaves its low byte in the sum's.  A small scale is lifted first, so that nothing underflows, and its values
+// are cut off where the codes end, which a rounded subnormal scale leaves below the largest of them.
+__device__ __forceinline__ uint4 codes_of(float *x, float s) {
+  if (!(s > 0.f)) return make_uint4(0u, 0u, 0u, 0u);
+  if (s < 0x1p-60f) {
+    s *= 0x1p64f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = fmaxf(-127.f * s, fminf(127.f * s, x[i] * 0x1p64f));
+  }
+  using namespace scalekv::tc;                     // (two values to an instruction)
+  const float r = __fdiv_rn(1.f, s);
+  const uint64_t r2 = pack2(r, r), minus_s2 = pack2(-s, -s), unit2 = pack2(12582912.f, 12582912.f);
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 16; i += 4) {
+    float c[4];
+#pragma unroll
+    for (int k = 0; k < 4; k += 2) {
+      const uint64_t x2 = pack2(x[i + k], x[i + k + 1]);
+      uint64_t q = mul2(x2, r2);
+      q = fma2(fma2(q, minus_s2, x2), r2, q);
+      q = fma2(fma2(q, minus_s2, x2), r2, q);
+      unpack2(add2(q, unit2), c[k], c[k + 1]);
+    }
+    w[i / 4] = __byte_perm(__byte_perm(__float_as_uint(c[0]), __float_as_uint(c[1]), 0x0040), __byte_perm(__float_as_uint(c[2]), __float_as_uint(c[3]), 0x0040), 0x5410);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// The numbers of four codes: 2^23 + (c + 128) as fp32 has c + 128 for its last byte, and the difference is exact.
+__device__ __forceinline__ void numbers_of(uint32_t w, float *c) {
+  w ^= 0x80808080u;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) c[k] = __fsub_rn(__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7440 + k)), 8388736.f);
+}
+
+// A thread's piece of the dense tensors and of the store.
+struct Piece {
+  int t, head;                                   // token of the block
+  bool is_v;
+  __device__ __forceinline__ Piece(const Moves &mv, int i, int lanes) {
+    t = mv.per_token.div(i);
+    const int e = (i - t * mv.per_token.d) / lanes;
+    is_v = e >= mv.s.heads;
+    head = is_v ? e - mv.s.heads : e;
+  }
+  template <typename T> __device__ __forceinline__ T *dense(const Moves &mv, int t0) const {
+    const Rows &X = is_v ? mv.V : mv.K;
+    return reinterpret_cast<T *>(X.ptr + (t0 + t) * X.st + head * X.sh);
+  }
+  __device__ __forceinline__ size_t row(const Moves &mv, long long row0) const { return (size_t)row0 + ((size_t)head << mv.s.page_shift); }
+};
+
+template <typename T, int D, bool kQ8>
+__global__ void __launch_bounds__(kStoreThreads) paged_write_kernel(const __grid_constant__ Moves mv) {
+  constexpr int kLanes = D / 16;
+  __shared__ long long row0[kMostTokens];
+  wait_for_grid();
+  next_grid();
+  const Store &s = mv.s;
+  const int t0 = blockIdx.x * mv.tokens, n = min(mv.tokens, mv.bt.n_tokens - t0), pieces = n * mv.per_token.d, x = threadIdx.x % kLanes;
+  // (the lanes of a row take every branch together, and the reduction names them alone)
+  const unsigned mask = ((1u << kLanes) - 1u) << ((threadIdx.x & 31) / kLanes * kLanes);
+  Raw16<T> raw;
+  if ((int)threadIdx.x < pieces) raw.load(Piece(mv, threadIdx.x, kLanes).dense<T>(mv, t0) + x * 16);       // (under the look-up)
+  place_tokens(mv, t0, n, row0);
+  for (int i = threadIdx.x; i < pieces; i += kStoreThreads) {
+    float v[16];
+    raw.numbers(v);
+    if (i + kStoreThreads < pieces) raw.load(Piece(mv, i + kStoreThreads, kLanes).dense<T>(mv, t0) + x * 16);
+    const Piece p(mv, i, kLanes);
+    if (row0[p.t] < 0) continue;
+    const size_t row = p.row(mv, row0[p.t]);
+    char *rows = p.is_v ? s.v_rows : s.k_rows;
+    if constexpr (!kQ8) {
+      store16(reinterpret_cast<__nv_bfloat16 *>(rows) + row * D + x * 16, v);
+    } else {
+      float a = fabsf(v[0]);
+#pragma unroll
+      for (int j = 1; j < 15; j += 2) a = max_nan(a, fabsf(v[j]), fabsf(v[j + 1]));
+      a = max_nan(a, fabsf(v[15]), 0.f);
+#pragma unroll
+      for (int o = kLanes / 2; o > 0; o >>= 1) a = max_nan(a, __shfl_xor_sync(mask, a, o), 0.f);
+      const float scale = a < CUDART_INF_F ? __fdiv_rn(a, 127.f) : CUDART_NAN_F;
+      *reinterpret_cast<uint4 *>(rows + row * D + x * 16) = codes_of(v, scale);
+      if (x == 0) (p.is_v ? s.v_scales : s.k_scales)[row] = scale;
+    }
+  }
+}
+
+template <typename T, int D, bool kQ8>
+__global__ void __launch_bounds__(kStoreThreads) paged_read_kernel(const __grid_constant__ Moves mv) {
+  constexpr int kLanes = D / 16;
+  __shared__ long long row0[kMostTokens];
+  wait_for_grid();
+  next_grid();
+  const Store &s = mv.s;
+  const int t0 = blockIdx.x * mv.tokens, n = min(mv.tokens, mv.bt.n_tokens - t0), pieces = n * mv.per_token.d, x = threadIdx.x % kLanes;
+  place_tokens(mv, t0, n, row0);
+  for (int i = threadIdx.x; i < pieces; i += kStoreThreads) {
+    const Piece p(mv, i, kLanes);
+    float y[16];
+    if (row0[p.t] < 0) {                         // (a row without a page, which is reported, comes back as zeros)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) y[j] = 0.f;
+    } else {
+      const size_t row = p.row(mv, row0[p.t]);
+      const char *rows = p.is_v ? s.v_rows : s.k_rows;
+      if constexpr (kQ8) {
+        const uint4 w = __ldg(reinterpret_cast<const uint4 *>(rows + row * D + x * 16));
+        const float scale = __ldg((p.is_v ? s.v_scales : s.k_scales) + row);
+        numbers_of(w.x, y);
+        numbers_of(w.y, y + 4);
+        numbers_of(w.z, y + 8);
+        numbers_of(w.w, y + 12);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) y[j] *= scale;
+      } else {
+        Raw16<__nv_bfloat16> raw;
+        raw.load(reinterpret_cast<const __nv_bfloat16 *>(rows) + row * D + x * 16);
+        raw.numbers(y);
+      }
+    }
+    store16(p.dense<T>(mv, t0) + x * 16, y);
   }
 }
 
