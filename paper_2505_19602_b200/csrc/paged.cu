@@ -143,13 +143,16 @@ void launch_store(Moves &mv, int n_sm, cudaStream_t stream) {
 template <int D, bool kQ8, int kN>
 scalekv_status launch_stream(scalekv_paged *c, const AttendArgs &a, long long keys, cudaStream_t stream) {
   using Y = StreamLayout<D, kQ8, kN>;
-  // CTAs that share a sequence's keys: within one wave down to 8 steps of 16 keys each (one sequence of 1 999 entries, 8 kv heads, 1 / 4 / 8 / 16 / 32
-  // CTAs for a head: 34.9 / 15.5 / 12.3 / 12.3 / 16.4 us); beyond it, for lengths that differ, up to two waves of 64 steps or more (32 x up to 10 521, 256 pairs of
-  // sequence and head, 1 / 2 / 4 / 8 / 16: 197 / 157 / 143 / 144 / 163; 64 x 1 028 keys of a window, 1 / 2 / 4: 45 / 54 / 64).
   const long long items = (long long)a.bt.n_seqs * a.s.heads, slots = (long long)c->n_sm * Y::kCtas, steps = (keys + 15) / 16;
-  // Otherwise the steps of all of them are dealt out evenly, where that gives a CTA 64 or more.
-  const long long room = std::min<long long>(kPartRows / ((long long)a.bt.n_tokens * a.n_heads), 256);      // parts that the workspace holds
-  long long split = std::max<long long>(1, std::min(std::min(slots / items, steps / 8), room));
+  const long long room = std::min<long long>(kPartRows / ((long long)a.bt.n_tokens * a.n_heads), Y::kMostParts);      // parts that the workspace holds
+  // CTAs that share a sequence's keys: one for every SM, down to two steps of 16 keys for each of its warps; two where that leaves them four; as many as
+  // fit where it leaves them 16.  (us, one sequence with 8 kv heads in codes, 4 / 8 / 16 / 32 / 74 CTAs a head: 1 999 entries 12.8 / 10.3 / 8.6 / 10.6 / 18.5, 8 000
+  // 31.7 / 19.8 / 13.4 / 13.3 / 17.9, 32 000 107.7 / 58.9 / 34.1 / 26.7 / 28.9.)  Then no more of them than the longest warp's number of steps asks for.
+  long long split = std::max(c->n_sm / items, std::max(std::min(2 * c->n_sm / items, steps / 16), std::min(slots / items, steps / 64)));
+  split = std::max<long long>(1, std::min(split, (steps + 7) / 8));
+  const long long each = ((steps + split - 1) / split + kStreamWarps - 1) / kStreamWarps * kStreamWarps;
+  split = std::max<long long>(1, std::min((steps + each - 1) / each, room));
+  // Sequences of different lengths have their parts dealt out on the device, where that gives a CTA 64 steps or more.
   const bool by_length = a.bt.n_seqs > 1 && a.bt.n_seqs <= 512 && items <= std::min<long long>(kMaxCounts, 3 * slots) && room >= 3 && items * steps >= slots * 64;
   if (items > kMaxCounts) split = 1;
   if (cudaFuncSetAttribute(paged_stream_kernel<D, kQ8, kN>, cudaFuncAttributeMaxDynamicSharedMemorySize, Y::kSmem) != cudaSuccess)

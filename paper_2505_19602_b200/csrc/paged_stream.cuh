@@ -41,7 +41,10 @@ struct StreamLayout {
   static constexpr int kStage = kScales + (kQ8 ? 128 : 0);
   static constexpr int kRing = kStreamWarps * kStages * kStage;
   static constexpr int kParts = kStreamWarps * 8 * kN * (D + 2) * 4;              // the warps' sums, over the ring once that is done with
-  static constexpr int kSmem = kRing > kParts ? kRing : kParts;
+  // the parts of a sequence and head that the last CTA combines: references and sums of every row, and sums of groups of threads
+  static constexpr int kMostParts = 256;
+  static constexpr int kJoin = 8 * kN * (kMostParts + 1) * 8 + 8 + kStreamThreads * 32;
+  static constexpr int kSmem = kRing > kParts ? (kRing > kJoin ? kRing : kJoin) : (kParts > kJoin ? kParts : kJoin);
   // where piece x (16 bytes) of row r lies
   static __device__ __forceinline__ int piece(int r, int x) {
     if (kRowBytes == 64) return r * 64 + ((x ^ ((r >> 1) & 3)) << 4);
@@ -133,6 +136,91 @@ __device__ __forceinline__ uint32_t word(const uint4 &v, int i) { return i == 0 
 // 16 bytes from global to shared memory, or zeros
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool on) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+
+// Token and query head of row r of a sequence and kv head.
+__device__ __forceinline__ void place_row(const AttendArgs &a, int start, int head, int r, int &t, int &h) {
+  t = a.group.div(r);
+  h = head * a.group.d + r - t * a.group.d;
+  t += start;
+}
+// 8 columns of a row, normalised, and with the first of them its log-sum-exp; ml: reference and sum.
+__device__ __forceinline__ void put_row(const AttendArgs &a, int t, int h, int piece, const float *acc, float2 ml) {
+  const float inv = ml.y == 0.f ? 0.f : 1.f / ml.y;
+  *(reinterpret_cast<uint4 *>(a.O.ptr + t * a.O.st + h * a.O.sh) + piece) =
+      make_uint4(pair_bf16(acc[0] * inv, acc[1] * inv), pair_bf16(acc[2] * inv, acc[3] * inv), pair_bf16(acc[4] * inv, acc[5] * inv), pair_bf16(acc[6] * inv, acc[7] * inv));
+  if (piece == 0 && a.lse != nullptr) a.lse[(size_t)t * a.n_heads + h] = ml.y == 0.f ? -INFINITY : (ml.x + log2f(ml.y)) * kLn2;
+}
+
+// What the last CTA of a sequence and kv head does: references and sums of all parts side by side, a weight for each (a row's by one warp), then the parts'
+// columns, dealt to as many groups of threads as there are.  (One part after the other, three loads each, cost 0.2 us a part.)  A function of its own, so that
+// the streaming loop is compiled without it: inlined it made that 5 to 10 % longer.
+template <int D, int kRows>
+__device__ __noinline__ void join_parts(const AttendArgs &a, int start, int rows, int head, int parts, char *smem) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const size_t all_rows = (size_t)a.bt.n_tokens * a.n_heads;
+  float2 *row_ml = reinterpret_cast<float2 *>(smem), *ml = row_ml + kRows;      // [row]; [row][part]
+  for (int i = threadIdx.x; i < rows * parts; i += kStreamThreads) {
+    const int r = i / parts;
+    int t, h;
+    place_row(a, start, head, r, t, h);
+    ml[i] = __ldcg(reinterpret_cast<const float2 *>(a.part_ml + ((size_t)(i - r * parts) * all_rows + (size_t)t * a.n_heads + h) * 2));
+  }
+  __syncthreads();
+  for (int r = warp; r < rows; r += kStreamWarps) {
+    float top = -INFINITY, sum = 0.f;
+    for (int e = lane; e < parts; e += 32) top = fmaxf(top, ml[r * parts + e].x);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    for (int e = lane; e < parts; e += 32) {
+      const float2 x = ml[r * parts + e];
+      const float f = exp2_approx(x.x - top);
+      sum += f * x.y;
+      ml[r * parts + e].x = f;
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    __syncwarp();
+    if (lane == 0) row_ml[r] = make_float2(top, sum);
+  }
+  __syncthreads();
+  const int pieces = rows * (D / 8), groups = max(1, kStreamThreads / pieces);
+  float4 *sums = reinterpret_cast<float4 *>(ml + rows * parts + (rows * parts & 1));      // [group][piece][2]
+  for (int i = threadIdx.x; i < groups * pieces; i += kStreamThreads) {
+    const int group = i / pieces, j = i - group * pieces, r = j / (D / 8), piece = j % (D / 8);
+    int t, h;
+    place_row(a, start, head, r, t, h);
+    const float *columns = a.part_o + ((size_t)t * a.n_heads + h) * D + piece * 8;
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int e = group; e < parts; e += groups) {
+      const float4 *v = reinterpret_cast<const float4 *>(columns + (size_t)e * all_rows * D);
+      const float4 lo = __ldcg(v), hi = __ldcg(v + 1);
+      const float f = ml[r * parts + e].x;
+      acc[0] += f * lo.x; acc[1] += f * lo.y; acc[2] += f * lo.z; acc[3] += f * lo.w;
+      acc[4] += f * hi.x; acc[5] += f * hi.y; acc[6] += f * hi.z; acc[7] += f * hi.w;
+    }
+    if (groups == 1) {
+      put_row(a, t, h, piece, acc, row_ml[r]);
+    } else {
+      sums[i * 2] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+      sums[i * 2 + 1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+    }
+  }
+  __syncthreads();
+  if (groups > 1 && (int)threadIdx.x < pieces) {
+    const int r = threadIdx.x / (D / 8), piece = threadIdx.x % (D / 8);
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int g = 0; g < groups; ++g) {
+      const float4 lo = sums[(g * pieces + threadIdx.x) * 2], hi = sums[(g * pieces + threadIdx.x) * 2 + 1];
+      acc[0] += lo.x; acc[1] += lo.y; acc[2] += lo.z; acc[3] += lo.w;
+      acc[4] += hi.x; acc[5] += hi.y; acc[6] += hi.z; acc[7] += hi.w;
+    }
+    int t, h;
+    place_row(a, start, head, r, t, h);
+    put_row(a, t, h, piece, acc, row_ml[r]);
+  }
+  __syncthreads();                                         // (what was the ring may be one again)
 }
 
 // One part of a sequence and kv head: steps step_lo .. step_hi - 1 of it, as part number `part` of `parts`.  All threads of the CTA.
@@ -357,17 +445,7 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
     }
   __syncthreads();
   const size_t all_rows = (size_t)a.bt.n_tokens * a.n_heads;
-  auto place = [&](int r, int &t, int &h) {
-    t = a.group.div(r);
-    h = head * a.group.d + r - t * a.group.d;
-    t += start;
-  };
-  auto put = [&](int t, int h, int piece, const float *acc, float2 ml) {
-    const float inv = ml.y == 0.f ? 0.f : 1.f / ml.y;
-    *(reinterpret_cast<uint4 *>(a.O.ptr + t * a.O.st + h * a.O.sh) + piece) =
-        make_uint4(pair_bf16(acc[0] * inv, acc[1] * inv), pair_bf16(acc[2] * inv, acc[3] * inv), pair_bf16(acc[4] * inv, acc[5] * inv), pair_bf16(acc[6] * inv, acc[7] * inv));
-    if (piece == 0 && a.lse != nullptr) a.lse[(size_t)t * a.n_heads + h] = ml.y == 0.f ? -INFINITY : (ml.x + log2f(ml.y)) * kLn2;
-  };
+  auto place = [&](int r, int &t, int &h) { place_row(a, start, head, r, t, h); };
   for (int i = threadIdx.x; i < rows * (D / 8); i += kStreamThreads) {
     const int r = i / (D / 8), piece = i % (D / 8);
     float acc[8], top = -INFINITY, sum = 0.f;
@@ -389,7 +467,7 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
     int t, h;
     place(r, t, h);
     if (parts == 1) {
-      put(t, h, piece, acc, ml);
+      put_row(a, t, h, piece, acc, ml);
     } else {
       const size_t at = (size_t)part * all_rows + (size_t)t * a.n_heads + h;
       float4 *dst = reinterpret_cast<float4 *>(a.part_o + at * D + piece * 8);
@@ -411,27 +489,7 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
   __syncthreads();
   if (!last) return;
   __threadfence();
-  for (int i = threadIdx.x; i < rows * (D / 8); i += kStreamThreads) {
-    const int r = i / (D / 8), piece = i % (D / 8);
-    int t, h;
-    place(r, t, h);
-    const size_t row = (size_t)t * a.n_heads + h;
-    auto ml_of = [&](int e) { return __ldcg(reinterpret_cast<const float2 *>(a.part_ml + ((size_t)e * all_rows + row) * 2)); };
-    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, top = -INFINITY, sum = 0.f;
-#pragma unroll 4
-    for (int e = 0; e < parts; ++e) top = fmaxf(top, ml_of(e).x);
-#pragma unroll 4
-    for (int e = 0; e < parts; ++e) {
-      const float2 x = ml_of(e);
-      const float4 *v = reinterpret_cast<const float4 *>(a.part_o + ((size_t)e * all_rows + row) * D + piece * 8);
-      const float4 lo = __ldcg(v), hi = __ldcg(v + 1);
-      const float f = exp2_approx(x.x - top);
-      sum += f * x.y;
-      acc[0] += f * lo.x; acc[1] += f * lo.y; acc[2] += f * lo.z; acc[3] += f * lo.w;
-      acc[4] += f * hi.x; acc[5] += f * hi.y; acc[6] += f * hi.z; acc[7] += f * hi.w;
-    }
-    put(t, h, piece, acc, make_float2(top, sum));
-  }
+  join_parts<D, 8 * kN>(a, sp.start, rows, head, parts, smem);
 }
 
 template <int D, bool kQ8, int kN>
