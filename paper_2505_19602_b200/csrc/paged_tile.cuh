@@ -132,15 +132,13 @@ __device__ __forceinline__ void tc_st8(uint32_t at, const uint32_t *r) {
                "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
 }
-// What a row sees of a key tile, relative to the tile's first key: columns [lo, hi) and [0, sink), less those of `holes` (a bit for
-// each 16: their page is out of range).
-struct Seen {
-  int lo, hi, sink;
-  uint32_t holes;
-  __device__ __forceinline__ bool operator()(int col) const {
-    return col < hi && (col >= lo || col < sink) && !((holes >> (col >> 4)) & 1u);
-  }
-};
+__device__ __forceinline__ uint32_t lowest_bits(int n) { return n >= 32 ? 0xffffffffu : (1u << max(n, 0)) - 1u; }
+// Of 32 columns of a key tile, from position `at`, those that a row with limits [lo, hi) and n_sink does not see, a bit for each; holes: a bit for each 16
+// columns whose page is out of range.
+__device__ __forceinline__ uint32_t hidden_bits(int at, int lo, int hi, int n_sink, uint32_t holes) {
+  const uint32_t seen = lowest_bits(hi - at) & (~lowest_bits(lo - at) | lowest_bits(n_sink - at));
+  return ~seen | ((holes & 1u) * 0xffffu) | ((holes & 2u) * 0x7fff8000u);
+}
 
 // tmK, tmV: the K and V rows of all layers, [layer * pages + page][kv head * page_tokens + row][head_dim]; page0: layer * pages
 template <int D, bool kQ8>
@@ -558,7 +556,6 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       // tensor core has not been given yet, and O, once the last product given to it has landed.
       // (One loop for both, not unrolled: the roles' loops together have to stay in the SM's instruction cache.  With a masked copy of the sweep above and a copy of
       // the raise in each of its chunks a step in codes, which has the converters' loop beside it, missed it 28 times in a hundred: 2 255 us for what is 1 247.)
-      const Seen seen = {row_lo - key0, row_hi - key0, n_sink - key0, holes};
       int landed = 0;                              // 1: the last step's product has; 2: the early part of this one's, too
 #pragma unroll 1
       for (; cc < kSweepChunks && ok; ++cc) {
@@ -571,14 +568,12 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           float x[32], top = -INFINITY;
           tc_ld32(s_addr + col0, x);
           tc_wait_ld();
-          uint32_t hidden = 0;
+          const uint32_t hidden = hidden_bits(at, row_lo, row_hi, n_sink, holes >> (2 * cc));
 #pragma unroll
           for (int i = 0; i < 32; i += 2) {
             const float2 k = kQ8 ? load_shared2(scales + (col0 + i) * 4) : make_float2(c, c);
-            const bool s0 = seen(col0 + i), s1 = seen(col0 + i + 1);
-            x[i] = s0 ? x[i] * k.x : -INFINITY;
-            x[i + 1] = s1 ? x[i + 1] * k.y : -INFINITY;
-            hidden |= (s0 ? 0u : 1u << i) | (s1 ? 0u : 2u << i);
+            x[i] = (hidden >> i) & 1u ? -INFINITY : x[i] * k.x;
+            x[i + 1] = (hidden >> i) & 2u ? -INFINITY : x[i + 1] * k.y;
             top = max3(top, x[i], x[i + 1]);
           }
           if (__any_sync(0xffffffffu, top > m + 8.f)) {
