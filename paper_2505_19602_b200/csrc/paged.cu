@@ -163,14 +163,24 @@ scalekv_status launch_stream(scalekv_paged *c, const AttendArgs &a, long long ke
 }
 
 template <int D, bool kQ8>
-scalekv_status launch_tile(scalekv_paged *c, int layer, const AttendArgs &a, int items, int split, cudaStream_t stream) {
-  constexpr uint32_t smem = TileLayout<D, kQ8>::kSmem;
-  // (per device and process; the answer is the same every time)
-  if (cudaFuncSetAttribute(paged_tile_kernel<D, kQ8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+scalekv_status launch_tile(scalekv_paged *c, int layer, const AttendArgs &a, int items, long long keys, cudaStream_t stream) {
+  using Y = TileLayout<D, kQ8>;
+  if (cudaFuncSetAttribute(paged_tile_kernel<D, kQ8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Y::kSmem) != cudaSuccess)
     return fail(c, SCALEKV_ERR_CUDA, "cannot raise the dynamic shared memory limit");
-  launch(paged_tile_kernel<D, kQ8>, dim3((unsigned)(items * a.s.heads), (unsigned)split), TileLayout<D, kQ8>::kThreads, smem, stream, c->maps.k, c->maps.v, a,
-         Divisor::of(a.s.heads), items, layer * c->cfg.n_pages);
-  return launched(c, "paged_attend");
+  // An item and kv head to a CTA.  Those that do not fill the SMs, and those of the last, partial wave, are shared by as many CTAs as find one, each with four
+  // key tiles or more: XXXT.
+  const int n = items * a.s.heads, sms = (int)std::min<long long>(c->n_sm, kPartRows / kItemRows), last = n % sms;
+  const long long tiles = (keys + kTileKeys - 1) / kTileKeys;
+  int parts = last ? (int)std::min<long long>(sms / last, tiles / 2) : 1;
+  if (n > sms && tiles < 24) parts = 1;
+  const int n_full = parts > 1 ? n - last : n;
+  const Cut cut = {Divisor::of(a.s.heads), Divisor::of(std::max(parts, 1)), items, n_full};
+  launch(paged_tile_kernel<D, kQ8>, dim3((unsigned)(n_full + (n - n_full) * parts)), Y::kThreads, Y::kSmem, stream, c->maps.k, c->maps.v, a, cut,
+         layer * c->cfg.n_pages);
+  if (scalekv_status st = launched(c, "paged_attend")) return st;
+  if (n_full == n) return SCALEKV_OK;
+  launch(paged_join_kernel<D>, dim3((unsigned)((n - n_full) * (kItemRows / kJoinRows))), 32 * kJoinRows, 0, stream, a, cut);
+  return launched(c, "paged_join");
 }
 
 template <bool kWrite>
@@ -302,8 +312,6 @@ scalekv_status scalekv_paged_attend(scalekv_paged *kv, int32_t layer, const scal
   if (a.mask.window > 0) keys = std::min<long long>(keys, (long long)a.mask.window + batch->max_new + a.mask.n_sink);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool q8 = c->cfg.store == SCALEKV_STORE_Q8;
-  long long split;
-  scalekv_status done;
   if (max_rows <= kStreamRows) {
     auto go = [&](auto dim, auto codes) {
       constexpr int kD = decltype(dim)::value;
@@ -314,22 +322,12 @@ scalekv_status scalekv_paged_attend(scalekv_paged *kv, int32_t layer, const scal
     using D128 = std::integral_constant<int, 128>;
     if (D == 128) return q8 ? go(D128{}, std::true_type{}) : go(D128{}, std::false_type{});
     return q8 ? go(D64{}, std::true_type{}) : go(D64{}, std::false_type{});
-  } else {
-    // no more items than this, whatever the starts say
-    const long long items = std::min<long long>((long long)a.bt.n_tokens * G / kItemRows + a.bt.n_seqs, (max_rows + kItemRows - 1) / kItemRows * a.bt.n_seqs);
-    if (items * H > 0x7fffffffLL) return fail(c, SCALEKV_ERR_UNSUPPORTED, "too many row tiles in a call");
-    const long long tiles_k = (keys + kTileKeys - 1) / kTileKeys;
-    split = std::min<long long>(c->n_sm / (items * H), tiles_k / 2);
-    split = std::max<long long>(1, std::min<long long>(split, kPartRows / all_rows));
-    if (D == 128) done = q8 ? launch_tile<128, true>(c, layer, a, (int)items, (int)split, st) : launch_tile<128, false>(c, layer, a, (int)items, (int)split, st);
-    else done = q8 ? launch_tile<64, true>(c, layer, a, (int)items, (int)split, st) : launch_tile<64, false>(c, layer, a, (int)items, (int)split, st);
   }
-  if (done) return done;
-  if (split == 1) return SCALEKV_OK;
-  const unsigned blocks = (unsigned)((all_rows + 7) / 8);
-  if (D == 128) launch(paged_join_kernel<128>, dim3(blocks), 256, 0, st, a, (int)split);
-  else launch(paged_join_kernel<64>, dim3(blocks), 256, 0, st, a, (int)split);
-  return launched(c, "paged_join");
+  // no more items than this, whatever the starts say
+  const long long items = std::min<long long>((long long)a.bt.n_tokens * G / kItemRows + a.bt.n_seqs, (max_rows + kItemRows - 1) / kItemRows * a.bt.n_seqs);
+  if (items * H > 0x3fffffffLL) return fail(c, SCALEKV_ERR_UNSUPPORTED, "too many row tiles in a call");
+  if (D == 128) return q8 ? launch_tile<128, true>(c, layer, a, (int)items, keys, st) : launch_tile<128, false>(c, layer, a, (int)items, keys, st);
+  return q8 ? launch_tile<64, true>(c, layer, a, (int)items, keys, st) : launch_tile<64, false>(c, layer, a, (int)items, keys, st);
 }
 
 scalekv_status scalekv_paged_sync(scalekv_paged *kv, void *stream) {

@@ -64,7 +64,7 @@ struct AttendArgs {
   Batch bt;
   Rows Q, O;                       // [tokens][heads][head_dim] bf16
   float *lse;                      // [tokens][heads] or null
-  float *part_o, *part_ml;         // [split][tokens * heads][head_dim], [split][tokens * heads][2]: base-2 reference and sum
+  float *part_o, *part_ml;         // parts of rows that CTAs share: columns, and base-2 reference and sum
   int *counts;                     // parts left so far, one for each sequence and kv head of a split launch; zero between launches
   Mask mask;
   Divisor group;                   // query heads of a kv head
@@ -576,44 +576,6 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8, kN>::kCta
     at = next;
   }
   next_grid();
-}
-
-// O = sum_e 2^(m_e - M) O_e / sum_e 2^(m_e - M) l_e, M the largest reference: a warp to each row.
-template <int D>
-__global__ void __launch_bounds__(256) paged_join_kernel(const AttendArgs a, int n_split) {
-  constexpr int kPer = D / 32;
-  const int lane = threadIdx.x & 31, row = blockIdx.x * 8 + (threadIdx.x >> 5), all_rows = a.bt.n_tokens * a.n_heads;
-  wait_for_grid();
-  next_grid();
-  if (row >= all_rows) return;
-  float m = -INFINITY, sum = 0.f, acc[kPer];
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
-  for (int e = lane; e < n_split; e += 32) m = fmaxf(m, a.part_ml[((size_t)e * all_rows + row) * 2]);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  for (int e = 0; e < n_split; ++e) {
-    const size_t part = (size_t)e * all_rows + row;
-    const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + part * 2);
-    if (ml.x == -INFINITY) continue;
-    const float f = exp2_approx(ml.x - m);
-    sum += f * ml.y;
-    float v[kPer];
-    if constexpr (kPer == 4) *reinterpret_cast<float4 *>(v) = *reinterpret_cast<const float4 *>(a.part_o + part * D + lane * kPer);
-    else *reinterpret_cast<float2 *>(v) = *reinterpret_cast<const float2 *>(a.part_o + part * D + lane * kPer);
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) acc[i] += f * v[i];
-  }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  const int t = row / a.n_heads, h = row - t * a.n_heads;
-  char *out = a.O.ptr + t * a.O.st + h * a.O.sh + lane * kPer * 2;
-#pragma unroll
-  for (int i = 0; i < kPer; i += 2) {
-    uint32_t u;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u) : "f"(acc[i + 1] * inv), "f"(acc[i] * inv));
-    *reinterpret_cast<uint32_t *>(out + i * 2) = u;
-  }
-  if (lane == 0 && a.lse != nullptr) a.lse[row] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * kLn2;
 }
 
 }  // namespace paged

@@ -2,8 +2,8 @@
 //
 // The query rows of a kv head (row r: head r mod G of the group, token r / G) are cut into items of 256, a pair of 128-row tiles A and B;
 // every 128-key tile is brought into shared memory once for both.  An item of 128 rows or fewer is a single: A and B are then the
-// same queries against the even and the odd key tiles, combined at the end.  gridDim.y CTAs share an item's key tiles where there are
-// few items; paged_join_kernel combines what they leave.
+// same queries against the even and the odd key tiles, combined at the end.  Where items do not fill the SMs, and for the last, partial wave of
+// them, several CTAs share an item's key tiles; paged_join_kernel combines what they leave.
 //
 // Roles in a CTA, by warpgroup (registers dealt out by setmaxnreg):
 //   warp 0        : tcgen05.mma issuer.  S_A(0), S_B(0), then per step j  PV_A(j), S_A(j+1), PV_B(j), S_B(j+1): the tensor pipe works
@@ -132,6 +132,40 @@ __device__ __forceinline__ void tc_st8(uint32_t at, const uint32_t *r) {
                "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
 }
+// The sequence and tile of item number `want`, items counted through the sequences; -1: there are fewer.  A whole warp.
+__device__ __forceinline__ void find_item(const AttendArgs &a, int want, int &seq, int &tile) {
+  const int lane = threadIdx.x & 31;
+  int before = 0;
+  seq = -1; tile = 0;
+  for (int b0 = 0; b0 < a.bt.n_seqs; b0 += 32) {
+    const int b = b0 + lane;
+    int n = 0;
+    if (b < a.bt.n_seqs) {
+      const int st = __ldg(a.bt.starts + b), en = min(__ldg(a.bt.starts + b + 1), a.bt.n_tokens);
+      if (st >= 0 && en > st) n = (int)(((long long)(en - st) * a.group.d + kItemRows - 1) / kItemRows);
+    }
+    int incl = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += up;
+    }
+    const unsigned behind = __ballot_sync(0xffffffffu, before + incl > want);
+    if (behind) {
+      const int src = __ffs(behind) - 1;
+      seq = b0 + src;
+      tile = want - before - __shfl_sync(0xffffffffu, incl - n, src);
+      return;
+    }
+    before += __shfl_sync(0xffffffffu, incl, 31);
+  }
+}
+// CTAs of a launch: the first n_full take an item of a kv head each, the items behind them are shared by `parts`.
+struct Cut {
+  Divisor heads, parts;
+  int n_items, n_full;
+};
+
 __device__ __forceinline__ uint32_t lowest_bits(int n) { return n >= 32 ? 0xffffffffu : (1u << max(n, 0)) - 1u; }
 // Of 32 columns of a key tile, from position `at`, those that a row with limits [lo, hi) and n_sink does not see, a bit for each; holes: a bit for each 16
 // columns whose page is out of range.
@@ -144,7 +178,7 @@ __device__ __forceinline__ uint32_t hidden_bits(int at, int lo, int hi, int n_si
 template <int D, bool kQ8>
 __global__ void __launch_bounds__(TileLayout<D, kQ8>::kThreads, 1)
 paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ AttendArgs a,
-                  const Divisor per_heads, int n_items, int page0) {
+                  const Cut cut, int page0) {
   using Y = TileLayout<D, kQ8>;
   constexpr int kStages = Y::kStages;
   constexpr uint32_t kTile = Y::kTile, kHalf = Y::kHalf;
@@ -158,35 +192,16 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x & 127;
   const Store &s = a.s;
   int *status = s.status;
-  const int e = per_heads.div(blockIdx.x), head = (int)blockIdx.x - e * per_heads.d;
+  const int beyond = (int)blockIdx.x - cut.n_full, shared_item = cut.parts.div(max(beyond, 0));
+  const int part = beyond < 0 ? 0 : beyond - shared_item * cut.parts.d, parts = beyond < 0 ? 1 : cut.parts.d;
+  const int at_item = beyond < 0 ? (int)blockIdx.x : cut.n_full + shared_item, e = cut.heads.div(at_item), head = at_item - e * cut.heads.d;
 
   // ---- set-up: barriers, TMEM, and the item.  Items are counted through the sequences, and taken from the end: of a causal chunk the
   // last rows see most.
   if (warp == 0) {
     wait_for_grid();
-    const int want = n_items - 1 - e;
-    int before = 0, seq = -1, tile = 0;
-    for (int b0 = 0; b0 < a.bt.n_seqs && seq < 0; b0 += 32) {
-      const int b = b0 + lane;
-      int n = 0;
-      if (b < a.bt.n_seqs) {
-        const int st = __ldg(a.bt.starts + b), en = min(__ldg(a.bt.starts + b + 1), a.bt.n_tokens);
-        if (st >= 0 && en > st) n = (int)(((long long)(en - st) * a.group.d + kItemRows - 1) / kItemRows);
-      }
-      int incl = n;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int up = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += up;
-      }
-      const unsigned behind = __ballot_sync(0xffffffffu, before + incl > want);
-      if (behind) {
-        const int src = __ffs(behind) - 1;
-        seq = b0 + src;
-        tile = want - before - (__shfl_sync(0xffffffffu, incl - n, src));
-      }
-      before += __shfl_sync(0xffffffffu, incl, 31);
-    }
+    int seq, tile;
+    find_item(a, cut.n_items - 1 - e, seq, tile);
     if (lane == 0) {
       int start = 0, n_new = 0, length = 0;
       if (seq >= 0) {
@@ -232,7 +247,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   const int lo_tile = lo_all >> 7, hi_tile = max((hi_all + 127) >> 7, lo_tile);
   const int sink_tiles = min((min(n_sink, hi_all) + 127) >> 7, lo_tile);
   const int n_tiles = sink_tiles + hi_tile - lo_tile;
-  const int lo = (int)((long long)n_tiles * blockIdx.y / gridDim.y), nt = (int)((long long)n_tiles * (blockIdx.y + 1) / gridDim.y) - lo;
+  const int lo = (int)((long long)n_tiles * part / parts), nt = (int)((long long)n_tiles * (part + 1) / parts) - lo;
   auto key_of = [&](int i) { i += lo; return (i < sink_tiles ? i : i - sink_tiles + lo_tile) << 7; };     // first position of key tile i of this CTA
   const bool shared = !pair && nt > 1;
   auto n_steps = [&](int qt) { return shared ? (nt + 1 - qt) >> 1 : (pair || qt == 0 ? nt : 0); };
@@ -632,13 +647,13 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     const bool mine = i_own < all && rows > 0;
     const int g = i_own - a.group.div(max(i_own, 0)) * a.group.d;
     const int h = head * a.group.d + g;
-    const size_t all_rows = (size_t)a.bt.n_tokens * a.n_heads, out_row = mine ? (size_t)(start + t_own) * a.n_heads + h : 0;
-    const bool split = gridDim.y > 1;
-    const size_t part = (size_t)blockIdx.y * all_rows + out_row;
+    const size_t out_row = mine ? (size_t)(start + t_own) * a.n_heads + h : 0;
+    const bool split = parts > 1;
+    const size_t part_row = ((size_t)shared_item * parts + part) * kItemRows + (tile_row0 - row0) + row;
     auto put = [&](float *o, int col0, float f) {          // 32 columns of this row
       if (!mine) return;
       if (split) {
-        float4 *to = reinterpret_cast<float4 *>(a.part_o + part * D + col0);
+        float4 *to = reinterpret_cast<float4 *>(a.part_o + part_row * D + col0);
 #pragma unroll
         for (int i = 0; i < 8; ++i) to[i] = make_float4(o[4 * i] * f, o[4 * i + 1] * f, o[4 * i + 2] * f, o[4 * i + 3] * f);
       } else {
@@ -651,7 +666,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     };
     auto put_sums = [&](float mr, float lr) {
       if (!mine) return;
-      if (split) *reinterpret_cast<float2 *>(a.part_ml + part * 2) = make_float2(lr == 0.f ? -INFINITY : mr, lr);
+      if (split) *reinterpret_cast<float2 *>(a.part_ml + part_row * 2) = make_float2(lr == 0.f ? -INFINITY : mr, lr);
       else if (a.lse != nullptr) a.lse[out_row] = lr == 0.f ? -INFINITY : (mr + log2f(lr)) * kLn2;
     };
     if (rows > 0 && ok && !shared && (pair || qt == 0)) {
@@ -706,6 +721,48 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
   }
+}
+
+// O = sum_e 2^(m_e - M) O_e / sum_e 2^(m_e - M) l_e, M the largest reference, of the items that several CTAs share: a warp to each row.
+constexpr int kJoinRows = 8;
+template <int D>
+__global__ void __launch_bounds__(32 * kJoinRows) paged_join_kernel(const __grid_constant__ AttendArgs a, const Cut cut) {
+  constexpr int kPer = D / 32, kBlocks = kItemRows / kJoinRows;
+  const int lane = threadIdx.x & 31, r = blockIdx.x % kBlocks * kJoinRows + (threadIdx.x >> 5), shared_item = blockIdx.x / kBlocks, parts = cut.parts.d;
+  const int at_item = cut.n_full + shared_item, e0 = cut.heads.div(at_item), head = at_item - e0 * cut.heads.d;
+  wait_for_grid();
+  next_grid();
+  const size_t row0 = (size_t)shared_item * parts * kItemRows + r;
+  float m = -INFINITY;
+  for (int e = lane; e < parts; e += 32) m = fmaxf(m, __ldg(a.part_ml + (row0 + (size_t)e * kItemRows) * 2));
+  int seq, tile;
+  find_item(a, cut.n_items - 1 - e0, seq, tile);
+  if (seq < 0) return;
+  const int start = __ldg(a.bt.starts + seq), all = (min(__ldg(a.bt.starts + seq + 1), a.bt.n_tokens) - start) * a.group.d, i = tile * kItemRows + r;
+  if (i >= all) return;
+  float sum = 0.f, acc[kPer];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+#pragma unroll
+  for (int c = 0; c < kPer; ++c) acc[c] = 0.f;
+#pragma unroll 8
+  for (int e = 0; e < parts; ++e) {
+    const size_t at = row0 + (size_t)e * kItemRows;
+    const float2 ml = __ldg(reinterpret_cast<const float2 *>(a.part_ml + at * 2));
+    const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - m);
+    sum += f * ml.y;
+    float v[kPer];
+    if constexpr (kPer == 4) *reinterpret_cast<float4 *>(v) = __ldg(reinterpret_cast<const float4 *>(a.part_o + at * D + lane * kPer));
+    else *reinterpret_cast<float2 *>(v) = __ldg(reinterpret_cast<const float2 *>(a.part_o + at * D + lane * kPer));
+#pragma unroll
+    for (int c = 0; c < kPer; ++c) acc[c] += f * v[c];
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const int t = a.group.div(i), h = head * a.group.d + i - t * a.group.d;
+  char *out = a.O.ptr + (start + t) * a.O.st + h * a.O.sh + lane * kPer * 2;
+#pragma unroll
+  for (int c = 0; c < kPer; c += 2) *reinterpret_cast<uint32_t *>(out + c * 2) = pack_bf16(acc[c] * inv, acc[c + 1] * inv);
+  if (lane == 0 && a.lse != nullptr) a.lse[(size_t)(start + t) * a.n_heads + h] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * kLn2;
 }
 
 // The tensor maps of a pool's rows, made once.
