@@ -567,7 +567,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       }
       // ---- chunk by chunk, from the raw products in columns 32 cc .. (P covers columns below 16 cc only): tiles of which some rows see a part, and what is
       // left of a tile once an exponent has left the band.  Where one is more than 2^8 above a row's reference, the references of all the warp's rows rise
-      // to their chunk's largest, and what was accumulated under the old one is multiplied by f = 2^(old - new): the sum, P of the chunks that the
+      // to their chunk's largest or just above, and what was accumulated under the old one is multiplied by f = 2^(old - new): the sum, P of the chunks that the
       // tensor core has not been given yet, and O, once the last product given to it has landed.
       // (One loop for both, not unrolled: the roles' loops together have to stay in the SM's instruction cache.  With a masked copy of the sweep above and a copy of
       // the raise in each of its chunks a step in codes, which has the converters' loop beside it, missed it 28 times in a hundred: 2 255 us for what is 1 247.)
@@ -592,7 +592,8 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             top = max3(top, x[i], x[i + 1]);
           }
           if (__any_sync(0xffffffffu, top > m + 8.f)) {
-            const float raised = fmaxf(m, top), f = ex2(m - raised);
+            // (to a whole number, so that f is a power of two and P, scaled, is not rounded again)
+            const float raised = fmaxf(m, ceilf(top)), f = __uint_as_float((uint32_t)(max((int)(m - raised), -127) + 127) << 23);
             m = raised;
             l *= f;
             const bool late = cc >= kEarly;

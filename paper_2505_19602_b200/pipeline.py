@@ -192,3 +192,77 @@ def pass_work(wl: synth.Workload, budgets, windows, recent=False, one_call_steps
                 hist = L
     out["per_scale_flop"] = per_scale_flop
     return out
+
+
+# ---- sequences of tokens beside the maps: captions in chunks, text token by token ----------------------------------------------
+class Sequences:
+    """Pages, lengths and tables of sequences that share a PagedKV's pool (binding.PagedKV): which page holds what is decided here,
+    on the host; the kernels read the tables.  A sequence's places [0, pages) of the table hold page ids, -1 where there is none."""
+
+    def __init__(self, n_pages, page_tokens, n_seqs, max_tokens):
+        self.page_tokens, self.n_seqs = page_tokens, n_seqs
+        self.free = list(range(n_pages - 1, -1, -1))
+        self.lengths = [0] * n_seqs
+        self.table = [[-1] * -(-max_tokens // page_tokens) for _ in range(n_seqs)]
+
+    def extend(self, new):
+        """new[b] tokens join sequence b: pages for them, and the lengths with them in.  Raises, and changes nothing, where pages run out."""
+        need = []
+        for b, n in enumerate(new):
+            last = -(-(self.lengths[b] + n) // self.page_tokens)
+            if last > len(self.table[b]):
+                raise ValueError(f"sequence {b} would outgrow its {len(self.table[b])} pages")
+            need += [(b, i) for i in range(last) if self.table[b][i] < 0 and i >= self.lengths[b] // self.page_tokens]
+        if len(need) > len(self.free):
+            raise MemoryError(f"{len(need)} pages needed, {len(self.free)} free")
+        for b, i in need:
+            self.table[b][i] = self.free.pop()
+        self.lengths = [length + n for length, n in zip(self.lengths, new)]
+
+    def trim(self, window, n_sink=0):
+        """Gives back the pages that a window with sinks hides from every token still to come."""
+        for b, length in enumerate(self.lengths):
+            for i in range(-(-n_sink // self.page_tokens), max(0, length - window + 1) // self.page_tokens):
+                if self.table[b][i] >= 0:
+                    self.free.append(self.table[b][i])
+                    self.table[b][i] = -1
+
+    def drop(self, b):
+        """Ends sequence b: its pages are free, its length 0."""
+        self.free += [p for p in self.table[b] if p >= 0]
+        self.table[b] = [-1] * len(self.table[b])
+        self.lengths[b] = 0
+
+    def batch(self, new, device=0):
+        """The descriptor of a step whose new tokens extend() has let in: one for all layers."""
+        dev = dict(dtype=torch.int32, device=f"cuda:{device}")
+        starts = [sum(new[:b]) for b in range(len(new) + 1)]
+        return binding.PagedBatch(torch.tensor(self.table, **dev), torch.tensor(self.lengths, **dev), torch.tensor(starts, **dev), sum(new),
+                                  max(new), max(self.lengths))
+
+
+def token_step(kv: binding.PagedKV, batch, rows, causal=True, window=0, n_sink=0):
+    """One step of every layer: the new tokens' rows join the cache, quantised if it holds codes, and their queries attend over it.
+    rows(layer) -> (Q, K, V) of the new tokens; returns the layers' outputs."""
+    out = []
+    for l in range(kv.n_layers):
+        Q, K, V = rows(l)
+        kv.scalekv_paged_write(l, batch, K, V)
+        out.append(kv.scalekv_paged_attend(l, batch, Q, causal=causal, window=window, n_sink=n_sink))
+    return out
+
+
+def prompts_and_tokens(kv: binding.PagedKV, seqs: Sequences, prompts, n_tokens, chunk, rows, window=0, n_sink=0):
+    """Continuous batching: sequence b brings a prompt of prompts[b] tokens, at most `chunk` of them a step, and then n_tokens
+    tokens one by one, whatever the others are doing; pages behind a window are given back as it moves on.
+    rows(layer, counts, positions) -> (Q, K, V): counts[b] tokens of sequence b from its position positions[b] on.  Yields each
+    step's (counts, positions, outputs of the layers)."""
+    total = [p + n_tokens for p in prompts]
+    while any(length < t for length, t in zip(seqs.lengths, total)):
+        at = list(seqs.lengths)
+        new = [min(chunk, p - a) if a < p else min(1, t - a) for a, p, t in zip(at, prompts, total)]
+        seqs.extend(new)
+        batch = seqs.batch(new, kv.device_index)
+        yield new, at, token_step(kv, batch, lambda l: rows(l, new, at), window=window, n_sink=n_sink)
+        if window:
+            seqs.trim(window, n_sink)
