@@ -341,42 +341,41 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       }
       next_grid();
     } else if (warp == 1 && rows > 0) {
-      // -------------------------------------------------------------- TMA producer (the whole warp walks, one elected lane issues)
-      // Ring tile t holds K (even) or V (odd) of key tile t / 2, which bRaw (codes) or bFull says.  A tile's holes go with its K.
+      // -------------------------------------------------------------- TMA producer (a lane to each box of rows of a page)
+      // Ring tile t holds K (even) or V (odd) of key tile t / 2, which bRaw (codes) or bFull says.  A tile's holes go with its K.  (One lane that issued all boxes,
+      // one after the other, needed 245 cycles for each: with pages of 16 tokens that was the larger part of a step.)
       const int box = min(1 << s.page_shift, kTileKeys), in_page = (1 << s.page_shift) - 1;
       constexpr int kLanded = kQ8 ? Y::bRaw : Y::bFull;
       constexpr uint32_t kRowBytes = D * (kQ8 ? 1 : 2);
-      int page = pages(0), page_next = pages(1), t = 0;
+      const int r0 = lane * box;
+      const uint32_t groups = ((1u << (box >> 4)) - 1u) << ((r0 >> 4) & 31);      // of this lane's box
+      int page = pages(0), page_next = pages(1), page_after = pages(2), t = 0;
       bool ok = true;
       for (; t < 2 * nt; ++t) {
         const int st = t % kStages, key0 = key_of(t >> 1);
+        const uint32_t there = __ballot_sync(0xffffffffu, page >= 0) & 0xffu, used = __ballot_sync(0xffffffffu, group_in_use(t >> 1)) & 0xffu;
+        // a box is loaded if one of its groups in use has a page (they share it)
+        const uint32_t mine = r0 < kTileKeys ? there & groups : 0u, boxes = __popc(__ballot_sync(0xffffffffu, mine != 0));
+        const int pg = __shfl_sync(0xffffffffu, page, max(__ffs(mine) - 1, 0));
         ok = mbar_wait_warp(bar(Y::bEmpty + st), ((t / kStages) & 1) ^ 1, abort_flag, status);
         if (!ok) break;
-        const uint32_t there = __ballot_sync(0xffffffffu, page >= 0) & 0xffu, used = __ballot_sync(0xffffffffu, group_in_use(t >> 1)) & 0xffu;
-        if (!(t & 1) && lane == 0)
-          asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + Y::kOffHoles + ((t >> 1) % kScaleSlots) * 4), "r"(used & ~there) : "memory");
-        // boxes whose first group in use has a page (the groups of a box share it)
-        const CUtensorMap *tm = (t & 1) ? &tmV : &tmK;
-        uint32_t boxes = 0;
-        for (int r0 = 0; r0 < kTileKeys; r0 += box)
-          if ((there >> (r0 >> 4)) & ((1u << (box >> 4)) - 1u)) ++boxes;
-        if (elect_one()) mbar_expect_tx(bar(kLanded + st), boxes * box * kRowBytes);
-        __syncwarp();
-        for (int r0 = 0; r0 < kTileKeys; r0 += box) {
-          const uint32_t mine = (there >> (r0 >> 4)) & ((1u << (box >> 4)) - 1u);
-          if (!mine) continue;
-          const int pg = __shfl_sync(0xffffffffu, page, (r0 >> 4) + __ffs(mine) - 1);
-          if (elect_one()) {
-            const int y = (head << s.page_shift) + ((key0 + r0) & in_page), z = page0 + pg;
-            const uint32_t dst = base + Y::kOffRing + st * kTile + (kQ8 ? kTile - 128 * D : 0u) + r0 * (kQ8 ? D : 128);
-            tma_load_3d(dst, tm, 0, y, z, bar(kLanded + st));
-            if constexpr (!kQ8 && D == 128) tma_load_3d(dst + kHalf, tm, 64, y, z, bar(kLanded + st));
-          }
-          __syncwarp();
+        if (lane == 0) {
+          if (!(t & 1)) asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + Y::kOffHoles + ((t >> 1) % kScaleSlots) * 4), "r"(used & ~there) : "memory");
+          mbar_expect_tx(bar(kLanded + st), boxes * box * kRowBytes);
         }
+        __syncwarp();
+        if (mine) {
+          const CUtensorMap *tm = (t & 1) ? &tmV : &tmK;
+          const int y = (head << s.page_shift) + ((key0 + r0) & in_page), z = page0 + pg;
+          const uint32_t dst = base + Y::kOffRing + st * kTile + (kQ8 ? kTile - 128 * D : 0u) + r0 * (kQ8 ? D : 128);
+          tma_load_3d(dst, tm, 0, y, z, bar(kLanded + st));
+          if constexpr (!kQ8 && D == 128) tma_load_3d(dst + kHalf, tm, 64, y, z, bar(kLanded + st));
+        }
+        __syncwarp();
         if (t & 1) {
           page = page_next;
-          page_next = pages((t >> 1) + 2);
+          page_next = page_after;
+          page_after = pages((t >> 1) + 3);
         }
       }
       if (!ok) {
