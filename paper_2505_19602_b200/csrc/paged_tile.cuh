@@ -35,7 +35,6 @@ constexpr int kItemRows = 256;
 constexpr int kTileKeys = 128;
 constexpr int kSweepChunks = 4;
 constexpr int kEarly = 3;                         // chunks whose part of the PV product is issued under the rest of the sweep
-constexpr int kScaleSlots = 4;                    // key tiles whose scales are held (see the loaders)
 
 template <int D, bool kQ8>
 struct TileLayout {
@@ -43,11 +42,15 @@ struct TileLayout {
   // registers of a thread of the first warpgroup, of the converters, of softmax: shares of what the block was launched with
   static constexpr int kRegs0 = kQ8 ? 56 : 72, kRegs1 = 104, kRegsS = kQ8 ? 176 : 216, kRegsLaunch = kQ8 ? 128 : 168;
   static_assert(kRegs0 + (kQ8 ? kRegs1 : 0) + 2 * kRegsS <= kRegsLaunch * (kThreads / 128), "a share would wait for registers that nobody returns");
-  static constexpr int kStages = kQ8 ? 4 : 5;
+  static constexpr int kStages = D == 64 ? (kQ8 ? 6 : 8) : (kQ8 ? 4 : 5);
+  // Key tiles whose scales and holes are held.  Tile i + kSlots writes over tile i's when the stage of its K is free, which is when ring tile
+  // 2 (i + kSlots) - kStages has been read: K of tile i + 2 or later (or V of i + 1 or later), whose product is issued behind the P of tile i.
+  static constexpr int kSlots = D == 64 ? 8 : 4;
+  static_assert(2 * kSlots - kStages >= 3, "tile i's scales may still be read");
   static constexpr uint32_t kTile = 128 * D * 2, kHalf = 128 * 128;      // an operand tile; 64 columns of it: one 128-byte swizzle span
   static constexpr uint32_t kOffQ = 0, kOffRing = 2 * kTile, kOffScale = kOffRing + kStages * kTile;
-  static constexpr uint32_t kOffHoles = kOffScale + (kQ8 ? kScaleSlots * 2 * 512 : 0);
-  static constexpr uint32_t kOffBar = kOffHoles + kScaleSlots * 4;
+  static constexpr uint32_t kOffHoles = kOffScale + (kQ8 ? kSlots * 2 * 512 : 0);
+  static constexpr uint32_t kOffBar = kOffHoles + kSlots * 4;
   enum { bQFull = 0, bFull = 2, bEmpty = bFull + kStages, bSFull = bEmpty + kStages, bPFull = bSFull + 2, bPvDone = bPFull + 2,
          bFinal = bPvDone + 2, bPEarly = bFinal + 2, bPvEarly = bPEarly + 2, bRaw = bPvEarly + 2, bCount = bRaw + (kQ8 ? kStages : 0) };
   static_assert(bCount <= 32, "one lane of a warp initialises each barrier");
@@ -280,7 +283,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       auto clean = [&](int vt) {
         const int key0 = key_of(vt >> 1);
         uint32_t holes;
-        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(holes) : "r"(base + Y::kOffHoles + ((vt >> 1) % kScaleSlots) * 4));
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(holes) : "r"(base + Y::kOffHoles + ((vt >> 1) % Y::kSlots) * 4));
         if (key0 >= lo_all && key0 + kTileKeys <= hi_all && holes == 0) return;
         const uint32_t tile = base + Y::kOffRing + (vt % kStages) * kTile;
         for (int r = lane; r < kTileKeys; r += 32) {
@@ -351,31 +354,33 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       const uint32_t groups = ((1u << (box >> 4)) - 1u) << ((r0 >> 4) & 31);      // of this lane's box
       int page = pages(0), page_next = pages(1), page_after = pages(2), t = 0;
       bool ok = true;
-      for (; t < 2 * nt; ++t) {
-        const int st = t % kStages, key0 = key_of(t >> 1);
-        const uint32_t there = __ballot_sync(0xffffffffu, page >= 0) & 0xffu, used = __ballot_sync(0xffffffffu, group_in_use(t >> 1)) & 0xffu;
+      for (int i = 0; i < nt && ok; ++i) {
+        const int key0 = key_of(i);
+        const uint32_t there = __ballot_sync(0xffffffffu, page >= 0) & 0xffu, used = __ballot_sync(0xffffffffu, group_in_use(i)) & 0xffu;
         // a box is loaded if one of its groups in use has a page (they share it)
-        const uint32_t mine = r0 < kTileKeys ? there & groups : 0u, boxes = __popc(__ballot_sync(0xffffffffu, mine != 0));
+        const uint32_t mine = r0 < kTileKeys ? there & groups : 0u, bytes = __popc(__ballot_sync(0xffffffffu, mine != 0)) * box * kRowBytes;
         const int pg = __shfl_sync(0xffffffffu, page, max(__ffs(mine) - 1, 0));
-        ok = mbar_wait_warp(bar(Y::bEmpty + st), ((t / kStages) & 1) ^ 1, abort_flag, status);
-        if (!ok) break;
-        if (lane == 0) {
-          if (!(t & 1)) asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + Y::kOffHoles + ((t >> 1) % kScaleSlots) * 4), "r"(used & ~there) : "memory");
-          mbar_expect_tx(bar(kLanded + st), boxes * box * kRowBytes);
-        }
-        __syncwarp();
-        if (mine) {
-          const CUtensorMap *tm = (t & 1) ? &tmV : &tmK;
-          const int y = (head << s.page_shift) + ((key0 + r0) & in_page), z = page0 + pg;
-          const uint32_t dst = base + Y::kOffRing + st * kTile + (kQ8 ? kTile - 128 * D : 0u) + r0 * (kQ8 ? D : 128);
-          tma_load_3d(dst, tm, 0, y, z, bar(kLanded + st));
-          if constexpr (!kQ8 && D == 128) tma_load_3d(dst + kHalf, tm, 64, y, z, bar(kLanded + st));
-        }
-        __syncwarp();
-        if (t & 1) {
-          page = page_next;
-          page_next = page_after;
-          page_after = pages((t >> 1) + 3);
+        const int y = (head << s.page_shift) + ((key0 + r0) & in_page), z = page0 + pg;
+        page = page_next;
+        page_next = page_after;
+        page_after = pages(i + 3);
+#pragma unroll
+        for (int v = 0; v < 2; ++v, ++t) {
+          const int st = t % kStages;
+          ok = mbar_wait_warp(bar(Y::bEmpty + st), ((t / kStages) & 1) ^ 1, abort_flag, status);
+          if (!ok) break;
+          if (lane == 0) {
+            if (v == 0) asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + Y::kOffHoles + (i % Y::kSlots) * 4), "r"(used & ~there) : "memory");
+            mbar_expect_tx(bar(kLanded + st), bytes);
+          }
+          __syncwarp();
+          if (mine) {
+            const CUtensorMap *tm = v ? &tmV : &tmK;
+            const uint32_t dst = base + Y::kOffRing + st * kTile + (kQ8 ? kTile - 128 * D : 0u) + r0 * (kQ8 ? D : 128);
+            tma_load_3d(dst, tm, 0, y, z, bar(kLanded + st));
+            if constexpr (!kQ8 && D == 128) tma_load_3d(dst + kHalf, tm, 64, y, z, bar(kLanded + st));
+          }
+          __syncwarp();
         }
       }
       if (!ok) {
@@ -389,7 +394,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   } else if (kQ8 && warp < 8) {
     registers_down<Y::kRegs1>();
     // ---------------------------------------------------------------- converters
-    // The scales of both go with K, into slot (t / 2) mod kScaleSlots; that slot's last readers are done: the stage of this K was
+    // The scales of both go with K, into slot (t / 2) mod Y::kSlots; that slot's last readers are done: the stage of this K was
     // released behind a product that was issued after their P.
     const int piece = tid & 3, sub = tid >> 2;      // 16 codes a piece, 64 columns at a time
     float k_scale = 0.f, v_scale = 0.f;
@@ -407,7 +412,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       ok = mbar_wait_warp(bar(Y::bRaw + t % kStages), (t / kStages) & 1, abort_flag, status);
       if (!ok) break;
       if (!(t & 1)) {
-        const uint32_t at = base + Y::kOffScale + ((t >> 1) % kScaleSlots) * 1024 + tid * 4;
+        const uint32_t at = base + Y::kOffScale + ((t >> 1) % Y::kSlots) * 1024 + tid * 4;
         asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(k_scale) : "memory");
         asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 512), "f"(v_scale) : "memory");
         if ((t >> 1) + 1 < nt) fetch_scales((t >> 1) + 1);
@@ -483,8 +488,8 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       if (!ok) break;
       tc_fence_after();
       uint32_t holes;
-      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(holes) : "r"(base + Y::kOffHoles + (i_tile % kScaleSlots) * 4));
-      const uint32_t scales = base + Y::kOffScale + (i_tile % kScaleSlots) * 1024;       // K's, 512 bytes further V's
+      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(holes) : "r"(base + Y::kOffHoles + (i_tile % Y::kSlots) * 4));
+      const uint32_t scales = base + Y::kOffScale + (i_tile % Y::kSlots) * 1024;       // K's, 512 bytes further V's
       auto hand_over = [&](int which) {
         tc_wait_st();
         tc_fence_before();
