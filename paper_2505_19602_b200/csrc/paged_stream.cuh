@@ -14,8 +14,8 @@
 //   - P is transposed from where the first product leaves it to where the second wants it by movmatrix.
 //   - V's pairs of keys are interleaved from two rows' pieces, and its dims are dealt to the m-tiles so that those are 16 bytes long, too.
 //   - Pieces are placed in a stage so that eight lanes' loads meet all banks, K's (two rows, four pieces) and V's (four rows, two pieces).
-//   - Codes become bf16 exactly (codes_bf16).  The key's scale multiplies the product, the value's scale multiplies P, both in fp32; P is rounded to bf16
-//     for its product with V, as it is where rows are bf16.
+//   - Codes become bf16 exactly (codes_bf16).  The key's scale multiplies the product, the value's scale multiplies P, both in fp32; P goes into its
+//     product in two pieces of bf16.
 // The running maximum of a row is raised when a step exceeds it by more than 2^3, and the sums with it: P stays below 2^8.
 // A CTA's four warps take the steps in turn and are combined in shared memory.  Where a sequence's heads are few, gridDim.z CTAs share its
 // keys; each leaves its part in the workspace, and the last one to do so, by a counter that it sets back, combines them in their order.
@@ -367,7 +367,9 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
           for (int i = 0; i < D / 16; ++i) { o[i][n][e] *= f; o[i][n][2 + e] *= f; }
         }
     }
-    uint32_t p[kN][2];
+    // P in two pieces, what bf16 has of it and what it leaves: rounded once, it would put as much error into a row of O as O's own rounding does, and the
+    // products cost little beside the loads
+    uint32_t p[kN][2], rest[kN][2];
 #pragma unroll
     for (int n = 0; n < kN; ++n) {
 #pragma unroll
@@ -381,8 +383,12 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
         for (int e = 0; e < 4; ++e)
           if ((hidden >> (4 * n + e)) & 1u) y[e] = 0.f;
       }
-      p[n][0] = transpose_8x8(pair_bf16(y[0], y[1]));
-      p[n][1] = transpose_8x8(pair_bf16(y[2], y[3]));
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t most = pair_bf16(y[2 * i], y[2 * i + 1]);
+        p[n][i] = transpose_8x8(most);
+        rest[n][i] = transpose_8x8(pair_bf16(y[2 * i] - __uint_as_float(most << 16), y[2 * i + 1] - __uint_as_float(most & 0xffff0000u)));
+      }
     }
     // O^T += V^T P^T
 #pragma unroll
@@ -408,6 +414,8 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
           for (int n = 0; n < kN; ++n) {
             mma_16816(o[2 * w][n], f0, p[n][0], p[n][1]);
             mma_16816(o[2 * w + 1][n], f1, p[n][0], p[n][1]);
+            mma_16816(o[2 * w][n], f0, rest[n][0], rest[n][1]);
+            mma_16816(o[2 * w + 1][n], f1, rest[n][0], rest[n][1]);
           }
         }
       } else {
@@ -416,7 +424,10 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
           const uint32_t c0 = word(v[0], w), c1 = word(v[1], w), c2 = word(v[2], w), c3 = word(v[3], w);
           const uint32_t f[4] = {__byte_perm(c0, c1, 0x5410), __byte_perm(c0, c1, 0x7632), __byte_perm(c2, c3, 0x5410), __byte_perm(c2, c3, 0x7632)};
 #pragma unroll
-          for (int n = 0; n < kN; ++n) mma_16816(o[4 * i + w][n], f, p[n][0], p[n][1]);
+          for (int n = 0; n < kN; ++n) {
+            mma_16816(o[4 * i + w][n], f, p[n][0], p[n][1]);
+            mma_16816(o[4 * i + w][n], f, rest[n][0], rest[n][1]);
+          }
         }
       }
     }
