@@ -141,9 +141,9 @@ void launch_store(Moves &mv, int n_sm, cudaStream_t stream) {
 }
 
 template <int D, bool kQ8, int kN>
-scalekv_status launch_stream(scalekv_paged *c, const AttendArgs &a, long long keys, cudaStream_t stream) {
+scalekv_status launch_stream(scalekv_paged *c, const AttendArgs &a, int tiles, long long keys, cudaStream_t stream) {
   using Y = StreamLayout<D, kQ8, kN>;
-  const long long items = (long long)a.bt.n_seqs * a.s.heads, slots = (long long)c->n_sm * Y::kCtas, steps = (keys + 15) / 16;
+  const long long items = (long long)a.bt.n_seqs * a.s.heads * tiles, slots = (long long)c->n_sm * Y::kCtas, steps = (keys + 15) / 16;
   const long long room = std::min<long long>(kPartRows / ((long long)a.bt.n_tokens * a.n_heads), Y::kMostParts);      // parts that the workspace holds
   // CTAs that share a sequence's keys: one for every SM, down to two steps of 16 keys for each of its warps; two where that leaves them four; as many as
   // fit where it leaves them 16.  (us, one sequence with 8 kv heads in codes, 4 / 8 / 16 / 32 / 74 CTAs a head: 1 999 entries 12.8 / 10.3 / 8.6 / 10.6 / 18.5, 8 000
@@ -155,24 +155,20 @@ scalekv_status launch_stream(scalekv_paged *c, const AttendArgs &a, long long ke
   // Sequences of different lengths have their parts dealt out on the device, where that gives a CTA 64 steps or more.
   const bool by_length = a.bt.n_seqs > 1 && a.bt.n_seqs <= 512 && items <= std::min<long long>(kMaxCounts, 3 * slots) && room >= 3 && items * steps >= slots * 64;
   if (items > kMaxCounts) split = 1;
-  if (cudaFuncSetAttribute(paged_stream_kernel<D, kQ8, kN>, cudaFuncAttributeMaxDynamicSharedMemorySize, Y::kSmem) != cudaSuccess)
-    return fail(c, SCALEKV_ERR_CUDA, "cannot raise the dynamic shared memory limit");
-  launch(paged_stream_kernel<D, kQ8, kN>, by_length ? dim3((unsigned)slots) : dim3(a.bt.n_seqs, a.s.heads, (unsigned)split), kStreamThreads, Y::kSmem, stream, a,
-         by_length ? (int)room : 0);
+  launch(paged_stream_kernel<D, kQ8, kN>, by_length ? dim3((unsigned)slots) : dim3(a.bt.n_seqs, a.s.heads * tiles, (unsigned)split), kStreamThreads, Y::kSmem, stream,
+         a, by_length ? (int)room : 0, tiles);
   return launched(c, "paged_attend");
 }
 
 template <int D, bool kQ8>
 scalekv_status launch_tile(scalekv_paged *c, int layer, const AttendArgs &a, int items, long long keys, cudaStream_t stream) {
   using Y = TileLayout<D, kQ8>;
-  if (cudaFuncSetAttribute(paged_tile_kernel<D, kQ8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Y::kSmem) != cudaSuccess)
-    return fail(c, SCALEKV_ERR_CUDA, "cannot raise the dynamic shared memory limit");
   // An item and kv head to a CTA.  Those that do not fill the SMs, and those of the last, partial wave, are shared by as many CTAs as find one, each with four
   // key tiles or more: XXXT.
   const int n = items * a.s.heads, sms = (int)std::min<long long>(c->n_sm, kPartRows / kItemRows), last = n % sms;
   const long long tiles = (keys + kTileKeys - 1) / kTileKeys;
   int parts = last ? (int)std::min<long long>(sms / last, tiles / 2) : 1;
-  if (n > sms && tiles < 24) parts = 1;
+  if (n > sms && tiles < 16) parts = 1;
   const int n_full = parts > 1 ? n - last : n;
   const Cut cut = {Divisor::of(a.s.heads), Divisor::of(std::max(parts, 1)), items, n_full};
   launch(paged_tile_kernel<D, kQ8>, dim3((unsigned)(n_full + (n - n_full) * parts)), Y::kThreads, Y::kSmem, stream, c->maps.k, c->maps.v, a, cut,
@@ -181,6 +177,14 @@ scalekv_status launch_tile(scalekv_paged *c, int layer, const AttendArgs &a, int
   if (n_full == n) return SCALEKV_OK;
   launch(paged_join_kernel<D>, dim3((unsigned)((n - n_full) * (kItemRows / kJoinRows))), 32 * kJoinRows, 0, stream, a, cut);
   return launched(c, "paged_join");
+}
+
+// Lets the attention kernels of a handle have the shared memory they ask for.
+template <int D, bool kQ8>
+bool room_for_attend() {
+  auto ask = [](auto kernel, size_t bytes) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess; };
+  return ask(paged_stream_kernel<D, kQ8, 1>, StreamLayout<D, kQ8, 1>::kSmem) && ask(paged_stream_kernel<D, kQ8, 2>, StreamLayout<D, kQ8, 2>::kSmem) &&
+         ask(paged_tile_kernel<D, kQ8>, TileLayout<D, kQ8>::kSmem);
 }
 
 template <bool kWrite>
@@ -253,6 +257,13 @@ scalekv_status scalekv_paged_init(const scalekv_paged_config *cfg, scalekv_paged
     delete c;
     return SCALEKV_ERR_CUDA;
   }
+  const bool q8 = cfg->store == SCALEKV_STORE_Q8;
+  if (!(cfg->head_dim == 128 ? (q8 ? room_for_attend<128, true>() : room_for_attend<128, false>()) : (q8 ? room_for_attend<64, true>() : room_for_attend<64, false>()))) {
+    fprintf(stderr, "scalekv_paged_init: cannot raise the dynamic shared memory limit\n");
+    cudaGetLastError();
+    delete c;
+    return SCALEKV_ERR_CUDA;
+  }
   if (!c->maps.make(cfg->pool, static_cast<char *>(cfg->pool) + y.rows_bytes, (long long)cfg->n_layers * cfg->n_pages, cfg->n_kv_heads, cfg->page_tokens,
                     cfg->head_dim, cfg->store == SCALEKV_STORE_Q8, err)) {
     fprintf(stderr, "scalekv_paged_init: %s\n", err.c_str());
@@ -296,7 +307,7 @@ scalekv_status scalekv_paged_attend(scalekv_paged *kv, int32_t layer, const scal
   const int G = n_heads / H;
   const long long max_rows = (long long)std::min(batch->max_new, a.bt.n_tokens) * G;      // query rows of a sequence and kv head
   if (all_rows > kMaxLength) return fail(c, SCALEKV_ERR_UNSUPPORTED, "more than 2^30 query rows in a call");
-  if (H > 65535) return fail(c, SCALEKV_ERR_UNSUPPORTED, "more than 65535 kv heads");
+  if (H > 32767) return fail(c, SCALEKV_ERR_UNSUPPORTED, "more than 32767 kv heads");
   a.s = layer_store(c, layer);
   a.Q = view(Q, 2); a.O = view(O, 2);
   a.lse = lse;
@@ -316,7 +327,8 @@ scalekv_status scalekv_paged_attend(scalekv_paged *kv, int32_t layer, const scal
     auto go = [&](auto dim, auto codes) {
       constexpr int kD = decltype(dim)::value;
       constexpr bool kQ8 = decltype(codes)::value;
-      return max_rows <= 8 ? launch_stream<kD, kQ8, 1>(c, a, keys, st) : launch_stream<kD, kQ8, 2>(c, a, keys, st);
+      const int row_tiles = (int)((max_rows + kTileRows - 1) / kTileRows);
+      return max_rows <= 8 ? launch_stream<kD, kQ8, 1>(c, a, 1, keys, st) : launch_stream<kD, kQ8, 2>(c, a, row_tiles, keys, st);
     };
     using D64 = std::integral_constant<int, 64>;
     using D128 = std::integral_constant<int, 128>;

@@ -16,7 +16,7 @@
 //   - Pieces are placed in a stage so that eight lanes' loads meet all banks, K's (two rows, four pieces) and V's (four rows, two pieces).
 //   - Codes become bf16 exactly (codes_bf16).  The key's scale multiplies the product, the value's scale multiplies P, both in fp32; P goes into its
 //     product in two pieces of bf16.
-// The running maximum of a row is raised when a step exceeds it by more than 2^3, and the sums with it: P stays below 2^8.
+// The running maximum of a row is raised when a step exceeds it by more than 2^3, and the sums with it: P stays below that.
 // A CTA's four warps take the steps in turn and are combined in shared memory.  Where a sequence's heads are few, gridDim.z CTAs share its
 // keys; each leaves its part in the workspace, and the last one to do so, by a counter that it sets back, combines them in their order.
 #pragma once
@@ -29,7 +29,8 @@ namespace scalekv {
 namespace paged {
 
 constexpr int kStreamThreads = 128, kStreamWarps = kStreamThreads / 32;
-constexpr int kStreamRows = 16;                   // query rows of a sequence and kv head that go this way
+constexpr int kStreamRows = 32;                   // query rows of a sequence and kv head that go this way
+constexpr int kTileRows = 16;                     // of them a CTA takes so many, at most
 
 // kN: n-tiles of eight query rows
 template <int D, bool kQ8, int kN>
@@ -104,7 +105,7 @@ __device__ __forceinline__ void mma_16816(float *c, const uint32_t *a, uint32_t 
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// What a sequence has to do with a launch: its query rows of a kv head, and the keys that some of them sees, in steps of 16: the sinks' steps,
+// What a sequence has to do with a launch: its query rows of a kv head, and the keys that some of them see, in steps of 16: the sinks' steps,
 // then those of [lo, hi).
 struct Span {
   int start, rows, length, first, lo, hi, n_sink, lo_step, sink_steps, steps;
@@ -156,14 +157,14 @@ __device__ __forceinline__ void put_row(const AttendArgs &a, int t, int h, int p
 // columns, dealt to as many groups of threads as there are.  (One part after the other, three loads each, cost 0.2 us a part.)  A function of its own, so that
 // the streaming loop is compiled without it: inlined it made that 5 to 10 % longer.
 template <int D, int kRows>
-__device__ __noinline__ void join_parts(const AttendArgs &a, int start, int rows, int head, int parts, char *smem) {
+__device__ __noinline__ void join_parts(const AttendArgs &a, int start, int row0, int rows, int head, int parts, char *smem) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const size_t all_rows = (size_t)a.bt.n_tokens * a.n_heads;
   float2 *row_ml = reinterpret_cast<float2 *>(smem), *ml = row_ml + kRows;      // [row]; [row][part]
   for (int i = threadIdx.x; i < rows * parts; i += kStreamThreads) {
     const int r = i / parts;
     int t, h;
-    place_row(a, start, head, r, t, h);
+    place_row(a, start, head, row0 + r, t, h);
     ml[i] = __ldcg(reinterpret_cast<const float2 *>(a.part_ml + ((size_t)(i - r * parts) * all_rows + (size_t)t * a.n_heads + h) * 2));
   }
   __syncthreads();
@@ -189,7 +190,7 @@ __device__ __noinline__ void join_parts(const AttendArgs &a, int start, int rows
   for (int i = threadIdx.x; i < groups * pieces; i += kStreamThreads) {
     const int group = i / pieces, j = i - group * pieces, r = j / (D / 8), piece = j % (D / 8);
     int t, h;
-    place_row(a, start, head, r, t, h);
+    place_row(a, start, head, row0 + r, t, h);
     const float *columns = a.part_o + ((size_t)t * a.n_heads + h) * D + piece * 8;
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
@@ -217,22 +218,21 @@ __device__ __noinline__ void join_parts(const AttendArgs &a, int start, int rows
       acc[4] += hi.x; acc[5] += hi.y; acc[6] += hi.z; acc[7] += hi.w;
     }
     int t, h;
-    place_row(a, start, head, r, t, h);
+    place_row(a, start, head, row0 + r, t, h);
     put_row(a, t, h, piece, acc, row_ml[r]);
   }
   __syncthreads();                                         // (what was the ring may be one again)
 }
 
-// One part of a sequence and kv head: steps step_lo .. step_hi - 1 of it, as part number `part` of `parts`.  All threads of the CTA.
+// One part of rows row0 .. of a sequence and kv head (item: a number of their own): steps step_lo .. step_hi - 1 of it, as part number `part` of `parts`.  All threads of the CTA.
 template <int D, bool kQ8, int kN>
-__device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp, char *smem, int *shared_word, int seq, int head, int step_lo, int step_hi, int part,
-                                            int parts) {
+__device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp, char *smem, int *shared_word, int seq, int head, int row0, int item, int step_lo, int step_hi,
+                                            int part, int parts) {
   using Y = StreamLayout<D, kQ8, kN>;
   constexpr int kRowBytes = Y::kRowBytes, kStages = Y::kStages;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = lane & 3, oct = lane >> 2;
   const Store &s = a.s;
-  const int item = seq * s.heads + head, start = sp.start, rows = sp.rows, length = sp.length, first = sp.first, n_sink = sp.n_sink;
-  const int t_last = a.group.div(rows - 1);
+  const int start = sp.start, rows = min(sp.rows - row0, 8 * kN), length = sp.length, first = sp.first, n_sink = sp.n_sink;      // (rows row0 .. of the sequence's)
   auto in_use = [&](int pos) { return pos < sp.hi && (pos >= sp.lo || pos < n_sink); };
   auto key_of = [&](int step) { return (step < sp.sink_steps ? step : step - sp.sink_steps + sp.lo_step) << 4; };
   auto page_at = [&](int step) { return step < step_hi ? page_of(s, a.bt, seq, key_of(step)) : -1; };
@@ -270,7 +270,7 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
   uint2 q[kN][D / 16];
 #pragma unroll
   for (int n = 0; n < kN; ++n) {
-    const int r = n * 8 + oct, t = a.group.div(r), g = r - t * a.group.d;
+    const int r = n * 8 + oct, t = a.group.div(row0 + r), g = row0 + r - t * a.group.d;
     const char *row = a.Q.ptr + (start + t) * a.Q.st + (head * a.group.d + g) * a.Q.sh;
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
@@ -279,7 +279,7 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
     }
   }
   // a step all of whose keys every row sees: [lo_full, hi_full)
-  const int lo_full = seen_lo(a.mask, first + t_last), hi_full = seen_hi(a.mask, first, length);
+  const int lo_full = seen_lo(a.mask, first + a.group.div(row0 + rows - 1)), hi_full = seen_hi(a.mask, first + a.group.div(row0), length);
 
   // O^T: rows 2 quad, 2 quad + 1 of every n-tile; references and sums of those rows (the sum over this lane's keys)
   float o[D / 16][kN][4], m[kN][2], l[kN][2];
@@ -341,7 +341,7 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
       for (int n = 0; n < kN; ++n)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int t = first + a.group.div(min(n * 8 + 2 * quad + (e & 1), rows - 1)), pos = key0 + oct + 8 * (e >> 1);
+          const int t = first + a.group.div(row0 + min(n * 8 + 2 * quad + (e & 1), rows - 1)), pos = key0 + oct + 8 * (e >> 1);
           if (page < 0 || pos >= seen_hi(a.mask, t, length) || (pos < seen_lo(a.mask, t) && pos >= n_sink)) {
             x[n][e] = -INFINITY;
             hidden |= 1u << (4 * n + e);
@@ -456,7 +456,7 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
     }
   __syncthreads();
   const size_t all_rows = (size_t)a.bt.n_tokens * a.n_heads;
-  auto place = [&](int r, int &t, int &h) { place_row(a, start, head, r, t, h); };
+  auto place = [&](int r, int &t, int &h) { place_row(a, start, head, row0 + r, t, h); };
   for (int i = threadIdx.x; i < rows * (D / 8); i += kStreamThreads) {
     const int r = i / (D / 8), piece = i % (D / 8);
     float acc[8], top = -INFINITY, sum = 0.f;
@@ -500,11 +500,11 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
   __syncthreads();
   if (!last) return;
   __threadfence();
-  join_parts<D, 8 * kN>(a, sp.start, rows, head, parts, smem);
+  join_parts<D, 8 * kN>(a, start, row0, rows, head, parts, smem);
 }
 
 template <int D, bool kQ8, int kN>
-__global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8, kN>::kCtas) paged_stream_kernel(const __grid_constant__ AttendArgs a, int most_parts) {
+__global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8, kN>::kCtas) paged_stream_kernel(const __grid_constant__ AttendArgs a, int most_parts, int tiles) {
   using Y = StreamLayout<D, kQ8, kN>;
   extern __shared__ __align__(16) char smem[];
   __shared__ int shared_word;
@@ -514,10 +514,11 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8, kN>::kCta
   // each as there are CTAs for; or, where that would leave the longest ones' parts too long, the steps of all of them one behind the other and an equal share to
   // every CTA, which may begin and end within a sequence.  That costs a CTA a second beginning and end: kSecond steps.  (At least one step to whoever has
   // rows, so that it is met; no more than most_parts shares to a sequence and head.)
-  const int heads = a.s.heads;
+  // Rows beyond the first kTileRows are a CTA's of their own, as if they were another head; `tiles` of them to a kv head.
+  const int heads = a.s.heads * tiles, most_rows = tiles > 1 ? tiles * kTileRows : 8 * kN;
   auto weight = [&](int b, bool tell) {
     if (b >= a.bt.n_seqs) return 0;
-    const Span sp(a, b, 8 * kN, tell);
+    const Span sp(a, b, most_rows, tell);
     return sp.rows > 0 ? max(sp.steps, 1) : 0;
   };
   long long at = 0, end = 1;
@@ -575,7 +576,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8, kN>::kCta
       head = (int)at / split % heads;
       seq = (int)at / split / heads;
     }
-    const Span sp(a, seq, 8 * kN, most_parts == 0 && threadIdx.x == 0);
+    const Span sp(a, seq, most_rows, most_parts == 0 && threadIdx.x == 0);
     if (share > 0) {
       lo = (int)(at - from);
       hi = min((int)(next - from), sp.steps);
@@ -583,7 +584,8 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8, kN>::kCta
       lo = (int)((long long)sp.steps * part / parts);
       hi = (int)((long long)sp.steps * (part + 1) / parts);
     }
-    if (sp.rows > 0) stream_part<D, kQ8, kN>(a, sp, smem, &shared_word, seq, head, lo, hi, part, parts);
+    const int real_head = head / tiles, row0 = (head - real_head * tiles) * kTileRows;
+    if (sp.rows > row0) stream_part<D, kQ8, kN>(a, sp, smem, &shared_word, seq, real_head, row0, seq * heads + head, lo, hi, part, parts);
     at = next;
   }
   next_grid();
