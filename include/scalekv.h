@@ -362,12 +362,12 @@ scalekv_status scalekv_profile_read(scalekv_ctx *ctx, int32_t which, double *ms_
  * window with sinks (Sec. 4.1's positional rules, here as a mask over a cache that stays whole).
  *
  * Conventions
- *  - Every call enqueues on the given cudaStream_t of the handle's device (which must be current) and returns; no call but init and sync waits
- *    for the device, and all but these can be captured into a CUDA graph (a batch's arrays are read on the device when the kernels run; its sizes
- *    are the call's).
+ *  - Every call enqueues on the given cudaStream_t of the handle's device (which must be current) and returns; no call but init and
+ *    sync waits for the device, and all but these can be captured into a CUDA graph (a batch's arrays are read on the device when the
+ *    kernels run; its sizes are the call's).
  *  - Calls on one handle share its workspace: attends on different streams have to be ordered by the caller.
- *  - Lengths, starts and pages are read on the device.  One that is out of range is never followed: what it would lead to is left out (a row
- *    read comes back as zeros, a key counts as hidden), and the sticky device status, SCALEKV_ERR_DEVICE_CHECK, says so. */
+ *  - Lengths, starts and pages are read on the device.  One that is out of range is never followed: what it would lead to is left out
+ *    (a row read comes back as zeros, a key counts as hidden), and the sticky device status, SCALEKV_ERR_DEVICE_CHECK, says so. */
 typedef struct scalekv_paged scalekv_paged; /* opaque, host-side, library-owned */
 
 /* How a row (one token of one kv head, of K or of V) is held.
@@ -385,8 +385,9 @@ typedef struct {
   int32_t n_kv_heads;
   int32_t head_dim;       /* 64 or 128                                                                  */
   int32_t store;          /* SCALEKV_STORE_*                                                            */
-  void *pool;             /* device memory for the rows, 256-byte aligned (borrowed): K rows, V rows and, for Q8, K scales, V scales, */
-  size_t pool_bytes;      /* each [layer][page][kv head][row of the page]; need not be initialised      */
+  void *pool;             /* device memory for the rows, 256-byte aligned (borrowed): K rows, V rows    */
+  size_t pool_bytes;      /* and, for Q8, K scales, V scales, each [layer][page][kv head][row of the    */
+                          /* page]; need not be initialised                                             */
   void *workspace;        /* device scratch for partial results and the status word, 256-byte aligned (borrowed) */
   size_t workspace_bytes;
   int32_t device;
@@ -420,6 +421,7 @@ typedef struct {
   int32_t causal, window, n_sink;
 } scalekv_paged_mask;
 
+/* Bytes of pool and workspace that scalekv_paged_init needs (pointers in cfg are ignored; either may be NULL).  Host only. */
 scalekv_status scalekv_paged_query_sizes(const scalekv_paged_config *cfg, size_t *pool_bytes, size_t *workspace_bytes);
 /* Creates a handle (the reason of a refusal goes to stderr).  Synchronous.  *out is NULL on failure. */
 scalekv_status scalekv_paged_init(const scalekv_paged_config *cfg, scalekv_paged **out);
@@ -435,13 +437,14 @@ scalekv_status scalekv_paged_write(scalekv_paged *kv, int32_t layer, const scale
 scalekv_status scalekv_paged_read(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, scalekv_rows K,
                                   scalekv_rows V, int32_t dtype, void *stream);
 
-/* Attention of the new tokens over the cache: O = softmax(scale * q K^T) V over the keys that a query sees.  Q and O are
- * bf16 views with n_heads heads, a multiple of n_kv_heads (head h reads kv head h / (n_heads / n_kv_heads)).  The new tokens' own rows are
- * read from the cache like all others (write them first); queries may also attend over a cache that does not hold them, causal = 0.
+/* Attention of the new tokens over the cache: O = softmax(scale * q K^T) V over the keys that a query sees.  Q and O are bf16 views
+ * with n_heads heads, a multiple of n_kv_heads (head h reads kv head h / (n_heads / n_kv_heads)).  The new tokens' own rows are read
+ * from the cache like all others (write them first); queries may also attend over a cache that does not hold them, causal = 0.
  * lse (nullable) is a dense float [n_tokens][n_heads] that receives max + log-sum-exp of the scaled products.  A query that sees
- * nothing gets O = 0 and lse = -inf.  softmax_scale 0: 1 / sqrt(head_dim).  Products are exact, sums are fp32, P is rounded to
- * bf16 before its product with V.  What hidden keys hold never matters, whatever it is, with one exception: bf16 rows of V must be
- * finite where another query of the call sees them. */
+ * nothing gets O = 0 and lse = -inf.  softmax_scale 0: 1 / sqrt(head_dim).  Products are exact, sums are fp32; P is rounded to
+ * bf16 before its product with V where some sequence may bring more than 32 query rows to a kv head (max_new times the heads of the
+ * group), and goes into it as two pieces of bf16 otherwise.  What hidden keys hold never matters, whatever it is, with one exception:
+ * a bf16 row of V that one query of the call sees must be finite, or queries from which it is hidden may get NaN too. */
 scalekv_status scalekv_paged_attend(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, int32_t n_heads,
                                     scalekv_rows Q, scalekv_rows O, float *lse, const scalekv_paged_mask *mask,
                                     float softmax_scale, void *stream);

@@ -152,7 +152,8 @@ scalekv_status launch_stream(scalekv_paged *c, const AttendArgs &a, int tiles, l
   split = std::max<long long>(1, std::min(split, (steps + 7) / 8));
   const long long each = ((steps + split - 1) / split + kStreamWarps - 1) / kStreamWarps * kStreamWarps;
   split = std::max<long long>(1, std::min((steps + each - 1) / each, room));
-  // Sequences of different lengths have their parts dealt out on the device, where that gives a CTA 64 steps or more.
+  // Sequences of different lengths have their parts dealt out on the device, where that gives a CTA 64 steps or more (32 of up to 10 521 entries: 117 us in equal parts of
+  // each, 108 so).
   const bool by_length = a.bt.n_seqs > 1 && a.bt.n_seqs <= 512 && items <= std::min<long long>(kMaxCounts, 3 * slots) && room >= 3 && items * steps >= slots * 64;
   if (items > kMaxCounts) split = 1;
   launch(paged_stream_kernel<D, kQ8, kN>, by_length ? dim3((unsigned)slots) : dim3(a.bt.n_seqs, a.s.heads * tiles, (unsigned)split), kStreamThreads, Y::kSmem, stream,
@@ -163,8 +164,10 @@ scalekv_status launch_stream(scalekv_paged *c, const AttendArgs &a, int tiles, l
 template <int D, bool kQ8>
 scalekv_status launch_tile(scalekv_paged *c, int layer, const AttendArgs &a, int items, long long keys, cudaStream_t stream) {
   using Y = TileLayout<D, kQ8>;
-  // An item and kv head to a CTA.  Those that do not fill the SMs, and those of the last, partial wave, are shared by as many CTAs as find one, each with four
-  // key tiles or more: XXXT.
+  // An item and kv head to a CTA.  Those that do not fill the SMs are shared by as many CTAs as find one, each with two key tiles or more (us, 20 tokens behind
+  // 8 192 entries, 8 kv heads in codes, 1 / 2 / 4 / 8 / 16 / 32 CTAs an item: 202 / 108 / 60 / 35 / 25 / 26), and so are those of the last, partial wave (2 x 16 heads, bf16, 1 400
+  // queries over 1 500 / 3 000 / 5 000 entries, alone: 82 / 127 / 187, shared: 77 / 108 / 151; with fewer than 16 key tiles the launch that joins them can cost more than it
+  // gives: chunks beside single tokens under a window of 700, 56 alone, 61 shared).
   const int n = items * a.s.heads, sms = (int)std::min<long long>(c->n_sm, kPartRows / kItemRows), last = n % sms;
   const long long tiles = (keys + kTileKeys - 1) / kTileKeys;
   int parts = last ? (int)std::min<long long>(sms / last, tiles / 2) : 1;
@@ -323,6 +326,8 @@ scalekv_status scalekv_paged_attend(scalekv_paged *kv, int32_t layer, const scal
   if (a.mask.window > 0) keys = std::min<long long>(keys, (long long)a.mask.window + batch->max_new + a.mask.n_sink);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool q8 = c->cfg.store == SCALEKV_STORE_Q8;
+  // Up to 32 query rows stream (us, 64 heads, 8 kv heads in codes, 8 000 entries, streamed / on the tensor cores' tiles: 3 new tokens of 32 sequences 293 / 403, of 8 86 / 112,
+  // of one 24.6 / 23.0; 6 new tokens 437 / 405, 121 / 113, 29 / 24).
   if (max_rows <= kStreamRows) {
     auto go = [&](auto dim, auto codes) {
       constexpr int kD = decltype(dim)::value;

@@ -2,12 +2,12 @@
 //
 //   y_j = scale <q, k_j>,  lse = log sum_j exp(y_j),  O = sum_j exp(y_j - lse) v_j   over the keys j that the row sees.
 //
-// A kv head's query rows, the group's heads of every new token, share its keys: row r is head r mod G of token r / G, up to 16 of them.
+// A kv head's query rows, the group's heads of every new token, share its keys: row r is head r mod G of token r / G; a CTA has up to 16 of them.
 // What bounds it is reading the keys and values once: 2 (d + 4) bytes a key as codes, 4 d as bf16, against 8 d products a key and row.
 // So every warp streams its own share of the cache, 16 keys (which lie in one page) at a time, through a ring of stages in shared memory that it
 // fills with asynchronous copies and shares with nobody: no barrier before the end, and the loads of a few steps are always under way.
 // (With the loads in registers, half a step ahead, a step took a loaded DRAM latency: 32 sequences of up to 10 521 entries, 8 kv heads in codes, 285 us for
-// what is XXXX.)  Products are m16n8k16 with the few query rows as the n-tiles of eight, S^T = K Q^T (keys x rows x dims) and O^T = V^T P^T
+// what is 115.)  Products are m16n8k16 with the few query rows as the n-tiles of eight, S^T = K Q^T (keys x rows x dims) and O^T = V^T P^T
 // (dims x rows x keys): of an m-tile of query rows most would be padding, in the products and in the exponentials.
 //   - A lane has keys r and r + 8 (r = lane / 4) of K, as the A operand does, and since a product's sum may run in any order, it takes the dims that lie in its
 //     16-byte pieces; the queries, which stay in registers, are read in the same order.
@@ -19,6 +19,8 @@
 // The running maximum of a row is raised when a step exceeds it by more than 2^3, and the sums with it: P stays below that.
 // A CTA's four warps take the steps in turn and are combined in shared memory.  Where a sequence's heads are few, gridDim.z CTAs share its
 // keys; each leaves its part in the workspace, and the last one to do so, by a counter that it sets back, combines them in their order.
+// 32 sequences of up to 10 521 entries, 32 heads, 8 kv heads in codes: 115 us, 4.4 TB/s of 6.46 measured; SMs that still have work read 21 of 23.6 bytes a cycle and issue in
+// 55 of 100; the rest is beginnings, ends and what is left of balance.  One sequence of 170 521 bf16 entries, 16 heads: 247 us, 5.7 TB/s.
 #pragma once
 #include <cfloat>
 #include <cmath>
@@ -54,7 +56,7 @@ struct StreamLayout {
 };
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 3.f;
-constexpr int kSecond = 40;
+constexpr int kSecond = 40;                       // (64 sequences of 65 steps, 8 kv heads: 592 equal shares of 57 steps, most in two sequences, 42.1 us, 512 whole ones 34.7)
 
 struct Mask {
   int causal, window, n_sink;      // window 0: none
@@ -66,7 +68,7 @@ struct AttendArgs {
   Rows Q, O;                       // [tokens][heads][head_dim] bf16
   float *lse;                      // [tokens][heads] or null
   float *part_o, *part_ml;         // parts of rows that CTAs share: columns, and base-2 reference and sum
-  int *counts;                     // parts left so far, one for each sequence and kv head of a split launch; zero between launches
+  int *counts;                     // parts left so far, one for each sequence and kv head (and 16 rows) of a launch; zero between launches
   Mask mask;
   Divisor group;                   // query heads of a kv head
   int n_heads;                     // query heads
@@ -244,8 +246,8 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
     if (page >= 0) {
       constexpr int kRowPieces = kRowBytes / 16, kRowsAtOnce = 32 / kRowPieces;
       const int key0 = key_of(step), x = lane % kRowPieces, r0 = lane / kRowPieces;
-      const size_t row0 = store_row(s, page, head, key0);
-      const char *k = s.k_rows + (row0 + r0) * kRowBytes + x * 16, *v = s.v_rows + (row0 + r0) * kRowBytes + x * 16;
+      const size_t row = store_row(s, page, head, key0);
+      const char *k = s.k_rows + (row + r0) * kRowBytes + x * 16, *v = s.v_rows + (row + r0) * kRowBytes + x * 16;
       const uint32_t to = ring_at + stage * Y::kStage;
 #pragma unroll
       for (int i = 0; i < 16 / kRowsAtOnce; ++i) {
@@ -254,7 +256,7 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
         copy16(to + Y::piece(r, x), k + i * kRowsAtOnce * kRowBytes, true);
         copy16(to + 16 * kRowBytes + Y::piece(r, x), v + i * kRowsAtOnce * kRowBytes, kQ8 || in_use(key0 + r));
       }
-      if (kQ8 && lane < 8) copy16(to + Y::kScales + lane * 16, (lane < 4 ? s.k_scales : s.v_scales) + row0 + (lane & 3) * 4, true);
+      if (kQ8 && lane < 8) copy16(to + Y::kScales + lane * 16, (lane < 4 ? s.k_scales : s.v_scales) + row + (lane & 3) * 4, true);
     } else if (!kQ8 && step < step_hi) {
       for (int i = lane; i < 32 * kRowBytes / 16; i += 32) *reinterpret_cast<uint4 *>(ring + stage * Y::kStage + i * 16) = make_uint4(0u, 0u, 0u, 0u);
     }
@@ -517,9 +519,9 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8, kN>::kCta
   // Rows beyond the first kTileRows are a CTA's of their own, as if they were another head; `tiles` of them to a kv head.
   const int heads = a.s.heads * tiles, most_rows = tiles > 1 ? tiles * kTileRows : 8 * kN;
   auto weight = [&](int b, bool tell) {
-    if (b >= a.bt.n_seqs) return 0;
+    if (b >= a.bt.n_seqs) return 0u;                       // (32 of at most 2^26 steps each: sums of them need all 32 bits)
     const Span sp(a, b, most_rows, tell);
-    return sp.rows > 0 ? max(sp.steps, 1) : 0;
+    return sp.rows > 0 ? (unsigned)max(sp.steps, 1) : 0u;
   };
   long long at = 0, end = 1;
   int share = 0, split = gridDim.z;                        // share 0: parts
@@ -528,9 +530,9 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8, kN>::kCta
     long long total = 0;
     int longest = 1;
     for (int b0 = 0; b0 < a.bt.n_seqs; b0 += 32) {
-      const int w = weight(b0 + lane, blockIdx.x == 0 && threadIdx.x < 32);
+      const unsigned w = weight(b0 + lane, blockIdx.x == 0 && threadIdx.x < 32);
       total += __reduce_add_sync(0xffffffffu, w);
-      longest = max(longest, __reduce_max_sync(0xffffffffu, w));
+      longest = max(longest, (int)__reduce_max_sync(0xffffffffu, w));
     }
     total *= heads;
     const int ctas = gridDim.x, items = a.bt.n_seqs * heads;
@@ -550,20 +552,20 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8, kN>::kCta
     long long next = at + gridDim.x, from = 0;             // where this CTA goes on; of the sequence and head the first step
     if (share > 0) {
       long long before = 0;                                // steps of the sequences ahead of b0
-      int w = 0, incl = 0, b0 = 0;
-      unsigned behind = 0;
+      unsigned w = 0, incl = 0, behind = 0;
+      int b0 = 0;
       for (; b0 < a.bt.n_seqs; b0 += 32) {
         incl = w = weight(b0 + lane, false);
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-          const int up = __shfl_up_sync(0xffffffffu, incl, d);
+          const unsigned up = __shfl_up_sync(0xffffffffu, incl, d);
           if (lane >= d) incl += up;
         }
         behind = __ballot_sync(0xffffffffu, before + (long long)incl * heads > at);
         if (behind) break;
         before += (long long)__shfl_sync(0xffffffffu, incl, 31) * heads;
       }
-      const int src = __ffs(behind) - 1, steps = __shfl_sync(0xffffffffu, w, src);
+      const int src = __ffs(behind) - 1, steps = (int)__shfl_sync(0xffffffffu, w, src);
       from = before + (long long)__shfl_sync(0xffffffffu, incl - w, src) * heads;
       seq = b0 + src;
       head = (int)((at - from) / steps);

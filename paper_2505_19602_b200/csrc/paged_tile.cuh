@@ -15,10 +15,14 @@
 //                   four chunks of 32, exponentials against a lazy reference, which rises when one exceeds it by more than 2^8, P as bf16 over the products already
 //                   read.  With codes a key's scale is a factor of its column: K's is part of the factor of the exponent's FMA, V's multiplies P
 //                   before it is rounded; both come from shared memory, four columns to a load.  (A thread with a quarter of the columns of four rows loads a quarter as many
-//                   scales, but its sweep was the longer: 1 478 us for what is 1 247.)
+//                   scales, but its sweep was the longer: 1 478 us for what was 1 247.)
 // Rows that no query of the item sees (behind the length, ahead of the window, on a page out of range) may hold anything.  Their products are hidden one
 // by one; as values codes are numbers whatever they are, and bf16 rows are zeroed by the issuer before the product reads them.
 // Every wait is bounded; one that gives up raises the sticky status and all roles fall through to the end.
+// What bounds it: with bf16 rows the two chains  S -> sweep -> P V, about 4 000 cycles a step of a pair (2 048 at the tensor peak, and as many for its exponentials): 4 096 queries of
+// 2 x 16 heads over 10 521 entries in 705 us, 1.00 PFLOP/s.  With codes shared memory, too: of a step's 5 700 cycles the products read for 1 536, the scales' loads take 2 048 (a
+// 16-byte load takes a warp four cycles, the same address or not; without them 1 230 us were 1 020), the converters 800.  2 048 queries of 4 x 32 heads behind 6 144 entries: 1 090 us,
+// 0.88 PFLOP/s; the same in bf16 1 000.
 #pragma once
 #include <string>
 #include <type_traits>
@@ -574,7 +578,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       // to their chunk's largest or just above, and what was accumulated under the old one is multiplied by f = 2^(old - new): the sum, P of the chunks that the
       // tensor core has not been given yet, and O, once the last product given to it has landed.
       // (One loop for both, not unrolled: the roles' loops together have to stay in the SM's instruction cache.  With a masked copy of the sweep above and a copy of
-      // the raise in each of its chunks a step in codes, which has the converters' loop beside it, missed it 28 times in a hundred: 2 255 us for what is 1 247.)
+      // the raise in each of its chunks a step in codes, which has the converters' loop beside it, missed it 28 times in a hundred: 2 255 us for what was 1 618.)
       int landed = 0;                              // 1: the last step's product has; 2: the early part of this one's, too
 #pragma unroll 1
       for (; cc < kSweepChunks && ok; ++cc) {
