@@ -8,7 +8,7 @@
 // Both kernels move every row once; what bounds them is that.  A lane has 16 values of a row, 8 lanes are a row of 128, 4 one of 64.  A block takes a few
 // tokens, all heads of K and V of them: one thread to a token finds its place, then the rows follow one another as they do in a dense tensor.
 // us per pass, eight values a lane and every row's place looked up by its own lanes / so: 84 168 tokens of 8 heads in codes read as bf16 118 / 92 (5.7 of 6.46 TB/s
-// measured), 24 646 of 16 heads written and read back 228 / 120: writing takes 66 of that for 306 MB, with 71 of 100 issue slots busy.
+// measured), 24 646 of 16 heads written and read back 228 / 114: writing takes about 60 of that, bound by its instructions.
 #pragma once
 #include <math_constants.h>
 
@@ -102,12 +102,19 @@ __device__ __forceinline__ void store16(float *p, const float *x) {
   for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4 *>(p + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
 }
 
+// The scale of a row whose largest value is a: a / 127, by the same step as below from the rounded reciprocal (all 2^23 significands give the division's quotient).
+__device__ __forceinline__ float scale_of(float a) {
+  if (a < 0x1p-60f) return __fdiv_rn(a, 127.f);
+  const float r = 1.f / 127.f, q = __fmul_rn(a, r);
+  return __fmaf_rn(__fmaf_rn(-q, 127.f, a), r, q);
+}
 // Codes of 16 values: x / s rounded to fp32 and then to an integer, half to even.  The quotient by Markstein's theorem (IBM J. Res. Dev. 34, 1990): with r the
 // rounded reciprocal, q within a unit in the last place of the quotient and e = x - q s, which a fused multiply-add gives exactly, q + e r is the rounded
-// quotient.  x r is within two units, one such step makes that one, a second the result.  (A division for each of them took the larger part of the kernel's
-// time.)  Adding 1.5 2^23 rounds to an integer and leaves its low byte in the sum's.  A small scale is lifted first, so that nothing underflows, and its values
+// quotient.  x r is within two units, one such step makes that one, a second the result.  Rows of bf16 need no second: with 8 bits of significand in x and in the
+// row's largest value there are few enough quotients to go through all of them (none of 614 592 codes differs; without the first step 72 do).  (A division for
+// each of them took the larger part of the kernel's time.)  Adding 1.5 2^23 rounds to an integer and leaves its low byte in the sum's.  A small scale is lifted first, so that nothing underflows, and its values
 // are cut off where the codes end, which a rounded subnormal scale leaves below the largest of them.
-__device__ __forceinline__ uint4 codes_of(float *x, float s) {
+template <int kSteps> __device__ __forceinline__ uint4 codes_of(float *x, float s) {
   if (!(s > 0.f)) return make_uint4(0u, 0u, 0u, 0u);
   if (s < 0x1p-60f) {
     s *= 0x1p64f;
@@ -115,7 +122,7 @@ __device__ __forceinline__ uint4 codes_of(float *x, float s) {
     for (int i = 0; i < 16; ++i) x[i] = fmaxf(-127.f * s, fminf(127.f * s, x[i] * 0x1p64f));
   }
   using namespace scalekv::tc;                     // (two values to an instruction)
-  const float r = __fdiv_rn(1.f, s);
+  const float r = __frcp_rn(s);
   const uint64_t r2 = pack2(r, r), minus_s2 = pack2(-s, -s), unit2 = pack2(12582912.f, 12582912.f);
   uint32_t w[4];
 #pragma unroll
@@ -125,8 +132,8 @@ __device__ __forceinline__ uint4 codes_of(float *x, float s) {
     for (int k = 0; k < 4; k += 2) {
       const uint64_t x2 = pack2(x[i + k], x[i + k + 1]);
       uint64_t q = mul2(x2, r2);
-      q = fma2(fma2(q, minus_s2, x2), r2, q);
-      q = fma2(fma2(q, minus_s2, x2), r2, q);
+#pragma unroll
+      for (int step = 0; step < kSteps; ++step) q = fma2(fma2(q, minus_s2, x2), r2, q);
       unpack2(add2(q, unit2), c[k], c[k + 1]);
     }
     w[i / 4] = __byte_perm(__byte_perm(__float_as_uint(c[0]), __float_as_uint(c[1]), 0x0040), __byte_perm(__float_as_uint(c[2]), __float_as_uint(c[3]), 0x0040), 0x5410);
@@ -168,29 +175,32 @@ __global__ void __launch_bounds__(kStoreThreads) paged_write_kernel(const __grid
   // (the lanes of a row take every branch together, and the reduction names them alone)
   const unsigned mask = ((1u << kLanes) - 1u) << ((threadIdx.x & 31) / kLanes * kLanes);
   Raw16<T> raw;
-  if ((int)threadIdx.x < pieces) raw.load(Piece(mv, threadIdx.x, kLanes).dense<T>(mv, t0) + x * 16);       // (under the look-up)
+  Piece p(mv, threadIdx.x, kLanes);
+  if ((int)threadIdx.x < pieces) raw.load(p.dense<T>(mv, t0) + x * 16);       // (under the look-up)
   place_tokens(mv, t0, n, row0);
   for (int i = threadIdx.x; i < pieces; i += kStoreThreads) {
     float v[16];
     raw.numbers(v);
-    if (i + kStoreThreads < pieces) raw.load(Piece(mv, i + kStoreThreads, kLanes).dense<T>(mv, t0) + x * 16);
-    const Piece p(mv, i, kLanes);
-    if (row0[p.t] < 0) continue;
-    const size_t row = p.row(mv, row0[p.t]);
-    char *rows = p.is_v ? s.v_rows : s.k_rows;
-    if constexpr (!kQ8) {
-      store16(reinterpret_cast<__nv_bfloat16 *>(rows) + row * D + x * 16, v);
-    } else {
-      float a = fabsf(v[0]);
+    const Piece next(mv, i + kStoreThreads, kLanes);
+    if (i + kStoreThreads < pieces) raw.load(next.dense<T>(mv, t0) + x * 16);
+    if (row0[p.t] >= 0) {
+      const size_t row = p.row(mv, row0[p.t]);
+      char *rows = p.is_v ? s.v_rows : s.k_rows;
+      if constexpr (!kQ8) {
+        store16(reinterpret_cast<__nv_bfloat16 *>(rows) + row * D + x * 16, v);
+      } else {
+        float a = fabsf(v[0]);
 #pragma unroll
-      for (int j = 1; j < 15; j += 2) a = max_nan(a, fabsf(v[j]), fabsf(v[j + 1]));
-      a = max_nan(a, fabsf(v[15]), 0.f);
+        for (int j = 1; j < 15; j += 2) a = max_nan(a, fabsf(v[j]), fabsf(v[j + 1]));
+        a = max_nan(a, fabsf(v[15]), 0.f);
 #pragma unroll
-      for (int o = kLanes / 2; o > 0; o >>= 1) a = max_nan(a, __shfl_xor_sync(mask, a, o), 0.f);
-      const float scale = a < CUDART_INF_F ? __fdiv_rn(a, 127.f) : CUDART_NAN_F;
-      *reinterpret_cast<uint4 *>(rows + row * D + x * 16) = codes_of(v, scale);
-      if (x == 0) (p.is_v ? s.v_scales : s.k_scales)[row] = scale;
+        for (int o = kLanes / 2; o > 0; o >>= 1) a = max_nan(a, __shfl_xor_sync(mask, a, o), 0.f);
+        const float scale = a < CUDART_INF_F ? scale_of(a) : CUDART_NAN_F;
+        *reinterpret_cast<uint4 *>(rows + row * D + x * 16) = codes_of<sizeof(T) == 2 ? 1 : 2>(v, scale);
+        if (x == 0) (p.is_v ? s.v_scales : s.k_scales)[row] = scale;
+      }
     }
+    p = next;
   }
 }
 
