@@ -19,10 +19,11 @@
 // Rows that no query of the item sees (behind the length, ahead of the window, on a page out of range) may hold anything.  Their products are hidden one
 // by one; as values codes are numbers whatever they are, and bf16 rows are zeroed by the issuer before the product reads them.
 // Every wait is bounded; one that gives up raises the sticky status and all roles fall through to the end.
-// What bounds it: with bf16 rows the two chains  S -> sweep -> P V, about 4 000 cycles a step of a pair (2 048 at the tensor peak, and as many for its exponentials): 4 096 queries of
-// 2 x 16 heads over 10 521 entries in 705 us, 1.00 PFLOP/s.  With codes shared memory, too: of a step's 5 700 cycles the products read for 1 536, the scales' loads take 2 048 (a
-// 16-byte load takes a warp four cycles, the same address or not; without them 1 230 us were 1 020), the converters 800.  2 048 queries of 4 x 32 heads behind 6 144 entries: 1 090 us,
-// 0.88 PFLOP/s; the same in bf16 1 000.
+// What bounds it: with bf16 rows the two chains  S -> sweep -> P V, 3 750 cycles a step of a pair (2 048 at the tensor peak, and as many for its
+// exponentials): 4 096 queries of 2 x 16 heads over 10 521 entries in 705 us, 1.00 PFLOP/s.  With codes shared memory, too: of a step's 5 000 cycles the
+// products read for 1 540 and the threads take 2 860, about 2 050 of these for the scales (a 16-byte load takes a warp four cycles, the same address or not;
+// without them 1 230 us were 1 020), the rest for the converters.  2 048 queries of 4 x 32 heads behind 6 144 entries: 1 090 us, 0.88 PFLOP/s; the same in
+// bf16 1 000.
 #pragma once
 #include <string>
 #include <type_traits>
