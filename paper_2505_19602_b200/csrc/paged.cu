@@ -84,8 +84,8 @@ Store layer_store(const scalekv_paged *c, int layer) {
   return s;
 }
 
-bool rows_ok(const scalekv_rows &x, int esize) {
-  return x.ptr != nullptr && !(reinterpret_cast<uintptr_t>(x.ptr) & 15) && (x.stride_t * esize) % 16 == 0 && (x.stride_h * esize) % 16 == 0;
+bool rows_ok(const scalekv_rows &x, int esize, int align = 16) {
+  return x.ptr != nullptr && !(reinterpret_cast<uintptr_t>(x.ptr) & (align - 1)) && (x.stride_t * esize) % align == 0 && (x.stride_h * esize) % align == 0;
 }
 
 Rows view(const scalekv_rows &x, int esize) { return {static_cast<char *>(const_cast<void *>(x.ptr)), x.stride_t * esize, x.stride_h * esize}; }
@@ -205,6 +205,7 @@ scalekv_status move_rows(scalekv_paged *c, int layer, const scalekv_paged_batch 
   mv.s = layer_store(c, layer);
   mv.bt = bt;
   mv.K = view(K, esize); mv.V = view(V, esize);
+  mv.wide = rows_ok(K, esize, 32) && rows_ok(V, esize, 32);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   auto go = [&](auto t, auto dim) {
     using T = decltype(t);

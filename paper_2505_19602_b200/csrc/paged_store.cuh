@@ -8,7 +8,7 @@
 // Both kernels move every row once; what bounds them is that.  A lane has 16 values of a row, 8 lanes are a row of 128, 4 one of 64.  A block takes a few
 // tokens, all heads of K and V of them: one thread to a token finds its place, then the rows follow one another as they do in a dense tensor.
 // us per pass, eight values a lane and every row's place looked up by its own lanes / so: 84 168 tokens of 8 heads in codes read as bf16 118 / 92 (5.7 of 6.46 TB/s
-// measured), 24 646 of 16 heads written and read back 228 / 114: writing takes about 60 of that, bound by its instructions.
+// measured), 24 646 of 16 heads written and read back 228 / 112: writing takes about 60 of that, bound by its instructions.
 #pragma once
 #include <math_constants.h>
 
@@ -27,6 +27,7 @@ struct Moves {
   Rows K, V;
   Divisor per_token;                             // 16-value pieces of a token: of K's heads, then of V's
   int tokens;                                    // of a block
+  int wide;                                      // every 16 values of the dense tensors begin on 32 bytes
 };
 
 // The first sequence that ends behind token t (n_seqs: none does).  All threads of the block, same t.
@@ -69,12 +70,29 @@ __device__ __forceinline__ float max_nan(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
+// A lane's 16 values are 32 bytes of bf16, a sector: one access where they begin on 32 bytes, or two of 16 bytes, each of which meets every sector of
+// the warp's and fills it by half (us, two / one, 24 646 tokens of 16 heads written and read back: f32 204 / 167, bf16 115 / 112).
+__device__ __forceinline__ void load32(const void *p, uint4 &a, uint4 &b) {
+  asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w)
+               : "l"(p));
+}
+__device__ __forceinline__ void store32(void *p, const uint4 &a, const uint4 &b) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y),
+               "r"(b.z), "r"(b.w)
+               : "memory");
+}
 // 16 values as they lie in memory, and as numbers
 template <typename T> struct Raw16 {
   uint4 w[sizeof(T)];
-  __device__ __forceinline__ void load(const T *p) {
+  __device__ __forceinline__ void load(const T *p, bool wide) {
+    if (wide) {
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T); ++i) w[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+      for (int i = 0; i < (int)sizeof(T); i += 2) load32(reinterpret_cast<const uint4 *>(p) + i, w[i], w[i + 1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T); ++i) w[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+    }
   }
   __device__ __forceinline__ void numbers(float *x) const {
 #pragma unroll
@@ -92,14 +110,30 @@ template <typename T> struct Raw16 {
     }
   }
 };
-__device__ __forceinline__ void store16(__nv_bfloat16 *p, const float *x) {
+__device__ __forceinline__ void store16(__nv_bfloat16 *p, const float *x, bool wide) {
+  uint4 w[2];
 #pragma unroll
-  for (int i = 0; i < 16; i += 8)
-    *reinterpret_cast<uint4 *>(p + i) = make_uint4(pair_bf16(x[i], x[i + 1]), pair_bf16(x[i + 2], x[i + 3]), pair_bf16(x[i + 4], x[i + 5]), pair_bf16(x[i + 6], x[i + 7]));
+  for (int i = 0; i < 2; ++i)
+    w[i] = make_uint4(pair_bf16(x[8 * i], x[8 * i + 1]), pair_bf16(x[8 * i + 2], x[8 * i + 3]), pair_bf16(x[8 * i + 4], x[8 * i + 5]),
+                      pair_bf16(x[8 * i + 6], x[8 * i + 7]));
+  if (wide) {
+    store32(p, w[0], w[1]);
+  } else {
+    reinterpret_cast<uint4 *>(p)[0] = w[0];
+    reinterpret_cast<uint4 *>(p)[1] = w[1];
+  }
 }
-__device__ __forceinline__ void store16(float *p, const float *x) {
+__device__ __forceinline__ void store16(float *p, const float *x, bool wide) {
+  auto four = [&](int i) { return make_uint4(__float_as_uint(x[i]), __float_as_uint(x[i + 1]), __float_as_uint(x[i + 2]), __float_as_uint(x[i + 3])); };
 #pragma unroll
-  for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4 *>(p + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+  for (int i = 0; i < 16; i += 8) {
+    if (wide) {
+      store32(p + i, four(i), four(i + 4));
+    } else {
+      reinterpret_cast<uint4 *>(p + i)[0] = four(i);
+      reinterpret_cast<uint4 *>(p + i)[1] = four(i + 4);
+    }
+  }
 }
 
 // The scale of a row whose largest value is a: a / 127, by the same step as below from the rounded reciprocal (all 2^23 significands give the division's quotient).
@@ -176,18 +210,18 @@ __global__ void __launch_bounds__(kStoreThreads) paged_write_kernel(const __grid
   const unsigned mask = ((1u << kLanes) - 1u) << ((threadIdx.x & 31) / kLanes * kLanes);
   Raw16<T> raw;
   Piece p(mv, threadIdx.x, kLanes);
-  if ((int)threadIdx.x < pieces) raw.load(p.dense<T>(mv, t0) + x * 16);       // (under the look-up)
+  if ((int)threadIdx.x < pieces) raw.load(p.dense<T>(mv, t0) + x * 16, mv.wide);       // (under the look-up)
   place_tokens(mv, t0, n, row0);
   for (int i = threadIdx.x; i < pieces; i += kStoreThreads) {
     float v[16];
     raw.numbers(v);
     const Piece next(mv, i + kStoreThreads, kLanes);
-    if (i + kStoreThreads < pieces) raw.load(next.dense<T>(mv, t0) + x * 16);
+    if (i + kStoreThreads < pieces) raw.load(next.dense<T>(mv, t0) + x * 16, mv.wide);
     if (row0[p.t] >= 0) {
       const size_t row = p.row(mv, row0[p.t]);
       char *rows = p.is_v ? s.v_rows : s.k_rows;
       if constexpr (!kQ8) {
-        store16(reinterpret_cast<__nv_bfloat16 *>(rows) + row * D + x * 16, v);
+        store16(reinterpret_cast<__nv_bfloat16 *>(rows) + row * D + x * 16, v, true);
       } else {
         float a = fabsf(v[0]);
 #pragma unroll
@@ -233,11 +267,11 @@ __global__ void __launch_bounds__(kStoreThreads) paged_read_kernel(const __grid_
         for (int j = 0; j < 16; ++j) y[j] *= scale;
       } else {
         Raw16<__nv_bfloat16> raw;
-        raw.load(reinterpret_cast<const __nv_bfloat16 *>(rows) + row * D + x * 16);
+        raw.load(reinterpret_cast<const __nv_bfloat16 *>(rows) + row * D + x * 16, true);
         raw.numbers(y);
       }
     }
-    store16(p.dense<T>(mv, t0) + x * 16, y);
+    store16(p.dense<T>(mv, t0) + x * 16, y, mv.wide);
   }
 }
 

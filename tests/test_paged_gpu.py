@@ -143,6 +143,27 @@ def test_strided_rows(dtype):
         assert np.array_equal(got.transpose(0, 1).float().cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("store", ["q8", "bf16"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("off", [(16, 16), (0, 16), (16, 0)])
+def test_rows_that_begin_on_16_bytes(dtype, store, off):
+    """K, V or both begin on 16 bytes but not on 32, in as in out; the same rows are held and come back."""
+    c = Case([50, 21], [50, 21], 4, d=64, store=store)
+    esize = torch.empty(0, dtype=dtype).element_size()
+    flat = [torch.zeros(71 * 4 * 64 + 16, device="cuda", dtype=dtype) for _ in range(4)]
+    K, V, K_out, V_out = (f[o // esize:][: 71 * 4 * 64].view(71, 4, 64) for f, o in zip(flat, off + off))
+    assert [x.data_ptr() % 32 for x in (K, V)] == list(off)
+    K.copy_(torch.from_numpy(c.K).cuda())
+    V.copy_(torch.from_numpy(c.V).cuda())
+    c.kv.scalekv_paged_write(c.layer, c.batch(), K, V)
+    c.kv.scalekv_paged_read(c.layer, c.batch(), K_out, V_out)
+    for got, x in zip((K_out, V_out), (K, V)):
+        want = po.stored(x.float().cpu().numpy(), store)
+        want = want if dtype == torch.float32 else po.to_bf16(want)
+        assert np.array_equal(got.float().cpu().numpy(), want)
+    assert all(bool((f[o // esize + 71 * 4 * 64:] == 0).all()) and bool((f[: o // esize] == 0).all()) for f, o in zip(flat, off + off))
+
+
 # ---- attention -------------------------------------------------------------------------------------------------------------------
 LENGTHS = [1, 2, 15, 16, 17, 31, 128, 129, 300]
 
