@@ -130,8 +130,8 @@ cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cu
 
 template <bool kWrite, typename T, int D, bool kQ8>
 void launch_store(Moves &mv, int n_sm, cudaStream_t stream) {
-  // as many tokens to a block as give its threads four pieces (read: one, two, four, eight of them, 84 168 tokens of 8 heads: 106 / 96 / 92 / 92 us), unless the
-  // blocks then leave SMs idle
+  // as many tokens to a block as give its threads four pieces (read: one, two, four, eight of them, 84 168 tokens of 8 heads: 106 / 96 / 92 / 92 us;
+  // written and read back, two, four, eight, 24 646 tokens of 16 heads: 116 / 112 / 112), unless the blocks then leave SMs idle
   mv.per_token = Divisor::of(2 * mv.s.heads * (D / 16));
   const int n = mv.bt.n_tokens, full = (4 * kStoreThreads + mv.per_token.d - 1) / mv.per_token.d;
   mv.tokens = std::max(1, std::min(std::min(full, kMostTokens), n / (2 * n_sm)));
