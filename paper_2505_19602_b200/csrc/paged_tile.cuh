@@ -123,6 +123,20 @@ __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, vo
   return __all_sync(0xffffffffu, ok);
 }
 
+// Whether all 128 threads of the converters bring true.  A named barrier, which knows no limit: whoever has given up comes, too, and all of them hear of it.
+__device__ __forceinline__ bool all_converters(bool mine) {
+  uint32_t all;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "bar.red.and.pred q, 3, 128, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(all)
+      : "r"(mine ? 1u : 0u)
+      : "memory");
+  return all != 0;
+}
+
 __device__ __forceinline__ float2 load_shared2(uint32_t at) {
   float2 x;
   asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(at));
@@ -411,18 +425,10 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       k_scale = on ? __ldg(s.k_scales + row) * (a.scale_log2e * kCodeUnit) : 0.f;
       v_scale = on ? __ldg(s.v_scales + row) * kCodeUnit : 0.f;
     };
-    bool ok = true;
     if (nt > 0 && rows > 0) fetch_scales(0);
     for (int t = 0; t < 2 * nt && rows > 0; ++t) {
       const uint32_t stage = base + Y::kOffRing + (t % kStages) * kTile;
-      ok = mbar_wait_warp(bar(Y::bRaw + t % kStages), (t / kStages) & 1, abort_flag, status);
-      if (!ok) break;
-      if (!(t & 1)) {
-        const uint32_t at = base + Y::kOffScale + ((t >> 1) % Y::kSlots) * 1024 + tid * 4;
-        asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(k_scale) : "memory");
-        asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 512), "f"(v_scale) : "memory");
-        if ((t >> 1) + 1 < nt) fetch_scales((t >> 1) + 1);
-      }
+      const bool landed = mbar_wait_warp(bar(Y::bRaw + t % kStages), (t / kStages) & 1, abort_flag, status);
       // 16 codes become two 16-byte pieces of a row's 128-byte span of 64 columns.  Eight lanes' stores, of two
       // neighbouring rows, meet all banks.
       auto convert = [&](const uint4 &raw, uint32_t span, int r) {
@@ -436,13 +442,21 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       // lie in is taken out by all threads before any puts it back.
       const uint32_t raw_at = stage + kTile - 128 * D + piece * 16;
       uint4 last[4];
+      if (landed) {
+        if (!(t & 1)) {
+          const uint32_t at = base + Y::kOffScale + ((t >> 1) % Y::kSlots) * 1024 + tid * 4;
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(k_scale) : "memory");
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + 512), "f"(v_scale) : "memory");
+          if ((t >> 1) + 1 < nt) fetch_scales((t >> 1) + 1);
+        }
 #pragma unroll
-      for (int it = 0; it < 4; ++it) last[it] = load_shared16(raw_at + (it * 32 + sub) * D + (D - 64));
-      if constexpr (D == 128) {
+        for (int it = 0; it < 4; ++it) last[it] = load_shared16(raw_at + (it * 32 + sub) * D + (D - 64));
+        if constexpr (D == 128) {
 #pragma unroll 2
-        for (int r = sub; r < 128; r += 32) convert(load_shared16(raw_at + r * D), stage, r);
+          for (int r = sub; r < 128; r += 32) convert(load_shared16(raw_at + r * D), stage, r);
+        }
       }
-      asm volatile("bar.sync 3, 128;" ::: "memory");
+      if (!all_converters(landed)) break;          // (a warp whose wait gave up comes here, or the others would wait for it for ever)
 #pragma unroll
       for (int it = 0; it < 4; ++it) convert(last[it], stage + (D == 128 ? kHalf : 0u), it * 32 + sub);
       fence_async_proxy();
