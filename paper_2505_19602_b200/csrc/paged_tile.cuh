@@ -123,6 +123,13 @@ __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, vo
   return __all_sync(0xffffffffu, ok);
 }
 
+// For what a CTA has asked for and must not leave behind, copies into its shared memory and products into its TMEM: waits until it is through, whatever the
+// status, a second at most.
+__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
+  const unsigned long long t0 = globaltimer();
+  while (!mbar_try(bar, parity) && globaltimer() - t0 < kWaitLimitNs / 2) {}
+}
+
 // Whether all 128 threads of the converters bring true.  A named barrier, which knows no limit: whoever has given up comes, too, and all of them hear of it.
 __device__ __forceinline__ bool all_converters(bool mine) {
   uint32_t all;
@@ -315,6 +322,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         __syncwarp();
       };
       bool ok = true;
+      uint32_t latest = 0, latest_parity = 0;      // barrier and phase of the commit that stands behind all products so far
       for (int qt = 0; qt < 2 && ok && steps[qt] > 0; ++qt) {
         const int kt = ring_of(0, qt);
         ok = mbar_wait_warp(bar(Y::bQFull + (pair ? qt : 0)), 0, abort_flag, status) && ring_full(kt);
@@ -325,6 +333,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           tc_commit(bar(Y::bSFull + qt));
           if (!pair || qt == 1) tc_commit(bar(Y::bEmpty + kt % kStages));
         }
+        latest = bar(Y::bSFull + qt);
         __syncwarp();
       }
       for (int j = 0; j < steps[0] && ok; ++j) {
@@ -345,6 +354,8 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           tc_fence_after();
           tc_mma_ts_n<2 * kEarly>(oa, pa, vd, dhi, idesc_pv, j > 0 ? 1u : 0u);
           if (leader) tc_commit(bar(Y::bPvEarly + qt));
+          latest = bar(Y::bPvEarly + qt);
+          latest_parity = j & 1;
           __syncwarp();
           ok = (!more || ring_full(kt)) && mbar_wait_warp(bar(Y::bPFull + qt), j & 1, abort_flag, status);
           if (!ok) break;
@@ -353,16 +364,19 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           if (more) mma_s(kd, qt);
           if (leader) {
             tc_commit(done);
-            tc_commit(bar(Y::bPvDone + qt));
             if (!pair || qt == 1) {
               tc_commit(v_empty);
               if (more) tc_commit(k_empty);
             }
+            tc_commit(bar(Y::bPvDone + qt));
           }
+          latest = bar(Y::bPvDone + qt);
           __syncwarp();
         }
       }
       next_grid();
+      // (whoever has given up: no product may be under way when TMEM is freed and the tiles that it reads are gone)
+      if (latest) drain(latest, latest_parity);
     } else if (warp == 1 && rows > 0) {
       // -------------------------------------------------------------- TMA producer (a lane to each box of rows of a page)
       // Ring tile t holds K (even) or V (odd) of key tile t / 2, which bRaw (codes) or bFull says.  A tile's holes go with its K.  (One lane that issued all boxes,
@@ -403,13 +417,8 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           __syncwarp();
         }
       }
-      if (!ok) {
-        // this CTA gives up: nothing may land in its shared memory once it is gone (a second at most)
-        for (int k = max(t - kStages, 0); k < t; ++k) {
-          const unsigned long long t0 = globaltimer();
-          while (!mbar_try(bar(kLanded + k % kStages), (k / kStages) & 1) && globaltimer() - t0 < kWaitLimitNs / 2) {}
-        }
-      }
+      // (whoever has given up: nothing may land in this CTA's shared memory once it is gone)
+      for (int k = max(t - kStages, 0); k < t; ++k) drain(bar(kLanded + k % kStages), (k / kStages) & 1);
     }
   } else if (kQ8 && warp < 8) {
     registers_down<Y::kRegs1>();
