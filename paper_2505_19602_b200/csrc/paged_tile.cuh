@@ -757,7 +757,8 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   }
 }
 
-// O = sum_e 2^(m_e - M) O_e / sum_e 2^(m_e - M) l_e, M the largest reference, of the items that several CTAs share: a warp to each row.
+// O = sum_e 2^(m_e - M) O_e / sum_e 2^(m_e - M) l_e, M the largest reference, of the items that several CTAs share: a warp to each row.  Once a wait has given
+// up (ever: the status is sticky), parts may be missing and old ones lie in their places: nothing is stored then.
 constexpr int kJoinRows = 8;
 template <int D>
 __global__ void __launch_bounds__(32 * kJoinRows) paged_join_kernel(const __grid_constant__ AttendArgs a, const Cut cut) {
@@ -766,6 +767,7 @@ __global__ void __launch_bounds__(32 * kJoinRows) paged_join_kernel(const __grid
   const int at_item = cut.n_full + shared_item, e0 = cut.heads.div(at_item), head = at_item - e0 * cut.heads.d;
   wait_for_grid();
   next_grid();
+  const bool complete = __ldcg(a.s.status) != kDevTimeout;
   const size_t row0 = (size_t)shared_item * parts * kItemRows + r;
   float m = -INFINITY;
   for (int e = lane; e < parts; e += 32) m = fmaxf(m, __ldg(a.part_ml + (row0 + (size_t)e * kItemRows) * 2));
@@ -790,6 +792,7 @@ __global__ void __launch_bounds__(32 * kJoinRows) paged_join_kernel(const __grid
 #pragma unroll
     for (int c = 0; c < kPer; ++c) acc[c] += f * v[c];
   }
+  if (!complete) return;
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   const int t = a.group.div(i), h = head * a.group.d + i - t * a.group.d;
   char *out = a.O.ptr + (start + t) * a.O.st + h * a.O.sh + lane * kPer * 2;
