@@ -367,7 +367,8 @@ scalekv_status scalekv_profile_read(scalekv_ctx *ctx, int32_t which, double *ms_
  *    kernels run; its sizes are the call's).
  *  - Calls on one handle share its workspace: attends on different streams have to be ordered by the caller.
  *  - Lengths, starts and pages are read on the device.  One that is out of range is never followed: what it would lead to is left out
- *    (a row read comes back as zeros, a key counts as hidden), and the sticky device status, SCALEKV_ERR_DEVICE_CHECK, says so. */
+ *    (a row read comes back as zeros, a key counts as hidden, O and lse of a token that belongs to no sequence keep what they held),
+ *    and the sticky device status, SCALEKV_ERR_DEVICE_CHECK, says so. */
 typedef struct scalekv_paged scalekv_paged; /* opaque, host-side, library-owned */
 
 /* How a row (one token of one kv head, of K or of V) is held.
@@ -404,7 +405,7 @@ typedef struct {
   int32_t table_stride;       /* from one sequence's entries to the next one's                          */
   int32_t table_pages;        /* entries of a sequence: no position behind them is looked up            */
   int32_t n_seqs, n_tokens;
-  int32_t max_new;            /* no sequence has more new tokens than this (reported otherwise)         */
+  int32_t max_new;            /* no sequence has more new tokens than this (an attend reports it otherwise) */
   int32_t max_length;         /* no sequence is longer than this; only sizes launches                   */
 } scalekv_paged_batch;
 

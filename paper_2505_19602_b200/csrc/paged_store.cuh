@@ -60,6 +60,14 @@ __device__ __forceinline__ void place_tokens(const Moves &mv, int t0, int n, lon
   __syncthreads();
 }
 
+// Tells of starts that are out of order, at the end of a launch's first block: their lines are at hand by then.
+__device__ __forceinline__ void check_starts(const Moves &mv) {
+  const Batch &bt = mv.bt;
+  if (blockIdx.x > 0) return;
+  for (int b = threadIdx.x; b < bt.n_seqs; b += kStoreThreads)
+    if (starts_wrong(bt, b, __ldg(bt.starts + b), __ldg(bt.starts + b + 1))) report(mv.s.status);
+}
+
 __device__ __forceinline__ uint32_t pair_bf16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -237,6 +245,7 @@ __global__ void __launch_bounds__(kStoreThreads) paged_write_kernel(const __grid
     }
     p = next;
   }
+  check_starts(mv);
 }
 
 template <typename T, int D, bool kQ8>
@@ -274,6 +283,7 @@ __global__ void __launch_bounds__(kStoreThreads) paged_read_kernel(const __grid_
     }
     store16(p.dense<T>(mv, t0) + x * 16, y, mv.wide);
   }
+  check_starts(mv);
 }
 
 }  // namespace paged

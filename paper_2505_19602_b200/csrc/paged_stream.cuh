@@ -114,8 +114,8 @@ struct Span {
   __device__ __forceinline__ Span(const AttendArgs &a, int seq, int most_rows, bool tell) {
     start = __ldg(a.bt.starts + seq);
     length = __ldg(a.bt.lengths + seq);
-    const int n_new = min(__ldg(a.bt.starts + seq + 1), a.bt.n_tokens) - start, room = a.bt.table_pages << a.s.page_shift;
-    if (tell && (n_new > a.max_new || (unsigned)length > (unsigned)room)) report(a.s.status);
+    const int end = __ldg(a.bt.starts + seq + 1), n_new = min(end, a.bt.n_tokens) - start, room = a.bt.table_pages << a.s.page_shift;
+    if (tell && (starts_wrong(a.bt, seq, start, end) || n_new > a.max_new || (unsigned)length > (unsigned)room)) report(a.s.status);
     length = max(min(length, room), 0);                    // (what lies behind the table counts as hidden)
     first = length - n_new;                                // position of the sequence's first new token
     rows = start < 0 || n_new <= 0 ? 0 : min(n_new * a.group.d, most_rows);

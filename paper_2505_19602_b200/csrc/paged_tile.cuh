@@ -238,9 +238,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     Item it = find_item(a, cut.n_items - 1 - e);
     if (lane == 0) {
       if (it.seq >= 0) {
-        const int room = a.bt.table_pages << s.page_shift;
-        if ((unsigned)it.length > (unsigned)room || it.n_new > a.max_new) report(status);
-        it.length = max(min(it.length, room), 0);
+        it.length = max(min(it.length, a.bt.table_pages << s.page_shift), 0);
       }
       if (*reinterpret_cast<volatile int *>(status) == kDevTimeout) it.seq = -1;      // an earlier CTA gave up: do not pile on
       if (base & 1023u) { report(status); it.seq = -1; }
@@ -258,6 +256,15 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   } else if (warp == 2) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + Y::kOffItem), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  } else if (warp == 3 && blockIdx.x == 0) {
+    // what is out of range in the batch, of sequences that have no item, too
+    wait_for_grid();
+    for (int b = lane; b < a.bt.n_seqs; b += 32) {
+      const int start_b = __ldg(a.bt.starts + b), end_b = __ldg(a.bt.starts + b + 1);
+      if (starts_wrong(a.bt, b, start_b, end_b) || end_b - start_b > a.max_new ||
+          (unsigned)__ldg(a.bt.lengths + b) > (unsigned)(a.bt.table_pages << s.page_shift))
+        report(status);
+    }
   }
   wait_for_grid();
   tc_fence_before();

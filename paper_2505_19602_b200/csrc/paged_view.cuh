@@ -36,6 +36,11 @@ __device__ __forceinline__ void next_grid() { asm volatile("griddepcontrol.launc
 // (a wait that gave up stays on record)
 __device__ __forceinline__ void report(int *status) { atomicCAS(status, 0, kDevCheck); }
 
+// Whether the starts of sequence b are out of order: from 0 to n_tokens, none below the one before it.
+__device__ __forceinline__ bool starts_wrong(const Batch &bt, int b, int start, int end) {
+  return start < 0 || end < start || end > bt.n_tokens || (b == 0 && start != 0) || (b == bt.n_seqs - 1 && end != bt.n_tokens);
+}
+
 // Page of position pos of sequence b, or -1 (reported) where the table has none.
 __device__ __forceinline__ int page_of(const Store &s, const Batch &bt, int b, int pos) {
   const int i = pos >> s.page_shift;
