@@ -19,10 +19,7 @@ using namespace scalekv::paged;
 
 namespace {
 
-// Rows of partial results that a launch may leave (rows of the call times CTAs that share a row's keys).
-constexpr long long kPartRows = 148 * 256;
 constexpr size_t kStatusBytes = 256;
-constexpr int kMaxCounts = 4096;         // sequences times kv heads of a launch whose keys are shared
 constexpr int kMaxLength = 1 << 30;      // tokens that a sequence's pages may hold: sums of a position and a window stay in 32 bits
 
 struct Layout {
@@ -143,21 +140,10 @@ void launch_store(Moves &mv, int n_sm, cudaStream_t stream) {
 template <int D, bool kQ8, int kN>
 scalekv_status launch_stream(scalekv_paged *c, const AttendArgs &a, int tiles, long long keys, cudaStream_t stream) {
   using Y = StreamLayout<D, kQ8, kN>;
-  const long long items = (long long)a.bt.n_seqs * a.s.heads * tiles, slots = (long long)c->n_sm * Y::kCtas, steps = (keys + 15) / 16;
-  const long long room = std::min<long long>(kPartRows / ((long long)a.bt.n_tokens * a.n_heads), Y::kMostParts);      // parts that the workspace holds
-  // CTAs that share a sequence's keys: one for every SM, down to two steps of 16 keys for each of its warps; two where that leaves them four; as many as
-  // fit where it leaves them 16.  (us, one sequence with 8 kv heads in codes, 4 / 8 / 16 / 32 / 74 CTAs a head: 1 999 entries 12.8 / 10.3 / 8.6 / 10.6 / 18.5, 8 000
-  // 31.7 / 19.8 / 13.4 / 13.3 / 17.9, 32 000 107.7 / 58.9 / 34.1 / 26.7 / 28.9.)  Then no more of them than the longest warp's number of steps asks for.
-  long long split = std::max(c->n_sm / items, std::max(std::min(2 * c->n_sm / items, steps / 16), std::min(slots / items, steps / 64)));
-  split = std::max<long long>(1, std::min(split, (steps + 7) / 8));
-  const long long each = ((steps + split - 1) / split + kStreamWarps - 1) / kStreamWarps * kStreamWarps;
-  split = std::max<long long>(1, std::min((steps + each - 1) / each, room));
-  // Sequences of different lengths have their parts dealt out on the device, where that gives a CTA 64 steps or more (32 of up to 10 521 entries: 117 us in equal parts of
-  // each, 108 so).
-  const bool by_length = a.bt.n_seqs > 1 && a.bt.n_seqs <= 512 && items <= std::min<long long>(kMaxCounts, 3 * slots) && room >= 3 && items * steps >= slots * 64;
-  if (items > kMaxCounts) split = 1;
-  launch(paged_stream_kernel<D, kQ8, kN>, by_length ? dim3((unsigned)slots) : dim3(a.bt.n_seqs, a.s.heads * tiles, (unsigned)split), kStreamThreads, Y::kSmem, stream,
-         a, by_length ? (int)room : 0, tiles);
+  const int slots = c->n_sm * Y::kCtas;
+  const StreamCut cut = cut_stream(c->n_sm, slots, a.bt.n_seqs, (long long)a.bt.n_seqs * a.s.heads * tiles, (long long)a.bt.n_tokens * a.n_heads, keys);
+  launch(paged_stream_kernel<D, kQ8, kN>, cut.most_parts > 0 ? dim3((unsigned)slots) : dim3(a.bt.n_seqs, a.s.heads * tiles, (unsigned)cut.split), kStreamThreads, Y::kSmem,
+         stream, a, cut.most_parts, tiles);
   return launched(c, "paged_attend");
 }
 

@@ -26,11 +26,12 @@
 #include <cmath>
 
 #include "paged_store.cuh"
+#include "stream_cut.h"
 
 namespace scalekv {
 namespace paged {
 
-constexpr int kStreamThreads = 128, kStreamWarps = kStreamThreads / 32;
+constexpr int kStreamThreads = 32 * kStreamWarps;
 constexpr int kStreamRows = 32;                   // query rows of a sequence and kv head that go this way
 constexpr int kTileRows = 16;                     // of them a CTA takes so many, at most
 
@@ -39,13 +40,12 @@ template <int D, bool kQ8, int kN>
 struct StreamLayout {
   static constexpr int kRowBytes = D * (kQ8 ? 1 : 2);
   static constexpr int kStages = kRowBytes >= 128 ? 3 : 4;
-  static constexpr int kCtas = kRowBytes >= 256 ? 2 : kN == 2 && D == 128 ? 3 : 4;            // CTAs that an SM has room for
+  static constexpr int kCtas = stream_ctas(D, kQ8, kN);
   static constexpr int kScales = 32 * kRowBytes;                                  // offsets in a stage: K rows, V rows, the scales of both
   static constexpr int kStage = kScales + (kQ8 ? 128 : 0);
   static constexpr int kRing = kStreamWarps * kStages * kStage;
   static constexpr int kParts = kStreamWarps * 8 * kN * (D + 2) * 4;              // the warps' sums, over the ring once that is done with
   // the parts of a sequence and head that the last CTA combines: references and sums of every row, and sums of groups of threads
-  static constexpr int kMostParts = 256;
   static constexpr int kJoin = 8 * kN * (kMostParts + 1) * 8 + 8 + kStreamThreads * 32;
   static constexpr int kSmem = kRing > kParts ? (kRing > kJoin ? kRing : kJoin) : (kParts > kJoin ? kParts : kJoin);
   // where piece x (16 bytes) of row r lies
@@ -56,7 +56,6 @@ struct StreamLayout {
 };
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kRaise = 3.f;
-constexpr int kSecond = 40;                       // (64 sequences of 65 steps, 8 kv heads: 592 equal shares of 57 steps, most in two sequences, 42.1 us, 512 whole ones 34.7)
 
 struct Mask {
   int causal, window, n_sink;      // window 0: none
@@ -536,10 +535,10 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8, kN>::kCta
     }
     total *= heads;
     const int ctas = gridDim.x, items = a.bt.n_seqs * heads;
-    split = max(1, min(min(ctas / items, longest / 8), most_parts));
-    share = max((int)((total + ctas - 1) / ctas), (longest + most_parts - 2) / (most_parts - 1));
-    if (share + kSecond >= (items + ctas - 1) / ctas * ((longest + split - 1) / split)) {
-      share = 0;
+    const StreamDeal deal = deal_steps(total, longest, items, ctas, most_parts);
+    split = deal.split;
+    share = deal.share;
+    if (share == 0) {
       at = blockIdx.x;
       end = (long long)items * split;
     } else {
