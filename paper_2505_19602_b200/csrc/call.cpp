@@ -6,6 +6,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <exception>
 #include <vector>
 
@@ -86,6 +87,9 @@ bool arguments(Py_ssize_t n, Py_ssize_t want) {
   return false;
 }
 
+// A whole number.  One beyond 32 bits becomes the limit that it lies beyond, which no call takes for a layer or a scale; its low half might be one.
+int number(PyObject *obj) { return (int)std::min<long>(std::max<long>(PyLong_AsLong(obj), INT32_MIN), INT32_MAX); }
+
 #define CALL(expr)            \
   int st;                     \
   if (PyErr_Occurred()) return nullptr; \
@@ -101,7 +105,7 @@ PyObject *step(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (!arguments(n, 11) || !view(a[4], &q) || !view(a[5], &k) || !view(a[6], &v) || !view(a[7], &o) || !floats(a[8], &lse)) return nullptr;
   const auto fn = address<decltype(&scalekv_step)>(a[0]);
   const auto ctx = address<scalekv_ctx *>(a[1]);
-  const int layer = (int)PyLong_AsLong(a[2]), scale = (int)PyLong_AsLong(a[3]), w = (int)PyLong_AsLong(a[9]);
+  const int layer = number(a[2]), scale = number(a[3]), w = number(a[9]);
   const auto window = address<const int32_t *>(a[10]);
   CALL(fn(ctx, layer, scale, q, k, v, o, lse, w, window));
 }
@@ -113,7 +117,7 @@ PyObject *step_ex(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (!arguments(n, 13) || !view(a[4], &q) || !view(a[5], &k) || !view(a[6], &v) || !view(a[7], &o) || !floats(a[8], &lse)) return nullptr;
   const auto fn = address<decltype(&scalekv_step_ex)>(a[0]);
   const auto ctx = address<scalekv_ctx *>(a[1]);
-  const int layer = (int)PyLong_AsLong(a[2]), scale = (int)PyLong_AsLong(a[3]), compress = (int)PyLong_AsLong(a[9]), w = (int)PyLong_AsLong(a[10]);
+  const int layer = number(a[2]), scale = number(a[3]), compress = number(a[9]), w = number(a[10]);
   const auto window = address<const int32_t *>(a[11]);
   const auto opts = address<const scalekv_select_opts *>(a[12]);
   CALL(fn(ctx, layer, scale, q, k, v, o, lse, compress, w, window, opts));
@@ -125,7 +129,7 @@ PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (!arguments(n, 6) || !view(a[4], &k) || !view(a[5], &v)) return nullptr;
   const auto fn = address<decltype(&scalekv_append)>(a[0]);
   const auto ctx = address<scalekv_ctx *>(a[1]);
-  const int layer = (int)PyLong_AsLong(a[2]), scale = (int)PyLong_AsLong(a[3]);
+  const int layer = number(a[2]), scale = number(a[3]);
   CALL(fn(ctx, layer, scale, k, v));
 }
 
@@ -136,7 +140,7 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (!arguments(n, 6) || !view(a[3], &q) || !view(a[4], &o) || !floats(a[5], &lse)) return nullptr;
   const auto fn = address<decltype(&scalekv_attend)>(a[0]);
   const auto ctx = address<scalekv_ctx *>(a[1]);
-  const int layer = (int)PyLong_AsLong(a[2]);
+  const int layer = number(a[2]);
   CALL(fn(ctx, layer, q, o, lse));
 }
 
@@ -146,7 +150,7 @@ PyObject *compress_ex(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (!arguments(n, 8) || (a[3] != Py_None && !view(a[3], &q))) return nullptr;
   const auto fn = address<decltype(&scalekv_compress_ex)>(a[0]);
   const auto ctx = address<scalekv_ctx *>(a[1]);
-  const int layer = (int)PyLong_AsLong(a[2]), w = (int)PyLong_AsLong(a[4]), full = (int)PyLong_AsLong(a[6]);
+  const int layer = number(a[2]), w = number(a[4]), full = number(a[6]);
   const auto window = address<const int32_t *>(a[5]);
   const auto opts = address<const scalekv_select_opts *>(a[7]);
   CALL(fn(ctx, layer, q, w, window, full, opts));
@@ -174,7 +178,7 @@ PyObject *layer_stats_ex(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (!arguments(n, 8) || !view(a[3], &q)) return nullptr;
   const auto fn = address<decltype(&scalekv_layer_stats_ex)>(a[0]);
   const auto ctx = address<scalekv_ctx *>(a[1]);
-  const int layer = (int)PyLong_AsLong(a[2]), topk = (int)PyLong_AsLong(a[4]), stride = (int)PyLong_AsLong(a[5]);
+  const int layer = number(a[2]), topk = number(a[4]), stride = number(a[5]);
   const Py_ssize_t batch = PyLong_AsSsize_t(a[6]), heads = PyLong_AsSsize_t(a[7]);
   if (PyErr_Occurred()) return nullptr;
   double car = 0.0, htk = 0.0;
@@ -227,7 +231,7 @@ PyObject *paged_move(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (!arguments(n, 11)) return nullptr;
   const auto fn = address<decltype(&scalekv_paged_write)>(a[0]);
   const auto kv = address<scalekv_paged *>(a[1]);
-  const int layer = (int)PyLong_AsLong(a[2]);
+  const int layer = number(a[2]);
   const auto batch = address<const scalekv_paged_batch *>(a[3]);
   const long tokens = PyLong_AsLong(a[4]), heads = PyLong_AsLong(a[5]), dim = PyLong_AsLong(a[6]), device = PyLong_AsLong(a[7]);
   const auto stream = address<void *>(a[10]);
@@ -243,7 +247,7 @@ PyObject *paged_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (!arguments(n, 15)) return nullptr;
   const auto fn = address<decltype(&scalekv_paged_attend)>(a[0]);
   const auto kv = address<scalekv_paged *>(a[1]);
-  const int layer = (int)PyLong_AsLong(a[2]);
+  const int layer = number(a[2]);
   const auto batch = address<const scalekv_paged_batch *>(a[3]);
   const long tokens = PyLong_AsLong(a[4]), dim = PyLong_AsLong(a[5]), device = PyLong_AsLong(a[6]);
   const long window = PyLong_AsLong(a[11]), sinks = PyLong_AsLong(a[12]);
@@ -277,7 +281,7 @@ PyObject *paged_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
           return true;
         })) return nullptr;
   }
-  CALL(fn(kv, layer, batch, (int32_t)heads, q, o, lse, &mask, (float)scale, stream));
+  CALL(fn(kv, layer, batch, (int32_t)std::min<long>(heads, INT32_MAX), q, o, lse, &mask, (float)scale, stream));
 }
 
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
