@@ -220,7 +220,11 @@ class Sequences:
         self.lengths = [length + n for length, n in zip(self.lengths, new)]
 
     def trim(self, window, n_sink=0):
-        """Gives back the pages that a window with sinks hides from every token still to come."""
+        """Gives back the pages that a window with sinks hides from every token still to come; window 0 is none, and hides nothing."""
+        if window < 0 or n_sink < 0:
+            raise ValueError(f"window and n_sink must be >= 0, got {window} and {n_sink}")
+        if window == 0:
+            return
         for b, length in enumerate(self.lengths):
             for i in range(-(-n_sink // self.page_tokens), max(0, length - window + 1) // self.page_tokens):
                 if self.table[b][i] >= 0:
