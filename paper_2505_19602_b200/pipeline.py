@@ -207,6 +207,8 @@ class Sequences:
 
     def extend(self, new):
         """new[b] tokens join sequence b: pages for them, and the lengths with them in.  Raises, and changes nothing, where pages run out."""
+        if len(new) != self.n_seqs or min(new, default=0) < 0:
+            raise ValueError(f"expected {self.n_seqs} numbers of tokens, none below 0, got {new}")
         need = []
         for b, n in enumerate(new):
             last = -(-(self.lengths[b] + n) // self.page_tokens)

@@ -32,3 +32,12 @@ def test_windows_that_are_none(window, n_sink):
     with pytest.raises(ValueError):
         s.trim(window, n_sink)
     assert state(s) == before
+
+
+@pytest.mark.parametrize("new", [[1, 1], [1, 1, 1, 1], [], [1, -1, 0]])
+def test_tokens_for_every_sequence(new):
+    s = book()
+    before = state(s)
+    with pytest.raises(ValueError):
+        s.extend(new)
+    assert state(s) == before
