@@ -36,7 +36,7 @@ __device__ __forceinline__ int block_seq_of(const Batch &bt, int t) {
   int seq = 0;
   for (int i0 = 0; i0 < bt.n_seqs; i0 += kStoreThreads) {
     const int i = i0 + (int)threadIdx.x;
-    seq += __syncthreads_count(i < bt.n_seqs && __ldg(bt.starts + i + 1) <= t);
+    seq += __syncthreads_count(i < bt.n_seqs && bt.starts[i + 1] <= t);
   }
   return seq;
 }
@@ -47,12 +47,19 @@ __device__ __forceinline__ void place_tokens(const Moves &mv, int t0, int n, lon
   int seq = block_seq_of(bt, t0);
   if ((int)threadIdx.x < n) {
     const int t = t0 + (int)threadIdx.x;
-    while (seq < bt.n_seqs && __ldg(bt.starts + seq + 1) <= t) ++seq;
+    // (start, end and length side by side: one behind the other they are three trips to memory; us, a token of 8 sequences written and read back 5.4 / 5.2)
+    int start = 0, end = 0, length = 0;
+    for (; seq < bt.n_seqs; ++seq) {
+      start = bt.starts[seq];
+      end = bt.starts[seq + 1];
+      length = bt.lengths[seq];
+      if (end > t) break;
+    }
     long long at = -1;
-    if (seq >= bt.n_seqs || t < __ldg(bt.starts + seq)) {
+    if (seq >= bt.n_seqs || t < start) {
       report(mv.s.status);
     } else {
-      const int pos = __ldg(bt.lengths + seq) - __ldg(bt.starts + seq + 1) + t, page = page_of(mv.s, bt, seq, pos);
+      const int pos = length - end + t, page = page_of(mv.s, bt, seq, pos);
       if (page >= 0) at = (long long)store_row(mv.s, page, 0, pos);
     }
     row[threadIdx.x] = at;
@@ -65,7 +72,7 @@ __device__ __forceinline__ void check_starts(const Moves &mv) {
   const Batch &bt = mv.bt;
   if (blockIdx.x > 0) return;
   for (int b = threadIdx.x; b < bt.n_seqs; b += kStoreThreads)
-    if (starts_wrong(bt, b, __ldg(bt.starts + b), __ldg(bt.starts + b + 1))) report(mv.s.status);
+    if (starts_wrong(bt, b, bt.starts[b], bt.starts[b + 1])) report(mv.s.status);
 }
 
 __device__ __forceinline__ uint32_t pair_bf16(float lo, float hi) {
@@ -82,7 +89,7 @@ __device__ __forceinline__ float max_nan(float a, float b, float c) {
 // A lane's 16 values are 32 bytes of bf16, a sector: one access where they begin on 32 bytes, or two of 16 bytes, each of which meets every sector of
 // the warp's and fills it by half (us, two / one, 24 646 tokens of 16 heads written and read back: f32 204 / 167, bf16 115 / 112).
 __device__ __forceinline__ void load32(const void *p, uint4 &a, uint4 &b) {
-  asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w)
                : "l"(p));
 }
@@ -100,7 +107,7 @@ template <typename T> struct Raw16 {
       for (int i = 0; i < (int)sizeof(T); i += 2) load32(reinterpret_cast<const uint4 *>(p) + i, w[i], w[i + 1]);
     } else {
 #pragma unroll
-      for (int i = 0; i < (int)sizeof(T); ++i) w[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+      for (int i = 0; i < (int)sizeof(T); ++i) w[i] = reinterpret_cast<const uint4 *>(p)[i];
     }
   }
   __device__ __forceinline__ void numbers(float *x) const {
@@ -267,8 +274,8 @@ __global__ void __launch_bounds__(kStoreThreads) paged_read_kernel(const __grid_
       const size_t row = p.row(mv, row0[p.t]);
       const char *rows = p.is_v ? s.v_rows : s.k_rows;
       if constexpr (kQ8) {
-        const uint4 w = __ldg(reinterpret_cast<const uint4 *>(rows + row * D + x * 16));
-        const float scale = __ldg((p.is_v ? s.v_scales : s.k_scales) + row);
+        const uint4 w = __ldcg(reinterpret_cast<const uint4 *>(rows + row * D + x * 16));
+        const float scale = __ldcg((p.is_v ? s.v_scales : s.k_scales) + row);
         numbers_of(w.x, y);
         numbers_of(w.y, y + 4);
         numbers_of(w.z, y + 8);

@@ -111,9 +111,9 @@ __device__ __forceinline__ void mma_16816(float *c, const uint32_t *a, uint32_t 
 struct Span {
   int start, rows, length, first, lo, hi, n_sink, lo_step, sink_steps, steps;
   __device__ __forceinline__ Span(const AttendArgs &a, int seq, int most_rows, bool tell) {
-    start = __ldg(a.bt.starts + seq);
-    length = __ldg(a.bt.lengths + seq);
-    const int end = __ldg(a.bt.starts + seq + 1), n_new = min(end, a.bt.n_tokens) - start, room = a.bt.table_pages << a.s.page_shift;
+    start = a.bt.starts[seq];
+    length = a.bt.lengths[seq];
+    const int end = a.bt.starts[seq + 1], n_new = min(end, a.bt.n_tokens) - start, room = a.bt.table_pages << a.s.page_shift;
     if (tell && (starts_wrong(a.bt, seq, start, end) || n_new > a.max_new || (unsigned)length > (unsigned)room)) report(a.s.status);
     length = max(min(length, room), 0);                    // (what lies behind the table counts as hidden)
     first = length - n_new;                                // position of the sequence's first new token
@@ -276,7 +276,7 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
       const int dim = kQ8 ? (k >> 2) * 64 + quad * 16 + (k & 3) * 4 : (k >> 1) * 32 + quad * 8 + (k & 1) * 4;
-      q[n][k] = r < rows ? __ldg(reinterpret_cast<const uint2 *>(row + dim * 2)) : make_uint2(0u, 0u);
+      q[n][k] = r < rows ? *reinterpret_cast<const uint2 *>(row + dim * 2) : make_uint2(0u, 0u);
     }
   }
   // a step all of whose keys every row sees: [lo_full, hi_full)

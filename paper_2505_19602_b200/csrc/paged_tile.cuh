@@ -174,9 +174,9 @@ __device__ __forceinline__ Item find_item(const AttendArgs &a, int want) {
     const int b = b0 + lane;
     int n = 0, st = 0, en = 0, length = 0;
     if (b < a.bt.n_seqs) {
-      st = __ldg(a.bt.starts + b);
-      en = min(__ldg(a.bt.starts + b + 1), a.bt.n_tokens);
-      length = __ldg(a.bt.lengths + b);
+      st = a.bt.starts[b];
+      en = min(a.bt.starts[b + 1], a.bt.n_tokens);
+      length = a.bt.lengths[b];
       if (st >= 0 && en > st) n = (int)(((long long)(en - st) * a.group.d + kItemRows - 1) / kItemRows);
     }
     int incl = n;
@@ -260,9 +260,9 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     // what is out of range in the batch, of sequences that have no item, too
     wait_for_grid();
     for (int b = lane; b < a.bt.n_seqs; b += 32) {
-      const int start_b = __ldg(a.bt.starts + b), end_b = __ldg(a.bt.starts + b + 1);
+      const int start_b = a.bt.starts[b], end_b = a.bt.starts[b + 1];
       if (starts_wrong(a.bt, b, start_b, end_b) || end_b - start_b > a.max_new ||
-          (unsigned)__ldg(a.bt.lengths + b) > (unsigned)(a.bt.table_pages << s.page_shift))
+          (unsigned)a.bt.lengths[b] > (unsigned)(a.bt.table_pages << s.page_shift))
         report(status);
     }
   }
@@ -438,8 +438,8 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       const int page = __shfl_sync(0xffffffffu, pages(i), tid >> 4), pos = key_of(i) + tid;
       const bool on = page >= 0 && in_use(pos);
       const size_t row = store_row(s, max(page, 0), head, pos);
-      k_scale = on ? __ldg(s.k_scales + row) * (a.scale_log2e * kCodeUnit) : 0.f;
-      v_scale = on ? __ldg(s.v_scales + row) * kCodeUnit : 0.f;
+      k_scale = on ? __ldcg(s.k_scales + row) * (a.scale_log2e * kCodeUnit) : 0.f;
+      v_scale = on ? __ldcg(s.v_scales + row) * kCodeUnit : 0.f;
     };
     if (nt > 0 && rows > 0) fetch_scales(0);
     for (int t = 0; t < 2 * nt && rows > 0; ++t) {
@@ -496,7 +496,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         uint4 v = make_uint4(0u, 0u, 0u, 0u);
         if (i < all) {
           const int t = a.group.div(i), g = i - t * a.group.d;
-          v = __ldg(reinterpret_cast<const uint4 *>(a.Q.ptr + (start + t) * a.Q.st + (head * a.group.d + g) * a.Q.sh) + piece);
+          v = reinterpret_cast<const uint4 *>(a.Q.ptr + (start + t) * a.Q.st + (head * a.group.d + g) * a.Q.sh)[piece];
         }
         store_shared(to + r * 128 + (((piece & 7) ^ (r & 7)) << 4), v.x, v.y, v.z, v.w);
       }
@@ -777,7 +777,7 @@ __global__ void __launch_bounds__(32 * kJoinRows) paged_join_kernel(const __grid
   const bool complete = __ldcg(a.s.status) != kDevTimeout;
   const size_t row0 = (size_t)shared_item * parts * kItemRows + r;
   float m = -INFINITY;
-  for (int e = lane; e < parts; e += 32) m = fmaxf(m, __ldg(a.part_ml + (row0 + (size_t)e * kItemRows) * 2));
+  for (int e = lane; e < parts; e += 32) m = fmaxf(m, __ldcg(a.part_ml + (row0 + (size_t)e * kItemRows) * 2));
   const Item it = find_item(a, cut.n_items - 1 - e0);
   if (it.seq < 0) return;
   const int start = it.start, all = it.n_new * a.group.d, i = it.tile * kItemRows + r;
@@ -790,12 +790,12 @@ __global__ void __launch_bounds__(32 * kJoinRows) paged_join_kernel(const __grid
 #pragma unroll 8
   for (int e = 0; e < parts; ++e) {
     const size_t at = row0 + (size_t)e * kItemRows;
-    const float2 ml = __ldg(reinterpret_cast<const float2 *>(a.part_ml + at * 2));
+    const float2 ml = __ldcg(reinterpret_cast<const float2 *>(a.part_ml + at * 2));
     const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - m);
     sum += f * ml.y;
     float v[kPer];
-    if constexpr (kPer == 4) *reinterpret_cast<float4 *>(v) = __ldg(reinterpret_cast<const float4 *>(a.part_o + at * D + lane * kPer));
-    else *reinterpret_cast<float2 *>(v) = __ldg(reinterpret_cast<const float2 *>(a.part_o + at * D + lane * kPer));
+    if constexpr (kPer == 4) *reinterpret_cast<float4 *>(v) = __ldcg(reinterpret_cast<const float4 *>(a.part_o + at * D + lane * kPer));
+    else *reinterpret_cast<float2 *>(v) = __ldcg(reinterpret_cast<const float2 *>(a.part_o + at * D + lane * kPer));
 #pragma unroll
     for (int c = 0; c < kPer; ++c) acc[c] += f * v[c];
   }

@@ -28,7 +28,9 @@ struct Rows {
   long long st, sh;
 };
 
-// The grid before this one in the stream has ended, and all that it wrote is there.  First of all in every kernel but for what needs no memory.
+// The grid before this one in the stream has ended, and all that it wrote is there.  First of all in every kernel but for what needs no memory.  What is read
+// behind it may have been written while this grid was there already, so nothing goes through the read-only path (__ldg, ld.global.nc), which is for memory that
+// nobody writes as long as the grid lives.
 __device__ __forceinline__ void wait_for_grid() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // The grid behind this one may be set up where it finds room.
 __device__ __forceinline__ void next_grid() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
@@ -45,7 +47,7 @@ __device__ __forceinline__ bool starts_wrong(const Batch &bt, int b, int start, 
 __device__ __forceinline__ int page_of(const Store &s, const Batch &bt, int b, int pos) {
   const int i = pos >> s.page_shift;
   int page = -1;
-  if (pos >= 0 && i < bt.table_pages) page = __ldg(bt.table + (size_t)b * bt.table_ld + i);
+  if (pos >= 0 && i < bt.table_pages) page = bt.table[(size_t)b * bt.table_ld + i];
   if ((unsigned)page >= (unsigned)s.n_pages) { report(s.status); return -1; }
   return page;
 }
