@@ -161,8 +161,8 @@ __device__ __forceinline__ float scale_of(float a) {
 // Codes of 16 values: x / s rounded to fp32 and then to an integer, half to even.  The quotient by Markstein's theorem (IBM J. Res. Dev. 34, 1990): with r the
 // rounded reciprocal, q within a unit in the last place of the quotient and e = x - q s, which a fused multiply-add gives exactly, q + e r is the rounded
 // quotient.  x r is within two units, one such step makes that one, a second the result.  Rows of bf16 need no second: with 8 bits of significand in x and in the
-// row's largest value there are few enough quotients to go through all of them (none of 614 592 codes differs; without the first step 72 do).  (A division for
-// each of them took the larger part of the kernel's time.)  Adding 1.5 2^23 rounds to an integer and leaves its low byte in the sum's.  A small scale is lifted first, so that nothing underflows, and its values
+// row's largest value there are few enough quotients to go through all of them: none of 14 507 841 gives another code than a division (614 592 at scales as they
+// are, where 72 do without the first step, and 13 893 249 at lifted ones).  (A division for each of them took the larger part of the kernel's time.)  Adding 1.5 2^23 rounds to an integer and leaves its low byte in the sum's.  A small scale is lifted first, so that nothing underflows, and its values
 // are cut off where the codes end, which a rounded subnormal scale leaves below the largest of them.
 template <int kSteps> __device__ __forceinline__ uint4 codes_of(float *x, float s) {
   if (!(s > 0.f)) return make_uint4(0u, 0u, 0u, 0u);
