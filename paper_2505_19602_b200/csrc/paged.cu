@@ -242,6 +242,7 @@ scalekv_status scalekv_paged_init(const scalekv_paged_config *cfg, scalekv_paged
   while ((1 << c->page_shift) < cfg->page_tokens) ++c->page_shift;
   if (cudaSetDevice(cfg->device) != cudaSuccess ||
       cudaDeviceGetAttribute(&c->n_sm, cudaDevAttrMultiProcessorCount, cfg->device) != cudaSuccess ||
+      cudaDeviceSynchronize() != cudaSuccess ||            // (whoever had this memory before may still be at work, on any stream)
       cudaMemset(cfg->workspace, 0, kStatusBytes + kMaxCounts * 4) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
     fprintf(stderr, "scalekv_paged_init: %s\n", cudaGetErrorString(cudaGetLastError()));
     delete c;
