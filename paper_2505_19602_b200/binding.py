@@ -584,6 +584,7 @@ class PagedKV:
             raise ValueError(f"pool must be a contiguous uint8 tensor on {self.device}")
         self.pool = pool
         self.workspace = torch.empty(wb.value, dtype=torch.uint8, device=self.device)
+        self._streams = set()                              # that have been seen
         cfg.pool, cfg.pool_bytes = pool.data_ptr(), pool.numel()
         cfg.workspace, cfg.workspace_bytes = self.workspace.data_ptr(), wb.value
         self.handle = C.c_void_p(None)
@@ -598,7 +599,12 @@ class PagedKV:
             raise ScaleKVError(st, self.lib.scalekv_paged_error_string(self.handle).decode())
 
     def _stream(self):
-        return torch._C._cuda_getCurrentRawStream(self.device_index)
+        stream = torch._C._cuda_getCurrentRawStream(self.device_index)
+        if stream not in self._streams:                    # the allocator has to know who works with this memory, or it gives it away too early
+            self._streams.add(stream)
+            for t in (self.pool, self.workspace):
+                t.record_stream(torch.cuda.current_stream(self.device))
+        return stream
 
     def close(self):
         if getattr(self, "handle", None) and self.handle.value:
