@@ -75,11 +75,6 @@ __device__ __forceinline__ void check_starts(const Moves &mv) {
     if (starts_wrong(bt, b, bt.starts[b], bt.starts[b + 1])) report(mv.s.status);
 }
 
-__device__ __forceinline__ uint32_t pair_bf16(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
 // (NaN if any of them is)
 __device__ __forceinline__ float max_nan(float a, float b, float c) {
   float r;
@@ -130,8 +125,8 @@ __device__ __forceinline__ void store16(__nv_bfloat16 *p, const float *x, bool w
   uint4 w[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i)
-    w[i] = make_uint4(pair_bf16(x[8 * i], x[8 * i + 1]), pair_bf16(x[8 * i + 2], x[8 * i + 3]), pair_bf16(x[8 * i + 4], x[8 * i + 5]),
-                      pair_bf16(x[8 * i + 6], x[8 * i + 7]));
+    w[i] = make_uint4(tc::pack_bf16(x[8 * i], x[8 * i + 1]), tc::pack_bf16(x[8 * i + 2], x[8 * i + 3]), tc::pack_bf16(x[8 * i + 4], x[8 * i + 5]),
+                      tc::pack_bf16(x[8 * i + 6], x[8 * i + 7]));
   if (wide) {
     store32(p, w[0], w[1]);
   } else {

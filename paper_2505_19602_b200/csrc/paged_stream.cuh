@@ -79,12 +79,6 @@ struct AttendArgs {
 __device__ __forceinline__ int seen_hi(const Mask &m, int p, int length) { return m.causal ? max(min(p + 1, length), 0) : length; }
 __device__ __forceinline__ int seen_lo(const Mask &m, int p) { return m.window > 0 ? max(p - m.window + 1, 0) : 0; }
 
-__device__ __forceinline__ float exp2_approx(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 // Codes as bf16, exactly and without a conversion instruction: a byte u = c + 128 (the code with its sign bit turned) alone in 16 bits is the
 // subnormal u 2^-133, so one fused multiply-add gives u 2^-133 2^127 - 2 = c 2^-6.  The 2^6 goes into the factor that the scale is anyway.
 constexpr float kCodeUnit = 64.f;
@@ -150,7 +144,7 @@ __device__ __forceinline__ void place_row(const AttendArgs &a, int start, int he
 __device__ __forceinline__ void put_row(const AttendArgs &a, int t, int h, int piece, const float *acc, float2 ml) {
   const float inv = ml.y == 0.f ? 0.f : 1.f / ml.y;
   *(reinterpret_cast<uint4 *>(a.O.ptr + t * a.O.st + h * a.O.sh) + piece) =
-      make_uint4(pair_bf16(acc[0] * inv, acc[1] * inv), pair_bf16(acc[2] * inv, acc[3] * inv), pair_bf16(acc[4] * inv, acc[5] * inv), pair_bf16(acc[6] * inv, acc[7] * inv));
+      make_uint4(tc::pack_bf16(acc[0] * inv, acc[1] * inv), tc::pack_bf16(acc[2] * inv, acc[3] * inv), tc::pack_bf16(acc[4] * inv, acc[5] * inv), tc::pack_bf16(acc[6] * inv, acc[7] * inv));
   if (piece == 0 && a.lse != nullptr) a.lse[(size_t)t * a.n_heads + h] = ml.y == 0.f ? -INFINITY : (ml.x + log2f(ml.y)) * kLn2;
 }
 
@@ -176,7 +170,7 @@ __device__ __noinline__ void join_parts(const AttendArgs &a, int start, int row0
     for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
     for (int e = lane; e < parts; e += 32) {
       const float2 x = ml[r * parts + e];
-      const float f = exp2_approx(x.x - top);
+      const float f = tc::ex2(x.x - top);
       sum += f * x.y;
       ml[r * parts + e].x = f;
     }
@@ -361,7 +355,7 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
           float raised = fmaxf(fmaxf(x[n][e], x[n][2 + e]), m[n][e]);
 #pragma unroll
           for (int d = 4; d < 32; d *= 2) raised = fmaxf(raised, __shfl_xor_sync(0xffffffffu, raised, d));
-          const float f = exp2_approx(m[n][e] - raised);
+          const float f = tc::ex2(m[n][e] - raised);
           m[n][e] = raised;
           l[n][e] *= f;
 #pragma unroll
@@ -375,7 +369,7 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
     for (int n = 0; n < kN; ++n) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        x[n][e] = exp2_approx(x[n][e] - m[n][e & 1]);
+        x[n][e] = tc::ex2(x[n][e] - m[n][e & 1]);
         l[n][e & 1] += x[n][e];
       }
       float y[4] = {x[n][0] * vs0, x[n][1] * vs0, x[n][2] * vs1, x[n][3] * vs1};
@@ -386,9 +380,9 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const uint32_t most = pair_bf16(y[2 * i], y[2 * i + 1]);
+        const uint32_t most = tc::pack_bf16(y[2 * i], y[2 * i + 1]);
         p[n][i] = transpose_8x8(most);
-        rest[n][i] = transpose_8x8(pair_bf16(y[2 * i] - __uint_as_float(most << 16), y[2 * i + 1] - __uint_as_float(most & 0xffff0000u)));
+        rest[n][i] = transpose_8x8(tc::pack_bf16(y[2 * i] - __uint_as_float(most << 16), y[2 * i + 1] - __uint_as_float(most & 0xffff0000u)));
       }
     }
     // O^T += V^T P^T
@@ -468,7 +462,7 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
 #pragma unroll
     for (int w = 0; w < kStreamWarps; ++w) {
       const float2 x = *reinterpret_cast<const float2 *>(ml_smem + (w * kRows + r) * 2);
-      const float f = exp2_approx(x.x - top);
+      const float f = tc::ex2(x.x - top);
       sum += f * x.y;
       const float4 *v = reinterpret_cast<const float4 *>(o_smem + (w * kRows + r) * D + piece * 8);
       const float4 lo = v[0], hi = v[1];
