@@ -445,7 +445,8 @@ scalekv_status scalekv_paged_read(scalekv_paged *kv, int32_t layer, const scalek
  * nothing gets O = 0 and lse = -inf.  softmax_scale 0: 1 / sqrt(head_dim).  Products are exact, sums are fp32; P is rounded to
  * bf16 before its product with V where some sequence may bring more than 32 query rows to a kv head (max_new times the heads of the
  * group), and goes into it as two pieces of bf16 otherwise.  What hidden keys hold never matters, whatever it is, with one exception:
- * a bf16 row of V that one query of the call sees must be finite, or queries from which it is hidden may get NaN too. */
+ * a bf16 row of V that one query of the call sees must be finite, or queries from which it is hidden may get NaN too.  Sums are formed
+ * relative to a reference that lies up to 2^8 below a row's largest product: values beyond about 2^100 may overflow in them. */
 scalekv_status scalekv_paged_attend(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, int32_t n_heads,
                                     scalekv_rows Q, scalekv_rows O, float *lse, const scalekv_paged_mask *mask,
                                     float softmax_scale, void *stream);
