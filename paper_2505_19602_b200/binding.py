@@ -561,7 +561,9 @@ class PagedBatch:
 
 class PagedKV:
     """Owns the pool and the workspace of a paged token cache (torch tensors; `pool`: a uint8 tensor of the caller's instead) and one
-    library handle.  Every call runs on PyTorch's current stream of the device."""
+    library handle.  Every call runs on PyTorch's current stream of the device.  What calls on different streams share is for the caller to
+    order, as with any tensor: the rows of the pool, and the workspace, which every attend of the handle uses (two of them at once would join each other's
+    parts, and leave counters behind that are wrong for later ones)."""
 
     def __init__(self, n_layers, n_pages, n_kv_heads, head_dim, store="q8", page_tokens=64, device=0, pool=None):
         if not torch.cuda.is_available():

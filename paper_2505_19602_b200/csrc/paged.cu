@@ -152,8 +152,10 @@ scalekv_status launch_tile(scalekv_paged *c, int layer, const AttendArgs &a, int
   using Y = TileLayout<D, kQ8>;
   // An item and kv head to a CTA.  Those that do not fill the SMs are shared by as many CTAs as find one, each with two key tiles or more (us, 20 tokens behind
   // 8 192 entries, 8 kv heads in codes, 1 / 2 / 4 / 8 / 16 / 32 CTAs an item: 202 / 108 / 60 / 35 / 25 / 26), and so are those of the last, partial wave (2 x 16 heads, bf16, 1 400
-  // queries over 1 500 / 3 000 / 5 000 entries, alone: 82 / 127 / 187, shared: 77 / 108 / 151; with fewer than 16 key tiles the launch that joins them can cost more than it
-  // gives: chunks beside single tokens under a window of 700, 56 alone, 61 shared).
+  // queries over 1 500 / 3 000 / 5 000 entries, alone: 82 / 127 / 187, shared: 77 / 108 / 151).  Not with fewer than 16 key tiles: of a causal chunk the last wave are the items that see least, and
+  // the launch that joins them can cost more than it gives (us, alone / shared: chunks beside single tokens under a window of 700 56 / 61; 2 x 1 400 causal queries of 16 heads behind 100 entries,
+  // 44 of 192 items, in bf16 58 / 69, in codes 63 / 77; behind 800, 18 tiles, 84 / 86 and 94 / 98, behind 1 600 105 / 101 and 124 / 119).  What that leaves out: 12 last items with 10 CTAs each,
+  // 10 x 256 queries of 16 heads behind 444 / 944 entries, in bf16 64 / 61 and 79 / 69, in codes 67 / 63 and 88 / 75.
   const int n = items * a.s.heads, sms = (int)std::min<long long>(c->n_sm, kPartRows / kItemRows), last = n % sms;
   const long long tiles = (keys + kTileKeys - 1) / kTileKeys;
   int parts = last ? (int)std::min<long long>(sms / last, tiles / 2) : 1;
@@ -314,8 +316,10 @@ scalekv_status scalekv_paged_attend(scalekv_paged *kv, int32_t layer, const scal
   if (a.mask.window > 0) keys = std::min<long long>(keys, (long long)a.mask.window + batch->max_new + a.mask.n_sink);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool q8 = c->cfg.store == SCALEKV_STORE_Q8;
-  // Up to 32 query rows stream (us, 64 heads, 8 kv heads in codes, 8 000 entries, streamed / on the tensor cores' tiles: 3 new tokens of 32 sequences 293 / 403, of 8 86 / 112,
-  // of one 24.6 / 23.0; 6 new tokens 437 / 405, 121 / 113, 29 / 24).
+  // Up to 32 query rows stream.  (us, 64 heads, 8 kv heads of 128, 8 000 entries, streamed / on the tensor cores' tiles, one / 8 / 32 sequences.  Codes: 16 rows 23.7 / 23.5, 54 / 117, 149 / 420; 24 rows
+  // 24.9 / 23.6, 86 / 117, 268 / 420; 32 rows 25.0 / 23.7, 87 / 117, 270 / 420; 40 rows 29.4 / 24.0, 121 / 118, 394 / 421; 64 rows 32 / 25, 148 / 119, 519 / 423.  bf16: 16 rows 25.8 / 20.8, 61 / 63, 189 / 202;
+  // 24 rows 27.1 / 21.2, 96 / 64, 370 / 203; 32 rows 27.2 / 21.6, 96 / 65, 370 / 204; 64 rows 34 / 26, 191 / 69, 700 / 211.  By time alone bf16 rows would stream up to 16; up to 32 they do for the
+  // sake of P, which the tiles round to bf16.)
   if (max_rows <= kStreamRows) {
     auto go = [&](auto dim, auto codes) {
       constexpr int kD = decltype(dim)::value;

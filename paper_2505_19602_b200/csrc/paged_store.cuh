@@ -9,7 +9,7 @@
 // tokens, all heads of K and V of them: one thread to a token finds its place, then the rows follow one another as they do in a dense tensor.
 // us per pass, eight values a lane and every row's place looked up by its own lanes / so: 84 168 tokens of 8 heads in codes read as bf16 118 / 92 (5.7 of 6.46 TB/s
 // measured), 24 646 of 16 heads written and read back 228 / 112: writing takes 57 of that for 303 MB,
-// bound by its instructions (73 of 100 issue slots).
+// bound by its instructions (71 of 100 issue slots).
 #pragma once
 #include <math_constants.h>
 

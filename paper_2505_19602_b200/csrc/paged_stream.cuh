@@ -19,8 +19,8 @@
 // The running maximum of a row is raised when a step exceeds it by more than 2^3, and the sums with it: P stays below that.
 // A CTA's four warps take the steps in turn and are combined in shared memory.  Where a sequence's heads are few, gridDim.z CTAs share its
 // keys; each leaves its part in the workspace, and the last one to do so, by a counter that it sets back, combines them in their order.
-// 32 sequences of up to 10 521 entries, 32 heads, 8 kv heads in codes: 115 us, 4.4 TB/s of 6.46 measured; SMs that still have work read 21 of 23.6 bytes a cycle and issue in
-// 55 of 100; the rest is beginnings, ends and what is left of balance.  One sequence of 170 521 bf16 entries, 16 heads: 247 us, 5.7 TB/s.
+// 32 sequences of up to 10 521 entries, 32 heads, 8 kv heads in codes: 114 us, 4.4 TB/s of 6.46 measured; SMs that still have work read 21 of 23.6 bytes a cycle and issue in
+// 55 of 100; the rest is beginnings, ends and what is left of balance.  One sequence of 170 521 bf16 entries, 16 heads: 228 us, 6.1 TB/s.
 #pragma once
 #include <cfloat>
 #include <cmath>

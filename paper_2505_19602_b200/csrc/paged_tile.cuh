@@ -13,16 +13,17 @@
 //   warps 4-7     : with codes only, converters, which put the codes of a stage back into it as bf16 (exactly: codes_bf16) and bring the scales.
 //   the last eight: softmax, a warpgroup for each tile, a thread for each row (TMEM lane): one sweep over its 128 products in
 //                   four chunks of 32, exponentials against a lazy reference, which rises when one exceeds it by more than 2^8, P as bf16 over the products already
-//                   read.  With codes a key's scale is a factor of its column: K's is part of the factor of the exponent's FMA, V's multiplies P
-//                   before it is rounded; both come from shared memory, four columns to a load.  (A thread with a quarter of the columns of four rows loads a quarter as many
+//                   read (rounded: in two pieces, as few rows have it, its product would be twice as long, half as much again of all products).  With codes
+//                   a key's scale is a factor of its column: K's is part of the factor of the exponent's FMA, V's multiplies P before it is rounded; both come from shared memory, four columns to a load.  (A thread with a quarter of the columns of four rows loads a quarter as many
 //                   scales, but its sweep was the longer: 1 478 us for what was 1 247.)
 // Rows that no query of the item sees (behind the length, ahead of the window, on a page out of range) may hold anything.  Their products are hidden one
 // by one; as values codes are numbers whatever they are, and bf16 rows are zeroed by the issuer before the product reads them.
-// Every wait is bounded; one that gives up raises the sticky status and all roles fall through to the end.
+// Every wait is bounded; one that gives up raises the sticky status and all roles fall through to the end, behind the copies and products that are
+// under way.
 // What bounds it: with bf16 rows the two chains  S -> sweep -> P V, 3 750 cycles a step of a pair (2 048 at the tensor peak, and as many for its
-// exponentials): 4 096 queries of 2 x 16 heads over 10 521 entries in 705 us, 1.00 PFLOP/s.  With codes shared memory, too: of a step's 5 000 cycles the
+// exponentials): 4 096 queries of 2 x 16 heads over 10 521 entries in 717 us, 0.99 PFLOP/s.  With codes shared memory, too: of a step's 5 000 cycles the
 // products read for 1 540 and the threads take 2 860, about 2 050 of these for the scales (a 16-byte load takes a warp four cycles, the same address or not;
-// without them 1 230 us were 1 020), the rest for the converters.  2 048 queries of 4 x 32 heads behind 6 144 entries: 1 090 us, 0.88 PFLOP/s; the same in
+// without them 1 230 us were 1 020), the rest for the converters.  2 048 queries of 4 x 32 heads behind 6 144 entries: 1 124 us, 0.86 PFLOP/s; the same in
 // bf16 1 000.
 #pragma once
 #include <string>

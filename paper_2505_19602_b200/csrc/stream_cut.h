@@ -17,7 +17,10 @@ constexpr long long kPartRows = 148 * 256;
 constexpr int kMaxCounts = 4096;                  // sequences times kv heads of a launch whose keys are shared
 constexpr int kMostParts = 256;                   // of a sequence and head: what the last CTA's shared memory has room for
 constexpr int kStreamWarps = 4;                   // of a CTA
-constexpr int kSecond = 40;                       // (64 sequences of 65 steps, 8 kv heads: 592 equal shares of 57 steps, most in two sequences, 42.1 us, 512 whole ones 34.7)
+// What a share that begins in one sequence and ends in the next costs a CTA beyond a whole part, in steps.  (us, 8 kv heads in codes, n sequences of two fifths of L to L entries, equal
+// parts / equal shares: 32 x 10 521 131.1 / 105.6, 32 x 6 000 80.2 / 68.4, 64 x 6 000 141.9 / 119.6, 64 x 3 000 75.2 / 71.3, 100 x 3 000 107.0 / 102.9, and the other way round 64 x 1 500
+// 42.2 / 47.3, 64 all of 2 000 60.2 / 67.7.  Not the better side: 32 x 3 000 46.6 / 43.6 has parts, 100 x 1 500 60.4 / 64.6 and 200 x 1 500 104.5 / 118.4 shares.)
+constexpr int kSecond = 40;
 
 // CTAs that an SM has room for: n: n-tiles of eight query rows
 constexpr int stream_ctas(int head_dim, bool q8, int n) { return head_dim * (q8 ? 1 : 2) >= 256 ? 2 : n == 2 && head_dim == 128 ? 3 : 4; }
