@@ -31,12 +31,19 @@ struct Moves {
   int wide;                                      // every 16 values of the dense tensors begin on 32 bytes
 };
 
-// The first sequence that ends behind token t (n_seqs: none does).  All threads of the block, same t.
-__device__ __forceinline__ int block_seq_of(const Batch &bt, int t) {
+// The first sequence that ends behind token t (n_seqs: none does).  All threads of the block, same t.  A launch's first block tells of starts that are out of
+// order.
+__device__ __forceinline__ int block_seq_of(const Batch &bt, int t, int *status) {
   int seq = 0;
   for (int i0 = 0; i0 < bt.n_seqs; i0 += kStoreThreads) {
     const int i = i0 + (int)threadIdx.x;
-    seq += __syncthreads_count(i < bt.n_seqs && bt.starts[i + 1] <= t);
+    bool ended = false;
+    if (i < bt.n_seqs) {
+      const int end = bt.starts[i + 1];
+      if (blockIdx.x == 0 && starts_wrong(bt, i, bt.starts[i], end)) report(status);
+      ended = end <= t;
+    }
+    seq += __syncthreads_count(ended);
   }
   return seq;
 }
@@ -44,7 +51,7 @@ __device__ __forceinline__ int block_seq_of(const Batch &bt, int t) {
 // Row of head 0 of the block's tokens, in K as in V; -1 (reported) where a token belongs to no sequence or its page is out of range.
 __device__ __forceinline__ void place_tokens(const Moves &mv, int t0, int n, long long *row) {
   const Batch &bt = mv.bt;
-  int seq = block_seq_of(bt, t0);
+  int seq = block_seq_of(bt, t0, mv.s.status);
   if ((int)threadIdx.x < n) {
     const int t = t0 + (int)threadIdx.x;
     // (start, end and length side by side: one behind the other they are three trips to memory; us, a token of 8 sequences written and read back 5.4 / 5.2)
@@ -65,14 +72,6 @@ __device__ __forceinline__ void place_tokens(const Moves &mv, int t0, int n, lon
     row[threadIdx.x] = at;
   }
   __syncthreads();
-}
-
-// Tells of starts that are out of order, at the end of a launch's first block: their lines are at hand by then.
-__device__ __forceinline__ void check_starts(const Moves &mv) {
-  const Batch &bt = mv.bt;
-  if (blockIdx.x > 0) return;
-  for (int b = threadIdx.x; b < bt.n_seqs; b += kStoreThreads)
-    if (starts_wrong(bt, b, bt.starts[b], bt.starts[b + 1])) report(mv.s.status);
 }
 
 // (NaN if any of them is)
@@ -247,7 +246,6 @@ __global__ void __launch_bounds__(kStoreThreads) paged_write_kernel(const __grid
     }
     p = next;
   }
-  check_starts(mv);
 }
 
 template <typename T, int D, bool kQ8>
@@ -285,7 +283,6 @@ __global__ void __launch_bounds__(kStoreThreads) paged_read_kernel(const __grid_
     }
     store16(p.dense<T>(mv, t0) + x * 16, y, mv.wide);
   }
-  check_starts(mv);
 }
 
 }  // namespace paged
