@@ -451,6 +451,67 @@ scalekv_status scalekv_paged_attend(scalekv_paged *kv, int32_t layer, const scal
                                     scalekv_rows Q, scalekv_rows O, float *lse, const scalekv_paged_mask *mask,
                                     float softmax_scale, void *stream);
 
+/* ---- rows with their positions in them */
+
+/* How rows of Q and K turn by their positions: pair i of dimensions, (x, y), becomes (x cos f - y sin f, x sin f + y cos f) with
+ * f = frequency[i] times the token's position on axis[i].  Pair i is dimensions i and i + n_pairs, or, adjacent != 0, 2 i and 2 i + 1;
+ * dimensions from 2 n_pairs on stay as they are.  Several axes (time, height, width) share the pairs in any way; how much a pair
+ * turns for a position is the caller's, too. */
+typedef struct {
+  int32_t n_pairs;        /* a multiple of 8, from 8 to head_dim / 2                                    */
+  int32_t n_axes;         /* 1 .. 64                                                                    */
+  int32_t adjacent;
+  uint8_t axis[64];       /* below n_axes                                                               */
+  double frequency[64];   /* radians for each position, within [-1024, 1024]                            */
+} scalekv_rotary;
+
+/* scalekv_paged_write with the rows turned: K (in fp32, then held as the cache holds rows) and V join the cache, Q with its n_heads
+ * heads (any number; 0: no queries, Q and Q_out are not looked at) goes to Q_out, bf16 rows as an attend takes them, which may be Q itself where
+ * that is bf16.  positions: device, position of token t on axis x at positions[x * axis_stride + t], any 32-bit number.  Angles are formed in
+ * 64 bits: one is off by 2^-22 radians and 2^-52 of itself at most.  A position is the caller's alone, and need not be the place in the cache. */
+scalekv_status scalekv_paged_write_rotated(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, int32_t n_heads,
+                                           scalekv_rows Q, scalekv_rows Q_out, scalekv_rows K, scalekv_rows V, int32_t dtype,
+                                           const scalekv_rotary *rotary, const int32_t *positions, int64_t axis_stride,
+                                           void *stream);
+
+/* ---- drafts: tokens that may or may not stay */
+
+/* Attention of a draft: a sequence's new tokens see every entry before them, and of one another what `tree` says: token i (row
+ * t = starts[b] + i) sees new token j if bit j mod 32 of tree[t * tree_words + j / 32] is set (device; 32 tree_words >= max_new; bits from the
+ * number of new tokens on count for nothing).  For tokens that form a tree those are its ancestors and itself.  The rest is as with
+ * scalekv_paged_attend; of bf16 rows of V the draft's own must all be finite. */
+scalekv_status scalekv_paged_attend_tree(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, int32_t n_heads,
+                                         scalekv_rows Q, scalekv_rows O, float *lse, const int32_t *tree, int32_t tree_words,
+                                         float softmax_scale, void *stream);
+
+/* What is accepted of a draft moves up: of sequence b new token path[b * path_stride + i], i < counts[b] <= path_len, becomes the i'th
+ * behind what was there before (path, counts: device; a path ascends).  layer -1: in all layers.  The lengths are the caller's: lengths[b] less the
+ * new tokens, plus counts[b], once all layers are done.  A path that does not ascend, or names no new token, or a place whose page is out of range
+ * is reported, and it and what is behind it in the path stay where they are; so does all of a sequence whose count is out of range. */
+scalekv_status scalekv_paged_accept(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, const int32_t *path,
+                                    int32_t path_stride, int32_t path_len, const int32_t *counts, void *stream);
+
+/* ---- eviction: the entries that get the least attention leave */
+
+/* Adds to every entry the attention that the new tokens pay it.  weights: device, 16-byte aligned, one float for every row of the layer's K,
+ * [page][kv head][row of the page].  Of an entry that some new token of its sequence sees (an entry before them: weights = decay weights + p, a
+ * new one: weights = p), p = sum of exp(scale q.k - lse) over the new tokens that see it and the heads of its group; the others keep theirs.  lse: dense
+ * [n_tokens][n_heads], as scalekv_paged_attend fills it for the same batch, Q, mask and scale; a row whose lse is -inf pays nothing.  decay in [0, 1].
+ * Products are exact, sums are fp32 and always in the same order. */
+scalekv_status scalekv_paged_weigh(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, int32_t n_heads,
+                                   scalekv_rows Q, const float *lse, const scalekv_paged_mask *mask, float softmax_scale,
+                                   float *weights, float decay, void *stream);
+
+/* Of every sequence and kv head min(keep[b], lengths[b]) entries stay: the first n_sink, the last n_recent (as many as there is room for
+ * beside those) and of the rest those with the largest weights, of equal ones the first (a NaN counts as -inf).  They are copied, in their
+ * order, to positions 0, 1, .. of the pages that to_table names (to_pages of its to_stride entries for a sequence), K, V and weights alike; every kv head
+ * keeps entries of its own.  kept: device [n_seqs][n_kv_heads][kept_stride], receives the positions that stay, ascending.  Only table and lengths of the batch are looked
+ * at.  A page of to_table must not be one that the call reads; what was held in the old pages stays there.  A sequence whose keep is negative, or of
+ * which more would stay than kept_len or to_pages have room for, is reported and left out. */
+scalekv_status scalekv_paged_evict(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, const int32_t *to_table,
+                                   int32_t to_stride, int32_t to_pages, const int32_t *keep, float *weights, int32_t n_sink,
+                                   int32_t n_recent, int32_t *kept, int32_t kept_stride, int32_t kept_len, void *stream);
+
 /* Waits for the stream; returns the handle's sticky device status (OK, TIMEOUT or DEVICE_CHECK). */
 scalekv_status scalekv_paged_sync(scalekv_paged *kv, void *stream);
 /* Number of kernels this handle has launched (HOST out). */

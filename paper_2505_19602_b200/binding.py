@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import hashlib
+import math
 import os
 import subprocess
 import sysconfig
@@ -17,8 +18,8 @@ import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libscalekv.so")
-SOURCES = [os.path.join(_HERE, "csrc", f) for f in ("scalekv.cu", "select_static.cu", "paged.cu", "kernels_simt.cuh", "attend_tc.cuh", "attend_f32.cuh",
-                                                 "key_split.h", "stream_cut.h", "tc.cuh", "common.cuh", "paged_view.cuh", "paged_store.cuh", "paged_stream.cuh", "paged_tile.cuh")]
+SOURCES = [os.path.join(_HERE, "csrc", f) for f in ("scalekv.cu", "select_static.cu", "paged.cu", "paged_tree.cu", "paged_rotate.cu", "paged_weigh.cu", "paged_keep.cu", "kernels_simt.cuh", "attend_tc.cuh", "attend_f32.cuh",
+                                                 "key_split.h", "stream_cut.h", "tc.cuh", "common.cuh", "paged_view.cuh", "paged_store.cuh", "paged_stream.cuh", "paged_tile.cuh", "paged_host.cuh", "paged_attend.cuh")]
 HEADER = os.path.join(os.path.dirname(_HERE), "include", "scalekv.h")
 CALL_SOURCE = os.path.join(_HERE, "csrc", "call.cpp")
 
@@ -79,6 +80,10 @@ class scalekv_paged_mask(C.Structure):
     _fields_ = [("causal", C.c_int32), ("window", C.c_int32), ("n_sink", C.c_int32)]
 
 
+class scalekv_rotary(C.Structure):
+    _fields_ = [("n_pairs", C.c_int32), ("n_axes", C.c_int32), ("adjacent", C.c_int32), ("axis", C.c_uint8 * 64), ("frequency", C.c_double * 64)]
+
+
 def build_library(force=False, verbose=False):
     """Compiles the CUDA sources for sm_100a into libscalekv.so, and the native module of the hot calls (both in-tree), when out
     of date."""
@@ -88,7 +93,7 @@ def build_library(force=False, verbose=False):
         if os.path.getmtime(LIB_PATH) >= newest:
             return LIB_PATH
     cmd = ["nvcc", "-shared", "-Xcompiler", "-fPIC", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-           "-O3", "-std=c++17", "--threads", "3", *(f for f in SOURCES if f.endswith(".cu")), "-o", LIB_PATH]
+           "-O3", "-std=c++17", "--threads", "0", *(f for f in SOURCES if f.endswith(".cu")), "-o", LIB_PATH]
     if verbose:
         cmd.insert(1, "-Xptxas=-v")
     res = subprocess.run(cmd, capture_output=True, text=True)
@@ -195,6 +200,15 @@ def load_library():
         "scalekv_paged_read": [ctx_p, i32, P(scalekv_paged_batch), scalekv_rows, scalekv_rows, i32, C.c_void_p],
         "scalekv_paged_attend": [ctx_p, i32, P(scalekv_paged_batch), i32, scalekv_rows, scalekv_rows, C.c_void_p,
                                  P(scalekv_paged_mask), C.c_float, C.c_void_p],
+        "scalekv_paged_write_rotated": [ctx_p, i32, P(scalekv_paged_batch), i32, scalekv_rows, scalekv_rows, scalekv_rows, scalekv_rows,
+                                        i32, P(scalekv_rotary), C.c_void_p, i64, C.c_void_p],
+        "scalekv_paged_attend_tree": [ctx_p, i32, P(scalekv_paged_batch), i32, scalekv_rows, scalekv_rows, C.c_void_p, C.c_void_p, i32,
+                                      C.c_float, C.c_void_p],
+        "scalekv_paged_accept": [ctx_p, i32, P(scalekv_paged_batch), C.c_void_p, i32, i32, C.c_void_p, C.c_void_p],
+        "scalekv_paged_weigh": [ctx_p, i32, P(scalekv_paged_batch), i32, scalekv_rows, C.c_void_p, P(scalekv_paged_mask), C.c_float,
+                                C.c_void_p, C.c_float, C.c_void_p],
+        "scalekv_paged_evict": [ctx_p, i32, P(scalekv_paged_batch), C.c_void_p, i32, i32, C.c_void_p, C.c_void_p, i32, i32, C.c_void_p,
+                                i32, i32, C.c_void_p],
         "scalekv_paged_sync": [ctx_p, C.c_void_p],
         "scalekv_paged_launch_count": [ctx_p, P(i64)],
         "scalekv_select_static": [C.c_void_p, i32, i32, i32, i32, C.c_void_p, C.c_void_p],
@@ -559,6 +573,29 @@ class PagedBatch:
         self.address = C.addressof(self.struct)
 
 
+class Rotary:
+    """How Q and K turn by their positions (scalekv_rotary): sections[x] pairs of dimensions turn by axis x, in all a multiple of 8 and half of
+    head_dim at most; dimensions behind those pairs stay.  Pair i turns by theta^(-i / pairs) for each position, counted over all pairs or,
+    own_range, over those of its axis.  The pairs of an axis lie together or, in_turn, the axes take turns as long as they have some.  A pair is dimensions i and
+    i + pairs or, adjacent, 2 i and 2 i + 1."""
+
+    def __init__(self, sections, theta=10000.0, own_range=False, in_turn=False, adjacent=False):
+        sections, n = [int(s) for s in sections], sum(int(s) for s in sections)
+        if not 1 <= len(sections) <= 64 or min(sections) < 0 or n % 8 or not 8 <= n <= 64:
+            raise ValueError(f"sections must be numbers of pairs, in all a multiple of 8 from 8 to 64, got {sections}")
+        if not (math.isfinite(theta) and theta > 0):
+            raise ValueError(f"theta must be a positive number, got {theta}")
+        places = [(j, x) for x, s in enumerate(sections) for j in range(s)]      # the j'th pair of axis x
+        if in_turn:
+            places.sort()
+        self.n_pairs, self.n_axes = n, len(sections)
+        self.struct = scalekv_rotary(n, len(sections), int(bool(adjacent)))
+        for i, (j, x) in enumerate(places):
+            self.struct.axis[i] = x
+            self.struct.frequency[i] = theta ** (-j / sections[x] if own_range else -i / n)
+        self.address = C.addressof(self.struct)
+
+
 class PagedKV:
     """Owns the pool and the workspace of a paged token cache (torch tensors; `pool`: a uint8 tensor of the caller's instead) and one
     library handle.  Every call runs on PyTorch's current stream of the device.  What calls on different streams share is for the caller to
@@ -569,7 +606,7 @@ class PagedKV:
         if not torch.cuda.is_available():
             raise RuntimeError("PagedKV needs a CUDA device (sm_100a); there is no CPU path")
         self.lib, self._call = load_library(), load_call()
-        self._fn = {f: C.cast(getattr(self.lib, "scalekv_paged_" + f), C.c_void_p).value for f in ("write", "read", "attend")}
+        self._fn = {f: C.cast(getattr(self.lib, "scalekv_paged_" + f), C.c_void_p).value for f in ("write", "read", "attend", "write_rotated", "attend_tree", "accept", "weigh", "evict")}
         self.device, self.device_index = torch.device("cuda", device), device
         self.n_layers, self.n_pages, self.n_kv_heads, self.head_dim = n_layers, n_pages, n_kv_heads, head_dim
         self.store, self.page_tokens = store, page_tokens
@@ -647,6 +684,53 @@ class PagedKV:
         self._check(self._call.paged_attend(self._fn["attend"], self._handle, layer, self._batch(batch), batch.n_tokens, self.head_dim,
                                             self.device_index, Q, O, lse, causal, window, n_sink, softmax_scale, self._stream()))
         return O
+
+    def scalekv_paged_write_rotated(self, layer, batch, Q, K, V, rotary, positions, Q_out=None):
+        """scalekv_paged_write with K, and the queries Q [n_tokens, heads, head_dim] of the same type, turned by their positions (int32
+        [axes, n_tokens]) as `rotary` (Rotary) says -> Q_out, bf16, which may be Q itself where that is bf16.  Q None: no queries, and None."""
+        if Q is not None and Q_out is None:
+            Q_out = torch.empty(Q.shape, dtype=torch.bfloat16, device=self.device)
+        self._check(self._call.paged_write_rotated(self._fn["write_rotated"], self._handle, layer, self._batch(batch), batch.n_tokens, self.n_kv_heads,
+                                                   self.head_dim, self.device_index, Q, Q_out, K, V, rotary.address, rotary.n_axes, positions,
+                                                   self._stream()))
+        return Q_out
+
+    def scalekv_paged_attend_tree(self, layer, batch, Q, tree, O=None, lse=None, softmax_scale=0.0):
+        """Attention of drafted tokens: each sees all entries before the draft, and of the draft the tokens whose bits are set in its row of
+        `tree`, int32 [n_tokens, words] (bit j mod 32 of word j / 32 for token j of its sequence) -> O; lse as for scalekv_paged_attend."""
+        if O is None:
+            O = torch.empty_like(Q)
+        self._check(self._call.paged_attend_tree(self._fn["attend_tree"], self._handle, layer, self._batch(batch), batch.n_tokens, self.head_dim,
+                                                 self.device_index, Q, O, lse, tree, softmax_scale, self._stream()))
+        return O
+
+    def scalekv_paged_accept(self, batch, path, counts, layer=None):
+        """Of sequence b the new tokens path[b, :counts[b]] (int32, ascending) become the first ones behind the entries before the draft, in all
+        layers or in one.  The lengths are the caller's to change."""
+        self._check(self._call.paged_accept(self._fn["accept"], self._handle, -1 if layer is None else self._layer(layer), self._batch(batch), batch.n_seqs,
+                                            self.device_index, path, counts, self._stream()))
+
+    def scalekv_paged_weigh(self, layer, batch, Q, lse, weights, causal=True, window=0, n_sink=0, decay=1.0, softmax_scale=0.0):
+        """Adds to weights (float32 [n_pages, n_kv_heads, page_tokens], of this layer) the attention that the new tokens' queries Q pay each cached entry; lse [n_tokens,
+        heads] as scalekv_paged_attend filled it for the same queries, mask and scale.  What was there before fades by `decay` first."""
+        self._check(self._call.paged_weigh(self._fn["weigh"], self._handle, layer, self._batch(batch), batch.n_tokens, self.head_dim,
+                                           self.device_index, Q, lse, weights, self.n_pages, self.n_kv_heads, self.page_tokens, causal, window, n_sink,
+                                           decay, softmax_scale, self._stream()))
+
+    def scalekv_paged_evict(self, layer, batch, to_table, keep, weights, n_sink=0, n_recent=0, kept=None):
+        """Of each sequence and kv head keep[b] (int32) entries stay: the first n_sink, the last n_recent, and of the rest those with the largest weights
+        (as for scalekv_paged_weigh).  They are copied to the pages that to_table (int32 [n_seqs, pages]) names, weights along with them -> kept, int32
+        [n_seqs, n_kv_heads, most], the positions that stay (made here, as long as to_table has room for and filled up with -1, where not given)."""
+        if kept is None:
+            kept = torch.full((batch.n_seqs, self.n_kv_heads, to_table.shape[-1] * self.page_tokens), -1, dtype=torch.int32, device=self.device)
+        self._check(self._call.paged_evict(self._fn["evict"], self._handle, layer, self._batch(batch), batch.n_seqs, self.device_index, to_table, keep,
+                                           weights, self.n_pages, self.n_kv_heads, self.page_tokens, n_sink, n_recent, kept, self._stream()))
+        return kept
+
+    def _layer(self, layer):
+        if not 0 <= layer < self.n_layers:                 # (-1 means all of them to the library)
+            raise ScaleKVError(1, f"layer {layer} out of range")
+        return layer
 
     def scalekv_paged_sync(self):
         self._check(self.lib.scalekv_paged_sync(self.handle, self._stream()))

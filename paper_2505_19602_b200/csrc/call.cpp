@@ -8,6 +8,7 @@
 
 #include <algorithm>
 #include <exception>
+#include <initializer_list>
 #include <vector>
 
 #include "../../include/scalekv.h"
@@ -284,9 +285,163 @@ PyObject *paged_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
   CALL(fn(kv, layer, batch, (int32_t)std::min<long>(heads, INT32_MAX), q, o, lse, &mask, (float)scale, stream));
 }
 
+// A dense tensor of one type whose sizes are known but for those that are given as -1; the last axis is contiguous, and the one before it too where `strided` is null, which
+// otherwise receives its stride.
+bool dense(PyObject *obj, const char *name, at::ScalarType type, std::initializer_list<long> sizes, int device, void **out, long long *strided = nullptr) {
+  if (!THPVariable_Check(obj)) {
+    PyErr_Format(PyExc_TypeError, "%s: expected a tensor, got %s", name, Py_TYPE(obj)->tp_name);
+    return false;
+  }
+  return guarded([&] {
+    const at::Tensor &t = THPVariable_Unpack(obj);
+    const char *wrong = nullptr;
+    if (t.dim() != (int64_t)sizes.size()) wrong = "has another number of axes than it should";
+    for (size_t i = 0; !wrong && i < sizes.size(); ++i)
+      if (sizes.begin()[i] >= 0 && t.size(i) != sizes.begin()[i]) wrong = "has another shape than it should";
+    if (!wrong && (!t.is_cuda() || t.get_device() != device)) wrong = "is not on the cache's device";
+    if (!wrong && t.scalar_type() != type) wrong = type == at::kInt ? "is not int32" : "is not float32";
+    const int64_t n = t.dim();
+    if (!wrong && t.numel() > 0) {
+      if (!strided) {
+        if (!t.is_contiguous()) wrong = "must be contiguous";
+      } else {
+        if (t.stride(n - 1) != 1 && t.size(n - 1) > 1) wrong = "must have a contiguous last axis";
+        else if (t.size(n - 2) > 1 && (t.stride(n - 2) < 0 || t.stride(n - 2) > INT32_MAX)) wrong = "has a stride beyond 32 bits";
+        else if (n == 3 && t.size(0) > 1 && t.stride(0) != t.size(1) * t.stride(1)) wrong = "must have contiguous leading axes";
+      }
+    }
+    if (wrong) {
+      PyErr_Format(PyExc_ValueError, "%s %s", name, wrong);
+      return false;
+    }
+    *out = t.data_ptr();
+    if (strided) *strided = t.size(n - 2) > 1 || (n == 3 && t.size(0) > 1) ? t.stride(n - 2) : t.size(n - 1);
+    return true;
+  });
+}
+
+// A size or a number of entries within 32 bits.
+bool size(PyObject *obj, const char *name, int32_t *out) {
+  const long x = PyLong_AsLong(obj);
+  if (PyErr_Occurred()) return false;
+  if (x < 0 || x > INT32_MAX) {
+    PyErr_Format(PyExc_ValueError, "%s must lie in [0, 2^31)", name);
+    return false;
+  }
+  *out = (int32_t)x;
+  return true;
+}
+
+// paged_write_rotated(function, handle, layer, batch address, tokens, kv heads, head_dim, device, Q or None, Q_out or None, K, V, rotary address, axes, positions, stream)
+PyObject *paged_write_rotated(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arguments(n, 16)) return nullptr;
+  const auto fn = address<decltype(&scalekv_paged_write_rotated)>(a[0]);
+  const auto kv = address<scalekv_paged *>(a[1]);
+  const int layer = number(a[2]);
+  const auto batch = address<const scalekv_paged_batch *>(a[3]);
+  const long tokens = PyLong_AsLong(a[4]), kv_heads = PyLong_AsLong(a[5]), dim = PyLong_AsLong(a[6]), device = PyLong_AsLong(a[7]), axes = PyLong_AsLong(a[13]);
+  const auto rotary = address<const scalekv_rotary *>(a[12]);
+  const auto stream = address<void *>(a[15]);
+  if (PyErr_Occurred()) return nullptr;
+  scalekv_rows q = {}, q_out = {}, k, v;
+  at::ScalarType type = at::ScalarType::Undefined, out_type = at::kBFloat16;
+  long heads = 0;
+  void *positions;
+  long long axis_stride;
+  if (!rows(a[10], "K", tokens, kv_heads, dim, (int)device, &k, &type, nullptr) || !rows(a[11], "V", tokens, kv_heads, dim, (int)device, &v, &type, nullptr)) return nullptr;
+  if (a[8] != Py_None && (!rows(a[8], "Q", tokens, 0, dim, (int)device, &q, &type, &heads) || !rows(a[9], "Q_out", tokens, heads, dim, (int)device, &q_out, &out_type, nullptr))) return nullptr;
+  if (!dense(a[14], "positions", at::kInt, {axes, tokens}, (int)device, &positions, &axis_stride)) return nullptr;
+  CALL(fn(kv, layer, batch, (int32_t)std::min<long>(heads, INT32_MAX), q, q_out, k, v, type == at::kFloat ? SCALEKV_F32 : SCALEKV_BF16, rotary, static_cast<const int32_t *>(positions), axis_stride,
+          stream));
+}
+
+// paged_attend_tree(function, handle, layer, batch address, tokens, head_dim, device, Q, O, lse or None, tree, scale, stream)
+PyObject *paged_attend_tree(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arguments(n, 13)) return nullptr;
+  const auto fn = address<decltype(&scalekv_paged_attend_tree)>(a[0]);
+  const auto kv = address<scalekv_paged *>(a[1]);
+  const int layer = number(a[2]);
+  const auto batch = address<const scalekv_paged_batch *>(a[3]);
+  const long tokens = PyLong_AsLong(a[4]), dim = PyLong_AsLong(a[5]), device = PyLong_AsLong(a[6]);
+  const double scale = PyFloat_AsDouble(a[11]);
+  const auto stream = address<void *>(a[12]);
+  if (PyErr_Occurred()) return nullptr;
+  scalekv_rows q, o;
+  at::ScalarType type = at::kBFloat16;
+  long heads = 0;
+  void *lse = nullptr, *tree;
+  if (!rows(a[7], "Q", tokens, 0, dim, (int)device, &q, &type, &heads) || !rows(a[8], "O", tokens, heads, dim, (int)device, &o, &type, nullptr)) return nullptr;
+  if (a[9] != Py_None && !dense(a[9], "lse", at::kFloat, {tokens, heads}, (int)device, &lse)) return nullptr;
+  if (!dense(a[10], "tree", at::kInt, {tokens, -1}, (int)device, &tree)) return nullptr;
+  const long words = THPVariable_Unpack(a[10]).size(1);
+  CALL(fn(kv, layer, batch, (int32_t)std::min<long>(heads, INT32_MAX), q, o, static_cast<float *>(lse), static_cast<const int32_t *>(tree), (int32_t)std::min<long>(words, INT32_MAX), (float)scale, stream));
+}
+
+// paged_accept(function, handle, layer, batch address, sequences, device, path, counts, stream)
+PyObject *paged_accept(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arguments(n, 9)) return nullptr;
+  const auto fn = address<decltype(&scalekv_paged_accept)>(a[0]);
+  const auto kv = address<scalekv_paged *>(a[1]);
+  const int layer = number(a[2]);
+  const auto batch = address<const scalekv_paged_batch *>(a[3]);
+  const long seqs = PyLong_AsLong(a[4]), device = PyLong_AsLong(a[5]);
+  const auto stream = address<void *>(a[8]);
+  if (PyErr_Occurred()) return nullptr;
+  void *path, *counts;
+  long long stride;
+  if (!dense(a[6], "path", at::kInt, {seqs, -1}, (int)device, &path, &stride) || !dense(a[7], "counts", at::kInt, {seqs}, (int)device, &counts)) return nullptr;
+  const long len = THPVariable_Unpack(a[6]).size(1);
+  CALL(fn(kv, layer, batch, static_cast<const int32_t *>(path), (int32_t)stride, (int32_t)std::min<long>(len, INT32_MAX), static_cast<const int32_t *>(counts), stream));
+}
+
+// paged_weigh(function, handle, layer, batch address, tokens, head_dim, device, Q, lse, weights, pages, kv heads, page_tokens, causal, window, sinks, decay, scale, stream)
+PyObject *paged_weigh(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arguments(n, 19)) return nullptr;
+  const auto fn = address<decltype(&scalekv_paged_weigh)>(a[0]);
+  const auto kv = address<scalekv_paged *>(a[1]);
+  const int layer = number(a[2]);
+  const auto batch = address<const scalekv_paged_batch *>(a[3]);
+  const long tokens = PyLong_AsLong(a[4]), dim = PyLong_AsLong(a[5]), device = PyLong_AsLong(a[6]);
+  const long pages = PyLong_AsLong(a[10]), kv_heads = PyLong_AsLong(a[11]), page_tokens = PyLong_AsLong(a[12]);
+  const int causal = PyObject_IsTrue(a[13]);
+  const double decay = PyFloat_AsDouble(a[16]), scale = PyFloat_AsDouble(a[17]);
+  const auto stream = address<void *>(a[18]);
+  scalekv_paged_mask mask = {causal, 0, 0};
+  if (PyErr_Occurred() || !size(a[14], "window", &mask.window) || !size(a[15], "n_sink", &mask.n_sink)) return nullptr;
+  scalekv_rows q;
+  at::ScalarType type = at::kBFloat16;
+  long heads = 0;
+  void *lse, *weights;
+  if (!rows(a[7], "Q", tokens, 0, dim, (int)device, &q, &type, &heads) || !dense(a[8], "lse", at::kFloat, {tokens, heads}, (int)device, &lse) ||
+      !dense(a[9], "weights", at::kFloat, {pages, kv_heads, page_tokens}, (int)device, &weights)) return nullptr;
+  CALL(fn(kv, layer, batch, (int32_t)std::min<long>(heads, INT32_MAX), q, static_cast<const float *>(lse), &mask, (float)scale, static_cast<float *>(weights), (float)decay, stream));
+}
+
+// paged_evict(function, handle, layer, batch address, sequences, device, to_table, keep, weights, pages, kv heads, page_tokens, sinks, recent, kept, stream)
+PyObject *paged_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arguments(n, 16)) return nullptr;
+  const auto fn = address<decltype(&scalekv_paged_evict)>(a[0]);
+  const auto kv = address<scalekv_paged *>(a[1]);
+  const int layer = number(a[2]);
+  const auto batch = address<const scalekv_paged_batch *>(a[3]);
+  const long seqs = PyLong_AsLong(a[4]), device = PyLong_AsLong(a[5]), pages = PyLong_AsLong(a[9]), kv_heads = PyLong_AsLong(a[10]), page_tokens = PyLong_AsLong(a[11]);
+  const auto stream = address<void *>(a[15]);
+  int32_t sinks, recent;
+  if (PyErr_Occurred() || !size(a[12], "n_sink", &sinks) || !size(a[13], "n_recent", &recent)) return nullptr;
+  void *to, *keep, *weights, *kept;
+  long long to_stride, kept_stride;
+  if (!dense(a[6], "to_table", at::kInt, {seqs, -1}, (int)device, &to, &to_stride) || !dense(a[7], "keep", at::kInt, {seqs}, (int)device, &keep) ||
+      !dense(a[8], "weights", at::kFloat, {pages, kv_heads, page_tokens}, (int)device, &weights) ||
+      !dense(a[14], "kept", at::kInt, {seqs, kv_heads, -1}, (int)device, &kept, &kept_stride)) return nullptr;
+  const long to_pages = THPVariable_Unpack(a[6]).size(1), len = THPVariable_Unpack(a[14]).size(2);
+  CALL(fn(kv, layer, batch, static_cast<const int32_t *>(to), (int32_t)to_stride, (int32_t)std::min<long>(to_pages, INT32_MAX), static_cast<const int32_t *>(keep), static_cast<float *>(weights),
+          sinks, recent, static_cast<int32_t *>(kept), (int32_t)kept_stride, (int32_t)std::min<long>(len, INT32_MAX), stream));
+}
+
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(step), METHOD(step_ex), METHOD(append), METHOD(attend), METHOD(compress_ex), METHOD(layer_stats_ex), METHOD(paged_move),
-                         METHOD(paged_attend),
+                         METHOD(paged_attend), METHOD(paged_write_rotated), METHOD(paged_attend_tree), METHOD(paged_accept), METHOD(paged_weigh),
+                         METHOD(paged_evict),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_scalekv_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -69,6 +69,8 @@ struct AttendArgs {
   float *part_o, *part_ml;         // parts of rows that CTAs share: columns, and base-2 reference and sum
   int *counts;                     // parts left so far, one for each sequence and kv head (and 16 rows) of a launch; zero between launches
   Mask mask;
+  const int *tree;                 // of a draft: [tokens][tree_words], bit j of a token's words: it sees new token j of its sequence
+  int tree_words;
   Divisor group;                   // query heads of a kv head
   int n_heads;                     // query heads
   int max_new;                     // new tokens of a sequence that the launch was sized for
@@ -78,6 +80,16 @@ struct AttendArgs {
 // Keys that the query at position p of a sequence of `length` entries sees: [lo, hi) and [0, min(n_sink, lo)).
 __device__ __forceinline__ int seen_hi(const Mask &m, int p, int length) { return m.causal ? max(min(p + 1, length), 0) : length; }
 __device__ __forceinline__ int seen_lo(const Mask &m, int p) { return m.window > 0 ? max(p - m.window + 1, 0) : 0; }
+
+// Of 32 positions from `at` on those that token t (a row of the call) of a draft sees, a bit for each: what lies before the draft's first position and what its words
+// name.
+__device__ __forceinline__ uint32_t lowest_bits(int n) { return n >= 32 ? 0xffffffffu : (1u << max(n, 0)) - 1u; }
+__device__ __forceinline__ uint32_t tree_bits(const AttendArgs &a, int t, int first, int at, int length) {
+  const int *words = a.tree + (size_t)t * a.tree_words;
+  const int k = at - first, w = k >> 5;                    // (of a position before the first one the word is none, too)
+  auto word_at = [&](int i) { return i >= 0 && i < a.tree_words ? (uint32_t)words[i] : 0u; };
+  return (lowest_bits(first - at) | __funnelshift_r(word_at(w), word_at(w + 1), k & 31)) & lowest_bits(length - at);
+}
 
 // Codes as bf16, exactly and without a conversion instruction: a byte u = c + 128 (the code with its sign bit turned) alone in 16 bits is the
 // subnormal u 2^-133, so one fused multiply-add gives u 2^-133 2^127 - 2 = c 2^-6.  The 2^6 goes into the factor that the scale is anyway.
@@ -220,7 +232,7 @@ __device__ __noinline__ void join_parts(const AttendArgs &a, int start, int row0
 }
 
 // One part of rows row0 .. of a sequence and kv head (item: a number of their own): steps step_lo .. step_hi - 1 of it, as part number `part` of `parts`.  All threads of the CTA.
-template <int D, bool kQ8, int kN>
+template <int D, bool kQ8, int kN, bool kTree>
 __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp, char *smem, int *shared_word, int seq, int head, int row0, int item, int step_lo, int step_hi,
                                             int part, int parts) {
   using Y = StreamLayout<D, kQ8, kN>;
@@ -274,7 +286,7 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
     }
   }
   // a step all of whose keys every row sees: [lo_full, hi_full)
-  const int lo_full = seen_lo(a.mask, first + a.group.div(row0 + rows - 1)), hi_full = seen_hi(a.mask, first + a.group.div(row0), length);
+  const int lo_full = seen_lo(a.mask, first + a.group.div(row0 + rows - 1)), hi_full = kTree ? first : seen_hi(a.mask, first + a.group.div(row0), length);
 
   // O^T: rows 2 quad, 2 quad + 1 of every n-tile; references and sums of those rows (the sum over this lane's keys)
   float o[D / 16][kN][4], m[kN][2], l[kN][2];
@@ -331,7 +343,21 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
     for (int n = 0; n < kN; ++n) { x[n][0] *= ks0; x[n][1] *= ks0; x[n][2] *= ks1; x[n][3] *= ks1; }
     const bool whole = page >= 0 && key0 >= lo_full && key0 + 16 <= hi_full;
     uint32_t hidden = 0;
-    if (!whole) {
+    if (kTree && !whole) {
+#pragma unroll
+      for (int n = 0; n < kN; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t seen = page < 0 ? 0u : tree_bits(a, start + a.group.div(row0 + min(n * 8 + 2 * quad + e, rows - 1)), first, key0 + oct, length);
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            if (!((seen >> (8 * i)) & 1u)) {
+              x[n][e + 2 * i] = -INFINITY;
+              hidden |= 1u << (4 * n + e + 2 * i);
+            }
+        }
+    }
+    if (!kTree && !whole) {
 #pragma unroll
       for (int n = 0; n < kN; ++n)
 #pragma unroll
@@ -498,7 +524,7 @@ __device__ __forceinline__ void stream_part(const AttendArgs &a, const Span &sp,
   join_parts<D, 8 * kN>(a, start, row0, rows, head, parts, smem);
 }
 
-template <int D, bool kQ8, int kN>
+template <int D, bool kQ8, int kN, bool kTree = false>
 __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8, kN>::kCtas) paged_stream_kernel(const __grid_constant__ AttendArgs a, int most_parts, int tiles) {
   using Y = StreamLayout<D, kQ8, kN>;
   extern __shared__ __align__(16) char smem[];
@@ -580,7 +606,7 @@ __global__ void __launch_bounds__(kStreamThreads, StreamLayout<D, kQ8, kN>::kCta
       hi = (int)((long long)sp.steps * (part + 1) / parts);
     }
     const int real_head = head / tiles, row0 = (head - real_head * tiles) * kTileRows;
-    if (sp.rows > row0) stream_part<D, kQ8, kN>(a, sp, smem, &shared_word, seq, real_head, row0, seq * heads + head, lo, hi, part, parts);
+    if (sp.rows > row0) stream_part<D, kQ8, kN, kTree>(a, sp, smem, &shared_word, seq, real_head, row0, seq * heads + head, lo, hi, part, parts);
     at = next;
   }
   next_grid();

@@ -202,16 +202,15 @@ struct Cut {
   int n_items, n_full;
 };
 
-__device__ __forceinline__ uint32_t lowest_bits(int n) { return n >= 32 ? 0xffffffffu : (1u << max(n, 0)) - 1u; }
-// Of 32 columns of a key tile, from position `at`, those that a row with limits [lo, hi) and n_sink does not see, a bit for each; holes: a bit for each 16
-// columns whose page is out of range.
-__device__ __forceinline__ uint32_t hidden_bits(int at, int lo, int hi, int n_sink, uint32_t holes) {
-  const uint32_t seen = lowest_bits(hi - at) & (~lowest_bits(lo - at) | lowest_bits(n_sink - at));
+// Of 32 columns of a key tile, from position `at`, those that a row with limits [lo, hi) and n_sink sees, a bit for each; and those that it does not see if holes, a
+// bit for each 16 columns, says whose page is out of range.
+__device__ __forceinline__ uint32_t seen_bits(int at, int lo, int hi, int n_sink) { return lowest_bits(hi - at) & (~lowest_bits(lo - at) | lowest_bits(n_sink - at)); }
+__device__ __forceinline__ uint32_t hidden_bits(uint32_t seen, uint32_t holes) {
   return ~seen | ((holes & 1u) * 0xffffu) | ((holes & 2u) * 0x7fff8000u);
 }
 
 // tmK, tmV: the K and V rows of all layers, [layer * pages + page][kv head * page_tokens + row][head_dim]; page0: layer * pages
-template <int D, bool kQ8>
+template <int D, bool kQ8, bool kTree = false>
 __global__ void __launch_bounds__(TileLayout<D, kQ8>::kThreads, 1)
 paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ AttendArgs a,
                   const Cut cut, int page0) {
@@ -511,7 +510,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     const int t_own = token_of(i_own), p_top = first + token_of(tile_row0 + quarter * 32), p_end = first + token_of(tile_row0 + quarter * 32 + 31);
     const int row_lo = seen_lo(a.mask, first + t_own), row_hi = seen_hi(a.mask, first + t_own, length);
     const int warp_lo = seen_lo(a.mask, p_top), warp_lo_full = seen_lo(a.mask, p_end);
-    const int warp_hi = seen_hi(a.mask, p_end, length), warp_hi_full = seen_hi(a.mask, p_top, length);
+    const int warp_hi = seen_hi(a.mask, p_end, length), warp_hi_full = kTree ? first : seen_hi(a.mask, p_top, length);
     const float c = a.scale_log2e;
     const uint64_t c2 = pack2(c, c);
     // the reference starts at the lowest number: differences from it are numbers
@@ -624,7 +623,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           float x[32], top = -INFINITY;
           tc_ld32(s_addr + col0, x);
           tc_wait_ld();
-          const uint32_t hidden = hidden_bits(at, row_lo, row_hi, n_sink, holes >> (2 * cc));
+          const uint32_t hidden = hidden_bits(kTree ? tree_bits(a, start + t_own, first, at, length) : seen_bits(at, row_lo, row_hi, n_sink), holes >> (2 * cc));
 #pragma unroll
           for (int i = 0; i < 32; i += 2) {
             const float2 k = kQ8 ? load_shared2(scales + (col0 + i) * 4) : make_float2(c, c);
