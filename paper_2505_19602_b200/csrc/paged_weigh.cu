@@ -171,97 +171,337 @@ __global__ void __launch_bounds__(kStreamThreads) paged_weigh_stream_kernel(cons
   asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-// ---- many rows: a warp's 16 keys stay in registers, queries pass through shared memory, 64 rows at a time.
-constexpr int kQueryRows = 64, kManyWarps = 8;
+// ---- many rows: products on tcgen05 with the keys for rows, so that a key's sum is a thread's own.
+//
+// A CTA has 256 keys of a sequence and kv head, two tiles A and B of 128, whose rows lie in TMEM as the products' first operand for as long as queries pass: read from shared memory for every
+// product they took as much of its data path as the queries.  Query rows come 128 at a time through a ring in shared memory.  S^T = K Q^T is formed in units of 64 query rows, A's and B's
+// side by side, in three buffers that go round; units go to two pairs of softmax warpgroups in turn, half of a unit's columns to a warpgroup, a thread to each key of A and the same of B: a row's
+// log-sum-exp, which is a column's here, is loaded once for both.
+//   warp 0        : tcgen05.mma issuer
+//   warps 4-7     : the queries, by asynchronous copies of 16 bytes (rows are a token's heads, in any strides), and their log-sum-exps
+//   warps 8-23    : keys into TMEM (codes become bf16 exactly), then p = 2^(x ks - lse) and its sums
+// Every wait is bounded, as in paged_tile.cuh.
+constexpr int kKeyRows = 256, kQueryTile = 128, kUnit = 64, kUnits = 3, kSumGroups = 4;
 
 template <int D, bool kQ8>
-__global__ void __launch_bounds__(32 * kManyWarps) paged_weigh_kernel(const __grid_constant__ WeighArgs w) {
-  __shared__ __align__(16) uint2 q_smem[kQueryRows * D / 4 + kQueryRows];
-  __shared__ float lse_smem[kQueryRows];
+struct WeighTile {
+  static constexpr int kThreads = 256 + 128 * kSumGroups;
+  static constexpr int kRegs0 = 40, kRegs1 = 56, kRegsS = 96;
+  static_assert(kRegs0 + kRegs1 + kSumGroups * kRegsS <= 80 * 6, "a share would wait for registers that nobody returns");
+  static constexpr int kStages = 4, kSlots = 2 * kStages;      // of queries; of their log-sum-exps: a stage is free when its products are through, whose sums may still be under way
+  static constexpr uint32_t kTile = kQueryTile * D * 2, kHalf = kQueryTile * 128;
+  static constexpr uint32_t kOffLse = kStages * kTile, kOffVoid = kOffLse + kSlots * kQueryTile * 4, kOffBar = kOffVoid + kSlots * 16;
+  enum { bQFull = 0, bQEmpty = bQFull + kStages, bSFull = bQEmpty + kStages, bSFree = bSFull + kUnits, bKeys = bSFree + kUnits, bCount = bKeys + 1 };
+  static_assert(bCount <= 32, "one lane of a warp initialises each barrier");
+  static constexpr uint32_t kOffWord = kOffBar + 8 * bCount;   // TMEM address, abort flag
+  static constexpr uint32_t kOffSum = kOffWord + 16;           // sums of the other warpgroups, for the first
+  static constexpr uint32_t kSmem = kOffSum + (kSumGroups - 1) * kKeyRows * 4;
+  static_assert(kOffBar % 8 == 0, "barriers are 8 bytes");
+};
+
+// Whether all threads of the softmax warpgroups bring true.  A named barrier, which knows no limit: whoever has given up comes, too, and all of them hear of it.
+__device__ __forceinline__ bool all_agree(bool mine) {
+  uint32_t all;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "bar.red.and.pred q, 3, %2, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(all)
+      : "r"(mine ? 1u : 0u), "n"(128 * kSumGroups)
+      : "memory");
+  return all != 0;
+}
+
+// D/16 steps of a product, by one thread: A in TMEM (16 dims = 8 columns a step), B in shared memory, K-major (32 bytes a step inside a half of 64 dims).
+template <int D> __device__ __forceinline__ void mma_ts_k(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t hi, uint32_t idesc) {
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 db, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem + 8 * k), "r"(b_lo + (uint32_t)((k >> 2) * 1024 + (k & 3) * 2)), "r"(hi), "r"(idesc), "r"(k > 0 ? 1u : 0u)
+        : "memory");
+}
+
+template <int D, bool kQ8>
+__global__ void __launch_bounds__(WeighTile<D, kQ8>::kThreads, 1) paged_weigh_tile_kernel(const __grid_constant__ WeighArgs w) {
+  using Y = WeighTile<D, kQ8>;
+  constexpr int kStages = Y::kStages;
+  constexpr uint32_t kTile = Y::kTile, kHalf = Y::kHalf, kColK = kUnits * 2 * kUnit;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  const uint32_t base = smem_u32(smem_raw);
+  auto bar = [&](int i) { return base + Y::kOffBar + 8u * (uint32_t)i; };
+  volatile int *words = reinterpret_cast<volatile int *>(smem_raw + Y::kOffWord);
+  volatile int *abort_flag = words + 1;
   const AttendArgs &a = w.a;
   const Store &s = a.s;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = lane & 3, oct = lane >> 2, seq = blockIdx.x, head = blockIdx.y;
-  constexpr int kPitch = D * 2 + 8;              // bytes of a row of queries
+  int *status = s.status;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x & 127, head = blockIdx.y, seq = blockIdx.z;
+  if (warp == 1) {
+    if (lane < Y::bCount) {
+      // arrivals a phase: one lane of every warp that hands something over, or a commit
+      mbar_init(bar(lane), lane < Y::bQEmpty ? 4u : lane < Y::bSFree ? 1u : lane < Y::bKeys ? 8u : 4u * kSumGroups);
+    }
+    if (lane == 0) words[1] = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  } else if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + Y::kOffWord), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
   wait_for_grid();
-  next_grid();
-  const Span sp(a, seq, 0x7fffffff, blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0);
-  const int rows = sp.rows, start = sp.start, first = sp.first, length = sp.length;
-  for (int step0 = blockIdx.z * kManyWarps; step0 < sp.steps; step0 += gridDim.z * kManyWarps) {
-    const int step = step0 + warp, key0 = step < sp.steps ? key_of(sp, step) : 0, page = step < sp.steps ? page_of(s, a.bt, seq, key0) : -1;
-    const bool on = page >= 0;
-    uint32_t k[D / 16][4];
-    float ks[2] = {a.scale_log2e, a.scale_log2e};
+  const Span sp(a, seq, 0x7fffffff, blockIdx.x == 0 && head == 0 && threadIdx.x == 0);
+  const bool dead = (base & 1023u) || *reinterpret_cast<volatile int *>(status) == kDevTimeout;      // (an earlier CTA gave up: do not pile on)
+  if ((base & 1023u) && threadIdx.x == 0) report(status);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = (uint32_t)words[0];
+  const int rows = dead ? 0 : sp.rows, G = a.group.d;
+  // the blocks of 256 keys that some row sees: the sinks', then those of [lo, hi)
+  const int lo_block = sp.lo >> 8, sink_blocks = min((min(sp.n_sink, sp.hi) + 255) >> 8, lo_block);
+  const int n_blocks = rows > 0 ? sink_blocks + max((sp.hi + 255) >> 8, lo_block) - lo_block : 0;
+  auto key_of_block = [&](int i) { return (i < sink_blocks ? i : i - sink_blocks + lo_block) << 8; };
+  // the rows that see position pos: [row_lo, row_hi)
+  auto row_lo = [&](int pos) { return a.mask.causal ? (int)min((long long)rows, (long long)max(pos - sp.first, 0) * G) : 0; };
+  auto row_hi = [&](int pos) {
+    return a.mask.window > 0 && pos >= sp.n_sink ? (int)min((long long)rows, max((long long)pos - sp.first + a.mask.window, 0ll) * G) : rows;
+  };
+  // and the tiles of rows that see some of a block's
+  auto first_tile = [&](int key0) { return row_lo(key0) / kQueryTile; };
+  auto end_tile = [&](int key0) { return (row_hi(key0 < sp.n_sink ? key0 : min(key0 + kKeyRows, sp.length) - 1) + kQueryTile - 1) / kQueryTile; };
+
+  if (warp < 4) {
+    registers_down<Y::kRegs0>();
+    if (warp == 0) {
+      constexpr uint32_t idesc = tile_desc(false, kUnit), dhi = desc_hi(1024);
+      const bool leader = elect_one();
+      bool ok = true;
+      int q = 0, u = 0, n = 0;                   // query tiles, units and blocks so far
+      uint32_t latest = 0, latest_parity = 0;      // barrier and phase of the commit that stands behind all products so far
+      for (int i = blockIdx.x; i < n_blocks && ok; i += gridDim.x, ++n) {
+        const int key0 = key_of_block(i), tiles = max(end_tile(key0) - first_tile(key0), 0);
+        ok = mbar_wait_warp(bar(Y::bKeys), n & 1, abort_flag, status);
+        if (!ok) break;
+        tc_fence_after();
+        for (int j = 0; j < tiles && ok; ++j, ++q) {
+          ok = mbar_wait_warp(bar(Y::bQFull + q % kStages), (q / kStages) & 1, abort_flag, status);
+          if (!ok) break;
+          const uint32_t qd = desc_lo(base + (q % kStages) * kTile, 16);
+#pragma unroll 1
+          for (int h = 0; h < 2; ++h, ++u) {
+            const int buf = u % kUnits;
+            ok = mbar_wait_warp(bar(Y::bSFree + buf), ((u / kUnits) & 1) ^ 1, abort_flag, status);
+            if (!ok) break;
+            tc_fence_after();
+            if (leader) {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const size_t row = store_row(s, max(page, 0), head, key0 + oct + 8 * e);
-      if constexpr (kQ8) {
-        if (on) ks[e] *= kCodeUnit * s.k_scales[row];
-#pragma unroll
-        for (int c = 0; c < D / 64; ++c) {
-          uint4 x = on ? *reinterpret_cast<const uint4 *>(s.k_rows + row * D + (c * 4 + quad) * 16) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t u = turn_signs(word(x, i));
-            k[4 * c + i][e] = codes_low(u);
-            k[4 * c + i][2 + e] = codes_high(u);
+              for (int t = 0; t < 2; ++t) mma_ts_k<D>(tmem + buf * 2 * kUnit + t * kUnit, tmem + kColK + t * (D / 2), qd + h * (kUnit * 128 / 16), dhi, idesc);
+              tc_commit(bar(Y::bSFull + buf));
+              if (h == 1) tc_commit(bar(Y::bQEmpty + q % kStages));
+            }
+            latest = bar(Y::bSFull + buf);
+            latest_parity = (u / kUnits) & 1;
+            __syncwarp();
           }
         }
+      }
+      next_grid();
+      // (whoever has given up: no product may be under way when TMEM is freed and the tiles that it reads are gone)
+      if (latest) drain(latest, latest_parity);
+    }
+  } else if (warp < 8) {
+    registers_down<Y::kRegs1>();
+    constexpr int kPieces = D / 8, kAtOnce = 32 / kPieces, kAhead = 2;      // (a warp has 32 rows of a tile; tiles whose copies are under way beside the one that is waited for)
+    const int piece = lane % kPieces, sub = lane / kPieces, wq = warp & 3;
+    int q = 0;
+    bool ok = true;
+    for (int i = blockIdx.x; i < n_blocks && ok; i += gridDim.x) {
+      const int key0 = key_of_block(i), tile0 = first_tile(key0), tiles = max(end_tile(key0) - tile0, 0);
+      float lse[kAhead + 1];
+#pragma unroll
+      for (int k = 0; k <= kAhead; ++k) lse[k] = 0.f;
+      for (int j = 0; j < tiles + kAhead && ok; ++j) {
+        if (j < tiles) {
+          const int at = q + j;
+          ok = mbar_wait_warp(bar(Y::bQEmpty + at % kStages), ((at / kStages) & 1) ^ 1, abort_flag, status);
+          if (!ok) break;
+          // (a lane knows where one row lies, and the others ask it)
+          const int r = (tile0 + j) * kQueryTile + tid, row = min(r, rows - 1), t = a.group.div(row), h = head * G + row - t * G;
+          const char *mine = a.Q.ptr + (sp.start + t) * a.Q.st + h * a.Q.sh;
+          const uint32_t to = base + (at % kStages) * kTile + (piece >> 3) * kHalf + wq * 32 * 128;
+#pragma unroll
+          for (int it = 0; it < kPieces; ++it) {
+            const int from = it * kAtOnce + sub;
+            const char *src = reinterpret_cast<const char *>(__shfl_sync(0xffffffffu, (unsigned long long)mine, from));
+            copy16(to + from * 128 + (((piece & 7) ^ (from & 7)) << 4), src + piece * 16, r - tid + wq * 32 + from < rows);
+          }
+          const float x = a.lse[(size_t)(sp.start + t) * a.n_heads + h] * kLog2e;
+          lse[kAhead] = r < rows && x != -INFINITY ? x : INFINITY;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (j >= kAhead) {
+          const int at = q + j - kAhead, slot = at % Y::kSlots;
+          const float x = lse[0];
+          const uint32_t nothing = __ballot_sync(0xffffffffu, x == INFINITY);
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(base + Y::kOffLse + (slot * kQueryTile + tid) * 4), "f"(-x) : "memory");
+          if (lane == 0) asm volatile("st.shared.b32 [%0], %1;" ::"r"(base + Y::kOffVoid + slot * 16 + wq * 4), "r"(nothing) : "memory");
+          asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+          fence_async_proxy();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(Y::bQFull + at % kStages));
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) lse[k] = lse[k + 1];
+      }
+      q += tiles;
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  } else {
+    registers_up<Y::kRegsS>();
+    const int wg = (warp - 8) >> 2, quarter = warp & 3, row = quarter * 32 + lane, col0 = (wg & 1) * (kUnit / 2);
+    const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
+    int q = 0;
+    bool ok = true;
+    float total[2];
+    // This warpgroup's columns of unit u, rows r0 .. of the sequence's.
+    auto unit = [&](int u, int r0, int all_lo, int all_hi, const int *lo, const int *hi, const uint64_t *k2) {
+      const bool there = mbar_wait_warp(bar(Y::bSFull + u % kUnits), (u / kUnits) & 1, abort_flag, status);
+      if (!there) return there;
+      tc_fence_after();
+      float x[2][32];
+      const uint32_t s_addr = lane_addr + (u % kUnits) * 2 * kUnit + col0;
+      tc_ld32(s_addr, x[0]);
+      tc_ld32(s_addr + kUnit, x[1]);
+      const int slot = (u >> 1) % Y::kSlots, col = (u & 1) * kUnit + col0;      // (column of the query tile)
+      const uint32_t lse_at = base + Y::kOffLse + (slot * kQueryTile + col) * 4;
+      uint32_t nothing;
+      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(nothing) : "r"(base + Y::kOffVoid + slot * 16 + (col >> 5) * 4) : "memory");
+      tc_wait_ld();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(Y::bSFree + u % kUnits));
+      uint64_t sum[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+      auto sweep = [&](auto masked, const uint32_t *seen) {
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) {
+          const float4 l = load_shared4(lse_at + e * 4);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            float y[4];
+            unpack2(fma2(pack2(x[t][e], x[t][e + 1]), k2[t], pack2(l.x, l.y)), y[0], y[1]);
+            unpack2(fma2(pack2(x[t][e + 2], x[t][e + 3]), k2[t], pack2(l.z, l.w)), y[2], y[3]);
+#pragma unroll
+            for (int f = 0; f < 4; ++f) {
+              y[f] = ex2(y[f]);
+              if (decltype(masked)::value) y[f] = (seen[t] >> (e + f)) & 1u ? y[f] : 0.f;
+            }
+            sum[t] = add2(sum[t], add2(pack2(y[0], y[1]), pack2(y[2], y[3])));
+          }
+        }
+      };
+      if (nothing == 0 && all_lo <= r0 && all_hi >= r0 + 32) {
+        sweep(std::false_type{}, nullptr);
       } else {
+        uint32_t seen[2];
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          const uint4 x = on ? *reinterpret_cast<const uint4 *>(s.k_rows + row * D * 2 + (c * 4 + quad) * 16) : make_uint4(0u, 0u, 0u, 0u);
-          k[2 * c][e] = x.x; k[2 * c][2 + e] = x.y;
-          k[2 * c + 1][e] = x.z; k[2 * c + 1][2 + e] = x.w;
+        for (int t = 0; t < 2; ++t) seen[t] = lowest_bits(hi[t] - r0) & ~lowest_bits(lo[t] - r0) & ~nothing;
+        sweep(std::true_type{}, seen);
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        float s0, s1;
+        unpack2(sum[t], s0, s1);
+        total[t] += s0 + s1;
+      }
+      return there;
+    };
+    for (int i = blockIdx.x; i < n_blocks; i += gridDim.x) {
+      const int key0 = key_of_block(i), tile0 = first_tile(key0), tiles = max(end_tile(key0) - tile0, 0);
+      // keys into TMEM: warpgroups 0 and 1 have halves of A's dims, 2 and 3 of B's (what reads them is through: its results have been waited for)
+      bool there[2];
+      size_t at_row[2];
+      uint64_t k2[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int pos = key0 + t * 128 + row, page = some_see(sp, pos) ? page_of(s, a.bt, seq, pos) : -1;
+        there[t] = page >= 0;
+        at_row[t] = store_row(s, max(page, 0), head, pos);
+        float ks = a.scale_log2e;
+        if (kQ8 && there[t]) ks *= kCodeUnit * s.k_scales[at_row[t]];
+        k2[t] = pack2(ks, ks);
+      }
+      {
+        const int tile = wg >> 1, half = wg & 1;
+        const bool on = tile ? there[1] : there[0];
+        const char *from = s.k_rows + (tile ? at_row[1] : at_row[0]) * (D * (kQ8 ? 1 : 2)) + half * (D / 2) * (kQ8 ? 1 : 2);
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {       // 32 dims, 16 columns
+          uint32_t k[16];
+#pragma unroll
+          for (int x = 0; x < (kQ8 ? 2 : 4); ++x) {
+            const uint4 v = on ? *reinterpret_cast<const uint4 *>(from + (c * (kQ8 ? 2 : 4) + x) * 16) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              if constexpr (kQ8) {
+                const uint32_t u = turn_signs(word(v, e));
+                k[x * 8 + 2 * e] = codes_low(u);
+                k[x * 8 + 2 * e + 1] = codes_high(u);
+              } else {
+                k[x * 4 + e] = word(v, e);
+              }
+            }
+          }
+          tc_st16(lane_addr + kColK + tile * (D / 2) + half * (D / 4) + c * 16, k);
+        }
+        tc_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(Y::bKeys));
+      }
+      // the rows that see this thread's keys, and those that see all of the warp's
+      int lo[2], hi[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int pos = key0 + t * 128 + row;
+        lo[t] = row_lo(pos);
+        hi[t] = there[t] ? row_hi(pos) : 0;
+      }
+      const int all_lo = __reduce_max_sync(0xffffffffu, max(lo[0], lo[1])), all_hi = __reduce_min_sync(0xffffffffu, min(hi[0], hi[1]));
+      total[0] = total[1] = 0.f;
+      for (int j = 0; j < tiles && ok; ++j) ok = unit(2 * (q + j) + (wg >> 1), (tile0 + j) * kQueryTile + (wg >> 1) * kUnit + col0, all_lo, all_hi, lo, hi, k2);
+      q += tiles;
+      // the warpgroups' shares of the rows are put together, in their order
+      const uint32_t sum_at = base + Y::kOffSum + row * 4;
+      if (wg > 0) {
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(sum_at + (wg - 1) * 1024), "f"(total[0]) : "memory");
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(sum_at + (wg - 1) * 1024 + 512), "f"(total[1]) : "memory");
+      }
+      if (!all_agree(ok)) break;                 // (a warp whose wait gave up comes here, too)
+      if (wg == 0) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          float sum = total[t];
+#pragma unroll
+          for (int k = 0; k < kSumGroups - 1; ++k) {
+            float other;
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(other) : "r"(sum_at + k * 1024 + t * 512) : "memory");
+            sum += other;
+          }
+          if (there[t]) {
+            float *to = w.weights + at_row[t];
+            *to = (key0 + t * 128 + row < sp.first ? w.decay * *to : 0.f) + sum;
+          }
         }
       }
+      if (!all_agree(true)) break;               // (the sums have been read)
     }
-    float sum[2] = {0.f, 0.f};
-    for (int r0 = 0; r0 < rows; r0 += kQueryRows) {
-      __syncthreads();
-      for (int i = threadIdx.x; i < kQueryRows * D / 4; i += 32 * kManyWarps) {
-        const int r = i / (D / 4), x = i % (D / 4);
-        int t, h;
-        place_row(a, start, head, min(r0 + r, rows - 1), t, h);
-        *reinterpret_cast<uint2 *>(reinterpret_cast<char *>(q_smem) + r * kPitch + x * 8) = *reinterpret_cast<const uint2 *>(a.Q.ptr + t * a.Q.st + h * a.Q.sh + x * 8);
-        if (x == 0) {
-          const float l = a.lse[(size_t)t * a.n_heads + h] * kLog2e;
-          lse_smem[r] = r0 + r < rows && l != -INFINITY ? l : INFINITY;
-        }
-      }
-      __syncthreads();
-      if (!on) continue;
-#pragma unroll 1
-      for (int n = 0; n < kQueryRows; n += 8) {
-        float x[4] = {0.f, 0.f, 0.f, 0.f};
-        const char *row = reinterpret_cast<const char *>(q_smem) + (n + oct) * kPitch;
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-          const int dim = kQ8 ? (i >> 2) * 64 + quad * 16 + (i & 3) * 4 : (i >> 1) * 32 + quad * 8 + (i & 1) * 4;
-          const uint2 b = *reinterpret_cast<const uint2 *>(row + dim * 2);
-          mma_16816(x, k[i], b.x, b.y);
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float l = lse_smem[n + 2 * quad + (e & 1)];
-          const int i = r0 + n + 2 * quad + (e & 1), t = first + a.group.div(min(i, rows - 1)), pos = key0 + oct + 8 * (e >> 1);
-          float p = tc::ex2(x[e] * ks[e >> 1] - l);
-          if (l == INFINITY || pos >= seen_hi(a.mask, t, length) || (pos < seen_lo(a.mask, t) && pos >= sp.n_sink)) p = 0.f;
-          sum[e >> 1] += p;
-        }
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 1);
-      sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 2);
-    }
-    if (quad < 2 && on) {
-      const int pos = key0 + oct + 8 * quad;
-      if (some_see(sp, pos)) {
-        float *at = w.weights + store_row(s, page, head, pos);
-        *at = (pos < first ? w.decay * *at : 0.f) + sum[quad];
-      }
-    }
+    tc_fence_before();
+  }
+  __syncthreads();
+  if (warp == 2) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
   }
 }
 
@@ -269,7 +509,8 @@ template <int D, bool kQ8>
 bool room() {
   auto ask = [](auto kernel, size_t bytes) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess; };
   return ask(paged_weigh_stream_kernel<D, kQ8, 1>, WeighLayout<D, kQ8, 1>::kSmem) && ask(paged_weigh_stream_kernel<D, kQ8, 2>, WeighLayout<D, kQ8, 2>::kSmem) &&
-         ask(paged_weigh_stream_kernel<D, kQ8, 4>, WeighLayout<D, kQ8, 4>::kSmem);
+         ask(paged_weigh_stream_kernel<D, kQ8, 4>, WeighLayout<D, kQ8, 4>::kSmem) &&
+         ask(paged_weigh_tile_kernel<D, kQ8>, WeighTile<D, kQ8>::kSmem);
 }
 
 }  // namespace paged
@@ -316,6 +557,7 @@ extern "C" scalekv_status scalekv_paged_weigh(scalekv_paged *kv, int32_t layer, 
   long long keys = std::max(batch->max_length, 1);
   if (a.mask.window > 0) keys = std::min<long long>(keys, (long long)a.mask.window + batch->max_new + a.mask.n_sink + 32);
   const int steps = (int)((keys + 15) / 16);
+  if (max_rows > kWeighRows && a.bt.n_seqs > 65535) return fail(c, SCALEKV_ERR_UNSUPPORTED, "more than 65535 sequences");
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   auto go = [&](auto dim, auto codes) {
     constexpr int kD = decltype(dim)::value;
@@ -326,8 +568,8 @@ extern "C" scalekv_status scalekv_paged_weigh(scalekv_paged *kv, int32_t layer, 
       else if (max_rows <= 16) launch(paged_weigh_stream_kernel<kD, kQ8, 2>, grid, kStreamThreads, WeighLayout<kD, kQ8, 2>::kSmem, st, w);
       else launch(paged_weigh_stream_kernel<kD, kQ8, 4>, grid, kStreamThreads, WeighLayout<kD, kQ8, 4>::kSmem, st, w);
     } else {
-      const dim3 grid(a.bt.n_seqs, H, (unsigned)std::min(65535, (steps + kManyWarps - 1) / kManyWarps));
-      launch(paged_weigh_kernel<kD, kQ8>, grid, 32 * kManyWarps, 0, st, w);
+      const dim3 grid((unsigned)((keys + 2 * kKeyRows - 2) / kKeyRows), H, a.bt.n_seqs);
+      launch(paged_weigh_tile_kernel<kD, kQ8>, grid, WeighTile<kD, kQ8>::kThreads, WeighTile<kD, kQ8>::kSmem, st, w);
     }
     return launched(c, "paged_weigh");
   };
