@@ -1,6 +1,8 @@
 // What stays of a sequence in the paged token cache: the accepted tokens of a draft, and the entries that attention has paid most to (see include/scalekv.h for the contract).
 #include <math_constants.h>
 
+#include <type_traits>
+
 #include "paged_host.cuh"
 
 using namespace scalekv;
@@ -92,11 +94,13 @@ __global__ void __launch_bounds__(kAcceptThreads) paged_accept_kernel(const __gr
 // the first.
 //
 // (1) paged_choose_kernel finds them: the weights as whole numbers of the same order, the k'th largest of them by three histograms of 11, 11 and 10 bits from the top, each of the keys that agree with
-// it so far.  A cluster of CTAs shares a sequence and head; every CTA holds its stretch of the keys in shared memory (those that find no room are read again), and the histograms
-// are summed over the cluster, a share of the bins by each.  Then every warp counts what it keeps of a stretch of its own and puts it down behind what lies before it.
+// it so far, in two copies, as the lanes of a warp often mean the same bin.  A long sequence's head is shared by a cluster of CTAs; every CTA holds its stretch of the keys in shared memory (those
+// that find no room are read again), four of them to a load, and the histograms are summed over the cluster, a share of the bins by each.  Then every warp counts what it keeps of a stretch of
+// its own and puts it down behind what lies before it.
 // (2) paged_gather_kernel moves the rows, which is most of the bytes, over all SMs whatever the heads and sequences are.
 constexpr int kChooseThreads = 512, kChooseWarps = kChooseThreads / 32, kBins = 2048, kMostCluster = 8;
-constexpr int kMostHeld = 49152;                 // keys that a CTA's shared memory holds, 192 KB
+constexpr int kCopies = 2;                       // of the histogram (so small that two CTAs with 21 000 keys each find room on an SM: clusters of eight need eight places near one another)
+constexpr int kMostHeld = 40960;                 // keys that a CTA's shared memory holds, 160 KB
 
 struct Evict {
   Store s;
@@ -125,9 +129,8 @@ __device__ __forceinline__ int kept_of(const Evict &a, int b, int &length, bool 
 
 // A weight as a whole number of the same order; -0 is 0, a NaN counts as -infinity.
 __device__ __forceinline__ uint32_t key_of(float w) {
-  if (w != w) w = -CUDART_INF_F;
   const uint32_t u = __float_as_uint(w + 0.f);
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  return w != w ? 0x007fffffu : u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
 }
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -141,9 +144,9 @@ __device__ __forceinline__ uint32_t peer_at(uint32_t at, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(at), "r"(rank));
   return r;
 }
-__device__ __forceinline__ uint32_t peer_load(uint32_t at) {
-  uint32_t r;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(r) : "r"(at) : "memory");
+__device__ __forceinline__ uint2 peer_load2(uint32_t at) {
+  uint2 r;
+  asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(at) : "memory");
   return r;
 }
 __device__ __forceinline__ void peer_store(uint32_t at, uint32_t v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
@@ -154,8 +157,8 @@ __device__ __forceinline__ void cluster_meet() {
 
 __global__ void __launch_bounds__(kChooseThreads) paged_choose_kernel(const __grid_constant__ Evict a, int cluster) {
   extern __shared__ __align__(16) uint32_t held[];
-  __shared__ uint32_t bins[kBins], total[kBins];
-  __shared__ uint32_t warp_sum[kChooseWarps], found[2], counted[2 * kMostCluster], warp_before[2 * kChooseWarps];
+  __shared__ __align__(16) uint32_t bins[kBins * kCopies];
+  __shared__ uint32_t total[kBins], warp_sum[kChooseWarps], found[3], counted[2 * kMostCluster], warp_before[2 * kChooseWarps];
   const int rank = cluster > 1 ? (int)cluster_rank() : 0, item = blockIdx.x / cluster, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int b = a.heads.div(item), head = item - b * a.heads.d;
   wait_for_grid();
@@ -163,51 +166,104 @@ __global__ void __launch_bounds__(kChooseThreads) paged_choose_kernel(const __gr
   int length;
   const int k = kept_of(a, b, length, head == 0 && rank == 0 && threadIdx.x == 0);
   if (k == 0) return;                            // (all of the cluster)
-  const int sinks = min(a.n_sink, k), recent = min(a.n_recent, k - sinks), middle = length - sinks - recent;
-  int need = k - sinks - recent;                 // of the entries sinks .. sinks + middle - 1
+  const int sinks = min(a.n_sink, k), recent = min(a.n_recent, k - sinks), end = length - recent;
+  int need = k - sinks - recent;                 // of the entries sinks .. end - 1
   int *kept = a.kept + ((size_t)b * a.s.heads + head) * a.kept_stride;
   if (rank == 0) {
     for (int i = threadIdx.x; i < sinks; i += kChooseThreads) kept[i] = i;
-    for (int i = threadIdx.x; i < recent; i += kChooseThreads) kept[k - recent + i] = length - recent + i;
+    for (int i = threadIdx.x; i < recent; i += kChooseThreads) kept[k - recent + i] = end + i;
   }
   if (need == 0) return;
   if (cluster > 1) cluster_meet();               // (all of them are there: from here on they look into each other's shared memory)
-  const int per = (middle + cluster - 1) / cluster, from = min(rank * per, middle), mine = min(from + per, middle) - from;      // this CTA's stretch
-  const bool in_shared = mine <= a.held;
-  auto load_key = [&](int i) {
-    const int pos = sinks + from + i, page = page_of(a.s, a.bt, b, pos);
-    return page < 0 ? key_of(-CUDART_INF_F) : key_of(__ldcg(a.weights + store_row(a.s, page, head, pos)));
+  // This CTA's stretch, in fours of positions: they lie together in a page.  A key of 0, which no weight has, is no entry to choose from.
+  const int four0 = sinks >> 2, fours = ((end + 3) >> 2) - four0, per = (fours + cluster - 1) / cluster, from = min(rank * per, fours), mine = min(from + per, fours) - from;
+  const bool in_shared = mine <= a.held >> 2;
+  auto to_keys = [&](int i, const float4 &w) {
+    const int pos = (four0 + from + i) << 2;
+    uint4 x = make_uint4(key_of(w.x), key_of(w.y), key_of(w.z), key_of(w.w));
+    if (pos < sinks || pos + 4 > end) {
+      auto inside = [&](int p) { return p >= sinks && p < end; };
+      x = make_uint4(inside(pos) ? x.x : 0u, inside(pos + 1) ? x.y : 0u, inside(pos + 2) ? x.z : 0u, inside(pos + 3) ? x.w : 0u);
+    }
+    return x;
   };
-  auto key_at = [&](int i) { return in_shared ? held[i] : load_key(i); };
+  const float4 least_w = make_float4(-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F);      // of entries without a page
+  auto load_keys = [&](int i) {
+    const int pos = (four0 + from + i) << 2, page = page_of(a.s, a.bt, b, pos);
+    return to_keys(i, page >= 0 ? __ldcg(reinterpret_cast<const float4 *>(a.weights + store_row(a.s, page, head, pos))) : least_w);
+  };
+  uint4 *held4 = reinterpret_cast<uint4 *>(held);
+  auto keys_at = [&](int i) { return in_shared ? held4[i] : load_keys(i); };
+  for (int i = threadIdx.x; i < kBins * kCopies / 4; i += kChooseThreads) reinterpret_cast<uint4 *>(bins)[i] = make_uint4(0u, 0u, 0u, 0u);
   if (in_shared) {
-#pragma unroll 4
-    for (int i = threadIdx.x; i < mine; i += kChooseThreads) held[i] = load_key(i);
+    // (look-ups side by side, and then what they lead to: with one behind the other a thread's five fours of 10 521 entries took ten trips to memory)
+    constexpr int kAtOnce = 6;
+    const int *table = a.bt.table + (size_t)b * a.bt.table_ld;
+    bool lost = false;
+    for (int i0 = threadIdx.x; i0 < mine; i0 += kAtOnce * kChooseThreads) {
+      int page[kAtOnce];
+      float4 w[kAtOnce];
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        const int i = min(i0 + j * kChooseThreads, mine - 1);      // (within the length, so within the table)
+        page[j] = table[((four0 + from + i) << 2) >> a.s.page_shift];
+      }
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        const int i = min(i0 + j * kChooseThreads, mine - 1);
+        const bool there = (unsigned)page[j] < (unsigned)a.s.n_pages;
+        lost = lost || !there;
+        w[j] = least_w;
+        if (there) w[j] = __ldcg(reinterpret_cast<const float4 *>(a.weights + store_row(a.s, page[j], head, (four0 + from + i) << 2)));
+      }
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j)
+        if (i0 + j * kChooseThreads < mine) held4[i0 + j * kChooseThreads] = to_keys(i0 + j * kChooseThreads, w[j]);
+    }
+    if (lost) report(a.s.status);
   }
+  __syncthreads();
   const uint32_t bins_at = tc::smem_u32(bins), total_at = tc::smem_u32(total), counted_at = tc::smem_u32(counted);
-  uint32_t prefix = 0, known = 0;                // of the k'th largest key, and which bits of it
-  const bool all = need == middle;
-  for (int pass = 0; pass < 3 && !all; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, n_bins = pass == 2 ? 1024 : kBins;
-    for (int i = threadIdx.x; i < n_bins; i += kChooseThreads) bins[i] = 0;
-    __syncthreads();
+  uint32_t prefix = 0;                           // of the k'th largest key, below which bits are zeros that are not known
+  bool ties = false;                             // some of the entries that have that key leave
+  // (keys of 0 are counted in bin 0, which no other key has, or not at all: nobody comes down to them)
+  auto narrow = [&](auto shift_, auto n_bins_) {
+    constexpr int shift = decltype(shift_)::value, n_bins = decltype(n_bins_)::value;
+    constexpr uint32_t known = shift == 21 ? 0u : ~0u << (shift == 0 ? 10 : shift + 11);
+    auto count = [&](uint32_t key) {
+      if (((key ^ prefix) & known) == 0u)
+        atomicAdd(&bins[((key >> shift) & (n_bins - 1)) * kCopies + (lane & (kCopies - 1))], 1u);
+    };
     for (int i = threadIdx.x; i < mine; i += kChooseThreads) {
-      const uint32_t key = key_at(i);
-      if ((key & known) == prefix) atomicAdd(&bins[(key >> shift) & (n_bins - 1)], 1u);
+      const uint4 x = keys_at(i);
+      count(x.x); count(x.y); count(x.z); count(x.w);
     }
     if (cluster > 1) cluster_meet(); else __syncthreads();
     const int share = n_bins / cluster;
     for (int i = threadIdx.x; i < share; i += kChooseThreads) {
       const int bin = rank * share + i;
-      uint32_t sum = 0;
-      for (int c = 0; c < cluster; ++c) sum += cluster > 1 ? peer_load(peer_at(bins_at + 4 * bin, c)) : bins[bin];
-      for (int c = 0; c < cluster; ++c) {
-        if (cluster > 1) peer_store(peer_at(total_at + 4 * bin, c), sum);
-        else total[bin] = sum;
+      if (cluster == 1) {
+        const uint2 x = reinterpret_cast<const uint2 *>(bins)[bin];
+        total[bin] = x.x + x.y;
+      } else {
+        uint2 x[kMostCluster];
+        uint32_t sum = 0;
+#pragma unroll
+        for (int c = 0; c < kMostCluster; ++c) x[c] = c < cluster ? peer_load2(peer_at(bins_at + 8 * bin, c)) : make_uint2(0u, 0u);
+#pragma unroll
+        for (int c = 0; c < kMostCluster; ++c) sum += x[c].x + x[c].y;
+#pragma unroll
+        for (int c = 0; c < kMostCluster; ++c)
+          if (c < cluster) peer_store(peer_at(total_at + 4 * bin, c), sum);
       }
     }
     if (cluster > 1) cluster_meet(); else __syncthreads();
-    // the bin of the need'th largest: threads from the top bin down, four or two bins each
-    const int each = n_bins / kChooseThreads, top = n_bins - 1 - (int)threadIdx.x * each;
+    if (shift > 0) {
+      for (int i = threadIdx.x; i < kBins * kCopies / 4; i += kChooseThreads) reinterpret_cast<uint4 *>(bins)[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
+    // the bin of the need'th largest: threads from the top bin down, two bins each or one
+    constexpr int each = n_bins / kChooseThreads;
+    const int top = n_bins - 1 - (int)threadIdx.x * each;
     uint32_t own = 0;
     for (int e = 0; e < each; ++e) own += total[top - e];
     uint32_t incl = own;
@@ -218,61 +274,91 @@ __global__ void __launch_bounds__(kChooseThreads) paged_choose_kernel(const __gr
     }
     if (lane == 31) warp_sum[warp] = incl;
     __syncthreads();
-    uint32_t above = incl - own;
-    for (int w = 0; w < warp; ++w) above += warp_sum[w];
+    const uint32_t before = __reduce_add_sync(0xffffffffu, lane < warp ? warp_sum[lane & (kChooseWarps - 1)] : 0u);
+    uint32_t above = before + incl - own;
     if (above < (uint32_t)need && above + own >= (uint32_t)need) {
       int e = 0;
       while (above + total[top - e] < (uint32_t)need) above += total[top - e++];
       found[0] = (uint32_t)(top - e);
       found[1] = above;
+      found[2] = total[top - e];
     }
     __syncthreads();
     prefix |= found[0] << shift;
-    known |= (uint32_t)(n_bins - 1) << shift;
     need -= (int)found[1];
-    __syncthreads();                             // (found is read before the next pass writes it)
+    ties = (uint32_t)need < found[2];
+  };
+  if (need < end - sinks) {
+    narrow(std::integral_constant<int, 21>{}, std::integral_constant<int, kBins>{});
+    if (ties) narrow(std::integral_constant<int, 10>{}, std::integral_constant<int, kBins>{});
+    if (ties) narrow(std::integral_constant<int, 0>{}, std::integral_constant<int, 1024>{});
+  } else {
+    prefix = 1;
   }
-  // Now `prefix` is the key, and `need` of the entries that have it stay (all: everything does).  A warp takes a stretch of the CTA's.
+  // Now every entry with a key of `prefix` or more stays or, where there are ties, those above it and the first `need` of those that have it.  A warp takes a stretch of the CTA's.
   const int warp_per = (mine + kChooseWarps - 1) / kChooseWarps, w0 = min(warp * warp_per, mine), w1 = min(w0 + warp_per, mine);
+  const uint32_t least = ties ? prefix + 1u : prefix;      // (no key is 2^32 - 1)
+  auto is_larger = [&](uint32_t key) { return key >= least ? 1u : 0u; };
+  auto is_equal = [&](uint32_t key) { return key == prefix ? 1u : 0u; };
   uint32_t larger = 0, equal = 0;
   for (int i = w0 + lane; i < w1; i += 32) {
-    const uint32_t key = all ? 0u : key_at(i);
-    larger += all || key > prefix;
-    equal += !all && key == prefix;
+    const uint4 x = keys_at(i);
+    larger += is_larger(x.x) + is_larger(x.y) + is_larger(x.z) + is_larger(x.w);
+    if (ties) equal += is_equal(x.x) + is_equal(x.y) + is_equal(x.z) + is_equal(x.w);
   }
   larger = __reduce_add_sync(0xffffffffu, larger);
   equal = __reduce_add_sync(0xffffffffu, equal);
   if (lane == 0) { warp_before[2 * warp] = larger; warp_before[2 * warp + 1] = equal; }
   __syncthreads();
-  if (threadIdx.x == 0) {
-    uint32_t l = 0, e = 0;
-    for (int w = 0; w < kChooseWarps; ++w) {
-      const uint32_t lw = warp_before[2 * w], ew = warp_before[2 * w + 1];
-      warp_before[2 * w] = l; warp_before[2 * w + 1] = e;
-      l += lw; e += ew;
+  static_assert(kChooseWarps <= 32, "a lane for each warp's counts");
+  const uint32_t l_all = lane < kChooseWarps ? warp_before[2 * lane] : 0u, e_all = lane < kChooseWarps ? warp_before[2 * lane + 1] : 0u;
+  uint32_t l = __reduce_add_sync(0xffffffffu, lane < warp ? l_all : 0u), e = __reduce_add_sync(0xffffffffu, lane < warp ? e_all : 0u);
+  if (cluster > 1) {
+    if (warp == 0) {
+      const uint32_t l_sum = __reduce_add_sync(0xffffffffu, l_all), e_sum = __reduce_add_sync(0xffffffffu, e_all);
+      if (lane < cluster) {
+        peer_store(peer_at(counted_at + 8 * rank, lane), l_sum);
+        peer_store(peer_at(counted_at + 8 * rank + 4, lane), e_sum);
+      }
     }
-    for (int c = 0; c < cluster; ++c) {
-      if (cluster > 1) { peer_store(peer_at(counted_at + 8 * rank, c), l); peer_store(peer_at(counted_at + 8 * rank + 4, c), e); }
-      else { counted[0] = l; counted[1] = e; }
-    }
+    cluster_meet();                              // (nobody reads another's shared memory behind this)
+    for (int c = 0; c < rank; ++c) { l += counted[2 * c]; e += counted[2 * c + 1]; }
   }
-  if (cluster > 1) cluster_meet(); else __syncthreads();      // (nobody reads another's shared memory behind this)
-  uint32_t l = warp_before[2 * warp], e = warp_before[2 * warp + 1];
-  for (int c = 0; c < rank; ++c) { l += counted[2 * c]; e += counted[2 * c + 1]; }
   for (int i0 = w0; i0 < w1; i0 += 32) {
-    const int i = i0 + lane;
-    const uint32_t key = i < w1 && !all ? key_at(i) : 0u;
-    const unsigned is_larger = __ballot_sync(0xffffffffu, i < w1 && (all || key > prefix)), is_equal = __ballot_sync(0xffffffffu, i < w1 && !all && key == prefix);
-    const unsigned below = (1u << lane) - 1u;
-    const uint32_t l_here = l + __popc(is_larger & below), e_here = e + __popc(is_equal & below);
-    const bool stays = ((is_larger >> lane) & 1u) || (((is_equal >> lane) & 1u) && e_here < (uint32_t)need);
-    if (stays) kept[sinks + l_here + min(e_here, (uint32_t)need)] = sinks + from + i;
-    l += __popc(is_larger);
-    e += __popc(is_equal);
+    const uint4 x = i0 + lane < w1 ? keys_at(i0 + lane) : make_uint4(0u, 0u, 0u, 0u);
+    const uint32_t key[4] = {x.x, x.y, x.z, x.w};
+    const int pos = (four0 + from + i0 + lane) << 2;
+    uint32_t own = 0;                            // larger ones in the low half, equal ones in the high one: 128 at most
+#pragma unroll
+    for (int j = 0; j < 4; ++j) own += is_larger(key[j]) + (ties ? is_equal(key[j]) << 16 : 0u);
+    uint32_t incl = own;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const uint32_t up = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane >= d) incl += up;
+    }
+    const uint32_t sum = __shfl_sync(0xffffffffu, incl, 31);
+    int *to = kept + sinks + l + ((incl - own) & 0xffffu);
+    if (!ties) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (key[j] >= least) *to++ = pos + j;
+    } else {
+      uint32_t e_here = e + ((incl - own) >> 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool larger_j = key[j] >= least, equal_j = key[j] == prefix;
+        if (larger_j || (equal_j && e_here < (uint32_t)need)) to[min(e_here, (uint32_t)need)] = pos + j;
+        to += larger_j;
+        e_here += equal_j;
+      }
+      e += sum >> 16;
+    }
+    l += sum & 0xffffu;
   }
 }
 
-constexpr int kGatherThreads = 256, kGatherRows = 32;
+constexpr int kGatherThreads = 256, kGatherRows = 128, kGatherBatch = 4;
 
 __global__ void __launch_bounds__(kGatherThreads) paged_gather_kernel(const __grid_constant__ Evict a) {
   __shared__ long long src[kGatherRows], dst[kGatherRows];
@@ -291,13 +377,23 @@ __global__ void __launch_bounds__(kGatherThreads) paged_gather_kernel(const __gr
     dst[threadIdx.x] = ok ? (long long)store_row(a.s, to, head, i) : 0;
   }
   __syncthreads();
-  const int both = 2 * a.row_pieces;
-  for (int i = threadIdx.x; i < n * both; i += kGatherThreads) {
-    const int r = i / both, c = i - r * both;
-    if (src[r] < 0) continue;
-    const bool v = c >= a.row_pieces;
-    uint4 *rows = reinterpret_cast<uint4 *>(v ? a.s.v_rows : a.s.k_rows) + (v ? c - a.row_pieces : c);
-    rows[(size_t)dst[r] * a.row_pieces] = __ldcg(rows + (size_t)src[r] * a.row_pieces);
+  const int both = 2 * a.row_pieces, shift = 31 - __clz(both);      // (a power of two)
+  for (int i0 = threadIdx.x; i0 < n * both; i0 += kGatherBatch * kGatherThreads) {
+    uint4 x[kGatherBatch], *to[kGatherBatch];
+#pragma unroll
+    for (int j = 0; j < kGatherBatch; ++j) {
+      const int i = i0 + j * kGatherThreads, r = i >> shift, c = i & (both - 1);
+      to[j] = nullptr;
+      if (i < n * both && src[r] >= 0) {
+        const bool v = c >= a.row_pieces;
+        uint4 *rows = reinterpret_cast<uint4 *>(v ? a.s.v_rows : a.s.k_rows) + (v ? c - a.row_pieces : c);
+        to[j] = rows + (size_t)dst[r] * a.row_pieces;
+        x[j] = __ldcg(rows + (size_t)src[r] * a.row_pieces);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kGatherBatch; ++j)
+      if (to[j]) *to[j] = x[j];
   }
   if ((int)threadIdx.x < n && src[threadIdx.x] >= 0) {
     const size_t from = (size_t)src[threadIdx.x], to = (size_t)dst[threadIdx.x];
@@ -366,8 +462,8 @@ scalekv_status scalekv_paged_evict(scalekv_paged *kv, int32_t layer, const scale
   a.blocks = Divisor::of((int)blocks);
   const int length = std::max(batch->max_length, 1);
   int cluster = 1;
-  while (cluster < kMostCluster && items * cluster <= c->n_sm && length > cluster * 2048) cluster *= 2;
-  a.held = std::min((length + cluster - 1) / cluster, kMostHeld);
+  while (cluster < kMostCluster && items * cluster <= c->n_sm && length > cluster * 16384) cluster *= 2;
+  a.held = std::min((length + cluster - 1) / cluster + 8, kMostHeld) & ~3;      // (fours that begin and end inside)
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
