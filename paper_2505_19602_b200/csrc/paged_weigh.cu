@@ -32,7 +32,7 @@ struct WeighLayout {
   static __device__ __forceinline__ int piece(int r, int x) { return StreamLayout<D, kQ8, 1>::piece(r, x); }
 };
 constexpr int kWeighRows = 32;                   // query rows of a sequence and kv head that go this way
-constexpr int kWeighSteps = 16;                  // of a warp, in a row
+constexpr int kWeighSteps = 8;                   // of a warp, in a row
 
 template <int D, bool kQ8, int kN>
 __global__ void __launch_bounds__(kStreamThreads) paged_weigh_stream_kernel(const __grid_constant__ WeighArgs w) {
@@ -45,41 +45,15 @@ __global__ void __launch_bounds__(kStreamThreads) paged_weigh_stream_kernel(cons
   wait_for_grid();
   next_grid();
   const Span sp(a, seq, 0x7fffffff, blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0);
-  // a warp's stretches of kWeighSteps: stretch number z * warps + warp, and as many behind it as the grid has CTAs for
-  const int stride = gridDim.z * kStreamWarps;
-  if ((long long)(blockIdx.z * kStreamWarps) * kWeighSteps >= sp.steps) return;
+  const int stride = gridDim.z * kStreamWarps;   // a warp's stretches of kWeighSteps: number z * warps + warp, and those a grid further
+  if (blockIdx.z * kStreamWarps * kWeighSteps >= sp.steps) return;
   const int rows = min(sp.rows, 8 * kN), start = sp.start, first = sp.first, length = sp.length;
-  int stretch = blockIdx.z * kStreamWarps + warp;
-  // step number i of this warp; -1: there are no more
-  auto step_of = [&](int i) {
-    const long long at = ((long long)stretch + (long long)(i / kWeighSteps) * stride) * kWeighSteps + i % kWeighSteps;
-    return at < sp.steps ? (int)at : -1;
-  };
-  auto page_at = [&](int step) { return step >= 0 ? page_of(s, a.bt, seq, key_of(sp, step)) : -1; };
   char *ring = smem + warp * kStages * Y::kStage;
   const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
-  auto fetch = [&](int step, int page, int stage) {
-    if (page >= 0) {
-      constexpr int kRowPieces = kRowBytes / 16, kRowsAtOnce = 32 / kRowPieces;
-      const int key0 = key_of(sp, step), x = lane % kRowPieces, r0 = lane / kRowPieces;
-      const size_t row = store_row(s, page, head, key0);
-      const uint32_t to = ring_at + stage * Y::kStage;
-      const char *k = s.k_rows + (row + r0) * kRowBytes + x * 16;
-#pragma unroll
-      for (int i = 0; i < 16 / kRowsAtOnce; ++i) copy16(to + Y::piece(r0 + i * kRowsAtOnce, x), k + i * kRowsAtOnce * kRowBytes, true);
-      if (kQ8 && lane < 4) copy16(to + Y::kScales + lane * 16, s.k_scales + row + lane * 4, true);
-      if (lane >= 28) copy16(to + Y::kOld + (lane & 3) * 16, w.weights + row + (lane & 3) * 4, true);
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-  int steps[kStages], pages[kStages];
-#pragma unroll
-  for (int i = 0; i < kStages; ++i) { steps[i] = step_of(i); pages[i] = page_at(steps[i]); }
-#pragma unroll
-  for (int i = 0; i < kStages - 1; ++i) fetch(steps[i], pages[i], i);
 
   uint2 q[kN][D / 16];
   float lse[kN][2];                              // of rows 2 quad, 2 quad + 1 of every n-tile, in base 2; +inf: the row counts for nothing
+  bool nothing = false;                          // some row saw nothing
 #pragma unroll
   for (int n = 0; n < kN; ++n) {
     int t, h;
@@ -97,78 +71,111 @@ __global__ void __launch_bounds__(kStreamThreads) paged_weigh_stream_kernel(cons
       place_row(a, start, head, min(i, rows - 1), t, h);
       const float x = a.lse[(size_t)t * a.n_heads + h] * kLog2e;
       lse[n][e] = i < rows && x != -INFINITY ? x : INFINITY;
+      nothing = nothing || (i < rows && x == -INFINITY);
     }
   }
+  nothing = __any_sync(0xffffffffu, nothing);
   // a step all of whose keys every row sees: [lo_full, hi_full)
   const int lo_full = seen_lo(a.mask, first + a.group.div(rows - 1)), hi_full = seen_hi(a.mask, first, length);
 
-  for (int i = 0, stage = 0; steps[0] >= 0; ++i) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-    __syncwarp();
-    fetch(steps[kStages - 1], pages[kStages - 1], stage == 0 ? kStages - 1 : stage - 1);
-    const int key0 = key_of(sp, steps[0]), page = pages[0];
+  for (int stretch = blockIdx.z * kStreamWarps + warp; stretch < (sp.steps + kWeighSteps - 1) / kWeighSteps; stretch += stride) {
+    const int step0 = stretch * kWeighSteps, n_steps = min(kWeighSteps, sp.steps - step0);
+    // a lane for each step's page
+    static_assert(kWeighSteps <= 32, "a lane for each step");
+    const int own_page = lane < n_steps ? page_of(s, a.bt, seq, key_of(sp, step0 + lane)) : -1;
+    auto fetch = [&](int i, int stage) {
+      if (i < n_steps) {
+        const int page = __shfl_sync(0xffffffffu, own_page, i);
+        if (page >= 0) {
+          constexpr int kRowPieces = kRowBytes / 16, kRowsAtOnce = 32 / kRowPieces;
+          const int x = lane % kRowPieces, r0 = lane / kRowPieces;
+          const size_t row = store_row(s, page, head, key_of(sp, step0 + i));
+          const uint32_t to = ring_at + stage * Y::kStage;
+          const char *k = s.k_rows + (row + r0) * kRowBytes + x * 16;
 #pragma unroll
-    for (int k = 0; k + 1 < kStages; ++k) { steps[k] = steps[k + 1]; pages[k] = pages[k + 1]; }
-    steps[kStages - 1] = step_of(i + kStages);
-    pages[kStages - 1] = page_at(steps[kStages - 1]);
-    const char *k_at = ring + stage * Y::kStage;
-    stage = stage + 1 == kStages ? 0 : stage + 1;
-    if (page < 0) continue;
-    float sum[2] = {0.f, 0.f};                   // of keys oct and oct + 8, over this lane's rows
-    float x[kN][4];
+          for (int j = 0; j < 16 / kRowsAtOnce; ++j) copy16(to + Y::piece(r0 + j * kRowsAtOnce, x), k + j * kRowsAtOnce * kRowBytes, true);
+          // (the scales by lanes 0-3, the weights by lanes 4-7)
+          if (lane < 8 && (kQ8 || lane >= 4)) copy16(to + (lane < 4 ? Y::kScales : Y::kOld) + (lane & 3) * 16, (lane < 4 ? s.k_scales : w.weights) + row + (lane & 3) * 4, true);
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
 #pragma unroll
-    for (int n = 0; n < kN; ++n) x[n][0] = x[n][1] = x[n][2] = x[n][3] = 0.f;
+    for (int i = 0; i < kStages - 1; ++i) fetch(i, i);
+    auto one = [&](int i, int stage) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+      __syncwarp();
+      fetch(i + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
+      const int key0 = key_of(sp, step0 + i), page = __shfl_sync(0xffffffffu, own_page, i);
+      if (page < 0) return;
+      const char *k_at = ring + stage * Y::kStage;
+      float x[kN][4];
 #pragma unroll
-    for (int c = 0; c < kRowBytes / 64; ++c) {
-      const uint4 lo = *reinterpret_cast<const uint4 *>(k_at + Y::piece(oct, c * 4 + quad)), hi = *reinterpret_cast<const uint4 *>(k_at + Y::piece(oct + 8, c * 4 + quad));
+      for (int n = 0; n < kN; ++n) x[n][0] = x[n][1] = x[n][2] = x[n][3] = 0.f;
+#pragma unroll
+      for (int c = 0; c < kRowBytes / 64; ++c) {
+        const uint4 lo = *reinterpret_cast<const uint4 *>(k_at + Y::piece(oct, c * 4 + quad)), hi = *reinterpret_cast<const uint4 *>(k_at + Y::piece(oct + 8, c * 4 + quad));
+        if constexpr (kQ8) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t w0 = turn_signs(word(lo, e)), w1 = turn_signs(word(hi, e));
+            const uint32_t f[4] = {codes_low(w0), codes_low(w1), codes_high(w0), codes_high(w1)};
+#pragma unroll
+            for (int n = 0; n < kN; ++n) mma_16816(x[n], f, q[n][4 * c + e].x, q[n][4 * c + e].y);
+          }
+        } else {
+          const uint32_t f0[4] = {lo.x, hi.x, lo.y, hi.y}, f1[4] = {lo.z, hi.z, lo.w, hi.w};
+#pragma unroll
+          for (int n = 0; n < kN; ++n) {
+            mma_16816(x[n], f0, q[n][2 * c].x, q[n][2 * c].y);
+            mma_16816(x[n], f1, q[n][2 * c + 1].x, q[n][2 * c + 1].y);
+          }
+        }
+      }
+      float ks0 = a.scale_log2e, ks1 = a.scale_log2e;
       if constexpr (kQ8) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t w0 = turn_signs(word(lo, e)), w1 = turn_signs(word(hi, e));
-          const uint32_t f[4] = {codes_low(w0), codes_low(w1), codes_high(w0), codes_high(w1)};
-#pragma unroll
-          for (int n = 0; n < kN; ++n) mma_16816(x[n], f, q[n][4 * c + e].x, q[n][4 * c + e].y);
-        }
-      } else {
-        const uint32_t f0[4] = {lo.x, hi.x, lo.y, hi.y}, f1[4] = {lo.z, hi.z, lo.w, hi.w};
-#pragma unroll
-        for (int n = 0; n < kN; ++n) {
-          mma_16816(x[n], f0, q[n][2 * c].x, q[n][2 * c].y);
-          mma_16816(x[n], f1, q[n][2 * c + 1].x, q[n][2 * c + 1].y);
-        }
+        const float *scales = reinterpret_cast<const float *>(k_at + Y::kScales) + oct;
+        ks0 *= kCodeUnit * scales[0];
+        ks1 *= kCodeUnit * scales[8];
       }
-    }
-    float ks0 = a.scale_log2e, ks1 = a.scale_log2e;
-    if constexpr (kQ8) {
-      const float *scales = reinterpret_cast<const float *>(k_at + Y::kScales) + oct;
-      ks0 *= kCodeUnit * scales[0];
-      ks1 *= kCodeUnit * scales[8];
-    }
-    const bool whole = key0 >= lo_full && key0 + 16 <= hi_full;
+      float sum[2] = {0.f, 0.f};                 // of keys oct and oct + 8, over this lane's rows
 #pragma unroll
-    for (int n = 0; n < kN; ++n)
+      for (int n = 0; n < kN; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float p = tc::ex2(x[n][e] * (e < 2 ? ks0 : ks1) - lse[n][e & 1]);
-        if (lse[n][e & 1] == INFINITY) p = 0.f;                   // (whatever the product is)
-        if (!whole) {
-          const int r = first + a.group.div(min(n * 8 + 2 * quad + (e & 1), rows - 1)), pos = key0 + oct + 8 * (e >> 1);
-          if (pos >= seen_hi(a.mask, r, length) || (pos < seen_lo(a.mask, r) && pos >= sp.n_sink)) p = 0.f;
-        }
-        sum[e >> 1] += p;
+        for (int e = 0; e < 4; ++e) x[n][e] = tc::ex2(x[n][e] * (e < 2 ? ks0 : ks1) - lse[n][e & 1]);
+      const bool whole = key0 >= lo_full && key0 + 16 <= hi_full;
+      if (!whole || nothing) {
+#pragma unroll
+        for (int n = 0; n < kN; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = first + a.group.div(min(n * 8 + 2 * quad + (e & 1), rows - 1)), pos = key0 + oct + 8 * (e >> 1);
+            if (lse[n][e & 1] == INFINITY || pos >= seen_hi(a.mask, r, length) || (pos < seen_lo(a.mask, r) && pos >= sp.n_sink)) x[n][e] = 0.f;      // (whatever the product is)
+          }
       }
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 1);
-      sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 2);
+      for (int n = 0; n < kN; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e >> 1] += x[n][e];
+      // lanes of even quads put the first key's sum together, those of odd quads the second's
+      const float give = quad & 1 ? sum[0] : sum[1], keep = quad & 1 ? sum[1] : sum[0];
+      float all = keep + __shfl_xor_sync(0xffffffffu, give, 1);
+      all += __shfl_xor_sync(0xffffffffu, all, 2);
+      if (quad < 2) {
+        const int pos = key0 + oct + 8 * quad;
+        const float old = reinterpret_cast<const float *>(k_at + Y::kOld)[oct + 8 * quad];
+        if (whole || some_see(sp, pos)) w.weights[store_row(s, page, head, pos)] = (pos < first ? w.decay * old : 0.f) + all;
+      }
+    };
+#pragma unroll 1
+    for (int i = 0; i < n_steps; i += kStages) {
+#pragma unroll
+      for (int j = 0; j < kStages; ++j)
+        if (i + j < n_steps) one(i + j, j);
     }
-    if (quad < 2) {
-      const int pos = key0 + oct + 8 * quad;
-      const float old = reinterpret_cast<const float *>(k_at + Y::kOld)[oct + 8 * quad];
-      if (some_see(sp, pos)) w.weights[store_row(s, page, head, pos)] = (pos < first ? w.decay * old : 0.f) + sum[quad];
-    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncwarp();                                // (the ring is free)
   }
-  asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 // ---- many rows: products on tcgen05 with the keys for rows, so that a key's sum is a thread's own.
