@@ -14,8 +14,8 @@ namespace paged {
 // ---- accept: row first + path[i] of a sequence moves to first + i, in every layer, of K and V and their scales.
 //
 // A draft's rows move to places at or below their own, in ascending order, so a thread that has a column of the rows (16 bytes of a head's, or a scale) to itself takes them in that
-// order, eight loads and then their stores: what a store puts down lies below everything that is still to be loaded.  Few bytes; what bounds it is the look-up of a path's places, four trips to memory one behind the other.
-constexpr int kAcceptThreads = 128, kAcceptRows = 64;
+// order, four loads and then their stores: what a store puts down lies below everything that is still to be loaded.  Few bytes; what bounds it is the look-up of a path's places, four trips to memory one behind the other.
+constexpr int kAcceptThreads = 256, kAcceptRows = 64;      // at most; of a block's paths
 
 struct Accept {
   Store s;                                       // of the first layer
@@ -26,26 +26,31 @@ struct Accept {
   int row_pieces, q8;                            // 16-byte pieces of a row
 };
 
-__global__ void __launch_bounds__(kAcceptThreads) paged_accept_kernel(const __grid_constant__ Accept a) {
+__global__ void __launch_bounds__(kAcceptThreads, 5) paged_accept_kernel(const __grid_constant__ Accept a) {
   __shared__ long long src[kAcceptRows], dst[kAcceptRows];
   __shared__ int stop;
   wait_for_grid();
   next_grid();
   const int b = blockIdx.x;
-  const int start = a.bt.starts[b], end = a.bt.starts[b + 1], length = a.bt.lengths[b];
-  int count = a.counts[b];
+  const int start = a.bt.starts[b], end = a.bt.starts[b + 1], length = a.bt.lengths[b], count = a.counts[b];
+  const int *path = a.path + (size_t)b * a.path_stride;
+  // (a path's first entries are asked for beside these, not behind them)
+  int j = 0, before = -1;
+  if ((int)threadIdx.x < min(kAcceptRows, a.path_len)) {
+    j = path[threadIdx.x];
+    if (threadIdx.x > 0) before = path[threadIdx.x - 1];
+  }
   const bool wrong = starts_wrong(a.bt, b, start, end) || count < 0 || count > a.path_len || count > end - start;
   if (wrong && threadIdx.x == 0) report(a.s.status);
   if (wrong || count == 0) return;
   const int first = length - (end - start);
-  const int half = a.s.heads * a.row_pieces, columns = 2 * half + (a.q8 ? 2 * a.s.heads : 0), column = blockIdx.y * kAcceptThreads + threadIdx.x;
+  const int half = a.s.heads * a.row_pieces, columns = 2 * half + (a.q8 ? 2 * a.s.heads : 0), column = blockIdx.y * blockDim.x + threadIdx.x;
   for (int i0 = 0; i0 < count; i0 += kAcceptRows) {
     if (threadIdx.x == 0) stop = min(kAcceptRows, count - i0);
     __syncthreads();
     if ((int)threadIdx.x < kAcceptRows && i0 + (int)threadIdx.x < count) {
       const int i = i0 + threadIdx.x;
-      const int *path = a.path + (size_t)b * a.path_stride + i;
-      const int j = path[0], before = i > 0 ? path[-1] : -1;
+      if (i0 > 0) { j = path[i]; before = path[i - 1]; }
       bool ok = j > before && j < end - start && before >= -1;
       if (!ok) report(a.s.status);
       const int from = ok ? page_of(a.s, a.bt, b, first + j) : -1, to = ok ? page_of(a.s, a.bt, b, first + i) : -1;
@@ -61,26 +66,26 @@ __global__ void __launch_bounds__(kAcceptThreads) paged_accept_kernel(const __gr
         const bool v = column >= half;
         const int c = v ? column - half : column, head = c / a.row_pieces, piece = c - head * a.row_pieces;
         uint4 *rows = reinterpret_cast<uint4 *>((v ? a.s.v_rows : a.s.k_rows) + blockIdx.z * a.layer_rows) + ((size_t)head << a.s.page_shift) * a.row_pieces + piece;
-        for (int i = 0; i < n; i += 8) {
-          uint4 x[8];
+        for (int i = 0; i < n; i += 4) {
+          uint4 x[4];
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
+          for (int k = 0; k < 4; ++k)
             if (i + k < n) x[k] = rows[(size_t)src[i + k] * a.row_pieces];
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
+          for (int k = 0; k < 4; ++k)
             if (i + k < n) rows[(size_t)dst[i + k] * a.row_pieces] = x[k];
         }
       } else {
         const bool v = column >= 2 * half + a.s.heads;
         const int head = column - 2 * half - (v ? a.s.heads : 0);
         float *scales = (v ? a.s.v_scales : a.s.k_scales) + blockIdx.z * a.layer_scales + ((size_t)head << a.s.page_shift);
-        for (int i = 0; i < n; i += 8) {
-          float x[8];
+        for (int i = 0; i < n; i += 4) {
+          float x[4];
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
+          for (int k = 0; k < 4; ++k)
             if (i + k < n) x[k] = scales[src[i + k]];
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
+          for (int k = 0; k < 4; ++k)
             if (i + k < n) scales[dst[i + k]] = x[k];
         }
       }
@@ -433,7 +438,9 @@ scalekv_status scalekv_paged_accept(scalekv_paged *kv, int32_t layer, const scal
   a.row_pieces = c->cfg.head_dim * (a.q8 ? 1 : 2) / 16;
   const long long columns = 2LL * c->cfg.n_kv_heads * (a.row_pieces + a.q8), blocks = (columns + kAcceptThreads - 1) / kAcceptThreads;
   if (blocks > 65535 || layers > 65535) return fail(c, SCALEKV_ERR_UNSUPPORTED, "more than 65535 layers, or too many kv heads");
-  launch(paged_accept_kernel, dim3((unsigned)a.bt.n_seqs, (unsigned)blocks, (unsigned)layers), kAcceptThreads, 0, static_cast<cudaStream_t>(stream), a);
+  // (blocks of as many threads as there are columns for, and enough for a stretch of a path)
+  const int threads = std::max(kAcceptRows, (int)((columns + blocks - 1) / blocks + 31) & ~31);
+  launch(paged_accept_kernel, dim3((unsigned)a.bt.n_seqs, (unsigned)blocks, (unsigned)layers), threads, 0, static_cast<cudaStream_t>(stream), a);
   return launched(c, "paged_accept");
 }
 

@@ -81,7 +81,7 @@ struct TwoPieces {
 };
 
 template <typename T, int D, bool kQ8>
-__global__ void __launch_bounds__(kStoreThreads) paged_rotate_kernel(const __grid_constant__ Turning r) {
+__global__ void __launch_bounds__(kStoreThreads, sizeof(T) == 2 ? 5 : 4) paged_rotate_kernel(const __grid_constant__ Turning r) {
   constexpr int kLanes = D / 16;
   __shared__ long long row0[kMostTokens];
   __shared__ __align__(16) float2 table[kMostTokens * (D / 2)];     // cosine and sine: [token][pair of pairs mod 4][pair / 8][pair mod 2], so that neighbouring lanes read neighbouring 16 bytes

@@ -180,15 +180,18 @@ __global__ void __launch_bounds__(kStreamThreads) paged_weigh_stream_kernel(cons
 
 // ---- many rows: products on tcgen05 with the keys for rows, so that a key's sum is a thread's own.
 //
-// A CTA has 256 keys of a sequence and kv head, two tiles A and B of 128, whose rows lie in TMEM as the products' first operand for as long as queries pass: read from shared memory for every
+// An item is 256 keys of a sequence and kv head, two tiles A and B of 128, whose rows lie in TMEM as the products' first operand for as long as queries pass: read from shared memory for every
 // product they took as much of its data path as the queries.  Query rows come 128 at a time through a ring in shared memory.  S^T = K Q^T is formed in units of 64 query rows, A's and B's
 // side by side, in three buffers that go round; units go to two pairs of softmax warpgroups in turn, half of a unit's columns to a warpgroup, a thread to each key of A and the same of B: a row's
-// log-sum-exp, which is a column's here, is loaded once for both.
+// log-sum-exp, which is a column's here, is loaded once for both.  A CTA takes items one after the other, as many as there are CTAs apart.
 //   warp 0        : tcgen05.mma issuer
-//   warps 4-7     : the queries, by asynchronous copies of 16 bytes (rows are a token's heads, in any strides), and their log-sum-exps
-//   warps 8-23    : keys into TMEM (codes become bf16 exactly), then p = 2^(x ks - lse) and its sums
+//   warp 1        : finds the items, ahead of the others
+//   warps 4-7     : the queries, by asynchronous copies of 16 bytes (rows are a token's heads, in any strides), and their log-sum-exps; the next item's keys, scales and weights
+//   warps 8-23    : keys from shared memory into TMEM (codes become bf16 exactly), then p = 2^(x ks - lse) and its sums
 // Every wait is bounded, as in paged_tile.cuh.
-constexpr int kKeyRows = 256, kQueryTile = 128, kUnit = 64, kUnits = 3, kSumGroups = 4;
+// What bounds it: exponentials, of which the special function unit does 16 a cycle (a unit of 128 x 128 takes it twice as long as the tensor core its product).  So one in four is
+// formed on the FMA pipe (exp2_pair).
+constexpr int kKeyRows = 256, kQueryTile = 128, kUnit = 64, kUnits = 3, kSumGroups = 4, kItems = 3;
 
 template <int D, bool kQ8>
 struct WeighTile {
@@ -196,14 +199,20 @@ struct WeighTile {
   static constexpr int kRegs0 = 40, kRegs1 = 56, kRegsS = 96;
   static_assert(kRegs0 + kRegs1 + kSumGroups * kRegsS <= 80 * 6, "a share would wait for registers that nobody returns");
   static constexpr int kStages = 4, kSlots = 2 * kStages;      // of queries; of their log-sum-exps: a stage is free when its products are through, whose sums may still be under way
+  static constexpr int kRowBytes = D * (kQ8 ? 1 : 2), kPitch = kRowBytes + 16;      // of keys as they are held (a thread reads a row of its own: eight of them meet all banks)
   static constexpr uint32_t kTile = kQueryTile * D * 2, kHalf = kQueryTile * 128;
-  static constexpr uint32_t kOffLse = kStages * kTile, kOffVoid = kOffLse + kSlots * kQueryTile * 4, kOffBar = kOffVoid + kSlots * 16;
-  enum { bQFull = 0, bQEmpty = bQFull + kStages, bSFull = bQEmpty + kStages, bSFree = bSFull + kUnits, bKeys = bSFree + kUnits, bCount = bKeys + 1 };
+  static constexpr uint32_t kOffLse = kStages * kTile, kOffVoid = kOffLse + kSlots * kQueryTile * 4, kOffKeys = kOffVoid + kSlots * 16;
+  static constexpr uint32_t kOffScale = kOffKeys + kKeyRows * kPitch, kOffOld = kOffScale + kKeyRows * 4, kOffRow = kOffOld + kKeyRows * 4;      // and of every key: scale, weight, row
+  static constexpr uint32_t kOffSum = kOffRow + kKeyRows * 8;  // sums of the other warpgroups, for the first
+  static constexpr uint32_t kOffItem = kOffSum + (kSumGroups - 1) * kKeyRows * 4;
+  static constexpr uint32_t kOffBar = kOffItem + kItems * 64;
+  enum { bQFull = 0, bQEmpty = bQFull + kStages, bSFull = bQEmpty + kStages, bSFree = bSFull + kUnits, bKeys = bSFree + kUnits, bRaw, bRawFree, bItem, bItemFree = bItem + kItems,
+         bCount = bItemFree + kItems };
   static_assert(bCount <= 32, "one lane of a warp initialises each barrier");
   static constexpr uint32_t kOffWord = kOffBar + 8 * bCount;   // TMEM address, abort flag
-  static constexpr uint32_t kOffSum = kOffWord + 16;           // sums of the other warpgroups, for the first
-  static constexpr uint32_t kSmem = kOffSum + (kSumGroups - 1) * kKeyRows * 4;
-  static_assert(kOffBar % 8 == 0, "barriers are 8 bytes");
+  static constexpr uint32_t kSmem = kOffWord + 16;
+  static_assert(kSmem <= 232448, "more shared memory than a CTA can have");
+  static_assert(kOffBar % 8 == 0 && kOffRow % 8 == 0 && kOffKeys % 16 == 0 && kOffItem % 16 == 0, "alignment");
 };
 
 // Whether all threads of the softmax warpgroups bring true.  A named barrier, which knows no limit: whoever has given up comes, too, and all of them hear of it.
@@ -231,6 +240,31 @@ template <int D> __device__ __forceinline__ void mma_ts_k(uint32_t d_tmem, uint3
         : "memory");
 }
 
+// Two powers of two on the FMA pipe: y = n + f with n a whole number (adding 1.5 2^23 leaves it in the low bits), 2^f for |f| <= 1/2 by the polynomial of degree 5 whose largest relative error,
+// 7.5e-8, is the least (by Remez' exchange; 2.1e-7 with coefficients and steps in fp32, where ex2.approx has 2^-22), times 2^n.  Exponents below -126 count as that: 2^-126 more in a sum.  NaN stays NaN.
+__device__ __forceinline__ uint64_t exp2_pair(uint64_t y2) {
+  float a, b;
+  unpack2(y2, a, b);
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(-126.f));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(b) : "f"(-126.f));
+  const uint64_t y = pack2(a, b), shifted = add2(y, pack2(12582912.f, 12582912.f)), f = add2(y, mul2(add2(shifted, pack2(-12582912.f, -12582912.f)), pack2(-1.f, -1.f)));
+  auto c = [](float x) { return pack2(x, x); };
+  uint64_t p = fma2(f, c(0.0013276472454890609f), c(0.009675540961325169f));
+  p = fma2(p, f, c(0.05550713092088699f));
+  p = fma2(p, f, c(0.24022120237350464f));
+  p = fma2(p, f, c(0.6931469440460205f));
+  p = fma2(p, f, c(1.0000001192092896f));
+  unpack2(shifted, a, b);
+  const uint32_t n0 = (__float_as_uint(a) << 23) + 0x3f800000u, n1 = (__float_as_uint(b) << 23) + 0x3f800000u;
+  return mul2(p, pack2(__uint_as_float(n0), __uint_as_float(n1)));
+}
+
+// What an item is: key0 < 0: there are no more.
+struct KeyItem {
+  int seq, head, key0, tile0, tiles;             // the tiles of 128 rows that see some of its keys
+  int start, rows, length, first, n_sink, lo, hi;
+};
+
 template <int D, bool kQ8>
 __global__ void __launch_bounds__(WeighTile<D, kQ8>::kThreads, 1) paged_weigh_tile_kernel(const __grid_constant__ WeighArgs w) {
   using Y = WeighTile<D, kQ8>;
@@ -244,11 +278,13 @@ __global__ void __launch_bounds__(WeighTile<D, kQ8>::kThreads, 1) paged_weigh_ti
   const AttendArgs &a = w.a;
   const Store &s = a.s;
   int *status = s.status;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x & 127, head = blockIdx.y, seq = blockIdx.z;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x & 127, G = a.group.d;
   if (warp == 1) {
     if (lane < Y::bCount) {
       // arrivals a phase: one lane of every warp that hands something over, or a commit
-      mbar_init(bar(lane), lane < Y::bQEmpty ? 4u : lane < Y::bSFree ? 1u : lane < Y::bKeys ? 8u : 4u * kSumGroups);
+      const uint32_t readers = 1 + 4 + 4 * kSumGroups;         // of an item
+      mbar_init(bar(lane), lane < Y::bQEmpty ? 4u : lane < Y::bSFree ? 1u : lane < Y::bKeys ? 8u : lane < Y::bRaw ? 4u * kSumGroups : lane < Y::bRawFree ? 4u : lane < Y::bItem ? 4u * kSumGroups
+                           : lane < Y::bItemFree ? 1u : readers);
     }
     if (lane == 0) words[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -257,41 +293,34 @@ __global__ void __launch_bounds__(WeighTile<D, kQ8>::kThreads, 1) paged_weigh_ti
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   wait_for_grid();
-  const Span sp(a, seq, 0x7fffffff, blockIdx.x == 0 && head == 0 && threadIdx.x == 0);
-  const bool dead = (base & 1023u) || *reinterpret_cast<volatile int *>(status) == kDevTimeout;      // (an earlier CTA gave up: do not pile on)
-  if ((base & 1023u) && threadIdx.x == 0) report(status);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = (uint32_t)words[0];
-  const int rows = dead ? 0 : sp.rows, G = a.group.d;
-  // the blocks of 256 keys that some row sees: the sinks', then those of [lo, hi)
-  const int lo_block = sp.lo >> 8, sink_blocks = min((min(sp.n_sink, sp.hi) + 255) >> 8, lo_block);
-  const int n_blocks = rows > 0 ? sink_blocks + max((sp.hi + 255) >> 8, lo_block) - lo_block : 0;
-  auto key_of_block = [&](int i) { return (i < sink_blocks ? i : i - sink_blocks + lo_block) << 8; };
-  // the rows that see position pos: [row_lo, row_hi)
-  auto row_lo = [&](int pos) { return a.mask.causal ? (int)min((long long)rows, (long long)max(pos - sp.first, 0) * G) : 0; };
-  auto row_hi = [&](int pos) {
-    return a.mask.window > 0 && pos >= sp.n_sink ? (int)min((long long)rows, max((long long)pos - sp.first + a.mask.window, 0ll) * G) : rows;
+  // Item number k of this CTA, as warp 1 has left it.
+  auto read_item = [&](int k, KeyItem &it) {
+    const bool there = mbar_wait_warp(bar(Y::bItem + k % kItems), (k / kItems) & 1, abort_flag, status);
+    const volatile int *v = reinterpret_cast<const volatile int *>(smem_raw + Y::kOffItem + (k % kItems) * 64);
+    it = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7], v[8], v[9], v[10], v[11]};
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar(Y::bItemFree + k % kItems));
+    return there && it.key0 >= 0;
   };
-  // and the tiles of rows that see some of a block's
-  auto first_tile = [&](int key0) { return row_lo(key0) / kQueryTile; };
-  auto end_tile = [&](int key0) { return (row_hi(key0 < sp.n_sink ? key0 : min(key0 + kKeyRows, sp.length) - 1) + kQueryTile - 1) / kQueryTile; };
 
   if (warp < 4) {
     registers_down<Y::kRegs0>();
     if (warp == 0) {
       constexpr uint32_t idesc = tile_desc(false, kUnit), dhi = desc_hi(1024);
       const bool leader = elect_one();
-      bool ok = true;
-      int q = 0, u = 0, n = 0;                   // query tiles, units and blocks so far
+      int q = 0, u = 0;                          // query tiles and units so far
       uint32_t latest = 0, latest_parity = 0;      // barrier and phase of the commit that stands behind all products so far
-      for (int i = blockIdx.x; i < n_blocks && ok; i += gridDim.x, ++n) {
-        const int key0 = key_of_block(i), tiles = max(end_tile(key0) - first_tile(key0), 0);
+      KeyItem it;
+      bool ok = true;
+      for (int n = 0; ok && read_item(n, it); ++n) {
         ok = mbar_wait_warp(bar(Y::bKeys), n & 1, abort_flag, status);
         if (!ok) break;
         tc_fence_after();
-        for (int j = 0; j < tiles && ok; ++j, ++q) {
+        for (int j = 0; j < it.tiles && ok; ++j, ++q) {
           ok = mbar_wait_warp(bar(Y::bQFull + q % kStages), (q / kStages) & 1, abort_flag, status);
           if (!ok) break;
           const uint32_t qd = desc_lo(base + (q % kStages) * kTile, 16);
@@ -316,35 +345,126 @@ __global__ void __launch_bounds__(WeighTile<D, kQ8>::kThreads, 1) paged_weigh_ti
       next_grid();
       // (whoever has given up: no product may be under way when TMEM is freed and the tiles that it reads are gone)
       if (latest) drain(latest, latest_parity);
+    } else if (warp == 1) {
+      // Items are counted through the sequences, and in one through the blocks of 256 keys that some row sees, the sinks' and those of [lo, hi), all heads of a block together.
+      const bool dead = (base & 1023u) || *reinterpret_cast<volatile int *>(status) == kDevTimeout;      // (an earlier CTA gave up: do not pile on)
+      if ((base & 1023u) && lane == 0) report(status);
+      auto blocks_of = [&](const Span &sp, int &lo_block, int &sink_blocks) {
+        lo_block = sp.lo >> 8;
+        sink_blocks = min((min(sp.n_sink, sp.hi) + 255) >> 8, lo_block);
+        return sp.rows > 0 ? sink_blocks + max((sp.hi + 255) >> 8, lo_block) - lo_block : 0;
+      };
+      bool ok = true;
+      long long before = 0, want = blockIdx.x;   // items ahead of sequence b0; the one that is looked for
+      int n = 0;
+      for (int b0 = 0; b0 < a.bt.n_seqs && ok && !dead; b0 += 32) {
+        int blocks = 0, lo_block, sink_blocks;
+        if (b0 + lane < a.bt.n_seqs) {
+          const Span sp(a, b0 + lane, 0x7fffffff, blockIdx.x == 0);
+          blocks = blocks_of(sp, lo_block, sink_blocks);
+        }
+        long long incl = (long long)blocks * s.heads;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const long long up = __shfl_up_sync(0xffffffffu, incl, d);
+          if (lane >= d) incl += up;
+        }
+        const long long all = __shfl_sync(0xffffffffu, incl, 31);
+        while (ok && want < before + all) {
+          const int src = __ffs(__ballot_sync(0xffffffffu, before + incl > want)) - 1;
+          const long long i = want - before - __shfl_sync(0xffffffffu, incl - (long long)blocks * s.heads, src);
+          const int block = (int)(i / s.heads);
+          const Span sp(a, b0 + src, 0x7fffffff, false);
+          blocks_of(sp, lo_block, sink_blocks);
+          const int key0 = (block < sink_blocks ? block : block - sink_blocks + lo_block) << 8, last = (key0 < sp.n_sink ? key0 : min(key0 + kKeyRows, sp.length) - 1);
+          // the rows that see key0, and those that see the last key: [.., end)
+          const int begin = a.mask.causal ? (int)min((long long)sp.rows, (long long)max(key0 - sp.first, 0) * G) : 0;
+          const int end = a.mask.window > 0 && last >= sp.n_sink ? (int)min((long long)sp.rows, max((long long)last - sp.first + a.mask.window, 0ll) * G) : sp.rows;
+          const int tile0 = begin / kQueryTile, tiles = (end + kQueryTile - 1) / kQueryTile - tile0;
+          if (tiles > 0) {
+            ok = mbar_wait_warp(bar(Y::bItemFree + n % kItems), ((n / kItems) & 1) ^ 1, abort_flag, status);
+            if (lane == 0 && ok) {
+              volatile int *v = reinterpret_cast<volatile int *>(smem_raw + Y::kOffItem + (n % kItems) * 64);
+              v[0] = b0 + src; v[1] = (int)(i - (long long)block * s.heads); v[2] = key0; v[3] = tile0; v[4] = tiles; v[5] = sp.start; v[6] = sp.rows;
+              v[7] = sp.length; v[8] = sp.first; v[9] = sp.n_sink; v[10] = sp.lo; v[11] = sp.hi;
+              mbar_arrive(bar(Y::bItem + n % kItems));
+            }
+            ++n;
+          }
+          want += gridDim.x;
+          __syncwarp();
+        }
+        before += all;
+      }
+      if (ok) ok = mbar_wait_warp(bar(Y::bItemFree + n % kItems), ((n / kItems) & 1) ^ 1, abort_flag, status);
+      if (lane == 0 && ok) {
+        volatile int *v = reinterpret_cast<volatile int *>(smem_raw + Y::kOffItem + (n % kItems) * 64);
+        v[2] = -1;
+        mbar_arrive(bar(Y::bItem + n % kItems));
+      }
     }
   } else if (warp < 8) {
     registers_down<Y::kRegs1>();
     constexpr int kPieces = D / 8, kAtOnce = 32 / kPieces, kAhead = 2;      // (a warp has 32 rows of a tile; tiles whose copies are under way beside the one that is waited for)
     const int piece = lane % kPieces, sub = lane / kPieces, wq = warp & 3;
+    KeyItem it, next;
+    // An item's keys, by this warp 64 of them: a lane knows where two lie, and the others ask it.
+    auto fetch_keys = [&](const KeyItem &of) {
+      constexpr int kRowPieces = Y::kRowBytes / 16, kRowsAtOnce = 32 / kRowPieces;
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {
+        const int own = wq * 64 + half * 32 + lane, pos = of.key0 + own;
+        const bool seen = pos < of.hi && (pos >= of.lo || pos < of.n_sink);
+        const int page = seen ? page_of(s, a.bt, of.seq, pos) : -1;
+        const unsigned long long row = store_row(s, max(page, 0), of.head, pos);
+        asm volatile("st.shared.b64 [%0], %1;" ::"r"(base + Y::kOffRow + own * 8), "l"(page >= 0 ? row : ~0ull) : "memory");
+        auto copy4 = [&](uint32_t to, const float *from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(page >= 0 ? 4 : 0) : "memory"); };
+        if (kQ8) copy4(base + Y::kOffScale + own * 4, s.k_scales + row);
+        copy4(base + Y::kOffOld + own * 4, w.weights + row);
+#pragma unroll 4
+        for (int i = 0; i < kRowPieces; ++i) {
+          const int from = i * kRowsAtOnce + lane / kRowPieces;
+          const unsigned long long r = __shfl_sync(0xffffffffu, row, from);
+          copy16(base + Y::kOffKeys + (wq * 64 + half * 32 + from) * Y::kPitch + (lane % kRowPieces) * 16, s.k_rows + r * Y::kRowBytes + (lane % kRowPieces) * 16, __shfl_sync(0xffffffffu, page, from) >= 0);
+        }
+      }
+    };
+    bool ok = true, more = read_item(0, it);
+    if (more) {
+      fetch_keys(it);
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(Y::bRaw));
+    }
     int q = 0;
-    bool ok = true;
-    for (int i = blockIdx.x; i < n_blocks && ok; i += gridDim.x) {
-      const int key0 = key_of_block(i), tile0 = first_tile(key0), tiles = max(end_tile(key0) - tile0, 0);
+    for (int n = 0; more && ok; ++n) {
+      more = false;
+      const int keys_at = min(kStages, it.tiles) - 1;          // behind this tile the next item's keys are asked for
       float lse[kAhead + 1];
 #pragma unroll
       for (int k = 0; k <= kAhead; ++k) lse[k] = 0.f;
-      for (int j = 0; j < tiles + kAhead && ok; ++j) {
-        if (j < tiles) {
+      for (int j = 0; j < it.tiles + kAhead && ok; ++j) {
+        if (j < it.tiles) {
           const int at = q + j;
           ok = mbar_wait_warp(bar(Y::bQEmpty + at % kStages), ((at / kStages) & 1) ^ 1, abort_flag, status);
           if (!ok) break;
-          // (a lane knows where one row lies, and the others ask it)
-          const int r = (tile0 + j) * kQueryTile + tid, row = min(r, rows - 1), t = a.group.div(row), h = head * G + row - t * G;
-          const char *mine = a.Q.ptr + (sp.start + t) * a.Q.st + h * a.Q.sh;
+          const int r = (it.tile0 + j) * kQueryTile + tid, row = min(r, it.rows - 1), t = a.group.div(row), h = it.head * G + row - t * G;
+          const char *mine = a.Q.ptr + (it.start + t) * a.Q.st + h * a.Q.sh;
           const uint32_t to = base + (at % kStages) * kTile + (piece >> 3) * kHalf + wq * 32 * 128;
 #pragma unroll
-          for (int it = 0; it < kPieces; ++it) {
-            const int from = it * kAtOnce + sub;
+          for (int k = 0; k < kPieces; ++k) {
+            const int from = k * kAtOnce + sub;
             const char *src = reinterpret_cast<const char *>(__shfl_sync(0xffffffffu, (unsigned long long)mine, from));
-            copy16(to + from * 128 + (((piece & 7) ^ (from & 7)) << 4), src + piece * 16, r - tid + wq * 32 + from < rows);
+            copy16(to + from * 128 + (((piece & 7) ^ (from & 7)) << 4), src + piece * 16, r - tid + wq * 32 + from < it.rows);
           }
-          const float x = a.lse[(size_t)(sp.start + t) * a.n_heads + h] * kLog2e;
-          lse[kAhead] = r < rows && x != -INFINITY ? x : INFINITY;
+          const float x = a.lse[(size_t)(it.start + t) * a.n_heads + h] * kLog2e;
+          lse[kAhead] = r < it.rows && x != -INFINITY ? x : INFINITY;
+        }
+        if (j == keys_at) {
+          more = read_item(n + 1, next);
+          if (more) ok = mbar_wait_warp(bar(Y::bRawFree), n & 1, abort_flag, status);
+          if (!ok) break;
+          if (more) fetch_keys(next);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
         if (j >= kAhead) {
@@ -356,12 +476,16 @@ __global__ void __launch_bounds__(WeighTile<D, kQ8>::kThreads, 1) paged_weigh_ti
           asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
           fence_async_proxy();
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar(Y::bQFull + at % kStages));
+          if (lane == 0) {
+            mbar_arrive(bar(Y::bQFull + at % kStages));
+            if (more && j == keys_at + kAhead) mbar_arrive(bar(Y::bRaw));
+          }
         }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) lse[k] = lse[k + 1];
       }
-      q += tiles;
+      q += it.tiles;
+      it = next;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
   } else {
@@ -369,7 +493,6 @@ __global__ void __launch_bounds__(WeighTile<D, kQ8>::kThreads, 1) paged_weigh_ti
     const int wg = (warp - 8) >> 2, quarter = warp & 3, row = quarter * 32 + lane, col0 = (wg & 1) * (kUnit / 2);
     const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
     int q = 0;
-    bool ok = true;
     float total[2];
     // This warpgroup's columns of unit u, rows r0 .. of the sequence's.
     auto unit = [&](int u, int r0, int all_lo, int all_hi, const int *lo, const int *hi, const uint64_t *k2) {
@@ -389,31 +512,36 @@ __global__ void __launch_bounds__(WeighTile<D, kQ8>::kThreads, 1) paged_weigh_ti
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(Y::bSFree + u % kUnits));
       uint64_t sum[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
-      auto sweep = [&](auto masked, const uint32_t *seen) {
+      if (nothing == 0 && all_lo <= r0 && all_hi >= r0 + 32) {
 #pragma unroll
         for (int e = 0; e < 32; e += 4) {
           const float4 l = load_shared4(lse_at + e * 4);
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
+            const uint64_t y0 = fma2(pack2(x[t][e], x[t][e + 1]), k2[t], pack2(l.x, l.y)), y1 = fma2(pack2(x[t][e + 2], x[t][e + 3]), k2[t], pack2(l.z, l.w));
+            float y[4];
+            unpack2(y0, y[0], y[1]);
+            unpack2(y1, y[2], y[3]);
+            const uint64_t p0 = pack2(ex2(y[0]), ex2(y[1]));
+            const uint64_t p1 = t == 0 ? exp2_pair(y1) : pack2(ex2(y[2]), ex2(y[3]));      // (one in four: us, none / one / three of eight / half of them 577 / 555 / 599 / 658)
+            sum[t] = add2(sum[t], add2(p0, p1));
+          }
+        }
+      } else {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const uint32_t seen = lowest_bits(hi[t] - r0) & ~lowest_bits(lo[t] - r0) & ~nothing;
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) {
+            const float4 l = load_shared4(lse_at + e * 4);
             float y[4];
             unpack2(fma2(pack2(x[t][e], x[t][e + 1]), k2[t], pack2(l.x, l.y)), y[0], y[1]);
             unpack2(fma2(pack2(x[t][e + 2], x[t][e + 3]), k2[t], pack2(l.z, l.w)), y[2], y[3]);
 #pragma unroll
-            for (int f = 0; f < 4; ++f) {
-              y[f] = ex2(y[f]);
-              if (decltype(masked)::value) y[f] = (seen[t] >> (e + f)) & 1u ? y[f] : 0.f;
-            }
+            for (int f = 0; f < 4; ++f) y[f] = (seen >> (e + f)) & 1u ? ex2(y[f]) : 0.f;
             sum[t] = add2(sum[t], add2(pack2(y[0], y[1]), pack2(y[2], y[3])));
           }
         }
-      };
-      if (nothing == 0 && all_lo <= r0 && all_hi >= r0 + 32) {
-        sweep(std::false_type{}, nullptr);
-      } else {
-        uint32_t seen[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) seen[t] = lowest_bits(hi[t] - r0) & ~lowest_bits(lo[t] - r0) & ~nothing;
-        sweep(std::true_type{}, seen);
       }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -423,31 +551,22 @@ __global__ void __launch_bounds__(WeighTile<D, kQ8>::kThreads, 1) paged_weigh_ti
       }
       return there;
     };
-    for (int i = blockIdx.x; i < n_blocks; i += gridDim.x) {
-      const int key0 = key_of_block(i), tile0 = first_tile(key0), tiles = max(end_tile(key0) - tile0, 0);
+    KeyItem it;
+    bool ok = true;
+    for (int n = 0;; ++n) {
+      const bool there = read_item(n, it);
+      if (!all_agree(there)) break;              // (a warp whose wait gave up comes here, too; and the last item's sums have been read)
+      ok = ok && mbar_wait_warp(bar(Y::bRaw), n & 1, abort_flag, status);
       // keys into TMEM: warpgroups 0 and 1 have halves of A's dims, 2 and 3 of B's (what reads them is through: its results have been waited for)
-      bool there[2];
-      size_t at_row[2];
-      uint64_t k2[2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int pos = key0 + t * 128 + row, page = some_see(sp, pos) ? page_of(s, a.bt, seq, pos) : -1;
-        there[t] = page >= 0;
-        at_row[t] = store_row(s, max(page, 0), head, pos);
-        float ks = a.scale_log2e;
-        if (kQ8 && there[t]) ks *= kCodeUnit * s.k_scales[at_row[t]];
-        k2[t] = pack2(ks, ks);
-      }
       {
         const int tile = wg >> 1, half = wg & 1;
-        const bool on = tile ? there[1] : there[0];
-        const char *from = s.k_rows + (tile ? at_row[1] : at_row[0]) * (D * (kQ8 ? 1 : 2)) + half * (D / 2) * (kQ8 ? 1 : 2);
+        const uint32_t from = base + Y::kOffKeys + (tile * 128 + row) * Y::kPitch + half * (Y::kRowBytes / 2);
 #pragma unroll
         for (int c = 0; c < D / 64; ++c) {       // 32 dims, 16 columns
           uint32_t k[16];
 #pragma unroll
           for (int x = 0; x < (kQ8 ? 2 : 4); ++x) {
-            const uint4 v = on ? *reinterpret_cast<const uint4 *>(from + (c * (kQ8 ? 2 : 4) + x) * 16) : make_uint4(0u, 0u, 0u, 0u);
+            const uint4 v = load_shared16(from + (c * (kQ8 ? 2 : 4) + x) * 16);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               if constexpr (kQ8) {
@@ -461,30 +580,48 @@ __global__ void __launch_bounds__(WeighTile<D, kQ8>::kThreads, 1) paged_weigh_ti
           }
           tc_st16(lane_addr + kColK + tile * (D / 2) + half * (D / 4) + c * 16, k);
         }
-        tc_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(Y::bKeys));
       }
-      // the rows that see this thread's keys, and those that see all of the warp's
+      unsigned long long at_row[2];
+      float old[2];
+      uint64_t k2[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int key = t * 128 + row;
+        float ks = a.scale_log2e, scale = 1.f;
+        asm volatile("ld.shared.b64 %0, [%1];" : "=l"(at_row[t]) : "r"(base + Y::kOffRow + key * 8) : "memory");
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(old[t]) : "r"(base + Y::kOffOld + key * 4) : "memory");
+        if constexpr (kQ8) {
+          asm volatile("ld.shared.f32 %0, [%1];" : "=f"(scale) : "r"(base + Y::kOffScale + key * 4) : "memory");
+          ks *= kCodeUnit * scale;
+        }
+        k2[t] = pack2(ks, ks);
+      }
+      tc_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(bar(Y::bKeys));
+        mbar_arrive(bar(Y::bRawFree));
+      }
+      // the rows that see this thread's keys, [lo, hi), and those that see all of the warp's
       int lo[2], hi[2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const int pos = key0 + t * 128 + row;
-        lo[t] = row_lo(pos);
-        hi[t] = there[t] ? row_hi(pos) : 0;
+        const int pos = it.key0 + t * 128 + row;
+        lo[t] = a.mask.causal ? (int)min((long long)it.rows, (long long)max(pos - it.first, 0) * G) : 0;
+        hi[t] = at_row[t] == ~0ull ? 0 : a.mask.window > 0 && pos >= it.n_sink ? (int)min((long long)it.rows, max((long long)pos - it.first + a.mask.window, 0ll) * G) : it.rows;
       }
       const int all_lo = __reduce_max_sync(0xffffffffu, max(lo[0], lo[1])), all_hi = __reduce_min_sync(0xffffffffu, min(hi[0], hi[1]));
       total[0] = total[1] = 0.f;
-      for (int j = 0; j < tiles && ok; ++j) ok = unit(2 * (q + j) + (wg >> 1), (tile0 + j) * kQueryTile + (wg >> 1) * kUnit + col0, all_lo, all_hi, lo, hi, k2);
-      q += tiles;
+      for (int j = 0; j < it.tiles && ok; ++j) ok = unit(2 * (q + j) + (wg >> 1), (it.tile0 + j) * kQueryTile + (wg >> 1) * kUnit + col0, all_lo, all_hi, lo, hi, k2);
+      q += it.tiles;
       // the warpgroups' shares of the rows are put together, in their order
       const uint32_t sum_at = base + Y::kOffSum + row * 4;
       if (wg > 0) {
         asm volatile("st.shared.f32 [%0], %1;" ::"r"(sum_at + (wg - 1) * 1024), "f"(total[0]) : "memory");
         asm volatile("st.shared.f32 [%0], %1;" ::"r"(sum_at + (wg - 1) * 1024 + 512), "f"(total[1]) : "memory");
       }
-      if (!all_agree(ok)) break;                 // (a warp whose wait gave up comes here, too)
+      if (!all_agree(ok)) break;
       if (wg == 0) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -495,13 +632,9 @@ __global__ void __launch_bounds__(WeighTile<D, kQ8>::kThreads, 1) paged_weigh_ti
             asm volatile("ld.shared.f32 %0, [%1];" : "=f"(other) : "r"(sum_at + k * 1024 + t * 512) : "memory");
             sum += other;
           }
-          if (there[t]) {
-            float *to = w.weights + at_row[t];
-            *to = (key0 + t * 128 + row < sp.first ? w.decay * *to : 0.f) + sum;
-          }
+          if (at_row[t] != ~0ull) w.weights[at_row[t]] = (it.key0 + t * 128 + row < it.first ? w.decay * old[t] : 0.f) + sum;
         }
       }
-      if (!all_agree(true)) break;               // (the sums have been read)
     }
     tc_fence_before();
   }
@@ -564,7 +697,6 @@ extern "C" scalekv_status scalekv_paged_weigh(scalekv_paged *kv, int32_t layer, 
   long long keys = std::max(batch->max_length, 1);
   if (a.mask.window > 0) keys = std::min<long long>(keys, (long long)a.mask.window + batch->max_new + a.mask.n_sink + 32);
   const int steps = (int)((keys + 15) / 16);
-  if (max_rows > kWeighRows && a.bt.n_seqs > 65535) return fail(c, SCALEKV_ERR_UNSUPPORTED, "more than 65535 sequences");
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   auto go = [&](auto dim, auto codes) {
     constexpr int kD = decltype(dim)::value;
@@ -575,8 +707,9 @@ extern "C" scalekv_status scalekv_paged_weigh(scalekv_paged *kv, int32_t layer, 
       else if (max_rows <= 16) launch(paged_weigh_stream_kernel<kD, kQ8, 2>, grid, kStreamThreads, WeighLayout<kD, kQ8, 2>::kSmem, st, w);
       else launch(paged_weigh_stream_kernel<kD, kQ8, 4>, grid, kStreamThreads, WeighLayout<kD, kQ8, 4>::kSmem, st, w);
     } else {
-      const dim3 grid((unsigned)((keys + 2 * kKeyRows - 2) / kKeyRows), H, a.bt.n_seqs);
-      launch(paged_weigh_tile_kernel<kD, kQ8>, grid, WeighTile<kD, kQ8>::kThreads, WeighTile<kD, kQ8>::kSmem, st, w);
+      // a CTA to an SM, and no more of them than there may be items
+      const long long items = std::min<long long>((keys + 2 * kKeyRows - 2) / kKeyRows * H, c->n_sm) * a.bt.n_seqs;
+      launch(paged_weigh_tile_kernel<kD, kQ8>, dim3((unsigned)std::min<long long>(items, c->n_sm)), WeighTile<kD, kQ8>::kThreads, WeighTile<kD, kQ8>::kSmem, st, w);
     }
     return launched(c, "paged_weigh");
   };

@@ -70,6 +70,22 @@ def test_trees(store, d, lengths, new, heads, group, page):
     check(c, [tree(c.rng, n) for n in new])
 
 
+@pytest.mark.parametrize("store,d", [("q8", 128), ("bf16", 64)])
+@pytest.mark.parametrize("lengths,new,heads,group", [
+    ([6000, 300, 2000], [70, 40, 64], 2, 2),                  # one item of a pair of tiles beside singles
+    ([4000], [65], 1, 8),                                     # one sequence, three items, one of them short
+    ([5000, 0, 33, 700, 40, 1300], [40, 0, 33, 9, 0, 64], 1, 1),      # sequences without a draft between others
+    ([40] * 40 + [3000], [33] * 41, 2, 1),                    # many short ones and a long one
+    ([200] * 170, [36] * 170, 1, 1),                          # more items than CTAs
+])
+def test_ragged_drafts(store, d, lengths, new, heads, group):
+    c = Case(lengths, new, heads, group, d, store, 64).fill()
+    sees = [tree(c.rng, n) for n in new]
+    check(c, sees)
+    again = draft(c, sees)
+    assert all(torch.equal(x, y) for x, y in zip(draft(c, sees), again))
+
+
 @pytest.mark.parametrize("store", ["q8", "bf16"])
 @pytest.mark.parametrize("new,group", [([6, 3], 1), ([31, 6], 1), ([50, 9], 3)])
 def test_any_bits(store, new, group):
