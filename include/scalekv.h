@@ -487,7 +487,8 @@ scalekv_status scalekv_paged_attend_tree(scalekv_paged *kv, int32_t layer, const
 /* What is accepted of a draft moves up: of sequence b new token path[b * path_stride + i], i < counts[b] <= path_len, becomes the i'th
  * behind what was there before (path, counts: device; a path ascends).  layer -1: in all layers.  The lengths are the caller's: lengths[b] less the
  * new tokens, plus counts[b], once all layers are done.  A path that does not ascend, or names no new token, or a place whose page is out of range
- * is reported, and it and what is behind it in the path stay where they are; so does all of a sequence whose count is out of range. */
+ * is reported, and it and what is behind it in the path stay where they are; so does all of a sequence whose count is out of range.  Pages that a draft lies in
+ * must not be other sequences', too. */
 scalekv_status scalekv_paged_accept(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, const int32_t *path,
                                     int32_t path_stride, int32_t path_len, const int32_t *counts, void *stream);
 
@@ -503,7 +504,7 @@ scalekv_status scalekv_paged_weigh(scalekv_paged *kv, int32_t layer, const scale
                                    float *weights, float decay, void *stream);
 
 /* Of every sequence and kv head min(keep[b], lengths[b]) entries stay: the first n_sink, the last n_recent (as many as there is room for
- * beside those) and of the rest those with the largest weights, of equal ones the first (a NaN counts as -inf).  They are copied, in their
+ * beside those) and of the rest those with the largest weights (as for scalekv_paged_weigh), of equal ones the first (a NaN counts as -inf).  They are copied, in their
  * order, to positions 0, 1, .. of the pages that to_table names (to_pages of its to_stride entries for a sequence), K, V and weights alike; every kv head
  * keeps entries of its own.  kept: device [n_seqs][n_kv_heads][kept_stride], receives the positions that stay, ascending.  Only table and lengths of the batch are looked
  * at.  A page of to_table must not be one that the call reads; what was held in the old pages stays there.  A sequence whose keep is negative, or of

@@ -239,6 +239,41 @@ class Sequences:
         self.table[b] = [-1] * len(self.table[b])
         self.lengths[b] = 0
 
+    def retract(self, n):
+        """The last n[b] tokens of sequence b are taken back (a draft's, once what was accepted of it has moved up): pages that hold none of its tokens any more are free."""
+        if len(n) != self.n_seqs or any(not 0 <= k <= length for k, length in zip(n, self.lengths)):
+            raise ValueError(f"expected {self.n_seqs} numbers of tokens, none below 0 or above the sequence's, got {n}")
+        self.lengths = [length - k for length, k in zip(self.lengths, n)]
+        for b, length in enumerate(self.lengths):
+            for i in range(-(-length // self.page_tokens), len(self.table[b])):
+                if self.table[b][i] >= 0:
+                    self.free.append(self.table[b][i])
+                    self.table[b][i] = -1
+
+    def survivors(self, keep):
+        """Free pages for what an eviction leaves of every sequence, keep[b] entries at most -> their table.  They stay free until survive() takes them: all layers
+        evict to the same ones first.  Raises where there are too few."""
+        if len(keep) != self.n_seqs or min(keep, default=0) < 0:
+            raise ValueError(f"expected {self.n_seqs} numbers of entries, none below 0, got {keep}")
+        if any(p < 0 for row, length in zip(self.table, self.lengths) for p in row[:-(-length // self.page_tokens)]):
+            raise ValueError("a window has taken pages of a sequence")
+        need = [-(-min(k, length) // self.page_tokens) for k, length in zip(keep, self.lengths)]
+        if sum(need) > len(self.free):
+            raise MemoryError(f"{sum(need)} pages needed, {len(self.free)} free")
+        table, at = [[-1] * len(row) for row in self.table], len(self.free)
+        for b, n in enumerate(need):
+            for i in range(n):
+                at -= 1
+                table[b][i] = self.free[at]
+        return table
+
+    def survive(self, table, keep):
+        """The sequences are what all layers have evicted to the pages of survivors(): the old pages are free."""
+        taken = {p for row in table for p in row if p >= 0}
+        self.free = [p for p in self.free if p not in taken] + [p for row in self.table for p in row if p >= 0]
+        self.table = [list(row) for row in table]
+        self.lengths = [min(k, length) for k, length in zip(keep, self.lengths)]
+
     def batch(self, new, device=0):
         """The descriptor of a step whose new tokens extend() has let in: one for all layers."""
         dev = dict(dtype=torch.int32, device=f"cuda:{device}")
@@ -247,15 +282,80 @@ class Sequences:
                                   max(new), max(self.lengths))
 
 
-def token_step(kv: binding.PagedKV, batch, rows, causal=True, window=0, n_sink=0):
+def token_step(kv: binding.PagedKV, batch, rows, causal=True, window=0, n_sink=0, rotary=None, positions=None, weights=None, decay=1.0):
     """One step of every layer: the new tokens' rows join the cache, quantised if it holds codes, and their queries attend over it.
-    rows(layer) -> (Q, K, V) of the new tokens; returns the layers' outputs."""
+    rows(layer) -> (Q, K, V) of the new tokens; returns the layers' outputs.  rotary (binding.Rotary) and positions (int32 [axes, tokens]): Q and K are turned by them
+    first.  weights (float32 [layers, pages, kv heads, rows of a page]): what attention each entry gets is added to it (see evict)."""
     out = []
     for l in range(kv.n_layers):
         Q, K, V = rows(l)
-        kv.scalekv_paged_write(l, batch, K, V)
-        out.append(kv.scalekv_paged_attend(l, batch, Q, causal=causal, window=window, n_sink=n_sink))
+        if rotary is None:
+            kv.scalekv_paged_write(l, batch, K, V)
+        else:
+            Q = kv.scalekv_paged_write_rotated(l, batch, Q, K, V, rotary, positions)
+        lse = None if weights is None else torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device)
+        out.append(kv.scalekv_paged_attend(l, batch, Q, lse=lse, causal=causal, window=window, n_sink=n_sink))
+        if weights is not None:
+            kv.scalekv_paged_weigh(l, batch, Q, lse, weights[l], causal=causal, window=window, n_sink=n_sink, decay=decay)
     return out
+
+
+def tree_bits(parents):
+    """What the tokens of drafts see of one another, and how deep each lies: parents[b][i] < i is the token that drafted token i of sequence b follows, -1 the sequence
+    itself.  -> (bits as scalekv_paged_attend_tree takes them, a list of words for every token; depths, 0 for those that follow the sequence)."""
+    words, bits, depths = -(-max((len(p) for p in parents), default=0) // 32), [], []
+    for b, draft in enumerate(parents):
+        seen, deep = [], []
+        for i, p in enumerate(draft):
+            if not -1 <= p < i:
+                raise ValueError(f"token {i} of sequence {b} cannot follow token {p}")
+            seen.append((seen[p] if p >= 0 else 0) | 1 << i)
+            deep.append(deep[p] + 1 if p >= 0 else 0)
+        for s in seen:
+            row = [s >> 32 * w & 0xFFFFFFFF for w in range(words)]
+            bits.append([w - (1 << 32) if w >> 31 else w for w in row])
+        depths += deep
+    return bits, depths
+
+
+def draft_step(kv: binding.PagedKV, seqs: Sequences, parents, rows, accept, rotary=None, positions=None):
+    """One step with drafted tokens: those of sequence b form the tree parents[b] (see tree_bits), attend over the cache and their ancestors, and of them
+    accept(layers' outputs)[b], a path's tokens in ascending order, stay.  rows(layer) -> (Q, K, V) of all drafted tokens; rotary and positions as for token_step (a
+    token's position is its sequence's length plus its depth).  -> (outputs, accepted paths)"""
+    new = [len(p) for p in parents]
+    bits, _ = tree_bits(parents)
+    seqs.extend(new)
+    batch, dev = seqs.batch(new, kv.device_index), dict(dtype=torch.int32, device=kv.device)
+    tree = torch.tensor(bits, **dev).view(sum(new), max(1, -(-max(new, default=0) // 32)))
+    out = []
+    for l in range(kv.n_layers):
+        Q, K, V = rows(l)
+        if rotary is None:
+            kv.scalekv_paged_write(l, batch, K, V)
+        else:
+            Q = kv.scalekv_paged_write_rotated(l, batch, Q, K, V, rotary, positions)
+        out.append(kv.scalekv_paged_attend_tree(l, batch, Q, tree))
+    paths = accept(out)
+    most = max((len(p) for p in paths), default=0)
+    kv.scalekv_paged_accept(batch, torch.tensor([list(p) + [-1] * (most - len(p)) for p in paths], **dev).view(len(paths), most),
+                            torch.tensor([len(p) for p in paths], **dev))
+    seqs.retract([n - len(p) for n, p in zip(new, paths)])
+    return out, paths
+
+
+def evict(kv: binding.PagedKV, seqs: Sequences, weights, keep, n_sink=0, n_recent=0):
+    """Of every sequence and kv head keep[b] entries stay in every layer: the first n_sink, the last n_recent, the heaviest of the rest by weights (see token_step), in pages
+    that were free; the old ones are given back.  -> positions that stay, int32 [n_seqs, kv heads, most] for each layer."""
+    table = seqs.survivors(keep)
+    dev = dict(dtype=torch.int32, device=kv.device)
+    batch = seqs.batch([0] * seqs.n_seqs, kv.device_index)
+    most = max(min(k, length) for k, length in zip(keep, seqs.lengths))
+    kept = [torch.full((seqs.n_seqs, kv.n_kv_heads, most), -1, **dev) for _ in range(kv.n_layers)]
+    to, counts = torch.tensor(table, **dev), torch.tensor(keep, **dev)
+    for l in range(kv.n_layers):
+        kv.scalekv_paged_evict(l, batch, to, counts, weights[l], n_sink, n_recent, kept[l])
+    seqs.survive(table, keep)
+    return kept
 
 
 def prompts_and_tokens(kv: binding.PagedKV, seqs: Sequences, prompts, n_tokens, chunk, rows, window=0, n_sink=0):

@@ -142,6 +142,8 @@ def test_refused_weighings():
         c.kv.scalekv_paged_weigh(c.layer, c.batch(), Q[:, :3], lse[:, :3].contiguous(), w)
     with pytest.raises(ValueError, match="window"):
         c.kv.scalekv_paged_weigh(c.layer, c.batch(), Q, lse, w, window=-1)
+    with pytest.raises(binding.ScaleKVError, match="aligned"):
+        c.kv.scalekv_paged_weigh(c.layer, c.batch(), Q, lse, torch.zeros(w.numel() + 1, device="cuda")[1:].view(w.shape))
     c.kv.scalekv_paged_sync()
     assert not w.any()
 
@@ -243,4 +245,6 @@ def test_refused_evictions():
             c.kv.scalekv_paged_evict(c.layer, c.batch(), to, keep, w, sink, recent, kept)
     with pytest.raises(binding.ScaleKVError, match="layer"):
         c.kv.scalekv_paged_evict(5, c.batch(), to, keep, w)
+    with pytest.raises(binding.ScaleKVError, match="aligned"):
+        c.kv.scalekv_paged_evict(c.layer, c.batch(), to, keep, torch.zeros(w.numel() + 1, device="cuda")[1:].view(w.shape))
     c.kv.scalekv_paged_sync()
