@@ -374,8 +374,8 @@ __global__ void __launch_bounds__(kGatherThreads) paged_gather_kernel(const __gr
   const int k = kept_of(a, b, length, false), r0 = block * kGatherRows, n = min(k - r0, kGatherRows);
   if (n <= 0) return;
   if ((int)threadIdx.x < n) {
-    const int i = r0 + threadIdx.x, pos = a.kept[((size_t)b * a.s.heads + head) * a.kept_stride + i], from = page_of(a.s, a.bt, b, pos);
-    const int to = a.to[(size_t)b * a.to_stride + (i >> a.s.page_shift)];
+    const int i = r0 + threadIdx.x, pos = a.kept[((size_t)b * a.s.heads + head) * a.kept_stride + i], to = a.to[(size_t)b * a.to_stride + (i >> a.s.page_shift)];
+    const int from = page_of(a.s, a.bt, b, pos);
     const bool ok = (unsigned)to < (unsigned)a.s.n_pages;
     if (!ok) report(a.s.status);
     src[threadIdx.x] = from >= 0 && ok ? (long long)store_row(a.s, from, head, pos) : -1;
