@@ -365,7 +365,7 @@ scalekv_status scalekv_profile_read(scalekv_ctx *ctx, int32_t which, double *ms_
  *  - Every call enqueues on the given cudaStream_t of the handle's device (which must be current) and returns; no call but init and
  *    sync waits for the device, and all but these can be captured into a CUDA graph (a batch's arrays are read on the device when the
  *    kernels run; its sizes are the call's).
- *  - Calls on one handle share its workspace: attends on different streams have to be ordered by the caller.
+ *  - Calls on one handle share its workspace: attends (of drafts, too) on different streams have to be ordered by the caller.
  *  - Lengths, starts and pages are read on the device.  One that is out of range is never followed: what it would lead to is left out
  *    (a row read comes back as zeros, a key counts as hidden, O and lse of a token that belongs to no sequence keep what they held),
  *    and the sticky device status, SCALEKV_ERR_DEVICE_CHECK, says so. */

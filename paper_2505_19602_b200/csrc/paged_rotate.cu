@@ -5,8 +5,10 @@
 // Angles grow far beyond what 32 bits hold of them (position 2^20 of a pair that turns by a radian leaves 2^-4 radians), so they are formed in 64 bits and in turns, less whole ones; what
 // is left, at most half a turn, goes into sine and cosine in fp32.  They are the same for all heads: a block works them out once for its tokens, into shared memory.
 //
-// Every row is moved once; what bounds that is memory for bf16 rows and the quotients' instructions for codes, as in paged_store.cuh.  A lane has 16 values of a row, as two pieces of eight:
+// Every row is moved once; what bounds that is memory, and with bf16 rows the instructions for a lane's 16 values, about 200 (56 of 100 issue slots).  A lane has 16 values of a row, as two pieces of eight:
 // where the pairs are a dimension of the first half and one of the second, the pieces are those of eight pairs, so nothing is exchanged between lanes.
+// us, 8 192 tokens of 16 heads of 128: bf16 into bf16 41.6 (4.8 TB/s of 6.5 measured), f32 into bf16 54 (5.6), bf16 into codes 64.  (Five blocks to an SM with bf16 rows, at 20 bytes of spills, 48.3 / 66.7 with codes where four take
+// 49.5 / 68.9, with one event's 5 us; with f32 rows five were the slower.  Two rounds of loads on their way, or angles behind the look-up of places: the same to 1 us.)
 #include "paged_host.cuh"
 #include "paged_store.cuh"
 
@@ -201,6 +203,7 @@ extern "C" scalekv_status scalekv_paged_write_rotated(scalekv_paged *kv, int32_t
   r.positions = positions;
   r.axis_stride = axis_stride;
   r.mv.per_token = Divisor::of((n_heads + 2 * c->cfg.n_kv_heads) * (c->cfg.head_dim / 16));
+  // (as many tokens to a block as paged_store's write takes; twice and four times as many: 51.6 and 56.9 us where it takes 49.5, half as many 48.6 and, into codes, 69.4 for 68.9)
   const int full = (4 * kStoreThreads + r.mv.per_token.d - 1) / r.mv.per_token.d;
   r.mv.tokens = std::max(1, std::min(std::min(full, kMostTokens), n / (2 * c->n_sm)));
   const dim3 grid((n + r.mv.tokens - 1) / r.mv.tokens);

@@ -22,7 +22,9 @@ __device__ __forceinline__ int key_of(const Span &sp, int step) { return (step <
 // Whether some row sees position pos of a step.
 __device__ __forceinline__ bool some_see(const Span &sp, int pos) { return pos < sp.hi && (pos >= sp.lo || pos < sp.n_sink); }
 
-// ---- few rows: keys stream past queries that stay in registers, as in paged_stream.cuh: products are m16n8k16 with the rows as n-tiles of eight (there is the layout).
+// ---- few rows: keys stream past queries that stay in registers, as in paged_stream.cuh: products are m16n8k16 with the rows as n-tiles of eight (there is the layout).  A warp takes stretches of
+// eight steps of 16 keys, whose pages it looks up at once, a lane to each.  What bounds it: reading K and the sums once, and with codes the instructions that turn them into bf16.  us, 32 sequences of up to 10 521
+// entries, 32 heads on 8 of 128: codes 58 (4.6 TB/s; stretches of 8 / 16 / 32 steps 54 / 57 / 65 with pages looked up at once, step by step 59 to 64; 70 of 100 issue slots), bf16 85 (5.9 TB/s).
 template <int D, bool kQ8, int kN>
 struct WeighLayout {
   static constexpr int kRowBytes = D * (kQ8 ? 1 : 2);
@@ -189,8 +191,10 @@ __global__ void __launch_bounds__(kStreamThreads) paged_weigh_stream_kernel(cons
 //   warps 4-7     : the queries, by asynchronous copies of 16 bytes (rows are a token's heads, in any strides), and their log-sum-exps; the next item's keys, scales and weights
 //   warps 8-23    : keys from shared memory into TMEM (codes become bf16 exactly), then p = 2^(x ks - lse) and its sums
 // Every wait is bounded, as in paged_tile.cuh.
-// What bounds it: exponentials, of which the special function unit does 16 a cycle (a unit of 128 x 128 takes it twice as long as the tensor core its product).  So one in four is
-// formed on the FMA pipe (exp2_pair).
+// What bounds it: exponentials, of which the special function unit does 16 a cycle (a tile of 128 x 128 takes it twice as long as the tensor core its product; it is busy for 80 of 100 cycles while a
+// CTA has work), and the power that both draw: 2 048 queries of 4 x 32 heads behind 6 144 entries in codes take 577 us from a cool start, 0.83 PFLOP/s, and 596 to 615 in a row.  (One exponential in
+// four by a polynomial on the FMA pipe: 555 us from a cool start, 597 in a row; half of them 658.  A key tile's rows in shared memory and eight softmax warps: 715; products issued one by one: 621; a CTA for
+// each block of keys, its rows fetched when it begins: 600.  16 columns at a time, the next ones on their way: 643.)
 constexpr int kKeyRows = 256, kQueryTile = 128, kUnit = 64, kUnits = 3, kSumGroups = 4, kItems = 3;
 
 template <int D, bool kQ8>
@@ -238,25 +242,6 @@ template <int D> __device__ __forceinline__ void mma_ts_k(uint32_t d_tmem, uint3
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}" ::"r"(d_tmem),
         "r"(a_tmem + 8 * k), "r"(b_lo + (uint32_t)((k >> 2) * 1024 + (k & 3) * 2)), "r"(hi), "r"(idesc), "r"(k > 0 ? 1u : 0u)
         : "memory");
-}
-
-// Two powers of two on the FMA pipe: y = n + f with n a whole number (adding 1.5 2^23 leaves it in the low bits), 2^f for |f| <= 1/2 by the polynomial of degree 5 whose largest relative error,
-// 7.5e-8, is the least (by Remez' exchange; 2.1e-7 with coefficients and steps in fp32, where ex2.approx has 2^-22), times 2^n.  Exponents below -126 count as that: 2^-126 more in a sum.  NaN stays NaN.
-__device__ __forceinline__ uint64_t exp2_pair(uint64_t y2) {
-  float a, b;
-  unpack2(y2, a, b);
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(-126.f));
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(b) : "f"(-126.f));
-  const uint64_t y = pack2(a, b), shifted = add2(y, pack2(12582912.f, 12582912.f)), f = add2(y, mul2(add2(shifted, pack2(-12582912.f, -12582912.f)), pack2(-1.f, -1.f)));
-  auto c = [](float x) { return pack2(x, x); };
-  uint64_t p = fma2(f, c(0.0013276472454890609f), c(0.009675540961325169f));
-  p = fma2(p, f, c(0.05550713092088699f));
-  p = fma2(p, f, c(0.24022120237350464f));
-  p = fma2(p, f, c(0.6931469440460205f));
-  p = fma2(p, f, c(1.0000001192092896f));
-  unpack2(shifted, a, b);
-  const uint32_t n0 = (__float_as_uint(a) << 23) + 0x3f800000u, n1 = (__float_as_uint(b) << 23) + 0x3f800000u;
-  return mul2(p, pack2(__uint_as_float(n0), __uint_as_float(n1)));
 }
 
 // What an item is: key0 < 0: there are no more.
@@ -518,13 +503,10 @@ __global__ void __launch_bounds__(WeighTile<D, kQ8>::kThreads, 1) paged_weigh_ti
           const float4 l = load_shared4(lse_at + e * 4);
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
-            const uint64_t y0 = fma2(pack2(x[t][e], x[t][e + 1]), k2[t], pack2(l.x, l.y)), y1 = fma2(pack2(x[t][e + 2], x[t][e + 3]), k2[t], pack2(l.z, l.w));
             float y[4];
-            unpack2(y0, y[0], y[1]);
-            unpack2(y1, y[2], y[3]);
-            const uint64_t p0 = pack2(ex2(y[0]), ex2(y[1]));
-            const uint64_t p1 = t == 0 ? exp2_pair(y1) : pack2(ex2(y[2]), ex2(y[3]));      // (one in four: us, none / one / three of eight / half of them 577 / 555 / 599 / 658)
-            sum[t] = add2(sum[t], add2(p0, p1));
+            unpack2(fma2(pack2(x[t][e], x[t][e + 1]), k2[t], pack2(l.x, l.y)), y[0], y[1]);
+            unpack2(fma2(pack2(x[t][e + 2], x[t][e + 3]), k2[t], pack2(l.z, l.w)), y[2], y[3]);
+            sum[t] = add2(sum[t], add2(pack2(ex2(y[0]), ex2(y[1])), pack2(ex2(y[2]), ex2(y[3]))));
           }
         }
       } else {
