@@ -103,11 +103,13 @@ __global__ void __launch_bounds__(kAcceptThreads, 5) paged_accept_kernel(const _
 // it so far, in two copies, as the lanes of a warp often mean the same bin.  A long sequence's head is shared by a cluster of CTAs; every CTA holds its stretch of the keys in shared memory (those
 // that find no room are read again), four of them to a load, and the histograms are summed over the cluster, a share of the bins by each.  Then every warp counts what it keeps of a stretch of
 // its own and puts it down behind what lies before it.
+// Up to 256 keys need no histogram: each counts those ahead of it (us, 24 items of 190 keys 14.2 so, 15.7 with histograms, 320 items of 490 keys 30.8 and 24.2, with one event's 10 us).
 // (2) paged_gather_kernel moves the rows, which is most of the bytes, over all SMs whatever the heads and sequences are.
 // us, (1) and (2), from cold caches: one sequence of 170 521 entries, 16 heads, bf16, to 17 052: 31 and 46 (6.0 TB/s); 8 of 10 521 entries, 8 heads in codes, to 1 052: 14 and 11.  (1) is bound by its chain: length, table, weights, and two
 // or three histograms; an entry's weight is little to read.  (First built, a weight to a load and its page looked up ahead of each, 66 and 22; 1 024 threads 40 and 13; a cluster of two for 10 521 entries 17.  (2) with 32 / 64 / 128 entries
 // a block: 49 / 46 / 45.5 and 16 / 14 / 11.)
 constexpr int kChooseThreads = 512, kChooseWarps = kChooseThreads / 32, kBins = 2048, kMostCluster = 8;
+constexpr int kFewKeys = 256;
 constexpr int kCopies = 2;                       // of the histogram (so small that two CTAs with 21 000 keys each find room on an SM: clusters of eight need eight places near one another)
 constexpr int kMostHeld = 40960;                 // keys that a CTA's shared memory holds, 160 KB
 
@@ -122,6 +124,7 @@ struct Evict {
   float *weights;                                // [page][head][row of the page]
   int n_sink, n_recent;
   int held;                                      // keys that the launch gave shared memory for
+  int moves;                                     // whoever chooses moves the rows, too
   int row_pieces, q8;
   Divisor heads, blocks;
 };
@@ -164,17 +167,56 @@ __device__ __forceinline__ void cluster_meet() {
   tc::cluster_wait();
 }
 
-__global__ void __launch_bounds__(kChooseThreads) paged_choose_kernel(const __grid_constant__ Evict a, int cluster) {
+constexpr int kGatherThreads = 256, kGatherRows = 128, kGatherBatch = 4;
+// With so few entries to move at most, whoever chooses them moves them.  (us, 10 521 entries of 64 / 2 heads to 128: 19.9 / 18.7 so, 21.3 / 20.5 in two launches; to 300 of 256 heads 32.5 / 31.5, to 1 052 of 2 heads 36.8 / 20.3; one
+// event's 10 us in each.)
+constexpr int kMostMoved = kGatherRows;
+
+// Moves the entries numbers r0 .. r0 + n - 1, n <= kGatherRows, of those of a sequence and head that stay.  All threads of a block.
+template <int kThreads>
+__device__ __forceinline__ void gather_rows(const Evict &a, int b, int head, int r0, int n, long long *src, long long *dst) {
+  if ((int)threadIdx.x < n) {
+    const int i = r0 + threadIdx.x, pos = __ldcg(a.kept + ((size_t)b * a.s.heads + head) * a.kept_stride + i), to = a.to[(size_t)b * a.to_stride + (i >> a.s.page_shift)];
+    const int from = page_of(a.s, a.bt, b, pos);
+    const bool ok = (unsigned)to < (unsigned)a.s.n_pages;
+    if (!ok) report(a.s.status);
+    src[threadIdx.x] = from >= 0 && ok ? (long long)store_row(a.s, from, head, pos) : -1;
+    dst[threadIdx.x] = ok ? (long long)store_row(a.s, to, head, i) : 0;
+  }
+  __syncthreads();
+  const int both = 2 * a.row_pieces, shift = 31 - __clz(both);      // (a power of two)
+  for (int i0 = threadIdx.x; i0 < n * both; i0 += kGatherBatch * kThreads) {
+    uint4 x[kGatherBatch], *to[kGatherBatch];
+#pragma unroll
+    for (int j = 0; j < kGatherBatch; ++j) {
+      const int i = i0 + j * kThreads, r = i >> shift, c = i & (both - 1);
+      to[j] = nullptr;
+      if (i < n * both && src[r] >= 0) {
+        const bool v = c >= a.row_pieces;
+        uint4 *rows = reinterpret_cast<uint4 *>(v ? a.s.v_rows : a.s.k_rows) + (v ? c - a.row_pieces : c);
+        to[j] = rows + (size_t)dst[r] * a.row_pieces;
+        x[j] = __ldcg(rows + (size_t)src[r] * a.row_pieces);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kGatherBatch; ++j)
+      if (to[j]) *to[j] = x[j];
+  }
+  if ((int)threadIdx.x < n && src[threadIdx.x] >= 0) {
+    const size_t from = (size_t)src[threadIdx.x], to = (size_t)dst[threadIdx.x];
+    a.weights[to] = __ldcg(a.weights + from);
+    if (a.q8) {
+      a.s.k_scales[to] = __ldcg(a.s.k_scales + from);
+      a.s.v_scales[to] = __ldcg(a.s.v_scales + from);
+    }
+  }
+}
+
+__device__ __forceinline__ void choose_entries(const Evict &a, int cluster, int rank, int b, int head, int length, int k) {
   extern __shared__ __align__(16) uint32_t held[];
   __shared__ __align__(16) uint32_t bins[kBins * kCopies];
   __shared__ uint32_t total[kBins], warp_sum[kChooseWarps], found[3], counted[2 * kMostCluster], warp_before[2 * kChooseWarps];
-  const int rank = cluster > 1 ? (int)cluster_rank() : 0, item = blockIdx.x / cluster, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int b = a.heads.div(item), head = item - b * a.heads.d;
-  wait_for_grid();
-  next_grid();
-  int length;
-  const int k = kept_of(a, b, length, head == 0 && rank == 0 && threadIdx.x == 0);
-  if (k == 0) return;                            // (all of the cluster)
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int sinks = min(a.n_sink, k), recent = min(a.n_recent, k - sinks), end = length - recent;
   int need = k - sinks - recent;                 // of the entries sinks .. end - 1
   int *kept = a.kept + ((size_t)b * a.s.heads + head) * a.kept_stride;
@@ -182,7 +224,7 @@ __global__ void __launch_bounds__(kChooseThreads) paged_choose_kernel(const __gr
     for (int i = threadIdx.x; i < sinks; i += kChooseThreads) kept[i] = i;
     for (int i = threadIdx.x; i < recent; i += kChooseThreads) kept[k - recent + i] = end + i;
   }
-  if (need == 0) return;
+  if (need == 0) return;                         // (all of the cluster)
   if (cluster > 1) cluster_meet();               // (all of them are there: from here on they look into each other's shared memory)
   // This CTA's stretch, in fours of positions: they lie together in a page.  A key of 0, which no weight has, is no entry to choose from.
   const int four0 = sinks >> 2, fours = ((end + 3) >> 2) - four0, per = (fours + cluster - 1) / cluster, from = min(rank * per, fours), mine = min(from + per, fours) - from;
@@ -203,7 +245,9 @@ __global__ void __launch_bounds__(kChooseThreads) paged_choose_kernel(const __gr
   };
   uint4 *held4 = reinterpret_cast<uint4 *>(held);
   auto keys_at = [&](int i) { return in_shared ? held4[i] : load_keys(i); };
-  for (int i = threadIdx.x; i < kBins * kCopies / 4; i += kChooseThreads) reinterpret_cast<uint4 *>(bins)[i] = make_uint4(0u, 0u, 0u, 0u);
+  const bool few = cluster == 1 && mine <= kFewKeys / 4 && in_shared;
+  if (!few)
+    for (int i = threadIdx.x; i < kBins * kCopies / 4; i += kChooseThreads) reinterpret_cast<uint4 *>(bins)[i] = make_uint4(0u, 0u, 0u, 0u);
   if (in_shared) {
     // (look-ups side by side, and then what they lead to: with one behind the other a thread's five fours of 10 521 entries took ten trips to memory)
     constexpr int kAtOnce = 6;
@@ -232,6 +276,26 @@ __global__ void __launch_bounds__(kChooseThreads) paged_choose_kernel(const __gr
     if (lost) report(a.s.status);
   }
   __syncthreads();
+  if (few) {
+    // a thread to each key, which counts those ahead of it: the larger ones, and the equal ones before it
+    const uint32_t key = (int)threadIdx.x < 4 * mine ? held[threadIdx.x] : 0u;
+    const int own = threadIdx.x >> 2;
+    uint32_t ahead = 0;
+    auto count = [&](const uint4 &x, uint32_t least) { ahead += (x.x >= least) + (x.y >= least) + (x.z >= least) + (x.w >= least); };
+    for (int i = 0; i < min(own, mine); ++i) count(held4[i], key);
+    for (int i = own + 1; i < mine; ++i) count(held4[i], key + 1u);
+    if (own < mine) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) ahead += held[own * 4 + j] >= key + (j < (int)(threadIdx.x & 3) ? 0u : 1u);
+    }
+    const bool stays = key != 0u && ahead < (uint32_t)need;
+    const unsigned vote = __ballot_sync(0xffffffffu, stays);
+    if (lane == 0) warp_sum[warp] = __popc(vote);
+    __syncthreads();
+    const uint32_t before = __reduce_add_sync(0xffffffffu, lane < warp ? warp_sum[lane & (kChooseWarps - 1)] : 0u);
+    if (stays) kept[sinks + before + __popc(vote & ((1u << lane) - 1u))] = (four0 << 2) + (int)threadIdx.x;
+    return;
+  }
   const uint32_t bins_at = tc::smem_u32(bins), total_at = tc::smem_u32(total), counted_at = tc::smem_u32(counted);
   uint32_t prefix = 0;                           // of the k'th largest key, below which bits are zeros that are not known
   bool ties = false;                             // some of the entries that have that key leave
@@ -367,7 +431,21 @@ __global__ void __launch_bounds__(kChooseThreads) paged_choose_kernel(const __gr
   }
 }
 
-constexpr int kGatherThreads = 256, kGatherRows = 128, kGatherBatch = 4;
+__global__ void __launch_bounds__(kChooseThreads) paged_choose_kernel(const __grid_constant__ Evict a, int cluster) {
+  __shared__ long long src[kGatherRows], dst[kGatherRows];
+  const int rank = cluster > 1 ? (int)cluster_rank() : 0, item = blockIdx.x / cluster, b = a.heads.div(item), head = item - b * a.heads.d;
+  wait_for_grid();
+  next_grid();
+  int length;
+  const int k = kept_of(a, b, length, head == 0 && rank == 0 && threadIdx.x == 0);
+  if (k > 0) choose_entries(a, cluster, rank, b, head, length, k);
+  if (!a.moves) return;
+  // (a cluster of one: its own writes are there)
+  for (int r0 = 0; r0 < k; r0 += kGatherRows) {
+    __syncthreads();
+    gather_rows<kChooseThreads>(a, b, head, r0, min(k - r0, kGatherRows), src, dst);
+  }
+}
 
 __global__ void __launch_bounds__(kGatherThreads) paged_gather_kernel(const __grid_constant__ Evict a) {
   __shared__ long long src[kGatherRows], dst[kGatherRows];
@@ -376,42 +454,7 @@ __global__ void __launch_bounds__(kGatherThreads) paged_gather_kernel(const __gr
   const int item = a.blocks.div(blockIdx.x), block = blockIdx.x - item * a.blocks.d, b = a.heads.div(item), head = item - b * a.heads.d;
   int length;
   const int k = kept_of(a, b, length, false), r0 = block * kGatherRows, n = min(k - r0, kGatherRows);
-  if (n <= 0) return;
-  if ((int)threadIdx.x < n) {
-    const int i = r0 + threadIdx.x, pos = a.kept[((size_t)b * a.s.heads + head) * a.kept_stride + i], to = a.to[(size_t)b * a.to_stride + (i >> a.s.page_shift)];
-    const int from = page_of(a.s, a.bt, b, pos);
-    const bool ok = (unsigned)to < (unsigned)a.s.n_pages;
-    if (!ok) report(a.s.status);
-    src[threadIdx.x] = from >= 0 && ok ? (long long)store_row(a.s, from, head, pos) : -1;
-    dst[threadIdx.x] = ok ? (long long)store_row(a.s, to, head, i) : 0;
-  }
-  __syncthreads();
-  const int both = 2 * a.row_pieces, shift = 31 - __clz(both);      // (a power of two)
-  for (int i0 = threadIdx.x; i0 < n * both; i0 += kGatherBatch * kGatherThreads) {
-    uint4 x[kGatherBatch], *to[kGatherBatch];
-#pragma unroll
-    for (int j = 0; j < kGatherBatch; ++j) {
-      const int i = i0 + j * kGatherThreads, r = i >> shift, c = i & (both - 1);
-      to[j] = nullptr;
-      if (i < n * both && src[r] >= 0) {
-        const bool v = c >= a.row_pieces;
-        uint4 *rows = reinterpret_cast<uint4 *>(v ? a.s.v_rows : a.s.k_rows) + (v ? c - a.row_pieces : c);
-        to[j] = rows + (size_t)dst[r] * a.row_pieces;
-        x[j] = __ldcg(rows + (size_t)src[r] * a.row_pieces);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < kGatherBatch; ++j)
-      if (to[j]) *to[j] = x[j];
-  }
-  if ((int)threadIdx.x < n && src[threadIdx.x] >= 0) {
-    const size_t from = (size_t)src[threadIdx.x], to = (size_t)dst[threadIdx.x];
-    a.weights[to] = __ldcg(a.weights + from);
-    if (a.q8) {
-      a.s.k_scales[to] = __ldcg(a.s.k_scales + from);
-      a.s.v_scales[to] = __ldcg(a.s.v_scales + from);
-    }
-  }
+  if (n > 0) gather_rows<kGatherThreads>(a, b, head, r0, n, src, dst);
 }
 
 }  // namespace paged
@@ -486,8 +529,10 @@ scalekv_status scalekv_paged_evict(scalekv_paged *kv, int32_t layer, const scale
   attr[1].val.clusterDim.x = (unsigned)cluster; attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.gridDim = dim3((unsigned)(items * cluster)); cfg.blockDim = dim3(kChooseThreads); cfg.dynamicSmemBytes = (size_t)a.held * 4; cfg.stream = st;
   cfg.attrs = attr; cfg.numAttrs = 2;
+  a.moves = cluster == 1 && kept_len <= kMostMoved;
   cudaLaunchKernelEx(&cfg, paged_choose_kernel, a, cluster);
   if (scalekv_status s = launched(c, "paged_choose")) return s;
+  if (a.moves) return SCALEKV_OK;
   launch(paged_gather_kernel, dim3((unsigned)(items * blocks)), kGatherThreads, 0, st, a);
   return launched(c, "paged_gather");
 }
