@@ -498,7 +498,7 @@ scalekv_status scalekv_paged_accept(scalekv_paged *kv, int32_t layer, const scal
  * [page][kv head][row of the page].  Of an entry that some new token of its sequence sees (an entry before them: weights = decay weights + p, a
  * new one: weights = p), p = sum of exp(scale q.k - lse) over the new tokens that see it and the heads of its group; the others keep theirs.  lse: dense
  * [n_tokens][n_heads], as scalekv_paged_attend fills it for the same batch, Q, mask and scale; a row whose lse is -inf pays nothing.  decay in [0, 1].
- * Products are exact, sums are fp32 and always in the same order. */
+ * Products are exact, sums are fp32 and always in the same order; an exponent is off by 2^-21 of scale sum |q_i k_i| and of itself at most. */
 scalekv_status scalekv_paged_weigh(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, int32_t n_heads,
                                    scalekv_rows Q, const float *lse, const scalekv_paged_mask *mask, float softmax_scale,
                                    float *weights, float decay, void *stream);

@@ -16,7 +16,10 @@ struct WeighArgs {
   AttendArgs a;                                  // without outputs; a.lse is read
   float *weights;                                // [page][head][row of the page]
   float decay;
+  double scale_log2e;                            // the factor of an exponent: a key's has it, and its scale, rounded once
 };
+
+constexpr double kLog2eExact = 1.4426950408889634074;
 
 __device__ __forceinline__ int key_of(const Span &sp, int step) { return (step < sp.sink_steps ? step : step - sp.sink_steps + sp.lo_step) << 4; }
 // Whether some row sees position pos of a step.
@@ -24,7 +27,7 @@ __device__ __forceinline__ bool some_see(const Span &sp, int pos) { return pos <
 
 // ---- few rows: keys stream past queries that stay in registers, as in paged_stream.cuh: products are m16n8k16 with the rows as n-tiles of eight (there is the layout).  A warp takes stretches of
 // eight steps of 16 keys, whose pages it looks up at once, a lane to each.  What bounds it: reading K and the sums once, and with codes the instructions that turn them into bf16.  us, 32 sequences of up to 10 521
-// entries, 32 heads on 8 of 128: codes 58 (4.6 TB/s; stretches of 8 / 16 / 32 steps 54 / 57 / 65 with pages looked up at once, step by step 59 to 64; 70 of 100 issue slots), bf16 85 (5.9 TB/s).
+// entries, 32 heads on 8 of 128: codes 59.4 (4.5 TB/s; 70 of 100 issue slots; with one sum for all products 57.5, then stretches of 16 / 32 steps 61 / 69, pages looked up step by step 63), bf16 85 (5.9 TB/s).
 template <int D, bool kQ8, int kN>
 struct WeighLayout {
   static constexpr int kRowBytes = D * (kQ8 ? 1 : 2);
@@ -54,7 +57,9 @@ __global__ void __launch_bounds__(kStreamThreads) paged_weigh_stream_kernel(cons
   const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
 
   uint2 q[kN][D / 16];
-  float lse[kN][2];                              // of rows 2 quad, 2 quad + 1 of every n-tile, in base 2; +inf: the row counts for nothing
+  // of rows 2 quad, 2 quad + 1 of every n-tile, in base 2, and what the rounding leaves of it; +inf: the row counts for nothing.  (An exponent of 20 in one float is off by 2^-21, and so is its power of two:
+  // with log-sum-exps and factors in two floats a sum's relative error, one heavy key's mostly, was 2e-7 where it was 1.7e-6.)
+  float lse[kN][2], lse_rest[kN][2];
   bool nothing = false;                          // some row saw nothing
 #pragma unroll
   for (int n = 0; n < kN; ++n) {
@@ -71,12 +76,14 @@ __global__ void __launch_bounds__(kStreamThreads) paged_weigh_stream_kernel(cons
     for (int e = 0; e < 2; ++e) {
       const int i = n * 8 + 2 * quad + e;
       place_row(a, start, head, min(i, rows - 1), t, h);
-      const float x = a.lse[(size_t)t * a.n_heads + h] * kLog2e;
+      const float l = a.lse[(size_t)t * a.n_heads + h], x = (float)((double)l * kLog2eExact);
       lse[n][e] = i < rows && x != -INFINITY ? x : INFINITY;
+      lse_rest[n][e] = fabsf(lse[n][e]) < INFINITY ? (float)((double)l * kLog2eExact - (double)x) : 0.f;
       nothing = nothing || (i < rows && x == -INFINITY);
     }
   }
   nothing = __any_sync(0xffffffffu, nothing);
+  const float scale_hi = (float)w.scale_log2e, scale_lo = (float)(w.scale_log2e - (double)scale_hi);
   // a step all of whose keys every row sees: [lo_full, hi_full)
   const int lo_full = seen_lo(a.mask, first + a.group.div(rows - 1)), hi_full = seen_hi(a.mask, first, length);
 
@@ -114,6 +121,19 @@ __global__ void __launch_bounds__(kStreamThreads) paged_weigh_stream_kernel(cons
       float x[kN][4];
 #pragma unroll
       for (int n = 0; n < kN; ++n) x[n][0] = x[n][1] = x[n][2] = x[n][3] = 0.f;
+      // (Products of two steps are summed by themselves: the tensor core cuts off what lies below the last place of a sum's largest part, at every step, and an exponent's error is a relative one of its power: 2.5e-6 of a sum that one key
+      // dominates with a single sum, 7e-7 so.)
+      float y[kN][4];
+      auto fresh = [&]() {
+#pragma unroll
+        for (int n = 0; n < kN; ++n) y[n][0] = y[n][1] = y[n][2] = y[n][3] = 0.f;
+      };
+      auto gather = [&]() {
+#pragma unroll
+        for (int n = 0; n < kN; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[n][e] += y[n][e];
+      };
 #pragma unroll
       for (int c = 0; c < kRowBytes / 64; ++c) {
         const uint4 lo = *reinterpret_cast<const uint4 *>(k_at + Y::piece(oct, c * 4 + quad)), hi = *reinterpret_cast<const uint4 *>(k_at + Y::piece(oct + 8, c * 4 + quad));
@@ -122,29 +142,37 @@ __global__ void __launch_bounds__(kStreamThreads) paged_weigh_stream_kernel(cons
           for (int e = 0; e < 4; ++e) {
             const uint32_t w0 = turn_signs(word(lo, e)), w1 = turn_signs(word(hi, e));
             const uint32_t f[4] = {codes_low(w0), codes_low(w1), codes_high(w0), codes_high(w1)};
+            if (!(e & 1)) fresh();
 #pragma unroll
-            for (int n = 0; n < kN; ++n) mma_16816(x[n], f, q[n][4 * c + e].x, q[n][4 * c + e].y);
+            for (int n = 0; n < kN; ++n) mma_16816(y[n], f, q[n][4 * c + e].x, q[n][4 * c + e].y);
+            if (e & 1) gather();
           }
         } else {
           const uint32_t f0[4] = {lo.x, hi.x, lo.y, hi.y}, f1[4] = {lo.z, hi.z, lo.w, hi.w};
+          fresh();
 #pragma unroll
           for (int n = 0; n < kN; ++n) {
-            mma_16816(x[n], f0, q[n][2 * c].x, q[n][2 * c].y);
-            mma_16816(x[n], f1, q[n][2 * c + 1].x, q[n][2 * c + 1].y);
+            mma_16816(y[n], f0, q[n][2 * c].x, q[n][2 * c].y);
+            mma_16816(y[n], f1, q[n][2 * c + 1].x, q[n][2 * c + 1].y);
           }
+          gather();
         }
       }
-      float ks0 = a.scale_log2e, ks1 = a.scale_log2e;
+      float ks[2] = {scale_hi, scale_hi}, ks_rest[2] = {scale_lo, scale_lo};
       if constexpr (kQ8) {
         const float *scales = reinterpret_cast<const float *>(k_at + Y::kScales) + oct;
-        ks0 *= kCodeUnit * scales[0];
-        ks1 *= kCodeUnit * scales[8];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float s = kCodeUnit * scales[8 * e];
+          ks[e] = scale_hi * s;
+          ks_rest[e] = fmaf(scale_lo, s, fmaf(scale_hi, s, -ks[e]));
+        }
       }
       float sum[2] = {0.f, 0.f};                 // of keys oct and oct + 8, over this lane's rows
 #pragma unroll
       for (int n = 0; n < kN; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[n][e] = tc::ex2(x[n][e] * (e < 2 ? ks0 : ks1) - lse[n][e & 1]);
+        for (int e = 0; e < 4; ++e) x[n][e] = tc::ex2(fmaf(x[n][e], ks[e >> 1], -lse[n][e & 1]) + fmaf(x[n][e], ks_rest[e >> 1], -lse_rest[n][e & 1]));
       const bool whole = key0 >= lo_full && key0 + 16 <= hi_full;
       if (!whole || nothing) {
 #pragma unroll
@@ -190,7 +218,7 @@ __global__ void __launch_bounds__(kStreamThreads) paged_weigh_stream_kernel(cons
 //   warp 1        : finds the items, ahead of the others
 //   warps 4-7     : the queries, by asynchronous copies of 16 bytes (rows are a token's heads, in any strides), and their log-sum-exps; the next item's keys, scales and weights
 //   warps 8-23    : keys from shared memory into TMEM (codes become bf16 exactly), then p = 2^(x ks - lse) and its sums
-// Every wait is bounded, as in paged_tile.cuh.
+// Every wait is bounded, as in paged_tile.cuh.  A product's sum is the tensor core's, whose cut-off (2^-22 of the largest part) is 2.5e-6 of a sum that one key of four times the others' length dominates.
 // What bounds it: exponentials, of which the special function unit does 16 a cycle (a tile of 128 x 128 takes it twice as long as the tensor core its product; it is busy for 80 of 100 cycles while a
 // CTA has work), and the power that both draw: 2 048 queries of 4 x 32 heads behind 6 144 entries in codes take 577 us from a cool start, 0.83 PFLOP/s, and 596 to 615 in a row.  (One exponential in
 // four by a polynomial on the FMA pipe: 555 us from a cool start, 597 in a row; half of them 658.  A key tile's rows in shared memory and eight softmax warps: 715; products issued one by one: 621; a CTA for
@@ -442,7 +470,7 @@ __global__ void __launch_bounds__(WeighTile<D, kQ8>::kThreads, 1) paged_weigh_ti
             const char *src = reinterpret_cast<const char *>(__shfl_sync(0xffffffffu, (unsigned long long)mine, from));
             copy16(to + from * 128 + (((piece & 7) ^ (from & 7)) << 4), src + piece * 16, r - tid + wq * 32 + from < it.rows);
           }
-          const float x = a.lse[(size_t)(it.start + t) * a.n_heads + h] * kLog2e;
+          const float x = (float)((double)a.lse[(size_t)(it.start + t) * a.n_heads + h] * kLog2eExact);
           lse[kAhead] = r < it.rows && x != -INFINITY ? x : INFINITY;
         }
         if (j == keys_at) {
@@ -569,13 +597,14 @@ __global__ void __launch_bounds__(WeighTile<D, kQ8>::kThreads, 1) paged_weigh_ti
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const int key = t * 128 + row;
-        float ks = a.scale_log2e, scale = 1.f;
+        float scale = 1.f;
         asm volatile("ld.shared.b64 %0, [%1];" : "=l"(at_row[t]) : "r"(base + Y::kOffRow + key * 8) : "memory");
         asm volatile("ld.shared.f32 %0, [%1];" : "=f"(old[t]) : "r"(base + Y::kOffOld + key * 4) : "memory");
         if constexpr (kQ8) {
           asm volatile("ld.shared.f32 %0, [%1];" : "=f"(scale) : "r"(base + Y::kOffScale + key * 4) : "memory");
-          ks *= kCodeUnit * scale;
+          scale *= kCodeUnit;
         }
+        const float ks = (float)(w.scale_log2e * (double)scale);
         k2[t] = pack2(ks, ks);
       }
       tc_wait_st();
@@ -672,7 +701,8 @@ extern "C" scalekv_status scalekv_paged_weigh(scalekv_paged *kv, int32_t layer, 
   a.group = Divisor::of(G);
   a.n_heads = n_heads;
   a.max_new = batch->max_new;
-  a.scale_log2e = (softmax_scale > 0.f ? softmax_scale : 1.f / std::sqrt((float)D)) * kLog2e;
+  a.scale_log2e = 0.f;
+  w.scale_log2e = (softmax_scale > 0.f ? (double)softmax_scale : 1. / std::sqrt((double)D)) * kLog2eExact;
   w.weights = weights;
   w.decay = decay;
   const long long max_rows = (long long)std::min(batch->max_new, a.bt.n_tokens) * G;      // query rows of a sequence and kv head
