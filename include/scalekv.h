@@ -455,7 +455,7 @@ scalekv_status scalekv_paged_attend(scalekv_paged *kv, int32_t layer, const scal
 
 /* How rows of Q and K turn by their positions: pair i of dimensions, (x, y), becomes (x cos f - y sin f, x sin f + y cos f) with
  * f = frequency[i] times the token's position on axis[i].  Pair i is dimensions i and i + n_pairs, or, adjacent != 0, 2 i and 2 i + 1;
- * dimensions from 2 n_pairs on stay as they are.  Several axes (time, height, width) share the pairs in any way; how much a pair
+ * dimensions from 2 n_pairs on stay as they are (the table is the call's: a captured call keeps it).  Several axes (time, height, width) share the pairs in any way; how much a pair
  * turns for a position is the caller's, too. */
 typedef struct {
   int32_t n_pairs;        /* a multiple of 8, from 8 to head_dim / 2                                    */
@@ -498,6 +498,7 @@ scalekv_status scalekv_paged_accept(scalekv_paged *kv, int32_t layer, const scal
  * [page][kv head][row of the page].  Of an entry that some new token of its sequence sees (an entry before them: weights = decay weights + p, a
  * new one: weights = p), p = sum of exp(scale q.k - lse) over the new tokens that see it and the heads of its group; the others keep theirs.  lse: dense
  * [n_tokens][n_heads], as scalekv_paged_attend fills it for the same batch, Q, mask and scale; a row whose lse is -inf pays nothing.  decay in [0, 1].
+ * No two sequences of a batch may see the same page: an entry's sum is one's alone.
  * Products are exact, sums are fp32 and always in the same order; an exponent is off by 2^-21 of scale sum |q_i k_i| and of itself at most. */
 scalekv_status scalekv_paged_weigh(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, int32_t n_heads,
                                    scalekv_rows Q, const float *lse, const scalekv_paged_mask *mask, float softmax_scale,

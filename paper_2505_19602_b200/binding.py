@@ -712,7 +712,8 @@ class PagedKV:
 
     def scalekv_paged_weigh(self, layer, batch, Q, lse, weights, causal=True, window=0, n_sink=0, decay=1.0, softmax_scale=0.0):
         """Adds to weights (float32 [n_pages, n_kv_heads, page_tokens], of this layer) the attention that the new tokens' queries Q pay each cached entry; lse [n_tokens,
-        heads] as scalekv_paged_attend filled it for the same queries, mask and scale.  What was there before fades by `decay` first."""
+        heads] as scalekv_paged_attend filled it for the same queries, mask and scale.  What was there before fades by `decay` first.  No two
+        sequences of the batch may see the same page."""
         self._check(self._call.paged_weigh(self._fn["weigh"], self._handle, layer, self._batch(batch), batch.n_tokens, self.head_dim,
                                            self.device_index, Q, lse, weights, self.n_pages, self.n_kv_heads, self.page_tokens, causal, window, n_sink,
                                            decay, softmax_scale, self._stream()))
