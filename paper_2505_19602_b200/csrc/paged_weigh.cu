@@ -27,7 +27,7 @@ __device__ __forceinline__ bool some_see(const Span &sp, int pos) { return pos <
 
 // ---- few rows: keys stream past queries that stay in registers, as in paged_stream.cuh: products are m16n8k16 with the rows as n-tiles of eight (there is the layout).  A warp takes stretches of
 // eight steps of 16 keys, whose pages it looks up at once, a lane to each.  What bounds it: reading K and the sums once, and with codes the instructions that turn them into bf16.  us, 32 sequences of up to 10 521
-// entries, 32 heads on 8 of 128: codes 59.4 (4.5 TB/s; 70 of 100 issue slots; with one sum for all products 57.5, then stretches of 16 / 32 steps 61 / 69, pages looked up step by step 63), bf16 85 (5.9 TB/s).
+// entries, 32 heads on 8 of 128: codes 58.7 (4.6 TB/s; 70 of 100 issue slots; with one sum for all products 57.5, then stretches of 16 / 32 steps 61 / 69, pages looked up step by step 63), bf16 85 (5.9 TB/s).
 template <int D, bool kQ8, int kN>
 struct WeighLayout {
   static constexpr int kRowBytes = D * (kQ8 ? 1 : 2);
@@ -422,28 +422,36 @@ __global__ void __launch_bounds__(WeighTile<D, kQ8>::kThreads, 1) paged_weigh_ti
     const int piece = lane % kPieces, sub = lane / kPieces, wq = warp & 3;
     KeyItem it, next;
     // An item's keys, by this warp 64 of them: a lane knows where two lie, and the others ask it.
+    int page[2];
+    auto find_keys = [&](const KeyItem &of) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int pos = of.key0 + wq * 64 + half * 32 + lane;
+        const bool seen = pos < of.hi && (pos >= of.lo || pos < of.n_sink);
+        page[half] = seen ? page_of(s, a.bt, of.seq, pos) : -1;
+      }
+    };
     auto fetch_keys = [&](const KeyItem &of) {
       constexpr int kRowPieces = Y::kRowBytes / 16, kRowsAtOnce = 32 / kRowPieces;
 #pragma unroll 1
       for (int half = 0; half < 2; ++half) {
-        const int own = wq * 64 + half * 32 + lane, pos = of.key0 + own;
-        const bool seen = pos < of.hi && (pos >= of.lo || pos < of.n_sink);
-        const int page = seen ? page_of(s, a.bt, of.seq, pos) : -1;
-        const unsigned long long row = store_row(s, max(page, 0), of.head, pos);
-        asm volatile("st.shared.b64 [%0], %1;" ::"r"(base + Y::kOffRow + own * 8), "l"(page >= 0 ? row : ~0ull) : "memory");
-        auto copy4 = [&](uint32_t to, const float *from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(page >= 0 ? 4 : 0) : "memory"); };
+        const int own = wq * 64 + half * 32 + lane, pg = half ? page[1] : page[0];
+        const unsigned long long row = store_row(s, max(pg, 0), of.head, of.key0 + own);
+        asm volatile("st.shared.b64 [%0], %1;" ::"r"(base + Y::kOffRow + own * 8), "l"(pg >= 0 ? row : ~0ull) : "memory");
+        auto copy4 = [&](uint32_t to, const float *from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(pg >= 0 ? 4 : 0) : "memory"); };
         if (kQ8) copy4(base + Y::kOffScale + own * 4, s.k_scales + row);
         copy4(base + Y::kOffOld + own * 4, w.weights + row);
 #pragma unroll 4
         for (int i = 0; i < kRowPieces; ++i) {
           const int from = i * kRowsAtOnce + lane / kRowPieces;
           const unsigned long long r = __shfl_sync(0xffffffffu, row, from);
-          copy16(base + Y::kOffKeys + (wq * 64 + half * 32 + from) * Y::kPitch + (lane % kRowPieces) * 16, s.k_rows + r * Y::kRowBytes + (lane % kRowPieces) * 16, __shfl_sync(0xffffffffu, page, from) >= 0);
+          copy16(base + Y::kOffKeys + (wq * 64 + half * 32 + from) * Y::kPitch + (lane % kRowPieces) * 16, s.k_rows + r * Y::kRowBytes + (lane % kRowPieces) * 16, __shfl_sync(0xffffffffu, pg, from) >= 0);
         }
       }
     };
     bool ok = true, more = read_item(0, it);
     if (more) {
+      find_keys(it);
       fetch_keys(it);
       asm volatile("cp.async.wait_all;" ::: "memory");
       __syncwarp();
@@ -475,6 +483,7 @@ __global__ void __launch_bounds__(WeighTile<D, kQ8>::kThreads, 1) paged_weigh_ti
         }
         if (j == keys_at) {
           more = read_item(n + 1, next);
+          if (more) find_keys(next);               // (while the softmax warps still have this item's: 848 items of one query tile 34.3 us where behind them it was 35.5)
           if (more) ok = mbar_wait_warp(bar(Y::bRawFree), n & 1, abort_flag, status);
           if (!ok) break;
           if (more) fetch_keys(next);

@@ -238,3 +238,62 @@ def test_steps_on_streams_of_their_own():
         for s, stream in zip(steps, streams):
             with torch.cuda.stream(stream):
                 s.kv.scalekv_paged_sync()
+
+
+def everything(kv, first_page, heads, d, new=40, length=200, strided=False, seed=0):
+    """All calls once on one sequence whose pages begin at first_page; what comes out, and what the cache then holds."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    dev = dict(dtype=torch.int32, device="cuda")
+    pages = -(-length // kv.page_tokens)
+    table = torch.arange(first_page, first_page + pages, **dev)[None]
+    to = torch.arange(first_page + pages, first_page + 2 * pages, **dev)[None]
+    random = lambda *shape: torch.randn(*shape, generator=g, device="cuda")  # noqa: E731
+    weights = torch.zeros(kv.n_pages, heads, kv.page_tokens, device="cuda")
+
+    def batch(n):
+        return binding.PagedBatch(table, torch.tensor([length], **dev), torch.tensor([0, n], **dev), n, n, length)
+
+    def rows(n, h):
+        x = random(n, h, d).bfloat16()
+        if not strided:
+            return x
+        wide = torch.zeros(h + 3, n, 2, d + 8, device="cuda", dtype=x.dtype)      # heads outermost, odd steps
+        wide[:h, :, 1, :d] = x.transpose(0, 1)
+        return wide[:h, :, 1, :d].transpose(0, 1)
+
+    r, out = binding.Rotary([d // 4, d // 4]), []
+    position = torch.randint(0, 10000, (2, length), generator=g, **dev)
+    kv.scalekv_paged_write_rotated(0, batch(length), None, rows(length, heads), rows(length, heads), r, position)
+    for n in (1, new):
+        bits = torch.randint(-2 ** 31, 2 ** 31 - 1, (n, 2), generator=g, **dev)
+        q = kv.scalekv_paged_write_rotated(0, batch(n), rows(n, 2 * heads), rows(n, heads), rows(n, heads), r, position[:, :n])
+        lse = torch.empty(n, 2 * heads, device="cuda")
+        out += [q, kv.scalekv_paged_attend_tree(0, batch(n), rows(n, 2 * heads), bits, lse=lse), lse.clone()]
+        Q = rows(n, 2 * heads)
+        kv.scalekv_paged_attend(0, batch(n), Q, lse=lse)
+        kv.scalekv_paged_weigh(0, batch(n), Q, lse, weights, decay=0.5)
+    kv.scalekv_paged_accept(batch(new), torch.tensor([[1, 5, 30]], **dev), torch.tensor([3], **dev))
+    out += [kv.scalekv_paged_evict(0, batch(0), to, torch.tensor([100], **dev), weights, 3, 7)[:, :, :100], weights[first_page:first_page + 2 * pages]]
+    out += list(kv.scalekv_paged_read(0, batch(length), dtype=torch.float32))
+    kept = binding.PagedBatch(to, torch.tensor([100], **dev), torch.tensor([0, 100], **dev), 100, 100, 100)
+    out += list(kv.scalekv_paged_read(0, kept, dtype=torch.float32))
+    kv.scalekv_paged_sync()
+    return out
+
+
+@pytest.mark.parametrize("store,d", [("q8", 128), ("bf16", 64)])
+def test_strides_change_nothing(store, d):
+    kv = binding.PagedKV(1, 40, 3, d, store=store, page_tokens=16)
+    kv.pool.zero_()
+    assert same([x.contiguous() for x in everything(kv, 4, 3, d)], [x.contiguous() for x in everything(kv, 4, 3, d, strided=True)])
+
+
+@pytest.mark.parametrize("store", ["q8", "bf16"])
+def test_offsets_beyond_32_bits(store):
+    """The same in a small pool and behind the first 4 GB of K rows of a large one."""
+    small = binding.PagedKV(1, 12, 16, 128, store=store, page_tokens=64)
+    pages = 36000 if store == "q8" else 18000                            # 4.7 GB of K rows
+    large = binding.PagedKV(1, pages, 16, 128, store=store, page_tokens=64)
+    for kv in (small, large):
+        kv.pool.zero_()
+    assert same(*([x.contiguous() for x in everything(kv, first, 16, 128)] for kv, first in ((small, 2), (large, pages - 9))))
