@@ -36,7 +36,9 @@ struct WeighLayout {
   static constexpr int kSmem = kStreamWarps * kStages * kStage;
   static __device__ __forceinline__ int piece(int r, int x) { return StreamLayout<D, kQ8, 1>::piece(r, x); }
 };
-constexpr int kWeighRows = 32;                   // query rows of a sequence and kv head that go this way
+// Query rows of a sequence and kv head that go this way.  (us, four sequences of 8 192 entries, 8 heads of 128 in codes, with one event's 5: 64 rows in two such launches 51, on tcgen05 40; one of 2 000 entries 25 and 15; 53 sequences
+// of 70 entries, 16 heads, 66 rows in three 71 and 36.)
+constexpr int kWeighRows = 32;
 constexpr int kWeighSteps = 8;                   // of a warp, in a row
 
 template <int D, bool kQ8, int kN>
