@@ -478,10 +478,8 @@ def _weigh_plain(s):
     y.sub_(lse.unsqueeze(-1)).exp_().masked_fill_(~seen[:, None, None], 0.0)
     got = y.sum((2, 3))                                                                # [sequences, kv heads, positions]
     seq, pos, at, row = _entries(s)
-    fade = torch.where(pos < first[seq], case["decay"], 0.0)
-    if case["window"]:                                     # entries that no new token sees keep what they have
-        fade = torch.where((pos > first[seq] - case["window"]) | (pos < case["sinks"]), fade, 1.0)
-    s["weights"][at, :, row] = s["weights"][at, :, row] * fade[:, None] + got[seq, :, pos]
+    old = s["weights"][at, :, row] * torch.where(pos < first[seq], case["decay"], 0.0)[:, None]
+    s["weights"][at, :, row] = old + got[seq, :, pos]
 
 
 def _evict_plain(s):
@@ -577,9 +575,7 @@ def exact(case, seed):
         hidden = delta < 0
         if case["window"]:
             hidden |= (delta >= case["window"]) & (torch.arange(length, device="cuda")[None] >= case["sinks"])
-        mine = old[r0: r0 + length].clone()
-        seen = ~hidden.all(0)
-        mine[seen] *= case["decay"]
+        mine = old[r0: r0 + length] * case["decay"]
         mine[first:] = 0.0
         for g in range(case["heads"]):
             y = (Q[t0: t0 + n, g].double() @ number(K, slice(r0, r0 + length), g // group).T) / math.sqrt(case["d"])
