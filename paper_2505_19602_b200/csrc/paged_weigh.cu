@@ -58,11 +58,13 @@ __global__ void __launch_bounds__(kStreamThreads) paged_weigh_stream_kernel(cons
   char *ring = smem + warp * kStages * Y::kStage;
   const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
 
+  // What fills the tile up is the last row once more, with a log-sum-exp of kNever: whatever a key holds, its power is 0 or what that row's own is, infinite or no number.  (Of zeros an infinite key would make NaN.)
+  constexpr float kNever = FLT_MAX;
   uint2 q[kN][D / 16];
-  // of rows 2 quad, 2 quad + 1 of every n-tile, in base 2, and what the rounding leaves of it; +inf: the row counts for nothing.  (An exponent of 20 in one float is off by 2^-21, and so is its power of two:
+  // of rows 2 quad, 2 quad + 1 of every n-tile, in base 2, and what the rounding leaves of it; kNever: the row counts for nothing.  (An exponent of 20 in one float is off by 2^-21, and so is its power of two:
   // with log-sum-exps and factors in two floats a sum's relative error, one heavy key's mostly, was 2e-7 where it was 1.7e-6.)
   float lse[kN][2], lse_rest[kN][2];
-  bool nothing = false;                          // some row saw nothing
+  bool nothing = false;                          // some row counts for nothing
 #pragma unroll
   for (int n = 0; n < kN; ++n) {
     int t, h;
@@ -72,20 +74,22 @@ __global__ void __launch_bounds__(kStreamThreads) paged_weigh_stream_kernel(cons
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
       const int dim = kQ8 ? (k >> 2) * 64 + quad * 16 + (k & 3) * 4 : (k >> 1) * 32 + quad * 8 + (k & 1) * 4;
-      q[n][k] = r < rows ? *reinterpret_cast<const uint2 *>(row + dim * 2) : make_uint2(0u, 0u);
+      q[n][k] = *reinterpret_cast<const uint2 *>(row + dim * 2);
     }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int i = n * 8 + 2 * quad + e;
       place_row(a, start, head, min(i, rows - 1), t, h);
       const float l = a.lse[(size_t)t * a.n_heads + h], x = (float)((double)l * kLog2eExact);
-      lse[n][e] = i < rows && x != -INFINITY ? x : INFINITY;
-      lse_rest[n][e] = fabsf(lse[n][e]) < INFINITY ? (float)((double)l * kLog2eExact - (double)x) : 0.f;
-      nothing = nothing || (i < rows && x == -INFINITY);
+      const bool never = i >= rows || fabsf(x) == INFINITY;
+      lse[n][e] = never ? kNever : x;
+      lse_rest[n][e] = never ? 0.f : (float)((double)l * kLog2eExact - (double)x);
+      nothing = nothing || (i < rows && never);
     }
   }
   nothing = __any_sync(0xffffffffu, nothing);
-  const float scale_hi = (float)w.scale_log2e, scale_lo = (float)(w.scale_log2e - (double)scale_hi);
+  // (the factor's parts have one sign: an infinite product stays what it is in both)
+  const float scale_hi = __double2float_rd(w.scale_log2e), scale_lo = fmaxf((float)(w.scale_log2e - (double)scale_hi), FLT_TRUE_MIN);
   // a step all of whose keys every row sees: [lo_full, hi_full)
   const int lo_full = seen_lo(a.mask, first + a.group.div(rows - 1)), hi_full = seen_hi(a.mask, first, length);
 
@@ -166,7 +170,7 @@ __global__ void __launch_bounds__(kStreamThreads) paged_weigh_stream_kernel(cons
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const float s = kCodeUnit * scales[8 * e];
-          ks[e] = scale_hi * s;
+          ks[e] = __fmul_rd(scale_hi, s);
           ks_rest[e] = fmaf(scale_lo, s, fmaf(scale_hi, s, -ks[e]));
         }
       }
@@ -182,7 +186,7 @@ __global__ void __launch_bounds__(kStreamThreads) paged_weigh_stream_kernel(cons
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int r = first + a.group.div(min(n * 8 + 2 * quad + (e & 1), rows - 1)), pos = key0 + oct + 8 * (e >> 1);
-            if (lse[n][e & 1] == INFINITY || pos >= seen_hi(a.mask, r, length) || (pos < seen_lo(a.mask, r) && pos >= sp.n_sink)) x[n][e] = 0.f;      // (whatever the product is)
+            if (lse[n][e & 1] == kNever || pos >= seen_hi(a.mask, r, length) || (pos < seen_lo(a.mask, r) && pos >= sp.n_sink)) x[n][e] = 0.f;      // (whatever the product is)
           }
       }
 #pragma unroll
