@@ -508,8 +508,9 @@ scalekv_status scalekv_paged_weigh(scalekv_paged *kv, int32_t layer, const scale
  * beside those) and of the rest those with the largest weights (as for scalekv_paged_weigh), of equal ones the first (a NaN counts as -inf).  They are copied, in their
  * order, to positions 0, 1, .. of the pages that to_table names (to_pages of its to_stride entries for a sequence), K, V and weights alike; every kv head
  * keeps entries of its own.  kept: device [n_seqs][n_kv_heads][kept_stride], receives the positions that stay, ascending.  Only table and lengths of the batch are looked
- * at.  A page of to_table must not be one that the call reads; what was held in the old pages stays there.  A sequence whose keep is negative, or of
- * which more would stay than kept_len or to_pages have room for, is reported and left out. */
+ * at.  A page of to_table must not be one that the call reads, nor stand there twice; what was held in the old pages stays there.  A sequence whose keep is
+ * negative, or of which more would stay than kept_len or to_pages have room for, is reported and left out.  Rows that overlap (kept_stride below kept_len,
+ * to_stride below to_pages, where there is more than one) are refused. */
 scalekv_status scalekv_paged_evict(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, const int32_t *to_table,
                                    int32_t to_stride, int32_t to_pages, const int32_t *keep, float *weights, int32_t n_sink,
                                    int32_t n_recent, int32_t *kept, int32_t kept_stride, int32_t kept_len, void *stream);

@@ -500,11 +500,13 @@ scalekv_status scalekv_paged_evict(scalekv_paged *kv, int32_t layer, const scale
   if (scalekv_status st = check_batch(c, layer, batch, a.bt)) return st;
   if (n_sink < 0 || n_recent < 0) return fail(c, SCALEKV_ERR_INVALID_ARG, "n_sink or n_recent negative");
   if (to_stride < 0 || to_pages < 0 || kept_stride < 0 || kept_len < 0) return fail(c, SCALEKV_ERR_INVALID_ARG, "a size of to_table or kept negative");
+  const int H = c->cfg.n_kv_heads;
+  const long long items = (long long)a.bt.n_seqs * H;
+  if ((a.bt.n_seqs > 1 && to_stride < to_pages) || (items > 1 && kept_stride < kept_len)) return fail(c, SCALEKV_ERR_INVALID_ARG, "rows of to_table or kept overlap");
   if (a.bt.n_seqs == 0 || kept_len == 0) return SCALEKV_OK;
   if (!a.bt.table || !a.bt.lengths || !to_table || !keep || !weights || !kept) return fail(c, SCALEKV_ERR_INVALID_ARG, "an array null");
   if (reinterpret_cast<uintptr_t>(weights) & 15) return fail(c, SCALEKV_ERR_INVALID_ARG, "weights not 16-byte aligned");
-  const int H = c->cfg.n_kv_heads;
-  const long long items = (long long)a.bt.n_seqs * H, blocks = (kept_len + kGatherRows - 1) / kGatherRows;
+  const long long blocks = (kept_len + kGatherRows - 1) / kGatherRows;
   if (items * std::max<long long>(blocks, kMostCluster) > 0x7fffffffLL) return fail(c, SCALEKV_ERR_UNSUPPORTED, "too many sequences, kv heads and entries in a call");
   a.s = layer_store(c, layer);
   a.keep = keep; a.kept = kept; a.kept_stride = kept_stride; a.kept_len = kept_len;
