@@ -506,7 +506,9 @@ scalekv_status scalekv_paged_evict(scalekv_paged *kv, int32_t layer, const scale
   if (a.bt.n_seqs == 0 || kept_len == 0) return SCALEKV_OK;
   if (!a.bt.table || !a.bt.lengths || !to_table || !keep || !weights || !kept) return fail(c, SCALEKV_ERR_INVALID_ARG, "an array null");
   if (reinterpret_cast<uintptr_t>(weights) & 15) return fail(c, SCALEKV_ERR_INVALID_ARG, "weights not 16-byte aligned");
-  const long long blocks = (kept_len + kGatherRows - 1) / kGatherRows;
+  // what the tables have room for, whatever the caller's bounds say
+  const long long room = (long long)a.bt.table_pages << c->page_shift, most = std::min<long long>(std::min<long long>(kept_len, room), (long long)to_pages << c->page_shift);
+  const long long blocks = std::max(1ll, (most + kGatherRows - 1) / kGatherRows);
   if (items * std::max<long long>(blocks, kMostCluster) > 0x7fffffffLL) return fail(c, SCALEKV_ERR_UNSUPPORTED, "too many sequences, kv heads and entries in a call");
   a.s = layer_store(c, layer);
   a.keep = keep; a.kept = kept; a.kept_stride = kept_stride; a.kept_len = kept_len;
@@ -517,7 +519,7 @@ scalekv_status scalekv_paged_evict(scalekv_paged *kv, int32_t layer, const scale
   a.row_pieces = c->cfg.head_dim * (a.q8 ? 1 : 2) / 16;
   a.heads = Divisor::of(H);
   a.blocks = Divisor::of((int)blocks);
-  const int length = std::max(batch->max_length, 1);
+  const int length = (int)std::max(1ll, std::min<long long>(batch->max_length, room));      // (at most kMaxLength)
   // as many CTAs to a sequence and head as find an SM, with more than 16 384 entries for each
   int cluster = 1;
   while (cluster < kMostCluster && items * cluster <= c->n_sm && length > cluster * 16384) cluster *= 2;
@@ -531,7 +533,7 @@ scalekv_status scalekv_paged_evict(scalekv_paged *kv, int32_t layer, const scale
   attr[1].val.clusterDim.x = (unsigned)cluster; attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.gridDim = dim3((unsigned)(items * cluster)); cfg.blockDim = dim3(kChooseThreads); cfg.dynamicSmemBytes = (size_t)a.held * 4; cfg.stream = st;
   cfg.attrs = attr; cfg.numAttrs = 2;
-  a.moves = cluster == 1 && kept_len <= kMostMoved;
+  a.moves = cluster == 1 && most <= kMostMoved;
   cudaLaunchKernelEx(&cfg, paged_choose_kernel, a, cluster);
   if (scalekv_status s = launched(c, "paged_choose")) return s;
   if (a.moves) return SCALEKV_OK;
