@@ -503,8 +503,9 @@ scalekv_status scalekv_paged_evict(scalekv_paged *kv, int32_t layer, const scale
   const int H = c->cfg.n_kv_heads;
   const long long items = (long long)a.bt.n_seqs * H;
   if ((a.bt.n_seqs > 1 && to_stride < to_pages) || (items > 1 && kept_stride < kept_len)) return fail(c, SCALEKV_ERR_INVALID_ARG, "rows of to_table or kept overlap");
-  if (a.bt.n_seqs == 0 || kept_len == 0) return SCALEKV_OK;
-  if (!a.bt.table || !a.bt.lengths || !to_table || !keep || !weights || !kept) return fail(c, SCALEKV_ERR_INVALID_ARG, "an array null");
+  if (a.bt.n_seqs == 0) return SCALEKV_OK;
+  // (places for nothing need no memory, but what should stay all the same is told)
+  if ((!a.bt.table && a.bt.table_pages > 0) || !a.bt.lengths || (!to_table && to_pages > 0) || !keep || !weights || (!kept && kept_len > 0)) return fail(c, SCALEKV_ERR_INVALID_ARG, "an array null");
   if (reinterpret_cast<uintptr_t>(weights) & 15) return fail(c, SCALEKV_ERR_INVALID_ARG, "weights not 16-byte aligned");
   // what the tables have room for, whatever the caller's bounds say
   const long long room = (long long)a.bt.table_pages << c->page_shift, most = std::min<long long>(std::min<long long>(kept_len, room), (long long)to_pages << c->page_shift);
