@@ -474,8 +474,9 @@ scalekv_status scalekv_paged_accept(scalekv_paged *kv, int32_t layer, const scal
   Accept a;
   if (scalekv_status st = check_batch(c, layer == -1 ? 0 : layer, batch, a.bt)) return st;
   if (path_stride < 0 || path_len < 0) return fail(c, SCALEKV_ERR_INVALID_ARG, "path_stride or path_len negative");
-  if (a.bt.n_tokens == 0 || path_len == 0) return SCALEKV_OK;
-  if (!path || !counts) return fail(c, SCALEKV_ERR_INVALID_ARG, "path or counts null");
+  // (without tokens, or places in a path, all counts have to be 0, which the device looks at; a batch without tokens may come without its arrays)
+  if (a.bt.n_seqs == 0 || (a.bt.n_tokens == 0 && (!a.bt.starts || !a.bt.lengths || !counts))) return SCALEKV_OK;
+  if ((!path && path_len > 0) || !counts) return fail(c, SCALEKV_ERR_INVALID_ARG, "path or counts null");
   const int layers = layer == -1 ? c->cfg.n_layers : 1;
   a.s = layer_store(c, layer == -1 ? 0 : layer);
   a.layer_rows = c->lay.rows_bytes / c->cfg.n_layers;
