@@ -498,11 +498,18 @@ scalekv_status scalekv_paged_accept(scalekv_paged *kv, int32_t layer, const scal
  * [page][kv head][row of the page].  Of an entry that some new token of its sequence sees (an entry before them: weights = decay weights + p, a
  * new one: weights = p), p = sum of exp(scale q.k - lse) over the new tokens that see it and the heads of its group; the others keep theirs.  lse: dense
  * [n_tokens][n_heads], as scalekv_paged_attend fills it for the same batch, Q, mask and scale; a row whose lse is -inf pays nothing.  decay in [0, 1].
- * No two sequences of a batch may see the same page: an entry's sum is one's alone.
+ * No two sequences of a batch may see the same page: an entry's sum is one's alone.  Entries that a window hides from all of them are left alone because their places
+ * in the table may hold anything: for sums by which entries inside and behind a window are ranked (scalekv_paged_evict), decay below 1, scalekv_paged_fade goes along.
  * Products are exact, sums are fp32 and always in the same order; an exponent is off by 2^-21 of scale sum |q_i k_i| and of itself at most. */
 scalekv_status scalekv_paged_weigh(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, int32_t n_heads,
                                    scalekv_rows Q, const float *lse, const scalekv_paged_mask *mask, float softmax_scale,
                                    float *weights, float decay, void *stream);
+
+/* The rest of a weigh under a window: weights = decay weights for every entry before the new tokens that the window (and its sinks) hides from all new tokens of its
+ * sequence.  Here the table has to name a sequence's own pages for them, or, where one was given back, nothing: a page out of range is passed over.  The same
+ * batch, mask and decay as the weigh's, before or after it. */
+scalekv_status scalekv_paged_fade(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, const scalekv_paged_mask *mask,
+                                  float *weights, float decay, void *stream);
 
 /* Of every sequence and kv head min(keep[b], lengths[b]) entries stay: the first n_sink, the last n_recent (as many as there is room for
  * beside those) and of the rest those with the largest weights (as for scalekv_paged_weigh), of equal ones the first (a NaN counts as -inf).  They are copied, in their

@@ -207,6 +207,7 @@ def load_library():
         "scalekv_paged_accept": [ctx_p, i32, P(scalekv_paged_batch), C.c_void_p, i32, i32, C.c_void_p, C.c_void_p],
         "scalekv_paged_weigh": [ctx_p, i32, P(scalekv_paged_batch), i32, scalekv_rows, C.c_void_p, P(scalekv_paged_mask), C.c_float,
                                 C.c_void_p, C.c_float, C.c_void_p],
+        "scalekv_paged_fade": [ctx_p, i32, P(scalekv_paged_batch), P(scalekv_paged_mask), C.c_void_p, C.c_float, C.c_void_p],
         "scalekv_paged_evict": [ctx_p, i32, P(scalekv_paged_batch), C.c_void_p, i32, i32, C.c_void_p, C.c_void_p, i32, i32, C.c_void_p,
                                 i32, i32, C.c_void_p],
         "scalekv_paged_sync": [ctx_p, C.c_void_p],
@@ -606,7 +607,7 @@ class PagedKV:
         if not torch.cuda.is_available():
             raise RuntimeError("PagedKV needs a CUDA device (sm_100a); there is no CPU path")
         self.lib, self._call = load_library(), load_call()
-        self._fn = {f: C.cast(getattr(self.lib, "scalekv_paged_" + f), C.c_void_p).value for f in ("write", "read", "attend", "write_rotated", "attend_tree", "accept", "weigh", "evict")}
+        self._fn = {f: C.cast(getattr(self.lib, "scalekv_paged_" + f), C.c_void_p).value for f in ("write", "read", "attend", "write_rotated", "attend_tree", "accept", "weigh", "fade", "evict")}
         self.device, self.device_index = torch.device("cuda", device), device
         self.n_layers, self.n_pages, self.n_kv_heads, self.head_dim = n_layers, n_pages, n_kv_heads, head_dim
         self.store, self.page_tokens = store, page_tokens
@@ -710,13 +711,21 @@ class PagedKV:
         self._check(self._call.paged_accept(self._fn["accept"], self._handle, -1 if layer is None else self._layer(layer), self._batch(batch), batch.n_seqs,
                                             self.device_index, path, counts, self._stream()))
 
-    def scalekv_paged_weigh(self, layer, batch, Q, lse, weights, causal=True, window=0, n_sink=0, decay=1.0, softmax_scale=0.0):
-        """Adds to weights (float32 [n_pages, n_kv_heads, page_tokens], of this layer) the attention that the new tokens' queries Q pay each cached entry; lse [n_tokens,
-        heads] as scalekv_paged_attend filled it for the same queries, mask and scale.  What was there before fades by `decay` first.  No two
-        sequences of the batch may see the same page."""
+    def scalekv_paged_weigh(self, layer, batch, Q, lse, weights, causal=True, window=0, n_sink=0, decay=1.0, softmax_scale=0.0, fade_hidden=False):
+        """Adds to weights (float32 [n_pages, n_kv_heads, page_tokens], of this layer) the attention that the new tokens' queries Q pay each cached entry that some of them see; lse
+        [n_tokens, heads] as scalekv_paged_attend filled it for the same queries, mask and scale.  What those entries had before fades by `decay` first; what others have,
+        behind a window, stays, or fades too where fade_hidden says so (see scalekv_paged_fade).  No two sequences of the batch may see the same page."""
         self._check(self._call.paged_weigh(self._fn["weigh"], self._handle, layer, self._batch(batch), batch.n_tokens, self.head_dim,
                                            self.device_index, Q, lse, weights, self.n_pages, self.n_kv_heads, self.page_tokens, causal, window, n_sink,
                                            decay, softmax_scale, self._stream()))
+        if fade_hidden:
+            self.scalekv_paged_fade(layer, batch, weights, window, n_sink, decay)
+
+    def scalekv_paged_fade(self, layer, batch, weights, window, n_sink=0, decay=1.0):
+        """The sums of entries that a window hides from all new tokens of their sequence fade by `decay`, as scalekv_paged_weigh fades the others: with both, all of a sequence's
+        entries rank alike.  The table has to name the sequence's own pages for them, or, where one was given back, a number out of range."""
+        self._check(self._call.paged_fade(self._fn["fade"], self._handle, layer, self._batch(batch), self.device_index, weights, self.n_pages, self.n_kv_heads,
+                                          self.page_tokens, window, n_sink, decay, self._stream()))
 
     def scalekv_paged_evict(self, layer, batch, to_table, keep, weights, n_sink=0, n_recent=0, kept=None):
         """Of each sequence and kv head keep[b] (int32) entries stay: the first n_sink, the last n_recent, and of the rest those with the largest weights

@@ -417,6 +417,23 @@ PyObject *paged_weigh(PyObject *, PyObject *const *a, Py_ssize_t n) {
   CALL(fn(kv, layer, batch, (int32_t)std::min<long>(heads, INT32_MAX), q, static_cast<const float *>(lse), &mask, (float)scale, static_cast<float *>(weights), (float)decay, stream));
 }
 
+// paged_fade(function, handle, layer, batch address, device, weights, pages, kv heads, page_tokens, window, n_sink, decay, stream)
+PyObject *paged_fade(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (!arguments(n, 13)) return nullptr;
+  const auto fn = address<decltype(&scalekv_paged_fade)>(a[0]);
+  const auto kv = address<scalekv_paged *>(a[1]);
+  const int layer = number(a[2]);
+  const auto batch = address<const scalekv_paged_batch *>(a[3]);
+  const long device = PyLong_AsLong(a[4]), pages = PyLong_AsLong(a[6]), kv_heads = PyLong_AsLong(a[7]), page_tokens = PyLong_AsLong(a[8]);
+  const double decay = PyFloat_AsDouble(a[11]);
+  const auto stream = address<void *>(a[12]);
+  scalekv_paged_mask mask = {1, 0, 0};
+  if (PyErr_Occurred() || !size(a[9], "window", &mask.window) || !size(a[10], "n_sink", &mask.n_sink)) return nullptr;
+  void *weights;
+  if (!dense(a[5], "weights", at::kFloat, {pages, kv_heads, page_tokens}, (int)device, &weights)) return nullptr;
+  CALL(fn(kv, layer, batch, &mask, static_cast<float *>(weights), (float)decay, stream));
+}
+
 // paged_evict(function, handle, layer, batch address, sequences, device, to_table, keep, weights, pages, kv heads, page_tokens, sinks, recent, kept, stream)
 PyObject *paged_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (!arguments(n, 16)) return nullptr;
@@ -440,7 +457,7 @@ PyObject *paged_evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
 
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(step), METHOD(step_ex), METHOD(append), METHOD(attend), METHOD(compress_ex), METHOD(layer_stats_ex), METHOD(paged_move),
-                         METHOD(paged_attend), METHOD(paged_write_rotated), METHOD(paged_attend_tree), METHOD(paged_accept), METHOD(paged_weigh),
+                         METHOD(paged_attend), METHOD(paged_write_rotated), METHOD(paged_attend_tree), METHOD(paged_accept), METHOD(paged_weigh), METHOD(paged_fade),
                          METHOD(paged_evict),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_scalekv_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

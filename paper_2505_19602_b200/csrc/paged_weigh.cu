@@ -1,6 +1,7 @@
 // What attention the entries of the paged token cache get, summed up entry by entry (see include/scalekv.h for the contract).
 //
-//   w_j <- (j before the new tokens ? decay w_j : 0) + sum over the rows that see j of exp(scale <q, k_j> - lse_row)
+//   w_j <- (j before the new tokens ? decay w_j : 0) + sum over the rows that see j of exp(scale <q, k_j> - lse_row)      for every j that some row sees,
+//   w_j <- decay w_j                                                                                                     for those that a window hides from all of them, in a call of its own.
 //
 // A kv head's query rows, the group's heads of every new token, pay their attention to the same keys.  The rows' log-sum-exps are known, so every key's sum stands by itself: keys are
 // cut over CTAs and warps at will, each is one warp's alone, and sums have one order.
@@ -671,6 +672,28 @@ __global__ void __launch_bounds__(WeighTile<D, kQ8>::kThreads, 1) paged_weigh_ti
   }
 }
 
+// ---- what a window hides from all new tokens of a sequence, entries n_sink .. lo - 1: one product each, eight bytes of traffic.  A page that is out of range was given back, as windows do.
+// us, 32 sequences of up to 10 521 entries of 8 heads behind a window of 1 024: the weigh 18.4, with this 24.6 (13 MB; a launch and its chain of length, table, sum).
+constexpr int kFadeThreads = 256, kFadeFours = 2;      // fours of entries for a thread, or so
+
+__global__ void __launch_bounds__(kFadeThreads) paged_fade_kernel(const __grid_constant__ WeighArgs w) {
+  const AttendArgs &a = w.a;
+  const Store &s = a.s;
+  const int seq = blockIdx.x, head = blockIdx.y;
+  wait_for_grid();
+  next_grid();
+  const Span sp(a, seq, 0x7fffffff, blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0);
+  const int from = sp.n_sink, to = sp.rows > 0 ? sp.lo : 0;
+  for (int i = (from >> 2) + blockIdx.z * kFadeThreads + threadIdx.x; i < (to + 3) >> 2; i += gridDim.z * kFadeThreads) {
+    const int pos = i << 2, page = a.bt.table[(size_t)seq * a.bt.table_ld + (pos >> s.page_shift)];      // (a four lies in one page)
+    if ((unsigned)page >= (unsigned)s.n_pages) continue;
+    float4 *at = reinterpret_cast<float4 *>(w.weights + store_row(s, page, head, pos));
+    auto faded = [&](float x, int p) { return p >= from && p < to ? w.decay * x : x; };
+    const float4 x = *at;
+    *at = make_float4(faded(x.x, pos), faded(x.y, pos + 1), faded(x.z, pos + 2), faded(x.w, pos + 3));
+  }
+}
+
 template <int D, bool kQ8>
 bool room() {
   auto ask = [](auto kernel, size_t bytes) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess; };
@@ -687,6 +710,39 @@ bool scalekv::paged::room_for_weigh(int head_dim, bool q8) {
   return q8 ? room<64, true>() : room<64, false>();
 }
 
+namespace {
+
+scalekv_status check_sums(scalekv_paged *c, const scalekv_paged_mask *mask, const float *weights, float decay, const Batch &bt) {
+  if (!mask || mask->window < 0 || mask->n_sink < 0) return fail(c, SCALEKV_ERR_INVALID_ARG, "mask null, or a negative size in it");
+  if (!(decay >= 0.f && decay <= 1.f)) return fail(c, SCALEKV_ERR_INVALID_ARG, "decay must lie in [0, 1]");
+  if (bt.n_tokens > 0 && (!weights || (reinterpret_cast<uintptr_t>(weights) & 15))) return fail(c, SCALEKV_ERR_INVALID_ARG, "weights null, or not 16-byte aligned");
+  if (c->cfg.n_kv_heads > 32767) return fail(c, SCALEKV_ERR_UNSUPPORTED, "more than 32767 kv heads");
+  return SCALEKV_OK;
+}
+
+}  // namespace
+
+extern "C" scalekv_status scalekv_paged_fade(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, const scalekv_paged_mask *mask, float *weights, float decay, void *stream) {
+  if (!kv) return SCALEKV_ERR_INVALID_ARG;
+  scalekv_paged *c = kv;
+  Range range("scalekv.paged_fade");
+  WeighArgs w = {};
+  AttendArgs &a = w.a;
+  if (scalekv_status st = check_batch(c, layer, batch, a.bt)) return st;
+  if (scalekv_status st = check_sums(c, mask, weights, decay, a.bt)) return st;
+  if (a.bt.n_tokens == 0 || mask->window == 0 || decay == 1.f) return SCALEKV_OK;
+  a.s = layer_store(c, layer);
+  a.mask = {mask->causal != 0, std::min(mask->window, kMaxLength), mask->n_sink};
+  a.group = Divisor::of(1);
+  a.max_new = batch->max_new;
+  w.weights = weights;
+  w.decay = decay;
+  const long long entries = std::min<long long>(batch->max_length, (long long)a.bt.table_pages << c->page_shift);
+  const dim3 grid(a.bt.n_seqs, c->cfg.n_kv_heads, (unsigned)std::clamp<long long>(entries / (4 * kFadeFours * kFadeThreads), 1, 65535));
+  launch(paged_fade_kernel, grid, kFadeThreads, 0, static_cast<cudaStream_t>(stream), w);
+  return launched(c, "paged_fade");
+}
+
 extern "C" scalekv_status scalekv_paged_weigh(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, int32_t n_heads, scalekv_rows Q, const float *lse,
                                               const scalekv_paged_mask *mask, float softmax_scale, float *weights, float decay, void *stream) {
   if (!kv) return SCALEKV_ERR_INVALID_ARG;
@@ -696,14 +752,11 @@ extern "C" scalekv_status scalekv_paged_weigh(scalekv_paged *kv, int32_t layer, 
   AttendArgs &a = w.a;
   if (scalekv_status st = check_batch(c, layer, batch, a.bt)) return st;
   if (scalekv_status st = check_heads(c, n_heads, softmax_scale)) return st;
-  if (!mask || mask->window < 0 || mask->n_sink < 0) return fail(c, SCALEKV_ERR_INVALID_ARG, "mask null, or a negative size in it");
-  if (!(decay >= 0.f && decay <= 1.f)) return fail(c, SCALEKV_ERR_INVALID_ARG, "decay must lie in [0, 1]");
+  if (scalekv_status st = check_sums(c, mask, weights, decay, a.bt)) return st;
   if (a.bt.n_tokens == 0) return SCALEKV_OK;
-  if (!rows_ok(Q, 2) || !lse || !weights || (reinterpret_cast<uintptr_t>(weights) & 15))
-    return fail(c, SCALEKV_ERR_INVALID_ARG, "Q, lse or weights null, or not 16-byte aligned");
+  if (!rows_ok(Q, 2) || !lse) return fail(c, SCALEKV_ERR_INVALID_ARG, "Q or lse null, or rows not 16-byte aligned");
   const int H = c->cfg.n_kv_heads, D = c->cfg.head_dim, G = n_heads / H;
   if ((long long)a.bt.n_tokens * n_heads > kMaxLength) return fail(c, SCALEKV_ERR_UNSUPPORTED, "more than 2^30 query rows in a call");
-  if (H > 32767) return fail(c, SCALEKV_ERR_UNSUPPORTED, "more than 32767 kv heads");
   a.s = layer_store(c, layer);
   a.Q = view(Q, 2);
   a.O = {};

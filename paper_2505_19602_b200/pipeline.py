@@ -285,7 +285,8 @@ class Sequences:
 def token_step(kv: binding.PagedKV, batch, rows, causal=True, window=0, n_sink=0, rotary=None, positions=None, weights=None, decay=1.0):
     """One step of every layer: the new tokens' rows join the cache, quantised if it holds codes, and their queries attend over it.
     rows(layer) -> (Q, K, V) of the new tokens; returns the layers' outputs.  rotary (binding.Rotary) and positions (int32 [axes, tokens]): Q and K are turned by them
-    first.  weights (float32 [layers, pages, kv heads, rows of a page]): what attention each entry gets is added to it (see evict)."""
+    first.  weights (float32 [layers, pages, kv heads, rows of a page]): what attention each entry gets is added to it (see evict), and what entries had before fades by `decay`, whether
+    the window hides them or not (of hidden pages the batch's table names the sequence's own, or none)."""
     out = []
     for l in range(kv.n_layers):
         Q, K, V = rows(l)
@@ -296,7 +297,7 @@ def token_step(kv: binding.PagedKV, batch, rows, causal=True, window=0, n_sink=0
         lse = None if weights is None else torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device)
         out.append(kv.scalekv_paged_attend(l, batch, Q, lse=lse, causal=causal, window=window, n_sink=n_sink))
         if weights is not None:
-            kv.scalekv_paged_weigh(l, batch, Q, lse, weights[l], causal=causal, window=window, n_sink=n_sink, decay=decay)
+            kv.scalekv_paged_weigh(l, batch, Q, lse, weights[l], causal=causal, window=window, n_sink=n_sink, decay=decay, fade_hidden=True)
     return out
 
 
