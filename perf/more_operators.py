@@ -323,7 +323,7 @@ def run(s):
         elif case["kind"] == "accept":
             kv.scalekv_paged_accept(batch, s["path"], s["counts"])
         elif case["kind"] == "weigh":
-            kv.scalekv_paged_weigh(layer, batch, s["Q"], s["lse"], s["weights"], window=case["window"], n_sink=case["sinks"], decay=case["decay"])
+            kv.scalekv_paged_weigh(layer, batch, s["Q"], s["lse"], s["weights"], window=case["window"], n_sink=case["sinks"], decay=case["decay"], fade_hidden=True)
         else:
             kv.scalekv_paged_evict(layer, batch, s["to"], s["keep"], s["weights"], n_sink=case["sinks"], n_recent=case["recent"], kept=s["kept"])
     else:
