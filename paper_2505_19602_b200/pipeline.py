@@ -322,21 +322,28 @@ def tree_bits(parents):
 def draft_step(kv: binding.PagedKV, seqs: Sequences, parents, rows, accept, rotary=None, positions=None):
     """One step with drafted tokens: those of sequence b form the tree parents[b] (see tree_bits), attend over the cache and their ancestors, and of them
     accept(layers' outputs)[b], a path's tokens in ascending order, stay.  rows(layer) -> (Q, K, V) of all drafted tokens; rotary and positions as for token_step (a
-    token's position is its sequence's length plus its depth).  -> (outputs, accepted paths)"""
+    token's position is its sequence's length plus its depth).  -> (outputs, accepted paths).  A step that raises, on its way or for paths that cannot be, takes the draft back: the page
+    book is what it was."""
     new = [len(p) for p in parents]
     bits, _ = tree_bits(parents)
     seqs.extend(new)
-    batch, dev = seqs.batch(new, kv.device_index), dict(dtype=torch.int32, device=kv.device)
-    tree = torch.tensor(bits, **dev).view(sum(new), max(1, -(-max(new, default=0) // 32)))
-    out = []
-    for l in range(kv.n_layers):
-        Q, K, V = rows(l)
-        if rotary is None:
-            kv.scalekv_paged_write(l, batch, K, V)
-        else:
-            Q = kv.scalekv_paged_write_rotated(l, batch, Q, K, V, rotary, positions)
-        out.append(kv.scalekv_paged_attend_tree(l, batch, Q, tree))
-    paths = accept(out)
+    try:
+        batch, dev = seqs.batch(new, kv.device_index), dict(dtype=torch.int32, device=kv.device)
+        tree = torch.tensor(bits, **dev).view(sum(new), max(1, -(-max(new, default=0) // 32)))
+        out = []
+        for l in range(kv.n_layers):
+            Q, K, V = rows(l)
+            if rotary is None:
+                kv.scalekv_paged_write(l, batch, K, V)
+            else:
+                Q = kv.scalekv_paged_write_rotated(l, batch, Q, K, V, rotary, positions)
+            out.append(kv.scalekv_paged_attend_tree(l, batch, Q, tree))
+        paths = accept(out)
+        if len(paths) != len(new) or any(a >= b for n, p in zip(new, paths) for a, b in zip([-1, *p], [*p, n])):
+            raise ValueError(f"expected {len(new)} paths, of each draft's tokens some in ascending order, got {paths}")
+    except BaseException:
+        seqs.retract(new)
+        raise
     most = max((len(p) for p in paths), default=0)
     kv.scalekv_paged_accept(batch, torch.tensor([list(p) + [-1] * (most - len(p)) for p in paths], **dev).view(len(paths), most),
                             torch.tensor([len(p) for p in paths], **dev))
