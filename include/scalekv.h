@@ -488,7 +488,8 @@ scalekv_status scalekv_paged_attend_tree(scalekv_paged *kv, int32_t layer, const
  * behind what was there before (path, counts: device; a path ascends).  layer -1: in all layers.  The lengths are the caller's: lengths[b] less the
  * new tokens, plus counts[b], once all layers are done.  A path that does not ascend, or names no new token, or a place whose page is out of range
  * is reported, and it and what is behind it in the path stay where they are; so does all of a sequence whose count is out of range.  Pages that a draft lies in
- * must not be other sequences', too. */
+ * must not be other sequences', too.  Sums of attention (scalekv_paged_weigh) do not move along: an accepted token's is what a weigh makes it in which it is a
+ * new token; until then its place holds what it held before. */
 scalekv_status scalekv_paged_accept(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, const int32_t *path,
                                     int32_t path_stride, int32_t path_len, const int32_t *counts, void *stream);
 

@@ -319,24 +319,28 @@ def tree_bits(parents):
     return bits, depths
 
 
-def draft_step(kv: binding.PagedKV, seqs: Sequences, parents, rows, accept, rotary=None, positions=None):
+def draft_step(kv: binding.PagedKV, seqs: Sequences, parents, rows, accept, rotary=None, positions=None, weights=None, decay=1.0):
     """One step with drafted tokens: those of sequence b form the tree parents[b] (see tree_bits), attend over the cache and their ancestors, and of them
     accept(layers' outputs)[b], a path's tokens in ascending order, stay.  rows(layer) -> (Q, K, V) of all drafted tokens; rotary and positions as for token_step (a
     token's position is its sequence's length plus its depth).  -> (outputs, accepted paths).  A step that raises, on its way or for paths that cannot be, takes the draft back: the page
-    book is what it was."""
+    book is what it was.
+    weights and decay as for token_step: what is added is the attention that the accepted tokens pay, as if they had come in a step of their own; what the others looked at counts for nothing.
+    Whoever ranks entries by weights (evict) gives them to every step: the places of accepted tokens hold whatever was there before otherwise."""
     new = [len(p) for p in parents]
     bits, _ = tree_bits(parents)
     seqs.extend(new)
     try:
         batch, dev = seqs.batch(new, kv.device_index), dict(dtype=torch.int32, device=kv.device)
         tree = torch.tensor(bits, **dev).view(sum(new), max(1, -(-max(new, default=0) // 32)))
-        out = []
+        out, queries = [], []
         for l in range(kv.n_layers):
             Q, K, V = rows(l)
             if rotary is None:
                 kv.scalekv_paged_write(l, batch, K, V)
             else:
                 Q = kv.scalekv_paged_write_rotated(l, batch, Q, K, V, rotary, positions)
+            if weights is not None:
+                queries.append(Q if rotary is not None else Q.clone())           # (rows() may fill the same tensor for every layer)
             out.append(kv.scalekv_paged_attend_tree(l, batch, Q, tree))
         paths = accept(out)
         if len(paths) != len(new) or any(a >= b for n, p in zip(new, paths) for a, b in zip([-1, *p], [*p, n])):
@@ -347,7 +351,16 @@ def draft_step(kv: binding.PagedKV, seqs: Sequences, parents, rows, accept, rota
     most = max((len(p) for p in paths), default=0)
     kv.scalekv_paged_accept(batch, torch.tensor([list(p) + [-1] * (most - len(p)) for p in paths], **dev).view(len(paths), most),
                             torch.tensor([len(p) for p in paths], **dev))
-    seqs.retract([n - len(p) for n, p in zip(new, paths)])
+    counts = [len(p) for p in paths]
+    seqs.retract([n - k for n, k in zip(new, counts)])
+    if weights is not None and sum(counts) > 0:
+        batch = seqs.batch(counts, kv.device_index)
+        picked = torch.tensor([sum(new[:b]) + int(j) for b, p in enumerate(paths) for j in p], **dev)
+        for l, Q in enumerate(queries):
+            Q = Q.index_select(0, picked)
+            lse = torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device)
+            kv.scalekv_paged_attend(l, batch, Q, lse=lse)
+            kv.scalekv_paged_weigh(l, batch, Q, lse, weights[l], decay=decay)
     return out, paths
 
 
