@@ -501,7 +501,9 @@ scalekv_status scalekv_paged_accept(scalekv_paged *kv, int32_t layer, const scal
  * [n_tokens][n_heads], as scalekv_paged_attend fills it for the same batch, Q, mask and scale; a row whose lse is -inf pays nothing.  decay in [0, 1].
  * No two sequences of a batch may see the same page: an entry's sum is one's alone.  Entries that a window hides from all of them are left alone because their places
  * in the table may hold anything: for sums by which entries inside and behind a window are ranked (scalekv_paged_evict), decay below 1, scalekv_paged_fade goes along.
- * Products are exact, sums are fp32 and always in the same order; an exponent is off by 2^-21 of scale sum |q_i k_i| and of itself at most. */
+ * Products are exact, sums are fp32 and always in the same order.  What an exponent scale q.k - lse is off by at most: where no sequence may bring more than 32
+ * query rows to a kv head (max_new times the heads of the group) 2^-19 of scale sum |q_i k_i| and 2^-23 of itself; otherwise head_dim 2^-24 of
+ * scale sum |q_i k_i| and 2^-23 of |lse| and of |scale q.k|. */
 scalekv_status scalekv_paged_weigh(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, int32_t n_heads,
                                    scalekv_rows Q, const float *lse, const scalekv_paged_mask *mask, float softmax_scale,
                                    float *weights, float decay, void *stream);

@@ -128,8 +128,8 @@ __global__ void __launch_bounds__(kStreamThreads) paged_weigh_stream_kernel(cons
       float x[kN][4];
 #pragma unroll
       for (int n = 0; n < kN; ++n) x[n][0] = x[n][1] = x[n][2] = x[n][3] = 0.f;
-      // (Products of two steps are summed by themselves: the tensor core cuts off what lies below the last place of a sum's largest part, at every step, and an exponent's error is a relative one of its power: 2.5e-6 of a sum that one key
-      // dominates with a single sum, 7e-7 so.)
+      // (Products of two steps are summed by themselves: of a step's 16 products and the sum so far the tensor core cuts each at 2^-25 of the largest, and the result at 2^-23 of itself (measured), 1.25 x 2^-21 at most; an exponent's error
+      // is a relative one of its power.  A sum that one key dominates is off by 2.5e-6 with a single sum, by 7e-7 so; at worst 8 steps in one sum make 80 x 2^-24, four sums of two and their three additions 23 x 2^-24.)
       float y[kN][4];
       auto fresh = [&]() {
 #pragma unroll
@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(kStreamThreads) paged_weigh_stream_kernel(cons
 //   warp 1        : finds the items, ahead of the others
 //   warps 4-7     : the queries, by asynchronous copies of 16 bytes (rows are a token's heads, in any strides), and their log-sum-exps; the next item's keys, scales and weights
 //   warps 8-23    : keys from shared memory into TMEM (codes become bf16 exactly), then p = 2^(x ks - lse) and its sums
-// Every wait is bounded, as in paged_tile.cuh.  A product's sum is the tensor core's, whose cut-off (2^-22 of the largest part) is 2.5e-6 of a sum that one key of four times the others' length dominates.
+// Every wait is bounded, as in paged_tile.cuh.  A product's sum is the tensor core's, with its cut-off at each of D / 16 steps (see above): 2.5e-6 of a sum that one key of four times the others' length dominates.
 // What bounds it: exponentials, of which the special function unit does 16 a cycle (a tile of 128 x 128 takes it twice as long as the tensor core its product; it is busy for 80 of 100 cycles while a
 // CTA has work), and the power that both draw: 2 048 queries of 4 x 32 heads behind 6 144 entries in codes take 577 us from a cool start, 0.83 PFLOP/s, and 596 to 615 in a row.  (One exponential in
 // four by a polynomial on the FMA pipe: 555 us from a cool start, 597 in a row; half of them 658.  A key tile's rows in shared memory and eight softmax warps: 715; products issued one by one: 621; a CTA for
