@@ -91,6 +91,13 @@ bool arguments(Py_ssize_t n, Py_ssize_t want) {
 // A whole number.  One beyond 32 bits becomes the limit that it lies beyond, which no call takes for a layer or a scale; its low half might be one.
 int number(PyObject *obj) { return (int)std::min<long>(std::max<long>(PyLong_AsLong(obj), INT32_MIN), INT32_MAX); }
 
+// A factor of products, as 32 bits hold it.  0 stands for another, so what only becomes 0 there is refused.
+float factor(PyObject *obj) {
+  const double x = PyFloat_AsDouble(obj);
+  if (x != 0. && (float)x == 0.f && !PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "softmax_scale is below what 32 bits hold");
+  return (float)x;
+}
+
 #define CALL(expr)            \
   int st;                     \
   if (PyErr_Occurred()) return nullptr; \
@@ -253,7 +260,7 @@ PyObject *paged_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
   const long tokens = PyLong_AsLong(a[4]), dim = PyLong_AsLong(a[5]), device = PyLong_AsLong(a[6]);
   const long window = PyLong_AsLong(a[11]), sinks = PyLong_AsLong(a[12]);
   const int causal = PyObject_IsTrue(a[10]);
-  const double scale = PyFloat_AsDouble(a[13]);
+  const float scale = factor(a[13]);
   const auto stream = address<void *>(a[14]);
   if (PyErr_Occurred()) return nullptr;
   if (window > 0x7fffffff || sinks > 0x7fffffff || window < 0 || sinks < 0) {
@@ -282,7 +289,7 @@ PyObject *paged_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
           return true;
         })) return nullptr;
   }
-  CALL(fn(kv, layer, batch, (int32_t)std::min<long>(heads, INT32_MAX), q, o, lse, &mask, (float)scale, stream));
+  CALL(fn(kv, layer, batch, (int32_t)std::min<long>(heads, INT32_MAX), q, o, lse, &mask, scale, stream));
 }
 
 // A dense tensor of one type whose sizes are known but for those that are given as -1; the last axis is contiguous, and the one before it too where `strided` is null, which
@@ -363,7 +370,7 @@ PyObject *paged_attend_tree(PyObject *, PyObject *const *a, Py_ssize_t n) {
   const int layer = number(a[2]);
   const auto batch = address<const scalekv_paged_batch *>(a[3]);
   const long tokens = PyLong_AsLong(a[4]), dim = PyLong_AsLong(a[5]), device = PyLong_AsLong(a[6]);
-  const double scale = PyFloat_AsDouble(a[11]);
+  const float scale = factor(a[11]);
   const auto stream = address<void *>(a[12]);
   if (PyErr_Occurred()) return nullptr;
   scalekv_rows q, o;
@@ -374,7 +381,7 @@ PyObject *paged_attend_tree(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (a[9] != Py_None && !dense(a[9], "lse", at::kFloat, {tokens, heads}, (int)device, &lse)) return nullptr;
   if (!dense(a[10], "tree", at::kInt, {tokens, -1}, (int)device, &tree)) return nullptr;
   const long words = THPVariable_Unpack(a[10]).size(1);
-  CALL(fn(kv, layer, batch, (int32_t)std::min<long>(heads, INT32_MAX), q, o, static_cast<float *>(lse), static_cast<const int32_t *>(tree), (int32_t)std::min<long>(words, INT32_MAX), (float)scale, stream));
+  CALL(fn(kv, layer, batch, (int32_t)std::min<long>(heads, INT32_MAX), q, o, static_cast<float *>(lse), static_cast<const int32_t *>(tree), (int32_t)std::min<long>(words, INT32_MAX), scale, stream));
 }
 
 // paged_accept(function, handle, layer, batch address, sequences, device, path, counts, stream)
@@ -404,7 +411,8 @@ PyObject *paged_weigh(PyObject *, PyObject *const *a, Py_ssize_t n) {
   const long tokens = PyLong_AsLong(a[4]), dim = PyLong_AsLong(a[5]), device = PyLong_AsLong(a[6]);
   const long pages = PyLong_AsLong(a[10]), kv_heads = PyLong_AsLong(a[11]), page_tokens = PyLong_AsLong(a[12]);
   const int causal = PyObject_IsTrue(a[13]);
-  const double decay = PyFloat_AsDouble(a[16]), scale = PyFloat_AsDouble(a[17]);
+  const double decay = PyFloat_AsDouble(a[16]);
+  const float scale = factor(a[17]);
   const auto stream = address<void *>(a[18]);
   scalekv_paged_mask mask = {causal, 0, 0};
   if (PyErr_Occurred() || !size(a[14], "window", &mask.window) || !size(a[15], "n_sink", &mask.n_sink)) return nullptr;
@@ -414,7 +422,7 @@ PyObject *paged_weigh(PyObject *, PyObject *const *a, Py_ssize_t n) {
   void *lse, *weights;
   if (!rows(a[7], "Q", tokens, 0, dim, (int)device, &q, &type, &heads) || !dense(a[8], "lse", at::kFloat, {tokens, heads}, (int)device, &lse) ||
       !dense(a[9], "weights", at::kFloat, {pages, kv_heads, page_tokens}, (int)device, &weights)) return nullptr;
-  CALL(fn(kv, layer, batch, (int32_t)std::min<long>(heads, INT32_MAX), q, static_cast<const float *>(lse), &mask, (float)scale, static_cast<float *>(weights), (float)decay, stream));
+  CALL(fn(kv, layer, batch, (int32_t)std::min<long>(heads, INT32_MAX), q, static_cast<const float *>(lse), &mask, scale, static_cast<float *>(weights), (float)decay, stream));
 }
 
 // paged_fade(function, handle, layer, batch address, device, weights, pages, kv heads, page_tokens, window, n_sink, decay, stream)
