@@ -468,7 +468,7 @@ typedef struct {
 /* scalekv_paged_write with the rows turned: K (in fp32, then held as the cache holds rows) and V join the cache, Q with its n_heads
  * heads (any number; 0: no queries, Q and Q_out are not looked at) goes to Q_out, bf16 rows as an attend takes them, which may be Q itself where
  * that is bf16.  positions: device, position of token t on axis x at positions[x * axis_stride + t], any 32-bit number.  Angles are formed in
- * 64 bits: one is off by 2^-22 radians and 2^-52 of itself at most.  A position is the caller's alone, and need not be the place in the cache. */
+ * 64 bits: one is off by 2^-22 radians and 2^-51 of itself at most.  A position is the caller's alone, and need not be the place in the cache. */
 scalekv_status scalekv_paged_write_rotated(scalekv_paged *kv, int32_t layer, const scalekv_paged_batch *batch, int32_t n_heads,
                                            scalekv_rows Q, scalekv_rows Q_out, scalekv_rows K, scalekv_rows V, int32_t dtype,
                                            const scalekv_rotary *rotary, const int32_t *positions, int64_t axis_stride,

@@ -522,7 +522,9 @@ scalekv_status scalekv_paged_evict(scalekv_paged *kv, int32_t layer, const scale
   a.heads = Divisor::of(H);
   a.blocks = Divisor::of((int)blocks);
   const int length = (int)std::max(1ll, std::min<long long>(batch->max_length, room));      // (at most kMaxLength)
-  // as many CTAs to a sequence and head as find an SM, with more than 16 384 entries for each
+  // as many CTAs to a sequence and head as find an SM, with more than 16 384 entries for each (us, one sequence to 1 000 entries, with one event's 7.  16 heads: 12 000 entries with 1 / 2 / 4 CTAs 25.9 / 26.4 / 25.5;
+  // 20 000 with 1 / 2 / 4 / 8 31.9 / 28.8 / 26.0 / 29.9; 40 000 with 2 / 4 / 8 32.8 / 25.7 / 29.5; 80 000 with 4 / 8 34.6 / 32.0.  4 heads, 40 000 with 2 / 4 / 8 33.9 / 28.8 / 27.6.  One head, 20 000 with 1 / 2 / 4 / 8 29.2 / 24.2 / 22.2 / 22.0.
+  // What the rule leaves out: four instead of two for 16 385 to 32 768 entries, a tenth.)
   int cluster = 1;
   while (cluster < kMostCluster && items * cluster <= c->n_sm && length > cluster * 16384) cluster *= 2;
   a.held = std::min((length + cluster - 1) / cluster + 8, kMostHeld) & ~3;      // (fours that begin and end inside)

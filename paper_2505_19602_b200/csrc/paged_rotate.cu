@@ -7,7 +7,8 @@
 //
 // Every row is moved once; what bounds that is memory, and with bf16 rows the instructions for a lane's 16 values, about 200 (56 of 100 issue slots).  A lane has 16 values of a row, as two pieces of eight:
 // where the pairs are a dimension of the first half and one of the second, the pieces are those of eight pairs, so nothing is exchanged between lanes.
-// us, 8 192 tokens of 16 heads of 128: bf16 into bf16 41.6 (4.8 TB/s of 6.5 measured), f32 into bf16 54 (5.6), bf16 into codes 64.  (Five blocks to an SM with bf16 rows, at 20 bytes of spills, 48.3 / 66.7 with codes where four take
+// us, 8 192 tokens of 16 heads of 128: bf16 into bf16 41.6 (4.8 TB/s of 6.5 measured), f32 into bf16 54 (5.6), bf16 into codes 64 (168.8 MB, 26 at the copy rate: rows that turn nothing, V's
+// above all, go through the same branches and both correction steps of a quotient).  (Five blocks to an SM with bf16 rows, at 28 to 36 bytes of spills, 8 into codes, 48.3 / 66.7 with codes where four take
 // 49.5 / 68.9, with one event's 5 us; with f32 rows five were the slower.  Two rounds of loads on their way, or angles behind the look-up of places: the same to 1 us.)
 #include "paged_host.cuh"
 #include "paged_store.cuh"

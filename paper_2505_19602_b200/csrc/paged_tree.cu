@@ -3,7 +3,8 @@
 // The draft's tokens are new tokens like others, and the kernels are those of paged_stream.cuh and paged_tile.cuh: everything before the draft is seen whole, by all rows, and
 // what bounds them is the same.  Only the last key tiles, in which the draft lies, are masked, by bits: 32 positions' worth are taken from two words of the row's token (tree_bits).
 // us, 32 heads on 8 of 128, codes: 8 tokens behind 1 991 entries 15.2, 64 tokens of 16 sequences of up to 10 521 entries 236 (128 items of up to 83 key tiles, one to an SM: the longest takes 2.8 us for each of its
-// tiles).  Equal shares of all items' tiles, a CTA with one item after the other, took 235 to 245: all SMs at work take 3.3 us for a tile, and the join of the parts 23.
+// tiles).  Equal shares of all items' tiles, a CTA with one item after the other, took 235 to 245: 52 tiles an SM at 3.3 us, which is what a tile takes with all SMs at work, are 173, the join of the
+// parts is 23, and what the other 40 were was not found.
 #include "paged_attend.cuh"
 
 using namespace scalekv;
