@@ -28,7 +28,7 @@ __device__ __forceinline__ bool some_see(const Span &sp, int pos) { return pos <
 
 // ---- few rows: keys stream past queries that stay in registers, as in paged_stream.cuh: products are m16n8k16 with the rows as n-tiles of eight (there is the layout).  A warp takes stretches of
 // eight steps of 16 keys, whose pages it looks up at once, a lane to each.  What bounds it: reading K and the sums once, and with codes the instructions that turn them into bf16.  us, 32 sequences of up to 10 521
-// entries, 32 heads on 8 of 128: codes 58.4 (4.6 TB/s; 72 of 100 issue slots; with one sum for all products 57.5, then stretches of 16 / 32 steps 61 / 69, pages looked up step by step 63), bf16 85 (5.9 TB/s).
+// entries, 32 heads on 8 of 128: codes 59.3 (4.5 TB/s; 72 of 100 issue slots; with one sum for all products 57.5, then stretches of 16 / 32 steps 61 / 69, pages looked up step by step 63), bf16 85 (5.9 TB/s).
 template <int D, bool kQ8, int kN>
 struct WeighLayout {
   static constexpr int kRowBytes = D * (kQ8 ? 1 : 2);
